@@ -339,18 +339,22 @@ def _own_qk(s):
         s["plan"] = dict(
             desc=desc, table=table, q=x[:, :heads * hd], k=x[:, heads * hd:(heads + kv) * hd],
             need=need, ws=torch.empty(max(need, 16), dtype=torch.uint8, device=DEV),
-            oq=torch.empty((n, heads * hd, v), dtype=x.dtype, device=DEV),
-            ok=torch.empty((n, kv * hd, v), dtype=x.dtype, device=DEV),
             dgq=torch.empty(hd, device=DEV), dgk=torch.empty(hd, device=DEV))
+        if case["op"] == "qk":
+            s["plan"].update(oq=torch.empty((n, heads * hd, v), dtype=x.dtype, device=DEV),
+                             ok=torch.empty((n, kv * hd, v), dtype=x.dtype, device=DEV))
+        else:  # the gradients lie side by side as q and k do, for the convolution before
+            dx = torch.zeros_like(x)
+            s["plan"].update(dq=dx[:, :heads * hd], dk=dx[:, heads * hd:(heads + kv) * hd])
     b = s["plan"]
     if case["op"] == "qk":
         R.rat3d_qk_norm_rope_fwd(b["desc"], b["q"], b["k"], s["gq"], s["gk"], b["table"], b["oq"],
                                  b["ok"])
         return dict(q=b["oq"], k=b["ok"])
     R.rat3d_qk_norm_rope_bwd(b["desc"], s["dq"], s["dk"], b["q"], b["k"], s["gq"], s["gk"],
-                             b["table"], b["oq"], b["ok"], b["dgq"], b["dgk"], 0, b["ws"],
+                             b["table"], b["dq"], b["dk"], b["dgq"], b["dgk"], 0, b["ws"],
                              b["need"])
-    return dict(dq=b["oq"], dk=b["ok"], dgq=b["dgq"], dgk=b["dgk"])
+    return dict(dq=b["dq"], dk=b["dk"], dgq=b["dgq"], dgk=b["dgk"])
 
 
 def _own_attn(s):

@@ -213,6 +213,134 @@ rat3d_status rat3d_softmask_bwd(int64_t count, rat3d_dtype dtype, const void* do
                                 void* dz, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Self-attention over the voxels of a map (token attention, beside the soft
+ * mask above: the paper names a self-attention layer without giving its form).
+ * A map [n][c][d][h][w] is a set of d*h*w tokens a volume, one a voxel, and its
+ * channels are heads x head_dim: head i is channels i*head_dim and up.  With the
+ * 1^3 convolutions (rat3d_conv3d_*) before and behind, a block is
+ *   qkv = conv(x); q, k = qk_norm_rope(q, k); o = attention(q, k, v);
+ *   y = x + dropout(conv(o)).
+ * Queries, keys and values may be channel ranges of one tensor: their pointers
+ * need only the alignment of an element, and the *_stride fields say how many
+ * elements lie between one volume and the next (0: packed, heads * head_dim *
+ * tokens).  Channels of a volume are always contiguous rows of its tokens.
+ * Grouped heads: heads is a multiple of kv_heads, and query head i reads key
+ * and value head i / (heads / kv_heads).
+ * ------------------------------------------------------------------------ */
+
+/* Norm of each head's query and key vector and rotation by the voxel's place, in
+ * one pass:
+ *   z = x * gamma / sqrt(mean(x^2) + eps)        (norm != 0; else z = x)
+ * over the head_dim channels of one head and token, and then, for each axis a of
+ * d, h, w in that order, the next rot_a channels of the head are turned in pairs
+ * (i, i + rot_a/2), i < rot_a/2, by the angle
+ *   (origin_a + place of the voxel on a) * base^(-2 i / rot_a);
+ * channels behind the three ranges stay as they are.  rot_a are even, may be 0,
+ * and sum to at most head_dim (<= 128).  origin is the place of voxel (0, 0, 0),
+ * for crops of a larger volume (|origin| <= 2^24).
+ * heads or kv_heads may be 0: that tensor is left out and its pointers are not
+ * read. */
+typedef struct {
+    int n, heads, kv_heads, head_dim;
+    int d, h, w;
+    int rot_d, rot_h, rot_w;
+    int origin_d, origin_h, origin_w;
+    int norm;
+    float base, eps;
+    int64_t q_stride, k_stride;   /* q, k and their gradients dq, dk */
+    int64_t oq_stride, ok_stride; /* the results oq, ok and their gradients doq, dok */
+    rat3d_dtype dtype;
+} rat3d_qk_desc;
+
+/* The cosines and sines of a descriptor's grid (angles are formed in float64):
+ * bytes, and the call that fills them.  They depend on d, h, w, rot, origin and
+ * base only and are made once; 0 bytes without rotation (table may then be NULL).
+ * (size_t)-1 if the descriptor is invalid. */
+size_t rat3d_rope_table_size(const rat3d_qk_desc* desc);
+rat3d_status rat3d_rope_table(const rat3d_qk_desc* desc, void* table, void* stream);
+
+/* oq, ok = the norm and rotation of q [n][heads*head_dim][d*h*w] and of k
+ * [n][kv_heads*head_dim][d*h*w]; gamma_q, gamma_k float32 [head_dim] (ignored
+ * without norm).  oq may be q and ok may be k (same strides). */
+rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, const void* k,
+                                    const float* gamma_q, const float* gamma_k,
+                                    const void* table, void* oq, void* ok, void* stream);
+
+/* Backward: from doq, dok and the forward's inputs q, k the gradients dq, dk
+ * (which may be doq, dok if their strides agree) and dgamma_q, dgamma_k float32
+ * [head_dim], summed over volumes, heads and voxels (written, or added to when
+ * accumulate != 0; ignored without norm). */
+size_t rat3d_qk_norm_rope_workspace_size(const rat3d_qk_desc* desc);
+rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, const void* dok,
+                                    const void* q, const void* k, const float* gamma_q,
+                                    const float* gamma_k, const void* table, void* dq, void* dk,
+                                    float* dgamma_q, float* dgamma_k, int accumulate, void* ws,
+                                    size_t ws_bytes, void* stream);
+
+/* Attention: for each volume, head and query token i
+ *   o_i = sum_j p_ij v_j,  p_ij = softmax over j of scale * (q_i . k_j),
+ * over the keys j of the volume whose mask byte is not 0 (mask uint8 [n][tk], or
+ * NULL: all keys).  q, o [n][heads*head_dim][tq], k, v [n][kv_heads*head_dim]
+ * [tk], 1 <= tq, tk <= 2^28, head_dim <= 128.  lse float32 [n][heads][tq]
+ * (nullable) receives log sum_j exp(scale q_i . k_j), which the backward reads.
+ * A query without keys has o = 0 and lse = -infinity, and no part in any
+ * gradient.  Masked keys and values are not read into a result, whatever they
+ * hold; their gradients are 0. */
+typedef struct {
+    int n, heads, kv_heads, head_dim;
+    int64_t tq, tk;
+    float scale; /* > 0; 0 stands for 1/sqrt(head_dim) */
+    int64_t q_stride, k_stride, v_stride, o_stride; /* also of dq, dk, dv, dout */
+    rat3d_dtype dtype;
+} rat3d_attention_desc;
+
+/* Bytes of workspace (pass 0 = fwd, 1 = bwd); (size_t)-1 if the descriptor is
+ * invalid. */
+size_t rat3d_attention_workspace_size(const rat3d_attention_desc* desc, int pass);
+rat3d_status rat3d_attention_fwd(const rat3d_attention_desc* desc, const void* q, const void* k,
+                                 const void* v, const uint8_t* mask, void* o, float* lse,
+                                 void* ws, size_t ws_bytes, void* stream);
+
+/* Backward from dout (the gradient of o), the forward's inputs, its o and its
+ * lse.  dq, dk, dv are written; every query head of a group adds to its key
+ * head's gradients, in a fixed order. */
+rat3d_status rat3d_attention_bwd(const rat3d_attention_desc* desc, const void* dout,
+                                 const void* q, const void* k, const void* v,
+                                 const uint8_t* mask, const void* o, const float* lse, void* dq,
+                                 void* dk, void* dv, void* ws, size_t ws_bytes, void* stream);
+
+/* Dropout with a mask that is never stored:
+ *   y_e = [residual_e +] (keep(e / unit) ? x_e / (1 - p) : 0),
+ * one rounding; a dropped x_e is not read into the result, whatever it holds.
+ * `unit` neighbouring elements share one decision: 1 drops elements, d*h*w whole
+ * channels, c*d*h*w a volume's whole branch.  Decision u is the 16-bit number
+ * u % 8 (low halves first) of the Philox4x32-10 block with counter (u / 8, step)
+ * and key seed (each a 64-bit number, low word first): dropped if it is below
+ * p * 65536 rounded to nearest, and p stands for that fraction of 65536 in the
+ * formula too.  The step is `step`, plus *step_dev (device, nullable) when the
+ * kernel runs, so that a captured graph draws a new mask on each replay if the
+ * caller counts *step_dev up between. */
+typedef struct {
+    int64_t count;  /* elements, >= 1 */
+    int64_t unit;   /* >= 1 */
+    double p;       /* in [0, 1]; 1 drops everything */
+    uint64_t seed;
+    rat3d_dtype dtype;
+} rat3d_dropout_desc;
+
+/* residual may be NULL; y may be x or residual. */
+rat3d_status rat3d_dropout_fwd(const rat3d_dropout_desc* desc, uint64_t step,
+                               const uint64_t* step_dev, const void* x, const void* residual,
+                               void* y, void* stream);
+
+/* dx (+)= keep ? dy / (1 - p) : 0, the forward's decisions formed again from
+ * (seed, step).  dx may be dy if accumulate == 0.  The residual's gradient is dy
+ * itself. */
+rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
+                               const uint64_t* step_dev, const void* dy, void* dx,
+                               int accumulate, void* stream);
+
+/* ------------------------------------------------------------------------
  * Classifier head and update (experiments section: cross-entropy, SGD).
  * ------------------------------------------------------------------------ */
 

@@ -318,6 +318,237 @@ rat3d_status rat3d_softmask_bwd(int64_t count, rat3d_dtype dtype, const void* do
                         (hipStream_t)stream);
 }
 
+// Channel ranges of a larger tensor start at any element.
+#define RAT3D_ELT(p, es, name)                                                        \
+    do {                                                                              \
+        RAT3D_REQUIRE((p) != nullptr, RAT3D_EINVAL, "%s must not be NULL", name);     \
+        RAT3D_REQUIRE(((uintptr_t)(p) & ((es)-1)) == 0, RAT3D_EALIGN,                 \
+                      "%s must be aligned to its elements", name);                    \
+    } while (0)
+
+// Elements from one volume to the next: 0 (packed), or at least what a volume holds.
+static rat3d_status check_stride(int64_t stride, double held, const char* name) {
+    RAT3D_REQUIRE(stride == 0 || ((double)stride >= held && (double)stride < 1.0e15), RAT3D_EINVAL,
+                  "%s must be 0 or at least the elements of a volume", name);
+    return RAT3D_OK;
+}
+#define RAT3D_STRIDE(v, held)                                            \
+    do {                                                                 \
+        const rat3d_status s_ = check_stride((v), (held), #v);           \
+        if (s_ != RAT3D_OK) return s_;                                   \
+    } while (0)
+
+static rat3d_status check_qk(const rat3d_qk_desc* d) {
+    RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "qk descriptor is NULL");
+    RAT3D_REQUIRE(d->n >= 1 && d->head_dim >= 1 && d->d >= 1 && d->h >= 1 && d->w >= 1,
+                  RAT3D_EINVAL, "qk sizes must be >= 1");
+    RAT3D_REQUIRE(d->heads >= 0 && d->kv_heads >= 0 && (d->heads > 0 || d->kv_heads > 0),
+                  RAT3D_EINVAL, "qk needs heads >= 0 and kv_heads >= 0, not both 0");
+    RAT3D_REQUIRE(d->head_dim <= 128, RAT3D_EUNSUPPORTED, "head_dim above 128 is not built");
+    const int rot[3] = {d->rot_d, d->rot_h, d->rot_w};
+    const int origin[3] = {d->origin_d, d->origin_h, d->origin_w};
+    int64_t all = 0;
+    for (int a = 0; a < 3; ++a) {
+        RAT3D_REQUIRE(rot[a] >= 0 && rot[a] % 2 == 0, RAT3D_EINVAL,
+                      "the rotated channels of an axis must be even and >= 0");
+        RAT3D_REQUIRE(origin[a] >= -(1 << 24) && origin[a] <= (1 << 24), RAT3D_EINVAL,
+                      "origin is beyond 2^24");
+        all += rot[a];
+    }
+    RAT3D_REQUIRE(all <= d->head_dim, RAT3D_EINVAL, "more rotated channels than head_dim");
+    RAT3D_REQUIRE(all == 0 || (d->base > 0.f && d->base < 1e30f), RAT3D_EINVAL,
+                  "rotation needs a positive, finite base");
+    RAT3D_REQUIRE(!d->norm || (d->eps > 0.f && d->eps < 1e30f), RAT3D_EINVAL,
+                  "the norm needs a positive, finite eps");
+    RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
+                  (int)d->dtype);
+    const double v = (double)d->d * d->h * d->w;
+    RAT3D_REQUIRE((double)d->d + d->h + d->w < 1.6e7, RAT3D_EUNSUPPORTED,
+                  "qk map too large for one launch");
+    RAT3D_REQUIRE((v / 128.0 + 1) * d->n * ((double)d->heads + d->kv_heads) < 1.6e7,
+                  RAT3D_EUNSUPPORTED, "qk map too large for one launch");
+    const double hv = (double)d->head_dim * v;
+    RAT3D_STRIDE(d->q_stride, hv * d->heads);
+    RAT3D_STRIDE(d->k_stride, hv * d->kv_heads);
+    RAT3D_STRIDE(d->oq_stride, hv * d->heads);
+    RAT3D_STRIDE(d->ok_stride, hv * d->kv_heads);
+    return RAT3D_OK;
+}
+
+size_t rat3d_rope_table_size(const rat3d_qk_desc* desc) {
+    if (check_qk(desc) != RAT3D_OK) return (size_t)-1;
+    return rope_table_bytes(*desc);
+}
+
+rat3d_status rat3d_rope_table(const rat3d_qk_desc* desc, void* table, void* stream) {
+    rat3d_status s = check_qk(desc);
+    if (s != RAT3D_OK) return s;
+    if (rope_table_bytes(*desc) == 0) return RAT3D_OK;
+    RAT3D_ACT(table, "table");
+    return rope_table(*desc, table, (hipStream_t)stream);
+}
+
+size_t rat3d_qk_norm_rope_workspace_size(const rat3d_qk_desc* desc) {
+    if (check_qk(desc) != RAT3D_OK) return (size_t)-1;
+    return qk_ws_bytes(*desc);
+}
+
+rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, const void* k,
+                                    const float* gamma_q, const float* gamma_k,
+                                    const void* table, void* oq, void* ok, void* stream) {
+    rat3d_status s = check_qk(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    if (desc->heads) {
+        RAT3D_ELT(q, es, "q");
+        RAT3D_ELT(oq, es, "oq");
+        RAT3D_REQUIRE(!desc->norm || gamma_q, RAT3D_EINVAL, "gamma_q must not be NULL");
+    }
+    if (desc->kv_heads) {
+        RAT3D_ELT(k, es, "k");
+        RAT3D_ELT(ok, es, "ok");
+        RAT3D_REQUIRE(!desc->norm || gamma_k, RAT3D_EINVAL, "gamma_k must not be NULL");
+    }
+    if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
+    return qk_rope_fwd(*desc, q, k, gamma_q, gamma_k, table, oq, ok, (hipStream_t)stream);
+}
+
+rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, const void* dok,
+                                    const void* q, const void* k, const float* gamma_q,
+                                    const float* gamma_k, const void* table, void* dq, void* dk,
+                                    float* dgamma_q, float* dgamma_k, int accumulate, void* ws,
+                                    size_t ws_bytes, void* stream) {
+    rat3d_status s = check_qk(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    if (desc->heads) {
+        RAT3D_ELT(doq, es, "doq");
+        RAT3D_ELT(dq, es, "dq");
+        if (desc->norm) {
+            RAT3D_ELT(q, es, "q");
+            RAT3D_REQUIRE(gamma_q && dgamma_q, RAT3D_EINVAL,
+                          "gamma_q and dgamma_q must not be NULL");
+        }
+    }
+    if (desc->kv_heads) {
+        RAT3D_ELT(dok, es, "dok");
+        RAT3D_ELT(dk, es, "dk");
+        if (desc->norm) {
+            RAT3D_ELT(k, es, "k");
+            RAT3D_REQUIRE(gamma_k && dgamma_k, RAT3D_EINVAL,
+                          "gamma_k and dgamma_k must not be NULL");
+        }
+    }
+    if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
+    s = check_ws(ws, ws_bytes, qk_ws_bytes(*desc));
+    if (s != RAT3D_OK) return s;
+    return qk_rope_bwd(*desc, doq, dok, q, k, gamma_q, gamma_k, table, dq, dk, dgamma_q, dgamma_k,
+                       accumulate ? 1 : 0, ws, (hipStream_t)stream);
+}
+
+static rat3d_status check_attention(const rat3d_attention_desc* d) {
+    RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "attention descriptor is NULL");
+    RAT3D_REQUIRE(d->n >= 1 && d->heads >= 1 && d->kv_heads >= 1 && d->head_dim >= 1 &&
+                      d->tq >= 1 && d->tk >= 1,
+                  RAT3D_EINVAL, "attention sizes must be >= 1");
+    RAT3D_REQUIRE(d->heads % d->kv_heads == 0, RAT3D_EINVAL,
+                  "heads must be a multiple of kv_heads (%d, %d)", d->heads, d->kv_heads);
+    RAT3D_REQUIRE(d->scale == 0.f || (d->scale > 0.f && d->scale < 1e30f), RAT3D_EINVAL,
+                  "scale must be positive and finite, or 0 for 1/sqrt(head_dim)");
+    RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
+                  (int)d->dtype);
+    RAT3D_REQUIRE(d->head_dim <= 128, RAT3D_EUNSUPPORTED, "head_dim above 128 is not built");
+    const int64_t most = (int64_t)1 << 28;
+    RAT3D_REQUIRE(d->tq <= most && d->tk <= most && (double)d->n * d->heads < 1.6e7,
+                  RAT3D_EUNSUPPORTED, "attention too large for one launch");
+    RAT3D_REQUIRE(attention_fits(*d), RAT3D_EUNSUPPORTED, "attention too large for one launch");
+    const double qh = (double)d->heads * d->head_dim * d->tq;
+    const double kh = (double)d->kv_heads * d->head_dim * d->tk;
+    RAT3D_STRIDE(d->q_stride, qh);
+    RAT3D_STRIDE(d->k_stride, kh);
+    RAT3D_STRIDE(d->v_stride, kh);
+    RAT3D_STRIDE(d->o_stride, qh);
+    return RAT3D_OK;
+}
+
+size_t rat3d_attention_workspace_size(const rat3d_attention_desc* desc, int pass) {
+    if (check_attention(desc) != RAT3D_OK || pass < 0 || pass > 1) return (size_t)-1;
+    return attention_ws_bytes(*desc, pass);
+}
+
+rat3d_status rat3d_attention_fwd(const rat3d_attention_desc* desc, const void* q, const void* k,
+                                 const void* v, const uint8_t* mask, void* o, float* lse,
+                                 void* ws, size_t ws_bytes, void* stream) {
+    rat3d_status s = check_attention(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(q, es, "q");
+    RAT3D_ELT(k, es, "k");
+    RAT3D_ELT(v, es, "v");
+    RAT3D_ELT(o, es, "o");
+    s = check_ws(ws, ws_bytes, attention_ws_bytes(*desc, 0));
+    if (s != RAT3D_OK) return s;
+    return attention_fwd(*desc, q, k, v, mask, o, lse, ws, (hipStream_t)stream);
+}
+
+rat3d_status rat3d_attention_bwd(const rat3d_attention_desc* desc, const void* dout,
+                                 const void* q, const void* k, const void* v,
+                                 const uint8_t* mask, const void* o, const float* lse, void* dq,
+                                 void* dk, void* dv, void* ws, size_t ws_bytes, void* stream) {
+    rat3d_status s = check_attention(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(dout, es, "dout");
+    RAT3D_ELT(q, es, "q");
+    RAT3D_ELT(k, es, "k");
+    RAT3D_ELT(v, es, "v");
+    RAT3D_ELT(o, es, "o");
+    RAT3D_ELT(dq, es, "dq");
+    RAT3D_ELT(dk, es, "dk");
+    RAT3D_ELT(dv, es, "dv");
+    RAT3D_REQUIRE(lse != nullptr, RAT3D_EINVAL, "lse must not be NULL");
+    s = check_ws(ws, ws_bytes, attention_ws_bytes(*desc, 1));
+    if (s != RAT3D_OK) return s;
+    return attention_bwd(*desc, dout, q, k, v, mask, o, lse, dq, dk, dv, ws,
+                         (hipStream_t)stream);
+}
+
+static rat3d_status check_dropout(const rat3d_dropout_desc* d) {
+    RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "dropout descriptor is NULL");
+    RAT3D_REQUIRE(d->count >= 1 && d->unit >= 1, RAT3D_EINVAL, "count and unit must be >= 1");
+    RAT3D_REQUIRE(d->p >= 0.0 && d->p <= 1.0, RAT3D_EINVAL, "dropout needs 0 <= p <= 1");
+    RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
+                  (int)d->dtype);
+    RAT3D_REQUIRE(d->count <= (int64_t)1 << 50 && d->unit <= (int64_t)1 << 50, RAT3D_EUNSUPPORTED,
+                  "more than 2^50 elements");
+    return RAT3D_OK;
+}
+
+rat3d_status rat3d_dropout_fwd(const rat3d_dropout_desc* desc, uint64_t step,
+                               const uint64_t* step_dev, const void* x, const void* residual,
+                               void* y, void* stream) {
+    rat3d_status s = check_dropout(desc);
+    if (s != RAT3D_OK) return s;
+    RAT3D_ACT(x, "x");
+    RAT3D_ACT(y, "y");
+    if (residual) RAT3D_ACT(residual, "residual");
+    RAT3D_REQUIRE(((uintptr_t)step_dev & 7u) == 0, RAT3D_EALIGN, "step_dev must be 8-byte aligned");
+    return dropout(desc->count, desc->unit, desc->p, desc->seed, step, step_dev, desc->dtype, x,
+                   residual, y, (hipStream_t)stream);
+}
+
+rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
+                               const uint64_t* step_dev, const void* dy, void* dx,
+                               int accumulate, void* stream) {
+    rat3d_status s = check_dropout(desc);
+    if (s != RAT3D_OK) return s;
+    RAT3D_ACT(dy, "dy");
+    RAT3D_ACT(dx, "dx");
+    RAT3D_REQUIRE(((uintptr_t)step_dev & 7u) == 0, RAT3D_EALIGN, "step_dev must be 8-byte aligned");
+    return dropout(desc->count, desc->unit, desc->p, desc->seed, step, step_dev, desc->dtype, dy,
+                   accumulate ? dx : nullptr, dx, (hipStream_t)stream);
+}
+
 size_t rat3d_head_workspace_size(int n, int c, int classes) {
     if (n < 1 || c < 1 || classes < 1) return (size_t)-1;
     return head_ws_bytes(n, c, classes);

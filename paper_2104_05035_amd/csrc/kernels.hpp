@@ -241,6 +241,31 @@ rat3d_status gradcam_maps(int N, int C, int Dt, int Ht, int Wt, rat3d_dtype dt, 
                           const void* dA, float* alpha, float* cam, int D0, int H0, int W0,
                           float* cam_up, hipStream_t st);
 
+// ---- voxel self-attention (qk_rope.hip, attention.hip, dropout.hip) -----
+size_t rope_table_bytes(const rat3d_qk_desc& d);
+rat3d_status rope_table(const rat3d_qk_desc& d, void* table, hipStream_t st);
+size_t qk_ws_bytes(const rat3d_qk_desc& d);
+rat3d_status qk_rope_fwd(const rat3d_qk_desc& d, const void* q, const void* k, const float* gq,
+                         const float* gk, const void* table, void* oq, void* ok, hipStream_t st);
+rat3d_status qk_rope_bwd(const rat3d_qk_desc& d, const void* doq, const void* dok, const void* q,
+                         const void* k, const float* gq, const float* gk, const void* table,
+                         void* dq, void* dk, float* dgq, float* dgk, int accumulate, void* ws,
+                         hipStream_t st);
+// Whether every launch of the attention stays within the launch limits.
+bool attention_fits(const rat3d_attention_desc& d);
+size_t attention_ws_bytes(const rat3d_attention_desc& d, int pass);
+rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const void* k,
+                           const void* v, const uint8_t* mask, void* o, float* lse, void* ws,
+                           hipStream_t st);
+rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, const void* q,
+                           const void* k, const void* v, const uint8_t* mask, const void* o,
+                           const float* lse, void* dq, void* dk, void* dv, void* ws,
+                           hipStream_t st);
+// y = [res +] (keep ? x / (1 - p) : 0); res may be y (an accumulating gradient).
+rat3d_status dropout(int64_t count, int64_t unit, double p, uint64_t seed, uint64_t step,
+                     const uint64_t* step_dev, rat3d_dtype dt, const void* x, const void* res,
+                     void* y, hipStream_t st);
+
 // ---- head, update, casts (head.hip) ------------------------------------
 size_t head_ws_bytes(int N, int C, int classes);
 rat3d_status head_fwd_bwd(int N, int C, int64_t V, int classes, rat3d_dtype dt, const void* x,

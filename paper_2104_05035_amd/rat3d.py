@@ -54,6 +54,28 @@ class NetDesc(ctypes.Structure):
                 ("bn_momentum", ctypes.c_float), ("dtype", ctypes.c_int)]
 
 
+class QkDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in
+                ("n", "heads", "kv_heads", "head_dim", "d", "h", "w", "rot_d", "rot_h", "rot_w",
+                 "origin_d", "origin_h", "origin_w", "norm")] + \
+               [("base", ctypes.c_float), ("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "oq_stride",
+                                              "ok_stride")] + \
+               [("dtype", ctypes.c_int)]
+
+
+class AttentionDesc(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int) for n in ("n", "heads", "kv_heads", "head_dim")] + \
+               [("tq", ctypes.c_int64), ("tk", ctypes.c_int64), ("scale", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride", "o_stride")] + \
+               [("dtype", ctypes.c_int)]
+
+
+class DropoutDesc(ctypes.Structure):
+    _fields_ = [("count", ctypes.c_int64), ("unit", ctypes.c_int64), ("p", ctypes.c_double),
+                ("seed", ctypes.c_uint64), ("dtype", ctypes.c_int)]
+
+
 class GabraParams(ctypes.Structure):
     _fields_ = [("population", ctypes.c_int), ("generations", ctypes.c_int),
                 ("crossover_p", ctypes.c_double), ("seed", ctypes.c_uint64),
@@ -72,6 +94,7 @@ _I = ctypes.c_int
 _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _F = ctypes.c_float
+_U64 = ctypes.c_uint64
 
 _SIGS = {
     "rat3d_last_error": (ctypes.c_char_p, []),
@@ -92,6 +115,16 @@ _SIGS = {
     "rat3d_softmask_up_bwd": (_I, [ctypes.POINTER(UpDesc), _VP, _VP, _I, _VP]),
     "rat3d_softmask_fwd": (_I, [_I64, _I, _VP, _VP, _VP, _VP, _VP]),
     "rat3d_softmask_bwd": (_I, [_I64, _I, _VP, _VP, _VP, _VP, _I, _VP, _VP]),
+    "rat3d_rope_table_size": (_SZ, [ctypes.POINTER(QkDesc)]),
+    "rat3d_rope_table": (_I, [ctypes.POINTER(QkDesc), _VP, _VP]),
+    "rat3d_qk_norm_rope_workspace_size": (_SZ, [ctypes.POINTER(QkDesc)]),
+    "rat3d_qk_norm_rope_fwd": (_I, [ctypes.POINTER(QkDesc)] + [_VP] * 8),
+    "rat3d_qk_norm_rope_bwd": (_I, [ctypes.POINTER(QkDesc)] + [_VP] * 11 + [_I, _VP, _SZ, _VP]),
+    "rat3d_attention_workspace_size": (_SZ, [ctypes.POINTER(AttentionDesc), _I]),
+    "rat3d_attention_fwd": (_I, [ctypes.POINTER(AttentionDesc)] + [_VP] * 7 + [_SZ, _VP]),
+    "rat3d_attention_bwd": (_I, [ctypes.POINTER(AttentionDesc)] + [_VP] * 11 + [_SZ, _VP]),
+    "rat3d_dropout_fwd": (_I, [ctypes.POINTER(DropoutDesc), _U64] + [_VP] * 5),
+    "rat3d_dropout_bwd": (_I, [ctypes.POINTER(DropoutDesc), _U64] + [_VP] * 3 + [_I, _VP]),
     "rat3d_head_workspace_size": (_SZ, [_I, _I, _I]),
     "rat3d_head_fwd_bwd": (_I, [_I, _I, _I64, _I, _I] + [_VP] * 9 + [_I, _VP, _SZ, _VP]),
     "rat3d_sgd": (_I, [_I64, _F, _VP, _VP, _VP]),
@@ -276,6 +309,75 @@ def rat3d_softmask_fwd(count, dtype, z, t, out, m, stream=None):
 def rat3d_softmask_bwd(count, dtype, dout, t, m, dt, accumulate_dt, dz, stream=None):
     _check(lib().rat3d_softmask_bwd(count, dtype, _p(dout), _p(t), _p(m), _p(dt),
                                     int(accumulate_dt), _p(dz), _stream(stream)))
+
+
+# ---------------------------------------------------------------- voxel self-attention
+def qk_desc(n, heads, kv_heads, head_dim, d, h, w, dtype, rot=(0, 0, 0), origin=(0, 0, 0),
+            base=100.0, eps=1e-6, norm=True, q_stride=0, k_stride=0, oq_stride=0, ok_stride=0):
+    return QkDesc(n, heads, kv_heads, head_dim, d, h, w, *rot, *origin, int(norm), base, eps,
+                  q_stride, k_stride, oq_stride, ok_stride, dtype)
+
+
+def rat3d_rope_table_size(desc):
+    return lib().rat3d_rope_table_size(ctypes.byref(desc))
+
+
+def rat3d_rope_table(desc, table, stream=None):
+    _check(lib().rat3d_rope_table(ctypes.byref(desc), _p(table), _stream(stream)))
+
+
+def rat3d_qk_norm_rope_workspace_size(desc):
+    return lib().rat3d_qk_norm_rope_workspace_size(ctypes.byref(desc))
+
+
+def rat3d_qk_norm_rope_fwd(desc, q, k, gamma_q, gamma_k, table, oq, ok, stream=None):
+    _check(lib().rat3d_qk_norm_rope_fwd(ctypes.byref(desc), _p(q), _p(k), _p(gamma_q),
+                                        _p(gamma_k), _p(table), _p(oq), _p(ok),
+                                        _stream(stream)))
+
+
+def rat3d_qk_norm_rope_bwd(desc, doq, dok, q, k, gamma_q, gamma_k, table, dq, dk, dgamma_q,
+                           dgamma_k, accumulate, ws, ws_bytes, stream=None):
+    _check(lib().rat3d_qk_norm_rope_bwd(ctypes.byref(desc), _p(doq), _p(dok), _p(q), _p(k),
+                                        _p(gamma_q), _p(gamma_k), _p(table), _p(dq), _p(dk),
+                                        _p(dgamma_q), _p(dgamma_k), int(accumulate), _p(ws),
+                                        ws_bytes, _stream(stream)))
+
+
+def attention_desc(n, heads, kv_heads, head_dim, tq, tk, dtype, scale=0.0, q_stride=0,
+                   k_stride=0, v_stride=0, o_stride=0):
+    return AttentionDesc(n, heads, kv_heads, head_dim, tq, tk, scale, q_stride, k_stride,
+                         v_stride, o_stride, dtype)
+
+
+def rat3d_attention_workspace_size(desc, pass_):
+    return lib().rat3d_attention_workspace_size(ctypes.byref(desc), pass_)
+
+
+def rat3d_attention_fwd(desc, q, k, v, mask, o, lse, ws, ws_bytes, stream=None):
+    _check(lib().rat3d_attention_fwd(ctypes.byref(desc), _p(q), _p(k), _p(v), _p(mask), _p(o),
+                                     _p(lse), _p(ws), ws_bytes, _stream(stream)))
+
+
+def rat3d_attention_bwd(desc, dout, q, k, v, mask, o, lse, dq, dk, dv, ws, ws_bytes,
+                        stream=None):
+    _check(lib().rat3d_attention_bwd(ctypes.byref(desc), _p(dout), _p(q), _p(k), _p(v),
+                                     _p(mask), _p(o), _p(lse), _p(dq), _p(dk), _p(dv), _p(ws),
+                                     ws_bytes, _stream(stream)))
+
+
+def dropout_desc(count, p, dtype, seed=0, unit=1):
+    return DropoutDesc(count, unit, p, seed & ((1 << 64) - 1), dtype)
+
+
+def rat3d_dropout_fwd(desc, step, step_dev, x, residual, y, stream=None):
+    _check(lib().rat3d_dropout_fwd(ctypes.byref(desc), step, _p(step_dev), _p(x), _p(residual),
+                                   _p(y), _stream(stream)))
+
+
+def rat3d_dropout_bwd(desc, step, step_dev, dy, dx, accumulate, stream=None):
+    _check(lib().rat3d_dropout_bwd(ctypes.byref(desc), step, _p(step_dev), _p(dy), _p(dx),
+                                   int(accumulate), _stream(stream)))
 
 
 # ---------------------------------------------------------------- head, sgd

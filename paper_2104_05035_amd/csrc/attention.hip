@@ -42,6 +42,31 @@ template <typename T> struct Mm;
 template <> struct Mm<bf16> {
     typedef bf16x8 frag;
     static constexpr int kR = 16, kT = 16, kPer = 8;
+    // The second operands that add, from a fragment of row constants, the first
+    // (slots 0 to 2) or the second (slots 3 to 5) constant of each row to a product.
+    __device__ __forceinline__ static frag pick(int second, int half) {
+        frag f;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = (__bf16)(half == 0 && j / 3 == second ? 1.f : 0.f);
+        return f;
+    }
+    __device__ __forceinline__ static f32x16 add_row(frag a, frag b, f32x16 c) { return mul(a, b, c); }
+    // a row's two constants as a lane of such a fragment: three bfloat16 terms each,
+    // which hold a float32 value to its last bit or next to it
+    __device__ __forceinline__ static u32x4 rows(float x, float y, int half) {
+        if (half) return u32x4{0, 0, 0, 0};
+        bf16 v[8] = {};
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            v[j] = f2bf(x);
+            x -= bf2f(v[j]);
+            v[3 + j] = f2bf(y);
+            y -= bf2f(v[3 + j]);
+        }
+        u32x4 u;
+        __builtin_memcpy(&u, v, 16);
+        return u;
+    }
     __device__ __forceinline__ static f32x16 mul(frag a, frag b, f32x16 c) {
         return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
     }
@@ -49,6 +74,15 @@ template <> struct Mm<bf16> {
 template <> struct Mm<float> {
     typedef f32x4 frag;
     static constexpr int kR = 8, kT = 8, kPer = 4;
+    __device__ __forceinline__ static frag pick(int second, int half) {
+        return frag{half == second ? 1.f : 0.f, 0.f, 0.f, 0.f};
+    }
+    __device__ __forceinline__ static f32x16 add_row(frag a, frag b, f32x16 c) {
+        return __builtin_amdgcn_mfma_f32_32x32x2f32(a[0], b[0], c, 0, 0, 0);
+    }
+    __device__ __forceinline__ static u32x4 rows(float x, float y, int half) {
+        return u32x4{__float_as_uint(half ? y : x), 0, 0, 0};
+    }
     __device__ __forceinline__ static f32x16 mul(frag a, frag b, f32x16 c) {
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[0], b[0], c, 0, 0, 0);
         c = __builtin_amdgcn_mfma_f32_32x32x2f32(a[1], b[1], c, 0, 0, 0);
@@ -132,8 +166,8 @@ struct PackJob {
     const void* src;     // [n][heads * D][tokens], volumes `stride` apart
     const void* other;   // o, where src is dout: D = sum over channels of src * other
     const float* lse;
-    void* r;             // form R, or null
-    void* t;             // form T, or null
+    u32x4* rec;          // records of 32 tokens, `units` 16-byte units each:
+    int units, r, t, x;  // where forms R and T and the row constants lie, or -1
     float* lse2;         // lse in units of log 2, padded with +infinity
     float* delta;        // D, padded with 0
     const int* idx;      // live tokens, or null
@@ -145,6 +179,7 @@ struct PackJob {
 struct PackArgs {
     PackJob job[4];
     int jobs, D, DB;
+    float scale;
 };
 
 constexpr int kPackTok = 64;
@@ -185,43 +220,48 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     }
     part[sub][col] = d;
     __syncthreads();
-    if (J.delta && threadIdx.x < kPackTok) {
-        const int64_t at = (int64_t)nh * J.tiles * kPackTok + t0 + threadIdx.x;
-        J.delta[at] = (part[0][threadIdx.x] + part[1][threadIdx.x]) +
-                      (part[2][threadIdx.x] + part[3][threadIdx.x]);
-        // without any key lse is -infinity and no key reads it; behind the last
-        // query +infinity makes every probability 0
-        J.lse2[at] = in ? J.lse[(int64_t)nh * J.tokens + t0 + threadIdx.x] * kLog2e : INFINITY;
+    const int64_t blk0 = ((int64_t)nh * J.tiles + tl) * 2;  // record of the first token
+    if (J.delta && threadIdx.x < 2 * kPackTok) {
+        const int tk = threadIdx.x & 63, half = threadIdx.x >> 6;
+        const bool on = t0 + tk < live;
+        const float d = (part[0][tk] + part[1][tk]) + (part[2][tk] + part[3][tk]);
+        const float e = on ? J.lse[(int64_t)nh * J.tokens + t0 + tk] : -INFINITY;
+        if (half == 0) {
+            const int64_t at = (int64_t)nh * J.tiles * kPackTok + t0 + tk;
+            J.delta[at] = d;
+            J.lse2[at] = on ? e * kLog2e : INFINITY;
+        }
+        // Row constants of the products with these rows: -lse in units of the scores,
+        // and -D.  Behind the last query, and where a query has no key, a number so low
+        // that its probabilities are 0, finite because it is multiplied by 0 elsewhere.
+        J.rec[(blk0 + (tk >> 5)) * J.units + J.x + half * 32 + (tk & 31)] =
+            M::rows(e == -INFINITY ? -1e30f : -e / a.scale, -d, half);
     }
     // fragments: 2 blocks of 32 tokens x Dp, 16 bytes a lane
-    const int units = 2 * 32 * Dp / M::kPer;  // 16-byte units of one form
-    const int64_t out0 = ((int64_t)nh * J.tiles + tl) * units;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int frags = units / 64;
-    for (int f = wave; f < frags; f += 4) {
-        typedef __attribute__((ext_vector_type(4))) uint32_t unit_t;
-        if (J.r) {
-            const int per = Dp / M::kR;  // fragments of one block
-            const int tk = (f / per) * 32 + (lane & 31);
-            const int ch = (f % per) * M::kR + (lane >> 5) * M::kPer;
+    const int per = Dp / M::kR;  // fragments of one block and form
+    for (int f = wave; f < 2 * per; f += 4) {
+        const int blk = f / per, g = f % per;
+        u32x4* to = J.rec + (blk0 + blk) * J.units + g * 64 + lane;
+        if (J.r >= 0) {
+            const int ch = g * M::kR + (lane >> 5) * M::kPer;
             T v[M::kPer];
 #pragma unroll
-            for (int j = 0; j < M::kPer; ++j) v[j] = tile[(ch + j) * ROW + tk];
-            unit_t u;
+            for (int j = 0; j < M::kPer; ++j) v[j] = tile[(ch + j) * ROW + blk * 32 + (lane & 31)];
+            u32x4 u;
             __builtin_memcpy(&u, v, 16);
-            ((unit_t*)J.r)[out0 + f * 64 + lane] = u;
+            to[J.r] = u;
         }
-        if (J.t) {
-            const int per = 32 / M::kT * a.DB;
-            const int blk = f / per, w = f % per / a.DB, e = f % a.DB;
+        if (J.t >= 0) {
+            const int w = g / a.DB, e = g % a.DB;
             const int ch = e * 32 + (lane & 31);
             T v[M::kPer];
 #pragma unroll
             for (int j = 0; j < M::kPer; ++j)
                 v[j] = tile[ch * ROW + blk * 32 + w * M::kT + 8 * (j / 4) + 4 * (lane >> 5) + j % 4];
-            unit_t u;
+            u32x4 u;
             __builtin_memcpy(&u, v, 16);
-            ((unit_t*)J.t)[out0 + f * 64 + lane] = u;
+            to[J.t] = u;
         }
     }
 }
@@ -231,7 +271,7 @@ struct AttnArgs {
     const void* q;  // forward only: queries as given
     void* o;
     float* lse;
-    const uint4 *kr, *kt, *vr, *vt, *qr, *qt, *or_, *ot;  // packed operands
+    const u32x4 *kv_rec, *q_rec;  // records of 32 keys, of 32 queries
     const float *lse2, *delta;
     const int *idx, *count;
     void *dq, *dk, *dv;
@@ -248,16 +288,16 @@ struct AttnArgs {
 // multiplied.
 template <int U> struct Stage {
     static constexpr int N = (U + 255) / 256;
-    uint4 v[N];
+    u32x4 v[N];
     __device__ __forceinline__ static bool mine(int i) {
         return (i + 1) * 256 <= U || i * 256 + (int)threadIdx.x < U;
     }
-    __device__ __forceinline__ void load(const uint4* __restrict__ p) {
+    __device__ __forceinline__ void load(const u32x4* __restrict__ p) {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (mine(i)) v[i] = p[i * 256 + threadIdx.x];
     }
-    __device__ __forceinline__ void store(uint4* s) const {
+    __device__ __forceinline__ void store(u32x4* s) const {
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (mine(i)) s[i * 256 + threadIdx.x] = v[i];
@@ -265,7 +305,7 @@ template <int U> struct Stage {
 };
 
 template <typename T>
-__device__ __forceinline__ typename Mm<T>::frag frag_of(const uint4* s, int f) {
+__device__ __forceinline__ typename Mm<T>::frag frag_of(const u32x4* s, int f) {
     return __builtin_bit_cast(typename Mm<T>::frag, s[f * 64 + (threadIdx.x & 63)]);
 }
 
@@ -297,16 +337,16 @@ __device__ __forceinline__ void split_range(int64_t live, int step, int splits, 
 }
 
 // ------------------------------------------------------------------ forward
-// A workgroup: 128 queries of one head, 32 a wave as columns; KB x 32 keys a turn.
-template <typename T, int DB, int KB, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a) {
+// A workgroup: 128 CB queries of one head, 32 CB a wave as columns; KB x 32 keys a turn.
+template <typename T, int DB, int CB, int KB, bool SPLIT>
+__global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k(AttnArgs a) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
     constexpr int NR = 32 * DB / M::kR;      // fragments of 32 tokens, form R
     constexpr int NT = 32 / M::kT;           // contraction steps of 32 tokens, form T
     constexpr int NF = 32 * DB / M::kPer * 32 / 64;  // fragments of 32 tokens (either form)
-    constexpr int U = KB * NF * 64;          // units of one operand's tile
-    __shared__ uint4 lds[2][2][U];
+    constexpr int U = 2 * NF * 64;           // units of a record: K in form R, V in form T
+    __shared__ u32x4 lds[2][KB * U];
     int bid = xcd_remap(blockIdx.x, gridDim.x);
     const int tile = bid % a.tiles;
     bid /= a.tiles;
@@ -316,47 +356,55 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a) {
     const int kvh = vol * a.kv + h / (a.heads / a.kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t live = a.count ? a.count[vol] : a.tk;
-    const int64_t qt = (int64_t)tile * 128 + wave * 32 + (lane & 31);
-    const bool in = qt < a.tq;
+    const int64_t q0 = ((int64_t)tile * 4 + wave) * 32 * CB + (lane & 31);
 
-    frag qf[NR];
-    load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq + qt, a.tq, a.D,
-                     in, qf);
+    frag qf[CB][NR];
+#pragma unroll
+    for (int c = 0; c < CB; ++c)
+        load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq + q0 + 32 * c,
+                         a.tq, a.D, q0 + 32 * c < a.tq, qf[c]);
 
-    f32x16 acc[DB];
+    f32x16 acc[CB][DB];
+    float m[CB], l4[CB][4];  // the running reference and the sum, of this lane's rows
 #pragma unroll
-    for (int e = 0; e < DB; ++e)
+    for (int c = 0; c < CB; ++c) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
-    float m = -INFINITY, l = 0.f;
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c][e][i] = 0.f;
+        m[c] = -INFINITY;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l4[c][i] = 0.f;
+    }
 
     int b0, b1;
     split_range(live, 32 * KB, SPLIT ? a.splits : 1, sp, b0, b1);
-    const uint4* kp = a.kr + ((int64_t)kvh * (a.tkp / 32) + (int64_t)b0 * KB) * NF * 64;
-    const uint4* vp = a.vt + ((int64_t)kvh * (a.tkp / 32) + (int64_t)b0 * KB) * NF * 64;
-    Stage<U> ks, vs;
+    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + (int64_t)b0 * KB) * U;
+    Stage<KB * U> next;
     if (b0 < b1) {
-        ks.load(kp);
-        vs.load(vp);
-        ks.store(lds[0][0]);
-        vs.store(lds[0][1]);
+        next.load(rec);
+        next.store(lds[0]);
     }
     __syncthreads();
     for (int b = b0; b < b1; ++b) {
         const int buf = (b - b0) & 1;
         if (b + 1 < b1) {
-            kp += U;
-            vp += U;
-            ks.load(kp);
-            vs.load(vp);
+            rec += KB * U;
+            next.load(rec);
         }
-        f32x16 s[KB];
+        f32x16 s[CB][KB];
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) s[k][i] = 0.f;
+            for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int f = 0; f < NR; ++f) s[k] = M::mul(frag_of<T>(lds[buf][0], k * NR + f), qf[f], s[k]);
+                for (int i = 0; i < 16; ++i) s[c][k][i] = 0.f;
+#pragma unroll
+            for (int f = 0; f < NR; ++f) {
+                const frag ka = frag_of<T>(lds[buf] + k * U, f);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) s[c][k] = M::mul(ka, qf[c][f], s[c][k]);
+            }
         }
         if ((int64_t)(b + 1) * 32 * KB > live) {  // the last tile: rows behind the last key
             const int left = (int)(live - (int64_t)b * 32 * KB);
@@ -364,83 +412,106 @@ __global__ __launch_bounds__(256, 2) void attn_fwd_k(AttnArgs a) {
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= left) s[k][i] = -INFINITY;
+                    if (k * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= left) {
+#pragma unroll
+                        for (int c = 0; c < CB; ++c) s[c][k][i] = -INFINITY;
+                    }
         }
-        float t = s[0][0];
+        float t[CB];
+        bool grew = false;
 #pragma unroll
-        for (int k = 0; k < KB; ++k)
+        for (int c = 0; c < CB; ++c) {
+            float x = s[c][0][0];
 #pragma unroll
-            for (int i = 0; i < 16; ++i) t = fmaxf(t, s[k][i]);
-        float ta, tb;
-        halves(t, ta, tb);
-        t = fmaxf(ta, tb) * a.c;
+            for (int k = 0; k < KB; ++k)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) x = fmaxf(x, s[c][k][i]);
+            float xa, xb;
+            halves(x, xa, xb);
+            t[c] = fmaxf(xa, xb) * a.c;
+            grew = grew || t[c] > m[c] + 8.f;
+        }
         // The reference of the exponentials follows the maximum only where it grew by
         // more than 8 (in log 2): probabilities then stay below 2^8, which neither
         // bfloat16 nor the float32 sums mind, and the sums are rescaled rarely.
-        if (__any(t > m + 8.f)) {
-            const float to = t > m + 8.f ? t : m;
-            const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
-            m = to;
-            l *= f;
+        if (__any(grew)) {
 #pragma unroll
-            for (int e = 0; e < DB; ++e)
+            for (int c = 0; c < CB; ++c) {
+                const float to = t[c] > m[c] + 8.f ? t[c] : m[c];
+                const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
+                m[c] = to;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[e][i] *= f;
+                for (int i = 0; i < 4; ++i) l4[c][i] *= f;
+#pragma unroll
+                for (int e = 0; e < DB; ++e)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) acc[c][e][i] *= f;
+            }
         }
-        const float ref = m == -INFINITY ? 0.f : m;
+        float ref[CB];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) ref[c] = m[c] == -INFINITY ? 0.f : m[c];
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                s[k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][i], a.c, -ref));
-                l += s[k][i];
-            }
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    s[c][k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][k][i], a.c, -ref[c]));
+                    l4[c][i % 4] += s[c][k][i];
+                }
 #pragma unroll
             for (int w = 0; w < NT; ++w) {
-                const frag p = to_frag<T>(s[k], w);
+                frag p[CB];
 #pragma unroll
-                for (int e = 0; e < DB; ++e)
-                    acc[e] = M::mul(frag_of<T>(lds[buf][1], (k * NT + w) * DB + e), p, acc[e]);
+                for (int c = 0; c < CB; ++c) p[c] = to_frag<T>(s[c][k], w);
+#pragma unroll
+                for (int e = 0; e < DB; ++e) {
+                    const frag va = frag_of<T>(lds[buf] + k * U, NF + w * DB + e);
+#pragma unroll
+                    for (int c = 0; c < CB; ++c) acc[c][e] = M::mul(va, p[c], acc[c][e]);
+                }
             }
         }
-        if (b + 1 < b1) {
-            ks.store(lds[buf ^ 1][0]);
-            vs.store(lds[buf ^ 1][1]);
-        }
+        if (b + 1 < b1) next.store(lds[buf ^ 1]);
         __syncthreads();
     }
-    float la, lb;
-    halves(l, la, lb);
-    l = la + lb;
-    if (!in) return;
     const int half = lane >> 5;
-    if (SPLIT) {
-        float* st = a.stat + ((int64_t)nh * a.splits + sp) * 2 * a.tqp + qt;
-        if (half == 0) {
-            st[0] = m;
-            st[a.tqp] = l;
+#pragma unroll
+    for (int c = 0; c < CB; ++c) {
+        float la, lb;
+        halves((l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), la, lb);
+        const float l = la + lb;
+        const int64_t qt = q0 + 32 * c;
+        if (qt >= a.tq) continue;
+        if (SPLIT) {
+            float* st = a.stat + ((int64_t)nh * a.splits + sp) * 2 * a.tqp + qt;
+            if (half == 0) {
+                st[0] = m[c];
+                st[a.tqp] = l;
+            }
+            float* to = a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt;
+#pragma unroll
+            for (int e = 0; e < DB; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                    if (ch < a.D) to[ch * a.tqp] = acc[c][e][i];
+                }
+        } else {
+            const float inv = l == 0.f ? 0.f : 1.f / l;
+            T* to = (T*)a.o + vol * a.o_stride + (int64_t)h * a.D * a.tq + qt;
+#pragma unroll
+            for (int e = 0; e < DB; ++e)
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                    if (ch < a.D) Elt<T>::st(to + ch * a.tq, acc[c][e][i] * inv);
+                }
+            if (a.lse && half == 0)
+                a.lse[(int64_t)nh * a.tq + qt] =
+                    l == 0.f ? -INFINITY : (m[c] + __builtin_amdgcn_logf(l)) * kLn2;
         }
-        float* to = a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt;
-#pragma unroll
-        for (int e = 0; e < DB; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                if (ch < a.D) to[ch * a.tqp] = acc[e][i];
-            }
-    } else {
-        const float inv = l == 0.f ? 0.f : 1.f / l;
-        T* to = (T*)a.o + vol * a.o_stride + (int64_t)h * a.D * a.tq + qt;
-#pragma unroll
-        for (int e = 0; e < DB; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                if (ch < a.D) Elt<T>::st(to + ch * a.tq, acc[e][i] * inv);
-            }
-        if (a.lse && half == 0)
-            a.lse[(int64_t)nh * a.tq + qt] =
-                l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
     }
 }
 
@@ -477,111 +548,40 @@ __global__ __launch_bounds__(256) void attn_join_k(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------ backward
-// dK, dV: a workgroup keeps 128 live keys of one key head, 32 a wave as columns, and
-// walks the queries of every head of the group, 32 a turn as rows.
+// Records of the backward, in fragments: 32 keys are K and V in form R and K in form
+// T; 32 queries are Q and dO in form R, the row constants, and Q and dO in form T.
+template <typename T, int DB> struct Rec {
+    static constexpr int NF = 32 * DB / Mm<T>::kPer * 32 / 64;  // fragments of one form
+    static constexpr int kK = 0, kV = NF, kKt = 2 * NF, kKeys = 3 * NF * 64;
+    static constexpr int kQ = 0, kO = NF, kX = 2 * NF, kQt = 2 * NF + 1, kOt = 3 * NF + 1;
+    static constexpr int kQueries = (4 * NF + 1) * 64;  // units
+};
+
+// Where a workgroup of the dK/dV kernels stands.
+struct DkvPlace {
+    int vol, hk, kvh, sp, tile;
+    int64_t live;
+    __device__ __forceinline__ DkvPlace(const AttnArgs& a, bool split) {
+        int bid = xcd_remap(blockIdx.x, gridDim.x);
+        tile = bid % a.tiles;
+        bid /= a.tiles;
+        sp = split ? bid % a.splits : 0;
+        kvh = split ? bid / a.splits : bid;
+        vol = kvh / a.kv;
+        hk = kvh - vol * a.kv;
+        live = a.count ? a.count[vol] : a.tk;
+    }
+};
+
+// The sums of 32 keys (block kb) leave: partial sums of a split, or the gradients.
 template <typename T, int DB, bool SPLIT>
-__global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a) {
-    typedef Mm<T> M;
-    typedef typename M::frag frag;
-    constexpr int NR = 32 * DB / M::kR, NT = 32 / M::kT, NF = 32 * DB / M::kPer * 32 / 64;
-    constexpr int U = NF * 64;
-    __shared__ uint4 lds[2][4][U];
-    int bid = xcd_remap(blockIdx.x, gridDim.x);
-    const int tile = bid % a.tiles;
-    bid /= a.tiles;
-    const int sp = SPLIT ? bid % a.splits : 0;
-    const int kvh = SPLIT ? bid / a.splits : bid;
-    const int vol = kvh / a.kv, hk = kvh - vol * a.kv;
-    const int grp = a.heads / a.kv;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t live = a.count ? a.count[vol] : a.tk;
-    if ((int64_t)tile * 128 >= live) return;
-    const int64_t kb = (int64_t)tile * 4 + wave;  // block of 32 keys
-    const bool have = kb * 32 < live;             // else packed blocks need not exist
-
-    frag kf[NR], vf[NR];
-#pragma unroll
-    for (int f = 0; f < NR; ++f) {
-        kf[f] = frag{};
-        vf[f] = frag{};
-        if (have) {
-            kf[f] = frag_of<T>(a.kr + ((int64_t)kvh * (a.tkp / 32) + kb) * U, f);
-            vf[f] = frag_of<T>(a.vr + ((int64_t)kvh * (a.tkp / 32) + kb) * U, f);
-        }
-    }
-    f32x16 dk[DB], dv[DB];
-#pragma unroll
-    for (int e = 0; e < DB; ++e)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) dk[e][i] = dv[e][i] = 0.f;
-
-    // turns: the query blocks of the group's heads one after another
-    const int nqb = (int)((a.tq + 31) / 32);
-    const int turns = nqb * grp;
-    const int per = SPLIT ? (turns + a.splits - 1) / a.splits : turns;
-    const int i0 = SPLIT ? (sp * per < turns ? sp * per : turns) : 0;
-    const int i1 = i0 + per < turns ? i0 + per : turns;
-    Stage<U> s0, s1, s2, s3;
-    auto fetch = [&](int i) {
-        const int g = i / nqb, b = i - g * nqb;
-        const int64_t at = ((int64_t)(vol * a.heads + hk * grp + g) * (a.tqp / 32) + b) * U;
-        s0.load(a.qr + at);
-        s1.load(a.qt + at);
-        s2.load(a.or_ + at);
-        s3.load(a.ot + at);
-    };
-    auto put = [&](int buf) {
-        s0.store(lds[buf][0]);
-        s1.store(lds[buf][1]);
-        s2.store(lds[buf][2]);
-        s3.store(lds[buf][3]);
-    };
-    if (i0 < i1) {
-        fetch(i0);
-        put(0);
-    }
-    __syncthreads();
-    for (int i = i0; i < i1; ++i) {
-        const int buf = (i - i0) & 1;
-        const int g = i / nqb, b = i - g * nqb;
-        const int64_t row = (int64_t)(vol * a.heads + hk * grp + g) * a.tqp + b * 32 + 4 * (lane >> 5);
-        f32x4 ls[4], de[4];
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            ls[r] = *reinterpret_cast<const f32x4*>(a.lse2 + row + 8 * r);
-            de[r] = *reinterpret_cast<const f32x4*>(a.delta + row + 8 * r);
-        }
-        if (i + 1 < i1) fetch(i + 1);
-        f32x16 s, dp;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
-#pragma unroll
-        for (int f = 0; f < NR; ++f) {
-            s = M::mul(frag_of<T>(lds[buf][0], f), kf[f], s);
-            dp = M::mul(frag_of<T>(lds[buf][2], f), vf[f], dp);
-        }
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -ls[r / 4][r % 4]));
-            dp[r] = s[r] * (dp[r] - de[r / 4][r % 4]);
-        }
-#pragma unroll
-        for (int w = 0; w < NT; ++w) {
-            const frag p = to_frag<T>(s, w), d = to_frag<T>(dp, w);
-#pragma unroll
-            for (int e = 0; e < DB; ++e) {
-                dv[e] = M::mul(frag_of<T>(lds[buf][3], w * DB + e), p, dv[e]);
-                dk[e] = M::mul(frag_of<T>(lds[buf][1], w * DB + e), d, dk[e]);
-            }
-        }
-        if (i + 1 < i1) put(buf ^ 1);
-        __syncthreads();
-    }
+__device__ __forceinline__ void dkv_store(const AttnArgs& a, const DkvPlace& p, int64_t kb,
+                                          const f32x16 (&dk)[DB], const f32x16 (&dv)[DB]) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
     const int64_t j = kb * 32 + (lane & 31);
-    if (j >= live) return;
-    const int half = lane >> 5;
+    if (j >= p.live) return;
     if (SPLIT) {
-        float* to = a.part + ((int64_t)kvh * a.splits + sp) * 2 * a.D * a.tkp + j;
+        float* to = a.part + ((int64_t)p.kvh * a.splits + p.sp) * 2 * a.D * a.tkp + j;
 #pragma unroll
         for (int e = 0; e < DB; ++e)
 #pragma unroll
@@ -593,9 +593,9 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a)
                 }
             }
     } else {
-        const int64_t tok = a.idx ? a.idx[vol * a.tkp + j] : j;
-        T* tk = (T*)a.dk + vol * a.k_stride + (int64_t)hk * a.D * a.tk + tok;
-        T* tv = (T*)a.dv + vol * a.v_stride + (int64_t)hk * a.D * a.tk + tok;
+        const int64_t tok = a.idx ? a.idx[p.vol * a.tkp + j] : j;
+        T* tk = (T*)a.dk + p.vol * a.k_stride + (int64_t)p.hk * a.D * a.tk + tok;
+        T* tv = (T*)a.dv + p.vol * a.v_stride + (int64_t)p.hk * a.D * a.tk + tok;
 #pragma unroll
         for (int e = 0; e < DB; ++e)
 #pragma unroll
@@ -609,15 +609,261 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a)
     }
 }
 
-// dQ: a workgroup keeps 128 queries of one head, 32 a wave as columns, and walks the
-// live keys, 32 a turn as rows.
+// dK, dV: a workgroup keeps 128 live keys of one key head, 32 a wave as columns, and
+// walks the queries of every head of the group, 32 a turn as rows.  Scores leave their
+// product as s - lse / scale and dO V^T as dO V^T - D: both constants of a row are added
+// by the matrix instruction, from a fragment of the record.
 template <typename T, int DB, bool SPLIT>
+__global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a) {
+    typedef Mm<T> M;
+    typedef typename M::frag frag;
+    typedef Rec<T, DB> R;
+    constexpr int NF = R::NF, NT = 32 / M::kT, U = R::kQueries;
+    __shared__ u32x4 lds[2][U];
+    const DkvPlace at(a, SPLIT);
+    if ((int64_t)at.tile * 128 >= at.live) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t kb = (int64_t)at.tile * 4 + wave;  // block of 32 keys
+
+    frag kf[NF], vf[NF];
+#pragma unroll
+    for (int f = 0; f < NF; ++f) {
+        kf[f] = frag{};
+        vf[f] = frag{};
+        if (kb * 32 < at.live) {  // else the record need not exist
+            const u32x4* rec = a.kv_rec + ((int64_t)at.kvh * (a.tkp / 32) + kb) * R::kKeys;
+            kf[f] = frag_of<T>(rec, R::kK + f);
+            vf[f] = frag_of<T>(rec, R::kV + f);
+        }
+    }
+    const frag one_s = M::pick(0, lane >> 5), one_d = M::pick(1, lane >> 5);
+    f32x16 dk[DB], dv[DB];
+#pragma unroll
+    for (int e = 0; e < DB; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) dk[e][i] = dv[e][i] = 0.f;
+
+    // turns: the records of the group's heads, one behind the other
+    const int grp = a.heads / a.kv;
+    const int turns = (int)(a.tqp / 32) * grp;
+    const int per = SPLIT ? (turns + a.splits - 1) / a.splits : turns;
+    const int i0 = SPLIT ? (at.sp * per < turns ? at.sp * per : turns) : 0;
+    const int i1 = i0 + per < turns ? i0 + per : turns;
+    const u32x4* rec =
+        a.q_rec + ((int64_t)(at.vol * a.heads + at.hk * grp) * (a.tqp / 32) + i0) * U;
+    Stage<U> next;
+    if (i0 < i1) {
+        next.load(rec);
+        next.store(lds[0]);
+    }
+    __syncthreads();
+    for (int i = i0; i < i1; ++i) {
+        const u32x4* cur = lds[(i - i0) & 1];
+        if (i + 1 < i1) {
+            rec += U;
+            next.load(rec);
+        }
+        f32x16 s, dp;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            s = M::mul(frag_of<T>(cur, R::kQ + f), kf[f], s);
+            dp = M::mul(frag_of<T>(cur, R::kO + f), vf[f], dp);
+        }
+        const frag x = frag_of<T>(cur, R::kX);
+        s = M::add_row(x, one_s, s);
+        dp = M::add_row(x, one_d, dp);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(s[r] * a.c);
+            dp[r] *= s[r];
+        }
+#pragma unroll
+        for (int w = 0; w < NT; ++w) {
+            const frag p = to_frag<T>(s, w), d = to_frag<T>(dp, w);
+#pragma unroll
+            for (int e = 0; e < DB; ++e) {
+                dv[e] = M::mul(frag_of<T>(cur, R::kOt + w * DB + e), p, dv[e]);
+                dk[e] = M::mul(frag_of<T>(cur, R::kQt + w * DB + e), d, dk[e]);
+            }
+        }
+        if (i + 1 < i1) next.store(lds[((i - i0) & 1) ^ 1]);
+        __syncthreads();
+    }
+    dkv_store<T, DB, SPLIT>(a, at, kb, dk, dv);
+}
+
+// The same in bfloat16 with 64 keys a wave, in two column blocks A and B, and the
+// phases of neighbouring turns laid over each other, so that the matrix cores work
+// while the vector ALU forms the other block's probabilities.  Turn i is
+//   X: dV, dK of B for turn i - 1, scores of B for turn i   beside   exp of A, turn i
+//   Y: dV, dK of A for turn i, scores of A for turn i + 1   beside   exp of B, turn i
+// A fragment read from LDS feeds both blocks (it stays in registers from Y to X, or
+// from X to Y): 8 (D <= 64: 17) reads for 20 (36) products of 32 cycles, where one
+// block a wave would ask LDS for as many cycles as the products take.  One wave a SIMD
+// holds all this (two at D <= 32); the order of instructions is pinned step by step.
+// Three LDS buffers: turn i reads T of record i and R of i + 1 and writes record i + 2.
+template <int DB, bool SPLIT>
+__global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a) {
+    typedef Mm<bf16> M;
+    typedef bf16x8 frag;
+    typedef Rec<bf16, DB> R;
+    constexpr int NF = R::NF, U = R::kQueries;
+    __shared__ u32x4 lds[3][U];
+    const DkvPlace at(a, SPLIT);
+    if ((int64_t)at.tile * 256 >= at.live) return;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t kb = ((int64_t)at.tile * 4 + wave) * 2;  // first block of 32 keys
+
+    frag kf[2][NF], vf[2][NF];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            kf[c][f] = frag{};
+            vf[c][f] = frag{};
+            if ((kb + c) * 32 < at.live) {  // else the record need not exist
+                const u32x4* rec = a.kv_rec + ((int64_t)at.kvh * (a.tkp / 32) + kb + c) * R::kKeys;
+                kf[c][f] = frag_of<bf16>(rec, R::kK + f);
+                vf[c][f] = frag_of<bf16>(rec, R::kV + f);
+            }
+        }
+    const frag one_s = M::pick(0, lane >> 5), one_d = M::pick(1, lane >> 5);
+    f32x16 dk[2][DB], dv[2][DB], s[2], dp[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[c][i] = dp[c][i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < DB; ++e) dk[c][e][i] = dv[c][e][i] = 0.f;
+        }
+    uint32_t pw[2][8], dw[2][8];  // probabilities and score gradients, two a word
+    frag qa[NF], oa[NF], xa, qt[NF], ot[NF];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) pw[1][i] = dw[1][i] = 0;
+#pragma unroll
+    for (int f = 0; f < NF; ++f) qt[f] = ot[f] = frag{};
+
+    const int grp = a.heads / a.kv;
+    const int turns = (int)(a.tqp / 32) * grp;
+    const int per = SPLIT ? (turns + a.splits - 1) / a.splits : turns;
+    const int i0 = SPLIT ? (at.sp * per < turns ? at.sp * per : turns) : 0;
+    const int i1 = i0 + per < turns ? i0 + per : turns;
+    const u32x4* rec =
+        a.q_rec + ((int64_t)(at.vol * a.heads + at.hk * grp) * (a.tqp / 32) + i0) * U;
+    Stage<U> next;
+
+    // one of the 2 NF products of dV and dK of block c
+    auto grad_step = [&](int c, int t) {
+        const int f = t >> 1, w = f / DB, e = f % DB;
+        const u32x4 p = t & 1 ? u32x4{dw[c][4 * w], dw[c][4 * w + 1], dw[c][4 * w + 2], dw[c][4 * w + 3]}
+                              : u32x4{pw[c][4 * w], pw[c][4 * w + 1], pw[c][4 * w + 2], pw[c][4 * w + 3]};
+        if (t & 1) dk[c][e] = M::mul(qt[f], __builtin_bit_cast(frag, p), dk[c][e]);
+        else dv[c][e] = M::mul(ot[f], __builtin_bit_cast(frag, p), dv[c][e]);
+    };
+    // one of the 2 NF + 2 products of the scores and of dO V^T of block c
+    auto score_step = [&](int c, int t) {
+        const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f,
+                             0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (t == 0) s[c] = M::mul(qa[0], kf[c][0], zero);
+        else if (t == 1) dp[c] = M::mul(oa[0], vf[c][0], zero);
+        else if (t == 2 * NF) s[c] = M::mul(xa, one_s, s[c]);
+        else if (t == 2 * NF + 1) dp[c] = M::mul(xa, one_d, dp[c]);
+        else if (t & 1) dp[c] = M::mul(oa[t >> 1], vf[c][t >> 1], dp[c]);
+        else s[c] = M::mul(qa[t >> 1], kf[c][t >> 1], s[c]);
+    };
+    // probabilities and score gradients of block c: the exponential of register r, and
+    // what follows it for register r - 1 (an exponential's result is not ready for the
+    // next instruction)
+    auto exp_step = [&](int c, int r) {
+        if (r < 16) s[c][r] = __builtin_amdgcn_exp2f(s[c][r] * a.c);
+        if (r == 0) return;
+        dp[c][r - 1] *= s[c][r - 1];
+        if (!(r & 1)) {
+            pw[c][(r >> 1) - 1] = pack_bf16x2(s[c][r - 2], s[c][r - 1]);
+            dw[c][(r >> 1) - 1] = pack_bf16x2(dp[c][r - 2], dp[c][r - 1]);
+            // formed here, not where it is used
+            asm volatile("" : "+v"(pw[c][(r >> 1) - 1]), "+v"(dw[c][(r >> 1) - 1]));
+        }
+    };
+    auto read_r = [&](const u32x4* b, int f) {
+        if (f < NF) qa[f] = frag_of<bf16>(b, R::kQ + f);
+        else if (f < 2 * NF) oa[f - NF] = frag_of<bf16>(b, R::kO + f - NF);
+        else xa = frag_of<bf16>(b, R::kX);
+    };
+    auto read_t = [&](const u32x4* b, int f) {
+        if (f < NF) ot[f] = frag_of<bf16>(b, R::kOt + f);
+        else qt[f - NF] = frag_of<bf16>(b, R::kQt + f - NF);
+    };
+    constexpr int N1 = 2 * NF, N2 = 2 * NF + 2, N = N1 + N2;  // products of X, as of Y
+
+    if (i0 < i1) {
+        next.load(rec);
+        next.store(lds[0]);
+        next.load(i0 + 1 < i1 ? rec + U : rec);
+        next.store(lds[1]);
+    }
+    const u32x4* last = rec + (int64_t)(i1 - i0 - 1) * U;
+    __syncthreads();
+    if (i0 < i1) {
+#pragma unroll
+        for (int f = 0; f < 2 * NF + 1; ++f) read_r(lds[0], f);
+#pragma unroll
+        for (int t = 0; t < N2; ++t) score_step(0, t);
+    }
+    int b0 = 0, b1 = 1, b2 = 2;  // buffers of records i, i + 1, i + 2
+    for (int i = i0; i < i1; ++i) {
+        // behind the last record it is taken again, so that no branch divides the turn:
+        // what is formed from it is not used
+        next.load(i + 2 < i1 ? rec + 2 * U : last);
+        // X
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if (t < N1) grad_step(1, t);
+            else score_step(1, t - N1);
+#pragma unroll
+            for (int r = 0; r < 17; ++r)
+                if (r * (N - 2) / 17 + 2 == t) exp_step(0, r);
+            if (t >= N1 && t - N1 < 2 * NF) read_t(lds[b0], t - N1);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int f = 0; f < 2 * NF + 1; ++f) read_r(lds[b1], f);
+        // Y
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if (t < N1) grad_step(0, t);
+            else score_step(0, t - N1);
+#pragma unroll
+            for (int r = 0; r < 17; ++r)
+                if (r * (N - 2) / 17 + 2 == t) exp_step(1, r);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        next.store(lds[b2]);
+        __syncthreads();
+        rec += U;
+        const int b = b0;
+        b0 = b1;
+        b1 = b2;
+        b2 = b;
+    }
+#pragma unroll
+    for (int t = 0; t < N1; ++t) grad_step(1, t);  // B of the last turn
+    dkv_store<bf16, DB, SPLIT>(a, at, kb, dk[0], dv[0]);
+    dkv_store<bf16, DB, SPLIT>(a, at, kb + 1, dk[1], dv[1]);
+}
+
+// dQ: a workgroup keeps 128 CB queries of one head, 32 CB a wave as columns, and walks
+// the live keys, 32 a turn as rows.
+template <typename T, int DB, int CB, bool SPLIT>
 __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
-    constexpr int NR = 32 * DB / M::kR, NT = 32 / M::kT, NF = 32 * DB / M::kPer * 32 / 64;
-    constexpr int U = NF * 64;
-    __shared__ uint4 lds[2][3][U];
+    typedef Rec<T, DB> R;
+    constexpr int NF = R::NF, NT = 32 / M::kT, U = R::kKeys;
+    __shared__ u32x4 lds[2][U];
     int bid = xcd_remap(blockIdx.x, gridDim.x);
     const int tile = bid % a.tiles;
     bid /= a.tiles;
@@ -627,92 +873,113 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
     const int kvh = vol * a.kv + h / (a.heads / a.kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t live = a.count ? a.count[vol] : a.tk;
-    const int64_t qb = (int64_t)tile * 4 + wave;
-    const bool have = qb * 32 < a.tqp;
-    frag qf[NR], of[NR];
+    const int64_t qb = ((int64_t)tile * 4 + wave) * CB;
+    frag qf[CB][NF], of[CB][NF];
+    float ls[CB], de[CB];
 #pragma unroll
-    for (int f = 0; f < NR; ++f) {
-        qf[f] = frag{};
-        of[f] = frag{};
-        if (have) {
-            qf[f] = frag_of<T>(a.qr + ((int64_t)nh * (a.tqp / 32) + qb) * U, f);
-            of[f] = frag_of<T>(a.or_ + ((int64_t)nh * (a.tqp / 32) + qb) * U, f);
+    for (int c = 0; c < CB; ++c) {
+        const bool have = (qb + c) * 32 < a.tqp;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            qf[c][f] = frag{};
+            of[c][f] = frag{};
+            if (have) {
+                const u32x4* rec = a.q_rec + ((int64_t)nh * (a.tqp / 32) + qb + c) * R::kQueries;
+                qf[c][f] = frag_of<T>(rec, R::kQ + f);
+                of[c][f] = frag_of<T>(rec, R::kO + f);
+            }
         }
+        const int64_t at = (int64_t)nh * a.tqp + (qb + c) * 32 + (lane & 31);
+        ls[c] = have ? a.lse2[at] : INFINITY;
+        de[c] = have ? a.delta[at] : 0.f;
     }
-    const int64_t qt = qb * 32 + (lane & 31);
-    const float ls = have ? a.lse2[(int64_t)nh * a.tqp + qt] : INFINITY;
-    const float de = have ? a.delta[(int64_t)nh * a.tqp + qt] : 0.f;
-    f32x16 dq[DB];
+    f32x16 dq[CB][DB];
 #pragma unroll
-    for (int e = 0; e < DB; ++e)
+    for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) dq[e][i] = 0.f;
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) dq[c][e][i] = 0.f;
     int b0, b1;
     split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
-    Stage<U> s0, s1, s2;
-    auto fetch = [&](int b) {
-        const int64_t at = ((int64_t)kvh * (a.tkp / 32) + b) * U;
-        s0.load(a.kr + at);
-        s1.load(a.kt + at);
-        s2.load(a.vr + at);
-    };
-    auto put = [&](int buf) {
-        s0.store(lds[buf][0]);
-        s1.store(lds[buf][1]);
-        s2.store(lds[buf][2]);
-    };
+    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
+    Stage<U> next;
     if (b0 < b1) {
-        fetch(b0);
-        put(0);
+        next.load(rec);
+        next.store(lds[0]);
     }
     __syncthreads();
     for (int b = b0; b < b1; ++b) {
-        const int buf = (b - b0) & 1;
-        if (b + 1 < b1) fetch(b + 1);
-        f32x16 s, dp;
+        const u32x4* cur = lds[(b - b0) & 1];
+        if (b + 1 < b1) {
+            rec += U;
+            next.load(rec);
+        }
+        f32x16 s[CB], dp[CB];
 #pragma unroll
-        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
+        for (int c = 0; c < CB; ++c)
 #pragma unroll
-        for (int f = 0; f < NR; ++f) {
-            s = M::mul(frag_of<T>(lds[buf][0], f), qf[f], s);
-            dp = M::mul(frag_of<T>(lds[buf][2], f), of[f], dp);
+            for (int r = 0; r < 16; ++r) s[c][r] = dp[c][r] = 0.f;
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            const frag ka = frag_of<T>(cur, R::kK + f), va = frag_of<T>(cur, R::kV + f);
+#pragma unroll
+            for (int c = 0; c < CB; ++c) {
+                s[c] = M::mul(ka, qf[c][f], s[c]);
+                dp[c] = M::mul(va, of[c][f], dp[c]);
+            }
+        }
+        frag df[CB][NT];
+#pragma unroll
+        for (int c = 0; c < CB; ++c) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                s[c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][r], a.c, -ls[c]));
+                dp[c][r] = s[c][r] * (dp[c][r] - de[c]);
+            }
         }
         // rows behind the last key have K = V = 0 and so give nothing to dq, as
         // long as their P stays finite, which exp(-lse) might not
         const int left = live - (int64_t)b * 32 < 32 ? (int)(live - (int64_t)b * 32) : 32;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -ls));
-            dp[r] = s[r] * (dp[r] - de);
-        }
         if (left < 32) {
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) dp[r] = 0.f;
+            for (int c = 0; c < CB; ++c)
+#pragma unroll
+                for (int r = 0; r < 16; ++r)
+                    if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) dp[c][r] = 0.f;
         }
 #pragma unroll
-        for (int w = 0; w < NT; ++w) {
-            const frag d = to_frag<T>(dp, w);
+        for (int c = 0; c < CB; ++c)
 #pragma unroll
-            for (int e = 0; e < DB; ++e)
-                dq[e] = M::mul(frag_of<T>(lds[buf][1], w * DB + e), d, dq[e]);
-        }
-        if (b + 1 < b1) put(buf ^ 1);
+            for (int w = 0; w < NT; ++w) df[c][w] = to_frag<T>(dp[c], w);
+#pragma unroll
+        for (int w = 0; w < NT; ++w)
+#pragma unroll
+            for (int e = 0; e < DB; ++e) {
+                const frag kt = frag_of<T>(cur, R::kKt + w * DB + e);
+#pragma unroll
+                for (int c = 0; c < CB; ++c) dq[c][e] = M::mul(kt, df[c][w], dq[c][e]);
+            }
+        if (b + 1 < b1) next.store(lds[((b - b0) & 1) ^ 1]);
         __syncthreads();
     }
-    if (qt >= a.tq) return;
     const int half = lane >> 5;
-    float* tp = SPLIT ? a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt : nullptr;
-    T* to = (T*)a.dq + vol * a.q_stride + (int64_t)h * a.D * a.tq + qt;
 #pragma unroll
-    for (int e = 0; e < DB; ++e)
+    for (int c = 0; c < CB; ++c) {
+        const int64_t qt = (qb + c) * 32 + (lane & 31);
+        if (qt >= a.tq) continue;
+        float* tp = SPLIT ? a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt : nullptr;
+        T* to = (T*)a.dq + vol * a.q_stride + (int64_t)h * a.D * a.tq + qt;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-            if (ch >= a.D) continue;
-            if (SPLIT) tp[ch * a.tqp] = dq[e][i] * a.scale;
-            else Elt<T>::st(to + ch * a.tq, dq[e][i] * a.scale);
-        }
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                if (ch >= a.D) continue;
+                if (SPLIT) tp[ch * a.tqp] = dq[c][e][i] * a.scale;
+                else Elt<T>::st(to + ch * a.tq, dq[c][e][i] * a.scale);
+            }
+    }
 }
 
 // Sums of the splits of a backward pass, in a fixed order: [nh][split][rows][tp] ->
@@ -760,18 +1027,25 @@ __global__ __launch_bounds__(256) void attn_dead_k(const uint8_t* __restrict__ m
 struct AttnPlan {
     int64_t tqp, tkp;
     int DB, es;
-    int fs, ks, qs;  // splits of the forward, of dK/dV, of dQ
-    size_t idx, count, kr, kt, vr, vt, qr, qt, orr, ot, lse2, delta, part, fpart, stat, bytes[2];
+    int fc, kc, qc;  // blocks of 32 kept tokens a wave: forward, dK/dV, dQ
+    int fs, ks, qs;  // splits of the same
+    size_t idx, count, kv_rec, q_rec, lse2, delta, part, fpart, stat, bytes[2];
 };
 
-// Ways to split a long walk: until there are two workgroups for each CU, but not
-// into pieces of fewer than `least` turns.
+// Ways to split a long walk: until there are about two workgroups for each CU, but
+// not into pieces of fewer than `least` turns.
 static int splits_for(int64_t groups, int64_t turns, int least) {
     const int64_t want = 2 * (int64_t)device_cus();
-    int64_t s = ceil_div(want, groups);
+    int64_t s = (want + groups / 2) / groups;
     if (s > turns / least) s = turns / least;
     if (s > 256) s = 256;
     return s < 2 ? 1 : (int)s;
+}
+
+// Two blocks of 32 kept tokens a wave in bfloat16, where the registers hold them and
+// there are workgroups enough: each fragment read from LDS then feeds two products.
+static int columns_for(const rat3d_attention_desc& d, int DB, int64_t groups) {
+    return d.dtype == RAT3D_BF16 && DB <= 2 && groups >= (int64_t)device_cus() ? 2 : 1;
 }
 
 static AttnPlan attn_plan(const rat3d_attention_desc& d) {
@@ -781,37 +1055,33 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
     p.tqp = ceil_div(d.tq, 64) * 64;
     p.tkp = ceil_div(d.tk, 64) * 64;
     const int64_t nq = (int64_t)d.n * d.heads, nk = (int64_t)d.n * d.kv_heads;
-    const int64_t qtiles = ceil_div(d.tq, 128), ktiles = ceil_div(d.tk, 128);
-    p.fs = splits_for(nq * qtiles, p.tkp / 64, 2);
-    p.qs = splits_for(nq * qtiles, p.tkp / 32, 4);
-    p.ks = splits_for(nk * ktiles, p.tqp / 32 * (d.heads / d.kv_heads), 4);
+    p.fc = p.qc = columns_for(d, p.DB, nq * ceil_div(d.tq, 256));
+    p.kc = columns_for(d, p.DB, nk * ceil_div(d.tk, 256));
+    p.fs = splits_for(nq * ceil_div(d.tq, 128 * p.fc), p.tkp / 64, 2);
+    p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, 4);
+    p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), 4);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t r = at;
         at += (bytes + 255) / 256 * 256;
         return r;
     };
-    const size_t qb = (size_t)nq * p.tqp * p.DB * 32 * p.es;
+    const size_t qb = (size_t)nq * p.tqp * p.DB * 32 * p.es;  // one form of the queries
     const size_t kb = (size_t)nk * p.tkp * p.DB * 32 * p.es;
     p.idx = take((size_t)d.n * p.tkp * sizeof(int));
     p.count = take((size_t)d.n * sizeof(int));
-    p.kr = take(kb);
     const size_t both = at;
     // forward
-    p.vt = take(kb);
+    p.kv_rec = take(2 * kb);
     if (p.fs > 1) {
         p.stat = take((size_t)nq * p.fs * 2 * p.tqp * sizeof(float));
         p.fpart = take((size_t)nq * p.fs * d.head_dim * p.tqp * sizeof(float));
     }
     p.bytes[0] = at;
-    // backward
+    // backward: records of three forms, and of four and the row constants
     at = both;
-    p.kt = take(kb);
-    p.vr = take(kb);
-    p.qr = take(qb);
-    p.qt = take(qb);
-    p.orr = take(qb);
-    p.ot = take(qb);
+    take(3 * kb);
+    p.q_rec = take(4 * qb + (size_t)nq * (p.tqp / 32) * 1024);
     p.lse2 = take((size_t)nq * p.tqp * sizeof(float));
     p.delta = take((size_t)nq * p.tqp * sizeof(float));
     const size_t kp = p.ks > 1 ? (size_t)nk * p.ks * 2 * d.head_dim * p.tkp * sizeof(float) : 0;
@@ -851,20 +1121,24 @@ static AttnArgs attn_args(const rat3d_attention_desc& d, const AttnPlan& p, char
     a.o_stride = d.o_stride ? d.o_stride : (int64_t)d.heads * d.head_dim * d.tq;
     a.k_stride = d.k_stride ? d.k_stride : (int64_t)d.kv_heads * d.head_dim * d.tk;
     a.v_stride = d.v_stride ? d.v_stride : (int64_t)d.kv_heads * d.head_dim * d.tk;
-    a.kr = (const uint4*)(w + p.kr);
+    a.kv_rec = (const u32x4*)(w + p.kv_rec);
     return a;
 }
 
-static PackJob pack_job(const void* src, int64_t stride, int64_t tokens, int heads, void* r,
-                        void* t, const AttnArgs& a, bool keys) {
+// r, t: fragments of the record where forms R and T begin, or -1.
+static PackJob pack_job(const void* src, int64_t stride, int64_t tokens, int heads,
+                        const u32x4* rec, int units, int r, int t, const AttnArgs& a, bool keys) {
     PackJob j = {};
     j.src = src;
     j.stride = stride;
     j.tokens = tokens;
     j.heads = heads;
     j.tiles = (int)ceil_div(tokens, kPackTok);
-    j.r = r;
-    j.t = t;
+    j.rec = const_cast<u32x4*>(rec);
+    j.units = units;
+    j.r = r < 0 ? -1 : r * 64;
+    j.t = t < 0 ? -1 : t * 64;
+    j.x = -1;
     if (keys) {
         j.idx = a.idx;
         j.count = a.count;
@@ -901,21 +1175,41 @@ static rat3d_status live_keys(const rat3d_attention_desc& d, const AttnPlan& p, 
         if (s_ != RAT3D_OK) return s_;        \
     } while (0)
 
+#define RAT3D_ATTN_LAUNCH(K, ...)                                                 \
+    do {                                                                          \
+        if (a.splits > 1) K<__VA_ARGS__, true><<<(unsigned)grid, 256, 0, st>>>(a); \
+        else K<__VA_ARGS__, false><<<(unsigned)grid, 256, 0, st>>>(a);            \
+    } while (0)
 template <typename T, int DB>
-static void fwd_launch(const AttnArgs& a, int64_t grid, hipStream_t st) {
+static void fwd_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
     constexpr int KB = sizeof(T) == 2 ? 2 : 1;
-    if (a.splits > 1) attn_fwd_k<T, DB, KB, true><<<(unsigned)grid, 256, 0, st>>>(a);
-    else attn_fwd_k<T, DB, KB, false><<<(unsigned)grid, 256, 0, st>>>(a);
+    if constexpr (sizeof(T) == 2 && DB <= 2) {
+        if (cb == 2) {
+            RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, 2, KB);
+            return;
+        }
+    }
+    RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, 1, KB);
 }
 template <typename T, int DB>
-static void dkv_launch(const AttnArgs& a, int64_t grid, hipStream_t st) {
-    if (a.splits > 1) attn_dkv_k<T, DB, true><<<(unsigned)grid, 256, 0, st>>>(a);
-    else attn_dkv_k<T, DB, false><<<(unsigned)grid, 256, 0, st>>>(a);
+static void dkv_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
+    if constexpr (sizeof(T) == 2 && DB <= 2) {
+        if (cb == 2) {
+            RAT3D_ATTN_LAUNCH(attn_dkv2_k, DB);
+            return;
+        }
+    }
+    RAT3D_ATTN_LAUNCH(attn_dkv_k, T, DB);
 }
 template <typename T, int DB>
-static void dq_launch(const AttnArgs& a, int64_t grid, hipStream_t st) {
-    if (a.splits > 1) attn_dq_k<T, DB, true><<<(unsigned)grid, 256, 0, st>>>(a);
-    else attn_dq_k<T, DB, false><<<(unsigned)grid, 256, 0, st>>>(a);
+static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
+    if constexpr (sizeof(T) == 2 && DB <= 2) {
+        if (cb == 2) {
+            RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB, 2);
+            return;
+        }
+    }
+    RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB, 1);
 }
 #define RAT3D_ATTN(F, dt, DB, ...)                                  \
     do {                                                            \
@@ -942,7 +1236,6 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
     a.q = q;
     a.o = o;
     a.lse = lse;
-    a.vt = (const uint4*)(w + p.vt);
     a.stat = (float*)(w + p.stat);
     a.part = (float*)(w + p.fpart);
     RAT3D_TRY(live_keys(d, p, w, mask, &a, st));
@@ -953,16 +1246,17 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
         pa.D = d.head_dim;
         pa.DB = p.DB;
         pa.jobs = 2;
-        pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, w + p.kr, nullptr, a, true);
-        pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, nullptr, w + p.vt, a, true);
+        const int nf = 2 * p.DB * p.es / 2;  // fragments of one form
+        pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, a.kv_rec, 128 * nf, 0, -1, a, true);
+        pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, a.kv_rec, 128 * nf, -1, nf, a, true);
         RAT3D_TRY(pack_launch(pa, d.n, d.dtype, st));
     }
     {
         ProfScope ps("attn_fwd", st, 4.0 * nq * d.tq * d.tk * d.head_dim, 0.0);
         a.splits = p.fs;
-        a.tiles = (int)ceil_div(d.tq, 128);
+        a.tiles = (int)ceil_div(d.tq, 128 * p.fc);
         const int64_t grid = (int64_t)d.n * d.heads * a.tiles * a.splits;
-        RAT3D_ATTN(fwd_launch, d.dtype, p.DB, a, grid, st);
+        RAT3D_ATTN(fwd_launch, d.dtype, p.DB, a, p.fc, grid, st);
     }
     if (p.fs > 1) {
         ProfScope ps("attn_join", st, 0.0, nq * d.tq * d.head_dim * (4.0 * p.fs + p.es));
@@ -981,12 +1275,7 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
     const AttnPlan p = attn_plan(d);
     char* w = (char*)ws;
     AttnArgs a = attn_args(d, p, w);
-    a.kt = (const uint4*)(w + p.kt);
-    a.vr = (const uint4*)(w + p.vr);
-    a.qr = (const uint4*)(w + p.qr);
-    a.qt = (const uint4*)(w + p.qt);
-    a.or_ = (const uint4*)(w + p.orr);
-    a.ot = (const uint4*)(w + p.ot);
+    a.q_rec = (const u32x4*)(w + p.q_rec);
     a.lse2 = (const float*)(w + p.lse2);
     a.delta = (const float*)(w + p.delta);
     a.part = (float*)(w + p.part);
@@ -1003,10 +1292,14 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
         pa.D = d.head_dim;
         pa.DB = p.DB;
         pa.jobs = 4;
-        pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, w + p.kr, w + p.kt, a, true);
-        pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, w + p.vr, nullptr, a, true);
-        pa.job[2] = pack_job(q, a.q_stride, d.tq, d.heads, w + p.qr, w + p.qt, a, false);
-        pa.job[3] = pack_job(dout, a.o_stride, d.tq, d.heads, w + p.orr, w + p.ot, a, false);
+        pa.scale = a.scale;
+        const int nf = 2 * p.DB * p.es / 2;  // fragments of one form
+        const int ku = 3 * nf * 64, qu = (4 * nf + 1) * 64;
+        pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, a.kv_rec, ku, 0, 2 * nf, a, true);
+        pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, a.kv_rec, ku, nf, -1, a, true);
+        pa.job[2] = pack_job(q, a.q_stride, d.tq, d.heads, a.q_rec, qu, 0, 2 * nf + 1, a, false);
+        pa.job[3] = pack_job(dout, a.o_stride, d.tq, d.heads, a.q_rec, qu, nf, 3 * nf + 1, a, false);
+        pa.job[3].x = 2 * nf * 64;
         pa.job[3].other = o;
         pa.job[3].lse = lse;
         pa.job[3].lse2 = (float*)(w + p.lse2);
@@ -1029,9 +1322,9 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
     {
         ProfScope ps("attn_dkv", st, 3.0 * one, 0.0);
         a.splits = p.ks;
-        a.tiles = (int)ceil_div(d.tk, 128);
+        a.tiles = (int)ceil_div(d.tk, 128 * p.kc);
         const int64_t grid = (int64_t)d.n * d.kv_heads * a.tiles * a.splits;
-        RAT3D_ATTN(dkv_launch, d.dtype, p.DB, a, grid, st);
+        RAT3D_ATTN(dkv_launch, d.dtype, p.DB, a, p.kc, grid, st);
         if (p.ks > 1) {
             JoinArgs j = {a.part, dk, dv, a.k_stride, a.v_stride, d.tk, p.tkp, a.idx, a.count,
                           d.kv_heads, d.head_dim, 2 * d.head_dim, p.ks, (int)ceil_div(d.tk, 64)};
@@ -1044,9 +1337,9 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
     {
         ProfScope ps("attn_dq", st, 2.0 * one, 0.0);
         a.splits = p.qs;
-        a.tiles = (int)ceil_div(d.tq, 128);
+        a.tiles = (int)ceil_div(d.tq, 128 * p.qc);
         const int64_t grid = (int64_t)d.n * d.heads * a.tiles * a.splits;
-        RAT3D_ATTN(dq_launch, d.dtype, p.DB, a, grid, st);
+        RAT3D_ATTN(dq_launch, d.dtype, p.DB, a, p.qc, grid, st);
         if (p.qs > 1) {
             JoinArgs j = {a.part, dq, dq, a.q_stride, a.q_stride, d.tq, p.tqp, nullptr, nullptr,
                           d.heads, d.head_dim, d.head_dim, p.qs, (int)ceil_div(d.tq, 64)};

@@ -10,10 +10,11 @@
 // The angles depend on the grid alone: a table of (cos, sin) for each axis, pair and
 // place (a few KB, formed in float64) is made once.
 //
-// Layout: a workgroup takes 128 neighbouring tokens of one head after another: 32
-// lanes along the tokens, four tokens each (one 8- or 16-byte access a channel), by
-// eight groups of threads along the head's channel pairs, so that both halves of a
-// pair are in one thread and a channel's row is read in whole cache lines.  The sum
+// Layout: a workgroup takes 128 or 256 neighbouring tokens of one head after another,
+// queries' heads and then keys': 32 lanes along the tokens, four or eight tokens each
+// (one 8- or 16-byte access a channel), by eight groups of threads along the head's
+// channel pairs, so that both halves of a pair are in one thread and a channel's row
+// is read in whole cache lines.  The cosines and sines are loaded once for all heads.  The sum
 // over the head's channels goes through LDS.  Rows need no alignment.
 // Bound: HBM, every tensor once.
 #include "kernels.hpp"
@@ -34,86 +35,84 @@ struct QkSide {  // queries or keys
     const void* dy;  // backward: gradient of the result
     void* out;       // the result, or the input's gradient
     const float* gamma;
-    int heads;
     int64_t x_stride, y_stride;  // from one volume to the next, of x (and dx), of y (and dy)
-    int chunk;                   // heads that a workgroup takes one after another
-    int chunks;                  // ceil(heads / chunk)
 };
 
 struct QkArgs {
     QkSide side[2];
     QkPairs pr;
     const float2* table;
-    float* part;  // backward: partial gradients of the gains, [side][channel][part]
-    int parts;    // of one side
+    float* part;   // backward: partial gradients of the gains, [side][channel][part]
+    int parts;     // workgroups
+    int heads, kv; // the heads of both sides in one list, queries first
+    int chunk, chunks;  // heads that a workgroup takes one after another; ceil(all / chunk)
     int n, H, W;
     int64_t V;
     float eps;
     int tiles;
 };
 
-constexpr int kQkTok = 4;                    // tokens per thread
-constexpr int kQkTile = 32 * kQkTok;         // tokens per workgroup
-constexpr int kQkGroups = 8;                 // thread groups along the channel pairs
+constexpr int kQkGroups = 8;  // thread groups along the channel pairs
 
-template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Tok4 { T v[kQkTok]; };
+template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Toks {
+    T v[TOK];
+};
 
-template <typename T>
-__device__ __forceinline__ void ld_tok(const T* p, int left, float (&o)[kQkTok]) {
-    if (left >= kQkTok) {
-        const Tok4<T> u = *reinterpret_cast<const Tok4<T>*>(p);
+template <typename T, int TOK>
+__device__ __forceinline__ void ld_tok(const T* p, int left, float (&o)[TOK]) {
+    if (left >= TOK) {
+        const Toks<T, TOK> u = *reinterpret_cast<const Toks<T, TOK>*>(p);
 #pragma unroll
-        for (int j = 0; j < kQkTok; ++j) o[j] = Elt<T>::from_bits(u.v[j]);
+        for (int j = 0; j < TOK; ++j) o[j] = Elt<T>::from_bits(u.v[j]);
     } else {
 #pragma unroll
-        for (int j = 0; j < kQkTok; ++j) o[j] = j < left ? Elt<T>::ld(p + j) : 0.f;
+        for (int j = 0; j < TOK; ++j) o[j] = j < left ? Elt<T>::ld(p + j) : 0.f;
     }
 }
-template <typename T>
-__device__ __forceinline__ void st_tok(T* p, int left, const float (&o)[kQkTok]) {
-    if (left >= kQkTok) {
-        Tok4<T> u;
+template <typename T, int TOK>
+__device__ __forceinline__ void st_tok(T* p, int left, const float (&o)[TOK]) {
+    if (left >= TOK) {
+        Toks<T, TOK> u;
 #pragma unroll
-        for (int j = 0; j < kQkTok; ++j) u.v[j] = Elt<T>::to_bits(o[j]);
-        *reinterpret_cast<Tok4<T>*>(p) = u;
+        for (int j = 0; j < TOK; ++j) u.v[j] = Elt<T>::to_bits(o[j]);
+        *reinterpret_cast<Toks<T, TOK>*>(p) = u;
     } else {
 #pragma unroll
-        for (int j = 0; j < kQkTok; ++j)
+        for (int j = 0; j < TOK; ++j)
             if (j < left) Elt<T>::st(p + j, o[j]);
     }
 }
 
-// PP: pairs per thread.
-template <typename T, int PP, bool NORM, bool BWD>
+// PP: pairs per thread, TOK: tokens per thread.
+template <typename T, int PP, int TOK, bool NORM, bool BWD>
 __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
-    __shared__ float sums[2][BWD ? 2 : 1][kQkGroups][kQkTile];  // [parity][sum][group][token]
+    constexpr int TILE = 32 * TOK;
+    __shared__ float sums[2][BWD ? 2 : 1][kQkGroups][TILE];  // [parity][sum][group][token]
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     int bid = blockIdx.x;
     const int tile = bid % a.tiles;
     bid /= a.tiles;
-    const int per = a.side[0].chunks + a.side[1].chunks;
-    int c = bid % per;
-    const int vol = bid / per;
-    const int si = c >= a.side[0].chunks ? 1 : 0;
-    if (si) c -= a.side[0].chunks;
-    const QkSide& s = a.side[si];
-    const int64_t t0 = (int64_t)tile * kQkTile + lane * kQkTok;
-    const int left = (int)(a.V - t0 < kQkTok ? (a.V - t0 > 0 ? a.V - t0 : 0) : kQkTok);
+    const int c = bid % a.chunks;
+    const int vol = bid / a.chunks;
+    const int64_t t0 = (int64_t)tile * TILE + lane * TOK;
+    const int left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
     const int D = a.pr.head_dim;
 
     // this thread's channels and their cosines and sines, the same for every head
     int ca[PP], cb[PP];
-    float cs[PP][kQkTok], sn[PP][kQkTok], ga[PP], gb[PP];
+    float cs[PP][TOK], sn[PP][TOK];
     {
-        int at[kQkTok][3];
+        int at[TOK][3];
+        bool row = left == TOK;  // all tokens in one row of the map
 #pragma unroll
-        for (int j = 0; j < kQkTok; ++j) {
+        for (int j = 0; j < TOK; ++j) {
             const int64_t t = j < left ? t0 + j : 0;
-            const int64_t row = t / a.W;
-            at[j][2] = (int)(t - row * a.W);
-            at[j][0] = (int)(row / a.H);
-            at[j][1] = (int)(row - (int64_t)at[j][0] * a.H);
+            const int64_t r = t / a.W;
+            at[j][2] = (int)(t - r * a.W);
+            at[j][0] = (int)(r / a.H);
+            at[j][1] = (int)(r - (int64_t)at[j][0] * a.H);
         }
+        row = row && at[0][2] + TOK - 1 == at[TOK - 1][2];
         const int e0 = a.pr.half[0], e1 = e0 + a.pr.half[1], e2 = e1 + a.pr.half[2];
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -141,55 +140,113 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
             if (ca[p] >= D) ca[p] = -1;
             if (cb[p] >= D) cb[p] = -1;
 #pragma unroll
-            for (int j = 0; j < kQkTok; ++j) {
-                const float2 v = tab ? tab[axis == 0 ? at[j][0] : axis == 1 ? at[j][1] : at[j][2]]
-                                     : make_float2(1.f, 0.f);
-                cs[p][j] = v.x;
-                sn[p][j] = v.y;
+            for (int j = 0; j < TOK; ++j) {
+                cs[p][j] = 1.f;
+                sn[p][j] = 0.f;
             }
-            ga[p] = NORM && ca[p] >= 0 ? s.gamma[ca[p]] : 1.f;
-            gb[p] = NORM && cb[p] >= 0 ? s.gamma[cb[p]] : 1.f;
+            if (tab && row) {
+                // one row: one place on the first two axes, neighbours on the third
+                if (axis < 2) {
+                    const float2 v = tab[axis == 0 ? at[0][0] : at[0][1]];
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) {
+                        cs[p][j] = v.x;
+                        sn[p][j] = v.y;
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < TOK; j += 2) {
+                        const Toks<float, 4> v =
+                            *reinterpret_cast<const Toks<float, 4>*>(tab + at[0][2] + j);
+                        cs[p][j] = v.v[0];
+                        sn[p][j] = v.v[1];
+                        cs[p][j + 1] = v.v[2];
+                        sn[p][j + 1] = v.v[3];
+                    }
+                }
+            } else if (tab) {
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) {
+                    const float2 v =
+                        tab[axis == 0 ? at[j][0] : axis == 1 ? at[j][1] : at[j][2]];
+                    cs[p][j] = v.x;
+                    sn[p][j] = v.y;
+                }
+            }
         }
     }
 
-    float dga[PP], dgb[PP];
+    float ga[PP], gb[PP], dga[PP], dgb[PP];
+    const int all = a.heads + a.kv;
+    const int h0 = c * a.chunk, h1 = h0 + a.chunk < all ? h0 + a.chunk : all;
+    // partial gradients of one side's gains, added up over this workgroup's tokens
+    auto put_gains = [&](int si) {
+#pragma unroll
+        for (int p = 0; p < PP; ++p) {
+            float u = dga[p], v = dgb[p];
+#pragma unroll
+            for (int m = 16; m >= 1; m >>= 1) {
+                u += __shfl_xor(u, m);
+                v += __shfl_xor(v, m);
+            }
+            if (lane == 0) {
+                float* to = a.part + (int64_t)si * D * a.parts + blockIdx.x;
+                if (ca[p] >= 0) to[(int64_t)ca[p] * a.parts] = u;
+                if (cb[p] >= 0) to[(int64_t)cb[p] * a.parts] = v;
+            }
+            dga[p] = dgb[p] = 0.f;
+        }
+    };
 #pragma unroll
     for (int p = 0; p < PP; ++p) dga[p] = dgb[p] = 0.f;
+    if (BWD && NORM) {
+        if (h0 >= a.heads) put_gains(0);  // no head of that side here: zeros
+        if (h1 <= a.heads) put_gains(1);
+    }
 
-    const int h1 = (c + 1) * s.chunk < s.heads ? (c + 1) * s.chunk : s.heads;
     int par = 0;
-    for (int h = c * s.chunk; h < h1; ++h, par ^= 1) {
-        const int64_t row = (int64_t)h * D;
-        const T* x = (const T*)s.x + vol * s.x_stride + row * a.V + t0;
-        const T* dy = BWD ? (const T*)s.dy + vol * s.y_stride + row * a.V + t0 : nullptr;
-        T* out = (T*)s.out + vol * (BWD ? s.x_stride : s.y_stride) + row * a.V + t0;
-        float xa[PP][kQkTok], xb[PP][kQkTok];
-        float da[PP][kQkTok], db[PP][kQkTok];
+    for (int h = h0; h < h1; ++h, par ^= 1) {
+        const int si = h >= a.heads ? 1 : 0;
+        const QkSide& s = a.side[si];
+        if (h == h0 || h == a.heads) {
+            if (BWD && NORM && h != h0) put_gains(0);
+#pragma unroll
+            for (int p = 0; p < PP; ++p) {
+                ga[p] = NORM && ca[p] >= 0 ? s.gamma[ca[p]] : 1.f;
+                gb[p] = NORM && cb[p] >= 0 ? s.gamma[cb[p]] : 1.f;
+            }
+        }
+        const int64_t first = (int64_t)(si ? h - a.heads : h) * D * a.V + t0;
+        const T* x = (const T*)s.x + vol * s.x_stride + first;
+        const T* dy = BWD ? (const T*)s.dy + vol * s.y_stride + first : nullptr;
+        T* out = (T*)s.out + vol * (BWD ? s.x_stride : s.y_stride) + first;
+        float xa[PP][TOK], xb[PP][TOK];
+        float da[PP][TOK], db[PP][TOK];
         const bool reads = NORM || !BWD;  // without a norm the backward needs dy alone
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
-            if (reads) ld_tok(x + ca[p] * a.V, ca[p] >= 0 ? left : 0, xa[p]);
-            if (reads) ld_tok(x + cb[p] * a.V, cb[p] >= 0 ? left : 0, xb[p]);
+            if (reads) ld_tok<T, TOK>(x + ca[p] * a.V, ca[p] >= 0 ? left : 0, xa[p]);
+            if (reads) ld_tok<T, TOK>(x + cb[p] * a.V, cb[p] >= 0 ? left : 0, xb[p]);
             if (BWD) {
-                ld_tok(dy + ca[p] * a.V, ca[p] >= 0 ? left : 0, da[p]);
-                ld_tok(dy + cb[p] * a.V, cb[p] >= 0 ? left : 0, db[p]);
+                ld_tok<T, TOK>(dy + ca[p] * a.V, ca[p] >= 0 ? left : 0, da[p]);
+                ld_tok<T, TOK>(dy + cb[p] * a.V, cb[p] >= 0 ? left : 0, db[p]);
             }
         }
-        float rs[kQkTok], mean[kQkTok];
+        float rs[TOK], mean[TOK];
         if (BWD) {
 #pragma unroll
             for (int p = 0; p < PP; ++p)
 #pragma unroll
-                for (int j = 0; j < kQkTok; ++j) {
+                for (int j = 0; j < TOK; ++j) {
                     const float u = da[p][j], v = db[p][j];
                     da[p][j] = u * cs[p][j] + v * sn[p][j];
                     db[p][j] = v * cs[p][j] - u * sn[p][j];
                 }
         }
         if (NORM) {
-            float ss[kQkTok], sd[kQkTok];
+            float ss[TOK], sd[TOK];
 #pragma unroll
-            for (int j = 0; j < kQkTok; ++j) {
+            for (int j = 0; j < TOK; ++j) {
                 ss[j] = sd[j] = 0.f;
 #pragma unroll
                 for (int p = 0; p < PP; ++p) {
@@ -198,20 +255,20 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                 }
             }
 #pragma unroll
-            for (int j = 0; j < kQkTok; ++j) {
-                sums[par][0][grp][lane * kQkTok + j] = ss[j];
-                if (BWD) sums[par][BWD][grp][lane * kQkTok + j] = sd[j];
+            for (int j = 0; j < TOK; ++j) {
+                sums[par][0][grp][j * 32 + lane] = ss[j];
+                if (BWD) sums[par][BWD][grp][j * 32 + lane] = sd[j];
             }
             // one barrier a head: the next head writes the other half, and this half
             // is written again only behind that head's barrier
             __syncthreads();
 #pragma unroll
-            for (int j = 0; j < kQkTok; ++j) {
+            for (int j = 0; j < TOK; ++j) {
                 float t = 0.f, d = 0.f;
 #pragma unroll
                 for (int g = 0; g < kQkGroups; ++g) {
-                    t += sums[par][0][g][lane * kQkTok + j];
-                    if (BWD) d += sums[par][BWD][g][lane * kQkTok + j];
+                    t += sums[par][0][g][j * 32 + lane];
+                    if (BWD) d += sums[par][BWD][g][j * 32 + lane];
                 }
                 rs[j] = 1.f / sqrtf(t / (float)D + a.eps);
                 if (BWD) mean[j] = d / (float)D;
@@ -219,9 +276,9 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
         }
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
-            float oa[kQkTok], ob[kQkTok];
+            float oa[TOK], ob[TOK];
 #pragma unroll
-            for (int j = 0; j < kQkTok; ++j) {
+            for (int j = 0; j < TOK; ++j) {
                 if (BWD) {
                     if (NORM) {
                         const float r = rs[j], f = r * r * mean[j];
@@ -240,41 +297,23 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                     ob[j] = za * sn[p][j] + zb * cs[p][j];
                 }
             }
-            st_tok(out + ca[p] * a.V, ca[p] >= 0 ? left : 0, oa);
-            st_tok(out + cb[p] * a.V, cb[p] >= 0 ? left : 0, ob);
+            st_tok<T, TOK>(out + ca[p] * a.V, ca[p] >= 0 ? left : 0, oa);
+            st_tok<T, TOK>(out + cb[p] * a.V, cb[p] >= 0 ? left : 0, ob);
         }
     }
-    if (BWD && NORM) {
-        const int part = (vol * s.chunks + c) * a.tiles + tile;
-#pragma unroll
-        for (int p = 0; p < PP; ++p) {
-            float u = dga[p], v = dgb[p];
-#pragma unroll
-            for (int m = 16; m >= 1; m >>= 1) {
-                u += __shfl_xor(u, m);
-                v += __shfl_xor(v, m);
-            }
-            if (lane == 0) {
-                float* to = a.part + (int64_t)si * D * a.parts;
-                if (ca[p] >= 0) to[(int64_t)ca[p] * a.parts + part] = u;
-                if (cb[p] >= 0) to[(int64_t)cb[p] * a.parts + part] = v;
-            }
-        }
-    }
+    if (BWD && NORM) put_gains(h1 > a.heads ? 1 : 0);
 }
 
 // dgamma[channel] (+)= the sum of its partial sums, in a fixed order.
-__global__ __launch_bounds__(256) void qk_gain_k(const float* __restrict__ part, int parts,
-                                                 int used0, int used1, int D, float* dgq,
-                                                 float* dgk, int accumulate) {
+__global__ __launch_bounds__(256) void qk_gain_k(const float* __restrict__ part, int parts, int D,
+                                                 float* dgq, float* dgk, int accumulate) {
     __shared__ float red[4];
     const int si = blockIdx.x / D, ch = blockIdx.x - si * D;
-    const int used = si ? used1 : used0;
     float* to = si ? dgk : dgq;
     if (!to) return;
     const float* p = part + ((int64_t)si * D + ch) * parts;
     float s = 0.f;
-    for (int i = threadIdx.x; i < used; i += 256) s += p[i];
+    for (int i = threadIdx.x; i < parts; i += 256) s += p[i];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -332,50 +371,62 @@ rat3d_status rope_table(const rat3d_qk_desc& d, void* table, hipStream_t st) {
     return RAT3D_OK;
 }
 
+// Tokens per thread: eight of bfloat16 (one 16-byte access a channel) where their
+// values and angles fit the registers of two waves a SIMD and there are tiles enough
+// to fill the GPU, else four.
+static int qk_tokens(const rat3d_qk_desc& d, bool bwd) {
+    const int64_t V = (int64_t)d.d * d.h * d.w;
+    const bool fits = d.dtype == RAT3D_BF16 && d.head_dim <= (bwd ? 32 : 64);
+    return fits && ceil_div(V, 256) * d.n >= 4 * (int64_t)device_cus() ? 8 : 4;
+}
+
 // Heads per workgroup: as many as leave four workgroups for each CU (the table's
 // values are then loaded once for several heads), at least one.
-static void qk_plan(const rat3d_qk_desc& d, QkArgs* a) {
+static void qk_plan(const rat3d_qk_desc& d, bool bwd, QkArgs* a) {
     a->V = (int64_t)d.d * d.h * d.w;
     a->n = d.n;
     a->H = d.h;
     a->W = d.w;
     a->eps = d.eps;
-    a->tiles = (int)ceil_div(a->V, kQkTile);
+    a->heads = d.heads;
+    a->kv = d.kv_heads;
+    a->tiles = (int)ceil_div(a->V, 32 * qk_tokens(d, bwd));
     const int64_t whole = (int64_t)a->tiles * d.n;
     const int64_t want = ceil_div(4 * (int64_t)device_cus(), whole);  // chunks a volume and tile
     const int both = d.heads + d.kv_heads;
-    int chunk = (int)(both / (want < both ? want : both));
-    if (chunk < 1) chunk = 1;
-    const int heads[2] = {d.heads, d.kv_heads};
-    for (int i = 0; i < 2; ++i) {
-        a->side[i].heads = heads[i];
-        a->side[i].chunk = chunk;
-        a->side[i].chunks = (int)ceil_div(heads[i], chunk);
-    }
-    const int most = a->side[0].chunks > a->side[1].chunks ? a->side[0].chunks : a->side[1].chunks;
-    a->parts = d.n * most * a->tiles;
+    a->chunk = (int)(both / (want < both ? want : both));
+    a->chunks = (int)ceil_div(both, a->chunk);
+    a->parts = d.n * a->chunks * a->tiles;
 }
 
 size_t qk_ws_bytes(const rat3d_qk_desc& d) {
     if (!d.norm) return 0;
     QkArgs a;
-    qk_plan(d, &a);
+    qk_plan(d, true, &a);
     return (size_t)2 * d.head_dim * a.parts * sizeof(float);
 }
 
 template <typename T, bool BWD>
 static void qk_launch(const rat3d_qk_desc& d, const QkArgs& a, hipStream_t st) {
-    const unsigned grid =
-        (unsigned)((int64_t)a.tiles * a.n * (a.side[0].chunks + a.side[1].chunks));
-#define RAT3D_QK(PP)                                                        \
-    do {                                                                    \
-        if (d.norm) qk_rope_k<T, PP, true, BWD><<<grid, 256, 0, st>>>(a);   \
-        else qk_rope_k<T, PP, false, BWD><<<grid, 256, 0, st>>>(a);         \
+    const unsigned grid = (unsigned)a.parts;
+    const bool wide = sizeof(T) == 2 && qk_tokens(d, BWD) == 8;
+#define RAT3D_QK(PP, TOK)                                                      \
+    do {                                                                       \
+        if (d.norm) qk_rope_k<T, PP, TOK, true, BWD><<<grid, 256, 0, st>>>(a); \
+        else qk_rope_k<T, PP, TOK, false, BWD><<<grid, 256, 0, st>>>(a);       \
     } while (0)
-    if (d.head_dim <= 16) RAT3D_QK(1);
-    else if (d.head_dim <= 32) RAT3D_QK(2);
-    else if (d.head_dim <= 64) RAT3D_QK(4);
-    else RAT3D_QK(8);
+    if constexpr (sizeof(T) == 2) {
+        if (wide) {
+            if (d.head_dim <= 16) RAT3D_QK(1, 8);
+            else if (d.head_dim <= 32) RAT3D_QK(2, 8);
+            else if constexpr (!BWD) RAT3D_QK(4, 8);
+            return;
+        }
+    }
+    if (d.head_dim <= 16) RAT3D_QK(1, 4);
+    else if (d.head_dim <= 32) RAT3D_QK(2, 4);
+    else if (d.head_dim <= 64) RAT3D_QK(4, 4);
+    else RAT3D_QK(8, 4);
 #undef RAT3D_QK
 }
 
@@ -389,7 +440,7 @@ rat3d_status qk_rope_fwd(const rat3d_qk_desc& d, const void* q, const void* k, c
     QkArgs a = {};
     int64_t total;
     a.pr = make_pairs(d, &total);
-    qk_plan(d, &a);
+    qk_plan(d, false, &a);
     a.table = (const float2*)table;
     a.side[0].x = q;
     a.side[0].out = oq;
@@ -415,7 +466,7 @@ rat3d_status qk_rope_bwd(const rat3d_qk_desc& d, const void* doq, const void* do
     QkArgs a = {};
     int64_t total;
     a.pr = make_pairs(d, &total);
-    qk_plan(d, &a);
+    qk_plan(d, true, &a);
     a.table = (const float2*)table;
     a.part = (float*)ws;
     a.side[0].x = q;
@@ -437,9 +488,8 @@ rat3d_status qk_rope_bwd(const rat3d_qk_desc& d, const void* doq, const void* do
         RAT3D_LAUNCH_CHECK();
     }
     if (d.norm) {
-        const int u0 = d.n * a.side[0].chunks * a.tiles, u1 = d.n * a.side[1].chunks * a.tiles;
-        ProfScope ps("qk_gain", st, 0.0, 4.0 * d.head_dim * ((double)u0 + u1));
-        qk_gain_k<<<2 * d.head_dim, 256, 0, st>>>(a.part, a.parts, u0, u1, d.head_dim,
+        ProfScope ps("qk_gain", st, 0.0, 8.0 * d.head_dim * a.parts);
+        qk_gain_k<<<2 * d.head_dim, 256, 0, st>>>(a.part, a.parts, d.head_dim,
                                                   d.heads ? dgq : nullptr,
                                                   d.kv_heads ? dgk : nullptr, accumulate);
         RAT3D_LAUNCH_CHECK();

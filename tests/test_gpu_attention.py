@@ -115,7 +115,12 @@ MASKS = [(2, 2, 1, 24, 50, tk, mk) for tk, mk in (
     (1, "all"), (1, "one"), (40, "half"), (64, "one"), (130, "half"), (130, "first_none"),
     (130, "all"), (130, "first65"), (300, "run"), (700, "half"), (700, "one"), (65, "first_none"),
     (5000, "half"), (4097, "one"))]
-ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS for dt in ("bf16", "f32")]
+# workgroups enough for the kernels with two column blocks a wave
+WIDE = [(64, 4, 4, 64, 77, 130, None), (64, 8, 4, 40, 130, 77, "half"), (64, 4, 4, 32, 33, 256, None),
+        (128, 2, 2, 64, 257, 300, "run"), (32, 8, 8, 24, 300, 290, "half"),
+        (90, 6, 3, 48, 1, 65, "first_none"), (256, 1, 1, 50, 97, 31, "one"),
+        (256, 1, 1, 33, 1, 1, None), (256, 2, 1, 17, 65, 2, None), (90, 3, 3, 64, 64, 96, "all")]
+ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE for dt in ("bf16", "f32")]
 
 
 @pytest.mark.parametrize("case", ALL, ids=lambda c: "n%d_h%d_%d_d%d_q%d_k%d_%s_%s" % c)

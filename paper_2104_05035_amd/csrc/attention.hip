@@ -27,6 +27,8 @@
 // the mask), so masked voxels cost nothing and what they hold is never read.
 #include <math.h>
 
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "prof.hpp"
 
@@ -172,6 +174,8 @@ struct PackJob {
     float* delta;        // D, padded with 0
     const int* idx;      // live tokens, or null
     const int* count;
+    const uint8_t* mask; // with it, what lies at masked tokens of `zero` (a gradient of
+    void* zero;          // src's layout) becomes 0
     int64_t stride, tokens;
     int heads, tiles;    // tiles of 64 tokens
     int first;           // first workgroup of the job
@@ -199,8 +203,12 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     const int vol = nh / J.heads, h = nh - vol * J.heads;
     const int64_t live = J.count ? J.count[vol] : J.tokens;
     const int64_t t0 = (int64_t)tl * kPackTok;
-    if (J.count && t0 >= live) return;  // never read: kernels stop at the live keys
     const int col = threadIdx.x & 63, sub = threadIdx.x >> 6;
+    if (J.zero && t0 + col < J.tokens && !J.mask[vol * J.tokens + t0 + col]) {
+        T* z = (T*)J.zero + vol * J.stride + (int64_t)h * a.D * J.tokens + t0 + col;
+        for (int c = sub; c < a.D; c += 4) Elt<T>::st(z + c * J.tokens, 0.f);
+    }
+    if (J.count && t0 >= live) return;  // never read: kernels stop at the live keys
     const bool in = t0 + col < live;
     const int64_t tok = in ? (J.idx ? J.idx[vol * (int64_t)J.tiles * kPackTok + t0 + col]
                                     : t0 + col)
@@ -285,22 +293,21 @@ struct AttnArgs {
 
 // U 16-byte units, copied by 256 threads from global memory into registers and from
 // there into LDS: the loads of the next tile are in flight while this one is
-// multiplied.
+// multiplied.  What is left behind the last 256 is copied by several threads alike, so
+// that no branch divides a turn.
 template <int U> struct Stage {
-    static constexpr int N = (U + 255) / 256;
+    static constexpr int N = (U + 255) / 256, kRest = U % 256 ? U % 256 : 256;
     u32x4 v[N];
-    __device__ __forceinline__ static bool mine(int i) {
-        return (i + 1) * 256 <= U || i * 256 + (int)threadIdx.x < U;
+    __device__ __forceinline__ static int at(int i) {
+        return i * 256 + (i + 1 < N ? (int)threadIdx.x : (int)threadIdx.x % kRest);
     }
     __device__ __forceinline__ void load(const u32x4* __restrict__ p) {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (mine(i)) v[i] = p[i * 256 + threadIdx.x];
+        for (int i = 0; i < N; ++i) v[i] = p[at(i)];
     }
     __device__ __forceinline__ void store(u32x4* s) const {
 #pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (mine(i)) s[i * 256 + threadIdx.x] = v[i];
+        for (int i = 0; i < N; ++i) s[at(i)] = v[i];
     }
 };
 
@@ -515,36 +522,266 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
     }
 }
 
-// Joins the splits of the forward: thread = query, a slice of the channels each.
+// Joins the splits of the forward: a workgroup takes 64 queries and 8 channels.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_k(AttnArgs a) {
     const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
-    const int tiles = (int)((a.tq + 63) / 64);
-    const int nh = blockIdx.x / tiles;
-    const int64_t qt = (int64_t)(blockIdx.x - nh * tiles) * 64 + lane;
+    const int tiles = (int)((a.tq + 63) / 64), groups = (a.D + 7) / 8;
+    int b = blockIdx.x;
+    const int tile = b % tiles;
+    b /= tiles;
+    const int c0 = b % groups * 8, nh = b / groups;
+    const int64_t qt = (int64_t)tile * 64 + lane;
     if (qt >= a.tq) return;
     const float* st = a.stat + (int64_t)nh * a.splits * 2 * a.tqp + qt;
+    const float* p = a.part + (int64_t)nh * a.splits * a.D * a.tqp + qt;
     float m = -INFINITY;
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) m = fmaxf(m, st[(int64_t)s * 2 * a.tqp]);
     const float ref = m == -INFINITY ? 0.f : m;
-    float l = 0.f;
-    for (int s = 0; s < a.splits; ++s)
-        l += st[((int64_t)s * 2 + 1) * a.tqp] *
-             __builtin_amdgcn_exp2f(st[(int64_t)s * 2 * a.tqp] - ref);
+    const int c1 = c0 + sub, c2 = c1 + 4;
+    float l = 0.f, v1 = 0.f, v2 = 0.f;
+#pragma unroll 4
+    for (int s = 0; s < a.splits; ++s) {
+        const float w = __builtin_amdgcn_exp2f(st[(int64_t)s * 2 * a.tqp] - ref);
+        l += st[((int64_t)s * 2 + 1) * a.tqp] * w;
+        if (c1 < a.D) v1 += p[((int64_t)s * a.D + c1) * a.tqp] * w;
+        if (c2 < a.D) v2 += p[((int64_t)s * a.D + c2) * a.tqp] * w;
+    }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int vol = nh / a.heads, h = nh - vol * a.heads;
     T* to = (T*)a.o + vol * a.o_stride + (int64_t)h * a.D * a.tq + qt;
-    const float* p = a.part + (int64_t)nh * a.splits * a.D * a.tqp + qt;
-    for (int c = sub; c < a.D; c += 4) {
-        float v = 0.f;
-        for (int s = 0; s < a.splits; ++s)
-            v += p[((int64_t)s * a.D + c) * a.tqp] *
-                 __builtin_amdgcn_exp2f(st[(int64_t)s * 2 * a.tqp] - ref);
-        Elt<T>::st(to + c * a.tq, v * inv);
-    }
-    if (a.lse && sub == 0)
+    if (c1 < a.D) Elt<T>::st(to + c1 * a.tq, v1 * inv);
+    if (c2 < a.D) Elt<T>::st(to + c2 * a.tq, v2 * inv);
+    if (a.lse && c0 + sub == 0)
         a.lse[(int64_t)nh * a.tq + qt] =
             l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------ few rows
+// A key head with at most four query rows (heads of its group times query tokens):
+// read-out tokens.  The keys and values are read once, as they lie: the scores of
+// neighbouring keys by neighbouring lanes (a channel's row is contiguous), then, with
+// the probabilities in registers, the sums over a channel's row of values.  4 ROWS
+// operations for each element read: bound by HBM.  A workgroup takes one piece of
+// 256 VEC keys; its part of the softmax (maximum, sum, unnormalised values) is joined
+// with the others' by attn_few_join_k.
+struct FewArgs {
+    const void *q, *k, *v;
+    const uint8_t* mask;
+    void* o;
+    float* lse;
+    float* part;  // [volume, key head][piece][row][2 + D]: maximum, sum, values
+    int64_t tq, tk, q_stride, k_stride, v_stride, o_stride;
+    int heads, kv, D, pieces, rows;
+    float c;
+};
+
+template <typename T, int VEC> struct __attribute__((packed, aligned(sizeof(T)))) Keys {
+    T v[VEC];
+};
+// VEC keys of a row, of which the first `left` are inside it; keys that are off (bit i
+// of on is 0) count as 0, whatever lies there.
+template <typename T, int VEC, bool ALL>
+__device__ __forceinline__ void ld_keys(const T* p, uint32_t on, int left, float (&o)[VEC]) {
+    if (ALL || left >= VEC) {
+        const Keys<T, VEC> u = *reinterpret_cast<const Keys<T, VEC>*>(p);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = ALL || (on >> j & 1) ? Elt<T>::from_bits(u.v[j]) : 0.f;
+    } else {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = j < left && (on >> j & 1) ? Elt<T>::ld(p + j) : 0.f;
+    }
+}
+
+template <typename T, int ROWS, int VEC>
+__global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
+    __shared__ float qs[128][ROWS];
+    __shared__ float ps[ROWS][256 * VEC];
+    __shared__ uint32_t ons[256];
+    __shared__ float red[2][4][ROWS];
+    const int piece = blockIdx.x % a.pieces, kvh = blockIdx.x / a.pieces;
+    const int vol = kvh / a.kv, hk = kvh - vol * a.kv, grp = a.heads / a.kv;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int64_t t0 = (int64_t)piece * 256 * VEC;
+    for (int i = tid; i < a.D * ROWS; i += 256) {
+        const int r = i % ROWS, ch = i / ROWS;  // row r: head r / tq of the group, token r % tq
+        const int h = hk * grp + r / (int)a.tq, tok = r % (int)a.tq;
+        qs[ch][r] = r < a.rows ? Elt<T>::ld((const T*)a.q + vol * a.q_stride +
+                                            ((int64_t)h * a.D + ch) * a.tq + tok) * a.c
+                               : 0.f;
+    }
+    const int64_t t = t0 + tid * VEC;
+    uint32_t on = 0;
+#pragma unroll
+    for (int j = 0; j < VEC; ++j)
+        on |= (t + j < a.tk && (!a.mask || a.mask[vol * a.tk + t + j]) ? 1u : 0u) << j;
+    ons[tid] = on;
+    const int left = (int)(a.tk - t < VEC ? (a.tk - t > 0 ? a.tk - t : 0) : VEC);
+    __syncthreads();
+
+    float s[ROWS][VEC];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) s[r][j] = 0.f;
+    const T* kp = (const T*)a.k + vol * a.k_stride + (int64_t)hk * a.D * a.tk + t;
+    auto scores = [&](auto all) {
+#pragma unroll 1
+        for (int c0 = 0; c0 < a.D; c0 += 8) {
+            // eight loads in flight; behind the last channel it is read again and not used
+            float x[8][VEC];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const int ch = c0 + i < a.D ? c0 + i : a.D - 1;
+                ld_keys<T, VEC, decltype(all)::value>(kp + ch * a.tk, on, left, x[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (c0 + i >= a.D) break;
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r) {
+                    const float q = qs[c0 + i][r];
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) s[r][j] = __builtin_fmaf(q, x[i][j], s[r][j]);
+                }
+            }
+        }
+    };
+    const bool full = __all(on == (1u << VEC) - 1);
+    if (full) scores(std::true_type{});
+    else scores(std::false_type{});
+
+    float m[ROWS], l[ROWS];
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        m[r] = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            if (!(on >> j & 1)) s[r][j] = -INFINITY;
+            m[r] = fmaxf(m[r], s[r][j]);
+        }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) m[r] = fmaxf(m[r], __shfl_xor(m[r], d));
+        if (lane == 0) red[0][wave][r] = m[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < ROWS; ++r) {
+        m[r] = fmaxf(fmaxf(red[0][0][r], red[0][1][r]), fmaxf(red[0][2][r], red[0][3][r]));
+        const float ref = m[r] == -INFINITY ? 0.f : m[r];
+        l[r] = 0.f;
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float p = __builtin_amdgcn_exp2f(s[r][j] - ref);
+            l[r] += p;
+            // [quarter of the piece][key of the vector][lane]: what a lane of any wave
+            // reads in the second half are the keys that the same lane has here
+            ps[r][(wave * VEC + j) * 64 + lane] = p;
+        }
+#pragma unroll
+        for (int d = 32; d >= 1; d >>= 1) l[r] += __shfl_xor(l[r], d);
+        if (lane == 0) red[1][wave][r] = l[r];
+    }
+    __syncthreads();
+    float* part = a.part + (int64_t)blockIdx.x * ROWS * (a.D + 2);
+    if (tid < ROWS) {
+        part[tid * (a.D + 2)] =
+            fmaxf(fmaxf(red[0][0][tid], red[0][1][tid]), fmaxf(red[0][2][tid], red[0][3][tid]));
+        part[tid * (a.D + 2) + 1] =
+            (red[1][0][tid] + red[1][1][tid]) + (red[1][2][tid] + red[1][3][tid]);
+    }
+    // values: a wave takes every fourth channel over all the piece's keys
+    float p[ROWS][4][VEC];
+    uint32_t live[4];
+    int rest[4];
+    bool every = true;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        live[k] = ons[k * 64 + lane];
+        const int64_t r = a.tk - t0 - (k * 64 + lane) * VEC;
+        rest[k] = (int)(r < VEC ? (r > 0 ? r : 0) : VEC);
+        every = every && live[k] == (1u << VEC) - 1;
+#pragma unroll
+        for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) p[r][k][j] = ps[r][(k * VEC + j) * 64 + lane];
+    }
+    const T* vp = (const T*)a.v + vol * a.v_stride + (int64_t)hk * a.D * a.tk + t0 + lane * VEC;
+    auto values = [&](auto all) {
+        for (int ch = wave; ch < a.D; ch += 4) {
+            float o[ROWS];
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) o[r] = 0.f;
+            float x[4][VEC];
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                ld_keys<T, VEC, decltype(all)::value>(vp + ch * a.tk + k * 64 * VEC, live[k],
+                                                      rest[k], x[k]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+#pragma unroll
+                for (int r = 0; r < ROWS; ++r)
+#pragma unroll
+                    for (int j = 0; j < VEC; ++j) o[r] = __builtin_fmaf(p[r][k][j], x[k][j], o[r]);
+#pragma unroll
+            for (int r = 0; r < ROWS; ++r) {
+#pragma unroll
+                for (int d = 32; d >= 1; d >>= 1) o[r] += __shfl_xor(o[r], d);
+                if (lane == 0) part[r * (a.D + 2) + 2 + ch] = o[r];
+            }
+        }
+    };
+    if (__all(every)) values(std::true_type{});
+    else values(std::false_type{});
+}
+
+// One workgroup a query row: weighs the pieces by their maxima and adds them up, thread =
+// channel and slice of the pieces, in a fixed order.
+template <typename T>
+__global__ __launch_bounds__(256) void attn_few_join_k(FewArgs a, int stride) {
+    __shared__ float red[256], rl[4];
+    const int nhq = blockIdx.x;  // [volume][head][query token]
+    const int nh = nhq / (int)a.tq, tok = nhq - nh * (int)a.tq;
+    const int vol = nh / a.heads, h = nh - vol * a.heads, grp = a.heads / a.kv;
+    const int kvh = vol * a.kv + h / grp, row = h % grp * (int)a.tq + tok;
+    const int tid = threadIdx.x;
+    const int64_t step = (int64_t)stride * (a.D + 2);  // from one piece to the next
+    const float* p = a.part + ((int64_t)kvh * a.pieces * stride + row) * (a.D + 2);
+    float m = -INFINITY;
+    for (int i = tid; i < a.pieces; i += 256) m = fmaxf(m, p[i * step]);
+#pragma unroll
+    for (int d = 32; d >= 1; d >>= 1) m = fmaxf(m, __shfl_xor(m, d));
+    if ((tid & 63) == 0) rl[tid >> 6] = m;
+    __syncthreads();
+    m = fmaxf(fmaxf(rl[0], rl[1]), fmaxf(rl[2], rl[3]));
+    const float ref = m == -INFINITY ? 0.f : m;
+    // channels 0 .. D - 1 and, as channel D, the sum itself
+    const int per = a.D < 32 ? 32 : a.D < 64 ? 64 : a.D < 128 ? 128 : 256;  // > D: threads a slice
+    const int ch = tid & (per - 1), slice = tid / per, slices = 256 / per;
+    float v = 0.f;
+    if (ch <= a.D) {
+        const int at = ch == a.D ? 1 : 2 + ch;
+#pragma unroll 4
+        for (int i = slice; i < a.pieces; i += slices)
+            v += p[i * step + at] * __builtin_amdgcn_exp2f(p[i * step] - ref);
+    }
+    __syncthreads();
+    red[tid] = v;
+    __syncthreads();
+    if (tid <= a.D) {
+        float l = 0.f;
+        v = 0.f;
+        for (int i = 0; i < slices; ++i) {
+            v += red[i * per + tid];
+            l += red[i * per + a.D];
+        }
+        if (tid < a.D)
+            Elt<T>::st((T*)a.o + vol * a.o_stride + ((int64_t)h * a.D + tid) * a.tq + tok,
+                       l == 0.f ? 0.f : v / l);
+        else if (a.lse)
+            a.lse[nhq] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
 }
 
 // ------------------------------------------------------------------ backward
@@ -788,14 +1025,15 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
             asm volatile("" : "+v"(pw[c][(r >> 1) - 1]), "+v"(dw[c][(r >> 1) - 1]));
         }
     };
+    // fragments in the order in which the products take them
     auto read_r = [&](const u32x4* b, int f) {
-        if (f < NF) qa[f] = frag_of<bf16>(b, R::kQ + f);
-        else if (f < 2 * NF) oa[f - NF] = frag_of<bf16>(b, R::kO + f - NF);
-        else xa = frag_of<bf16>(b, R::kX);
+        if (f == 2 * NF) xa = frag_of<bf16>(b, R::kX);
+        else if (f & 1) oa[f >> 1] = frag_of<bf16>(b, R::kO + (f >> 1));
+        else qa[f >> 1] = frag_of<bf16>(b, R::kQ + (f >> 1));
     };
     auto read_t = [&](const u32x4* b, int f) {
-        if (f < NF) ot[f] = frag_of<bf16>(b, R::kOt + f);
-        else qt[f - NF] = frag_of<bf16>(b, R::kQt + f - NF);
+        if (f & 1) qt[f >> 1] = frag_of<bf16>(b, R::kQt + (f >> 1));
+        else ot[f >> 1] = frag_of<bf16>(b, R::kOt + (f >> 1));
     };
     constexpr int N1 = 2 * NF, N2 = 2 * NF + 2, N = N1 + N2;  // products of X, as of Y
 
@@ -829,19 +1067,18 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
             if (t >= N1 && t - N1 < 2 * NF) read_t(lds[b0], t - N1);
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int f = 0; f < 2 * NF + 1; ++f) read_r(lds[b1], f);
         // Y
 #pragma unroll
         for (int t = 0; t < N; ++t) {
+            if (t < 2 * NF + 1) read_r(lds[b1], t);
             if (t < N1) grad_step(0, t);
             else score_step(0, t - N1);
 #pragma unroll
             for (int r = 0; r < 17; ++r)
                 if (r * (N - 2) / 17 + 2 == t) exp_step(1, r);
+            if (t == N - 4) next.store(lds[b2]);
             __builtin_amdgcn_sched_barrier(0);
         }
-        next.store(lds[b2]);
         __syncthreads();
         rec += U;
         const int b = b0;
@@ -982,44 +1219,44 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
     }
 }
 
-// Sums of the splits of a backward pass, in a fixed order: [nh][split][rows][tp] ->
-// the tensor's channels (rows = D for dq, 2 D for dk and dv).
-struct JoinArgs {
+// Sums of the splits of the backward passes, in a fixed order: [nh][split][rows][tp] ->
+// the tensors' channels (rows = D for dq, 2 D for dk and dv).  A workgroup takes 64
+// tokens and 8 channels.
+struct SumJob {
     const float* part;
     void *a, *b;               // channels 0 .. D-1 and D .. rows-1
     int64_t a_stride, b_stride, tokens, tp;
     const int *idx, *count;
-    int heads, D, rows, splits, tiles;
+    int heads, D, rows, splits, tiles, first;
+};
+struct SumArgs {
+    SumJob job[2];
+    int jobs;
 };
 template <typename T>
-__global__ __launch_bounds__(256) void attn_sum_k(JoinArgs j) {
+__global__ __launch_bounds__(256) void attn_sum_k(SumArgs g) {
+    const SumJob& j = g.job[g.jobs > 1 && (int)blockIdx.x >= g.job[1].first ? 1 : 0];
     const int lane = threadIdx.x & 63, sub = threadIdx.x >> 6;
-    const int tile = blockIdx.x % j.tiles, nh = blockIdx.x / j.tiles;
+    const int groups = (j.rows + 7) / 8;
+    int b = (int)blockIdx.x - j.first;
+    const int tile = b % j.tiles;
+    b /= j.tiles;
+    const int c0 = b % groups * 8, nh = b / groups;
     const int vol = nh / j.heads, h = nh - vol * j.heads;
     const int64_t t = (int64_t)tile * 64 + lane;
     if (t >= (j.count ? j.count[vol] : j.tokens)) return;
     const int64_t tok = j.idx ? j.idx[vol * j.tp + t] : t;
     const float* p = j.part + (int64_t)nh * j.splits * j.rows * j.tp + t;
-    for (int c = sub; c < j.rows; c += 4) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const int c = c0 + sub + 4 * k;
+        if (c >= j.rows) continue;
         float v = 0.f;
+#pragma unroll 4
         for (int s = 0; s < j.splits; ++s) v += p[((int64_t)s * j.rows + c) * j.tp];
         T* to = c < j.D ? (T*)j.a + vol * j.a_stride + ((int64_t)h * j.D + c) * j.tokens
                         : (T*)j.b + vol * j.b_stride + ((int64_t)h * j.D + c - j.D) * j.tokens;
         Elt<T>::st(to + tok, v);
-    }
-}
-
-// dK = dV = 0 at masked keys.
-template <typename T>
-__global__ __launch_bounds__(256) void attn_dead_k(const uint8_t* __restrict__ mask, int64_t tk,
-                                                   int tiles, int rows, int64_t k_stride,
-                                                   int64_t v_stride, T* dk, T* dv) {
-    const int vol = blockIdx.x / tiles;
-    const int64_t t = (int64_t)(blockIdx.x - vol * tiles) * 256 + threadIdx.x;
-    if (t >= tk || mask[vol * tk + t]) return;
-    for (int r = 0; r < rows; ++r) {
-        Elt<T>::st(dk + vol * k_stride + r * tk + t, 0.f);
-        Elt<T>::st(dv + vol * v_stride + r * tk + t, 0.f);
     }
 }
 
@@ -1029,12 +1266,12 @@ struct AttnPlan {
     int DB, es;
     int fc, kc, qc;  // blocks of 32 kept tokens a wave: forward, dK/dV, dQ
     int fs, ks, qs;  // splits of the same
-    size_t idx, count, kv_rec, q_rec, lse2, delta, part, fpart, stat, bytes[2];
+    size_t idx, count, kv_rec, q_rec, lse2, delta, part, qpart, fpart, stat, bytes[2];
 };
 
 // Ways to split a long walk: until there are about two workgroups for each CU, but
 // not into pieces of fewer than `least` turns.
-static int splits_for(int64_t groups, int64_t turns, int least) {
+static int splits_for(int64_t groups, int64_t turns, int64_t least) {
     const int64_t want = 2 * (int64_t)device_cus();
     int64_t s = (want + groups / 2) / groups;
     if (s > turns / least) s = turns / least;
@@ -1045,7 +1282,23 @@ static int splits_for(int64_t groups, int64_t turns, int least) {
 // Two blocks of 32 kept tokens a wave in bfloat16, where the registers hold them and
 // there are workgroups enough: each fragment read from LDS then feeds two products.
 static int columns_for(const rat3d_attention_desc& d, int DB, int64_t groups) {
-    return d.dtype == RAT3D_BF16 && DB <= 2 && groups >= (int64_t)device_cus() ? 2 : 1;
+    return d.dtype == RAT3D_BF16 && DB <= 2 && 2 * groups >= 3 * (int64_t)device_cus() ? 2 : 1;
+}
+
+// Keys of a piece of the kernel for few rows: 16-byte accesses where that leaves two
+// workgroups for each CU, else 4-byte ones.
+static int few_keys(const rat3d_attention_desc& d) {
+    const int es = d.dtype == RAT3D_BF16 ? 2 : 4;
+    const int64_t wide = 256 * 16 / es;
+    const bool many = (int64_t)d.n * d.kv_heads * ceil_div(d.tk, wide) >= 2 * (int64_t)device_cus();
+    return (int)(many ? wide : wide / 4);
+}
+static bool few_rows(const rat3d_attention_desc& d) {
+    return d.heads / d.kv_heads * d.tq <= 4;
+}
+static int few_stride(const rat3d_attention_desc& d) {  // rows that a workgroup is built for
+    const int64_t rows = d.heads / d.kv_heads * d.tq;
+    return rows <= 2 ? (int)rows : 4;
 }
 
 static AttnPlan attn_plan(const rat3d_attention_desc& d) {
@@ -1057,9 +1310,11 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
     const int64_t nq = (int64_t)d.n * d.heads, nk = (int64_t)d.n * d.kv_heads;
     p.fc = p.qc = columns_for(d, p.DB, nq * ceil_div(d.tq, 256));
     p.kc = columns_for(d, p.DB, nk * ceil_div(d.tk, 256));
-    p.fs = splits_for(nq * ceil_div(d.tq, 128 * p.fc), p.tkp / 64, 2);
-    p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, 4);
-    p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), 4);
+    // a turn of float32 takes microseconds, one of bfloat16 a fraction
+    const int least = d.dtype == RAT3D_BF16 ? 4 : 1;
+    p.fs = splits_for(nq * ceil_div(d.tq, 128 * p.fc), p.tkp / 32, least);
+    p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, least);
+    p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), least);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t r = at;
@@ -1072,8 +1327,15 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
     p.count = take((size_t)d.n * sizeof(int));
     const size_t both = at;
     // forward
-    p.kv_rec = take(2 * kb);
-    if (p.fs > 1) {
+    p.kv_rec = at;
+    if (few_rows(d)) {
+        take((size_t)nk * ceil_div(d.tk, few_keys(d)) * few_stride(d) * (d.head_dim + 2) *
+             sizeof(float));
+        p.bytes[0] = at;
+    } else {
+        take(2 * kb);
+    }
+    if (p.fs > 1 && !few_rows(d)) {
         p.stat = take((size_t)nq * p.fs * 2 * p.tqp * sizeof(float));
         p.fpart = take((size_t)nq * p.fs * d.head_dim * p.tqp * sizeof(float));
     }
@@ -1086,7 +1348,8 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
     p.delta = take((size_t)nq * p.tqp * sizeof(float));
     const size_t kp = p.ks > 1 ? (size_t)nk * p.ks * 2 * d.head_dim * p.tkp * sizeof(float) : 0;
     const size_t qp = p.qs > 1 ? (size_t)nq * p.qs * d.head_dim * p.tqp * sizeof(float) : 0;
-    p.part = take(kp > qp ? kp : qp);
+    p.part = take(kp);
+    p.qpart = take(qp);
     p.bytes[1] = at;
     return p;
 }
@@ -1103,6 +1366,9 @@ bool attention_fits(const rat3d_attention_desc& d) {
                (1 << 24) &&
            nq * ceil_div(d.tq, 128) * p.fs < (1 << 24) && nq * ceil_div(d.tq, 128) * p.qs < (1 << 24) &&
            (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 128) * p.ks < (1 << 24) &&
+           nq * ceil_div(d.tq, 64) * 16 + 32 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
+               (1ll << 31) &&
+           (!few_rows(d) || (int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) < (1 << 24)) &&
            p.tqp / 32 * (d.heads / d.kv_heads) < (1 << 30);
 }
 
@@ -1227,6 +1493,13 @@ static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
         RAT3D_LAUNCH_CHECK();                                       \
     } while (0)
 
+template <typename T, int VEC>
+static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
+    if (f.rows == 1) attn_few_k<T, 1, VEC><<<grid, 256, 0, st>>>(f);
+    else if (f.rows == 2) attn_few_k<T, 2, VEC><<<grid, 256, 0, st>>>(f);
+    else attn_few_k<T, 4, VEC><<<grid, 256, 0, st>>>(f);
+}
+
 rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const void* k,
                            const void* v, const uint8_t* mask, void* o, float* lse, void* ws,
                            hipStream_t st) {
@@ -1238,8 +1511,45 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
     a.lse = lse;
     a.stat = (float*)(w + p.stat);
     a.part = (float*)(w + p.fpart);
-    RAT3D_TRY(live_keys(d, p, w, mask, &a, st));
     const double nq = (double)d.n * d.heads, nk = (double)d.n * d.kv_heads;
+    if (few_rows(d)) {
+        FewArgs f = {};
+        f.q = q;
+        f.k = k;
+        f.v = v;
+        f.mask = mask;
+        f.o = o;
+        f.lse = lse;
+        f.part = (float*)(w + p.kv_rec);
+        f.tq = d.tq;
+        f.tk = d.tk;
+        f.q_stride = a.q_stride;
+        f.k_stride = a.k_stride;
+        f.v_stride = a.v_stride;
+        f.o_stride = a.o_stride;
+        f.heads = d.heads;
+        f.kv = d.kv_heads;
+        f.D = d.head_dim;
+        f.rows = (int)(d.heads / d.kv_heads * d.tq);
+        f.c = a.c;
+        const int keys = few_keys(d);
+        f.pieces = (int)ceil_div(d.tk, keys);
+        ProfScope ps("attn_few", st, 4.0 * nq * d.tq * d.tk * d.head_dim,
+                     2.0 * nk * d.tk * d.head_dim * p.es);
+        const unsigned grid = (unsigned)((int64_t)d.n * d.kv_heads * f.pieces);
+        if (d.dtype == RAT3D_BF16) {
+            if (keys == 2048) few_launch<bf16, 8>(f, grid, st);
+            else few_launch<bf16, 2>(f, grid, st);
+            attn_few_join_k<bf16><<<(unsigned)(d.n * d.heads * d.tq), 256, 0, st>>>(f, few_stride(d));
+        } else {
+            if (keys == 1024) few_launch<float, 4>(f, grid, st);
+            else few_launch<float, 1>(f, grid, st);
+            attn_few_join_k<float><<<(unsigned)(d.n * d.heads * d.tq), 256, 0, st>>>(f, few_stride(d));
+        }
+        RAT3D_LAUNCH_CHECK();
+        return RAT3D_OK;
+    }
+    RAT3D_TRY(live_keys(d, p, w, mask, &a, st));
     {
         ProfScope ps("attn_pack", st, 0.0, 4.0 * nk * d.tk * d.head_dim * p.es);
         PackArgs pa = {};
@@ -1260,7 +1570,8 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
     }
     if (p.fs > 1) {
         ProfScope ps("attn_join", st, 0.0, nq * d.tq * d.head_dim * (4.0 * p.fs + p.es));
-        const unsigned grid = (unsigned)((int64_t)d.n * d.heads * ceil_div(d.tq, 64));
+        const unsigned grid =
+            (unsigned)((int64_t)d.n * d.heads * ceil_div(d.tq, 64) * ceil_div(d.head_dim, 8));
         if (d.dtype == RAT3D_BF16) attn_join_k<bf16><<<grid, 256, 0, st>>>(a);
         else attn_join_k<float><<<grid, 256, 0, st>>>(a);
         RAT3D_LAUNCH_CHECK();
@@ -1297,6 +1608,11 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
         const int ku = 3 * nf * 64, qu = (4 * nf + 1) * 64;
         pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, a.kv_rec, ku, 0, 2 * nf, a, true);
         pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, a.kv_rec, ku, nf, -1, a, true);
+        if (mask) {
+            pa.job[0].mask = pa.job[1].mask = mask;
+            pa.job[0].zero = dk;
+            pa.job[1].zero = dv;
+        }
         pa.job[2] = pack_job(q, a.q_stride, d.tq, d.heads, a.q_rec, qu, 0, 2 * nf + 1, a, false);
         pa.job[3] = pack_job(dout, a.o_stride, d.tq, d.heads, a.q_rec, qu, nf, 3 * nf + 1, a, false);
         pa.job[3].x = 2 * nf * 64;
@@ -1307,47 +1623,41 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
         RAT3D_TRY(pack_launch(pa, d.n, d.dtype, st));
     }
     const bool bf = d.dtype == RAT3D_BF16;
-    if (mask) {
-        ProfScope ps("attn_dead", st, 0.0, nk * d.tk * d.head_dim * p.es);
-        const int tiles = (int)ceil_div(d.tk, 256);
-        const int rows = d.kv_heads * d.head_dim;
-        if (bf)
-            attn_dead_k<bf16><<<(unsigned)(d.n * tiles), 256, 0, st>>>(
-                mask, d.tk, tiles, rows, a.k_stride, a.v_stride, (bf16*)dk, (bf16*)dv);
-        else
-            attn_dead_k<float><<<(unsigned)(d.n * tiles), 256, 0, st>>>(
-                mask, d.tk, tiles, rows, a.k_stride, a.v_stride, (float*)dk, (float*)dv);
-        RAT3D_LAUNCH_CHECK();
-    }
     {
         ProfScope ps("attn_dkv", st, 3.0 * one, 0.0);
         a.splits = p.ks;
         a.tiles = (int)ceil_div(d.tk, 128 * p.kc);
         const int64_t grid = (int64_t)d.n * d.kv_heads * a.tiles * a.splits;
         RAT3D_ATTN(dkv_launch, d.dtype, p.DB, a, p.kc, grid, st);
-        if (p.ks > 1) {
-            JoinArgs j = {a.part, dk, dv, a.k_stride, a.v_stride, d.tk, p.tkp, a.idx, a.count,
-                          d.kv_heads, d.head_dim, 2 * d.head_dim, p.ks, (int)ceil_div(d.tk, 64)};
-            const unsigned g = (unsigned)((int64_t)d.n * d.kv_heads * j.tiles);
-            if (bf) attn_sum_k<bf16><<<g, 256, 0, st>>>(j);
-            else attn_sum_k<float><<<g, 256, 0, st>>>(j);
-            RAT3D_LAUNCH_CHECK();
-        }
     }
     {
         ProfScope ps("attn_dq", st, 2.0 * one, 0.0);
+        a.part = (float*)(w + p.qpart);
         a.splits = p.qs;
         a.tiles = (int)ceil_div(d.tq, 128 * p.qc);
         const int64_t grid = (int64_t)d.n * d.heads * a.tiles * a.splits;
         RAT3D_ATTN(dq_launch, d.dtype, p.DB, a, p.qc, grid, st);
-        if (p.qs > 1) {
-            JoinArgs j = {a.part, dq, dq, a.q_stride, a.q_stride, d.tq, p.tqp, nullptr, nullptr,
-                          d.heads, d.head_dim, d.head_dim, p.qs, (int)ceil_div(d.tq, 64)};
-            const unsigned g = (unsigned)((int64_t)d.n * d.heads * j.tiles);
-            if (bf) attn_sum_k<bf16><<<g, 256, 0, st>>>(j);
-            else attn_sum_k<float><<<g, 256, 0, st>>>(j);
-            RAT3D_LAUNCH_CHECK();
-        }
+    }
+    if (p.ks > 1 || p.qs > 1) {
+        SumArgs g = {};
+        int64_t blocks = 0;
+        auto add = [&](SumJob j) {
+            j.tiles = (int)ceil_div(j.tokens, 64);
+            j.first = (int)blocks;
+            blocks += (int64_t)d.n * j.heads * j.tiles * ceil_div(j.rows, 8);
+            g.job[g.jobs++] = j;
+        };
+        if (p.ks > 1)
+            add({(const float*)(w + p.part), dk, dv, a.k_stride, a.v_stride, d.tk, p.tkp, a.idx,
+                 a.count, d.kv_heads, d.head_dim, 2 * d.head_dim, p.ks, 0, 0});
+        if (p.qs > 1)
+            add({(const float*)(w + p.qpart), dq, dq, a.q_stride, a.q_stride, d.tq, p.tqp, nullptr,
+                 nullptr, d.heads, d.head_dim, d.head_dim, p.qs, 0, 0});
+        ProfScope ps("attn_sum", st, 0.0,
+                     4.0 * d.head_dim * (2.0 * nk * d.tk * p.ks + nq * d.tq * p.qs));
+        if (bf) attn_sum_k<bf16><<<(unsigned)blocks, 256, 0, st>>>(g);
+        else attn_sum_k<float><<<(unsigned)blocks, 256, 0, st>>>(g);
+        RAT3D_LAUNCH_CHECK();
     }
     return RAT3D_OK;
 }

@@ -120,7 +120,11 @@ WIDE = [(64, 4, 4, 64, 77, 130, None), (64, 8, 4, 40, 130, 77, "half"), (64, 4, 
         (128, 2, 2, 64, 257, 300, "run"), (32, 8, 8, 24, 300, 290, "half"),
         (90, 6, 3, 48, 1, 65, "first_none"), (256, 1, 1, 50, 97, 31, "one"),
         (256, 1, 1, 33, 1, 1, None), (256, 2, 1, 17, 65, 2, None), (90, 3, 3, 64, 64, 96, "all")]
-ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE for dt in ("bf16", "f32")]
+# few query rows: pieces of the keys, in both widths
+FEW = [(1, 1, 1, 1, 1, 1, None), (2, 2, 1, 33, 1, 513, "half"), (1, 4, 1, 40, 1, 2049, None),
+       (2, 2, 2, 128, 3, 700, "run"), (2, 3, 3, 64, 4, 1025, "first_none"), (1, 4, 2, 24, 2, 3000, "one"),
+       (40, 4, 2, 8, 1, 16400, "half"), (40, 2, 2, 9, 4, 13313, None), (60, 3, 3, 5, 3, 6145, "run")]
+ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE + FEW for dt in ("bf16", "f32")]
 
 
 @pytest.mark.parametrize("case", ALL, ids=lambda c: "n%d_h%d_%d_d%d_q%d_k%d_%s_%s" % c)

@@ -182,18 +182,19 @@ struct PackJob {
 };
 struct PackArgs {
     PackJob job[4];
-    int jobs, D, DB;
+    int jobs, D;
     float scale;
 };
 
 constexpr int kPackTok = 64;
 
 // One workgroup: 64 tokens of one head of one volume, through LDS.
-template <typename T>
+template <typename T, int DB>
 __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     typedef Mm<T> M;
+    constexpr int Dp = 32 * DB;
     constexpr int ROW = kPackTok + (sizeof(T) == 2 ? 2 : 1);  // odd in banks: columns spread
-    __shared__ T tile[128 * ROW];
+    __shared__ T tile[Dp * ROW];
     __shared__ float part[4][kPackTok];
     int ji = 0;
     while (ji + 1 < a.jobs && (int)blockIdx.x >= a.job[ji + 1].first) ++ji;
@@ -216,15 +217,22 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     const int64_t base = vol * J.stride + (int64_t)h * a.D * J.tokens + tok;
     const T* src = (const T*)J.src + base;
     const T* oth = J.other ? (const T*)J.other + base : nullptr;
-    const int Dp = 32 * a.DB;
     float d = 0.f;
-    for (int c = sub; c < Dp; c += 4) {
-        T v = Elt<T>::to_bits(0.f);
-        if (in && c < a.D) {
-            v = src[(int64_t)c * J.tokens];
-            if (oth) d += Elt<T>::cvt(v) * Elt<T>::ld(oth + (int64_t)c * J.tokens);
-        }
-        tile[c * ROW + col] = v;
+    // all of a thread's loads are issued before the first is used; behind the last
+    // channel it is read again, at a token that is there, and counts as 0
+    T v[8 * DB], o[8 * DB];
+#pragma unroll
+    for (int i = 0; i < 8 * DB; ++i) {
+        const int c = sub + 4 * i < a.D ? sub + 4 * i : a.D - 1;
+        v[i] = src[c * J.tokens];
+        if (oth) o[i] = oth[c * J.tokens];
+    }
+#pragma unroll
+    for (int i = 0; i < 8 * DB; ++i) {
+        const bool on = in && sub + 4 * i < a.D;
+        if (!on) v[i] = Elt<T>::to_bits(0.f);
+        if (oth && on) d += Elt<T>::from_bits(v[i]) * Elt<T>::from_bits(o[i]);
+        tile[(sub + 4 * i) * ROW + col] = v[i];
     }
     part[sub][col] = d;
     __syncthreads();
@@ -261,7 +269,7 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
             to[J.r] = u;
         }
         if (J.t >= 0) {
-            const int w = g / a.DB, e = g % a.DB;
+            const int w = g / DB, e = g % DB;
             const int ch = e * 32 + (lane & 31);
             T v[M::kPer];
 #pragma unroll
@@ -316,21 +324,29 @@ __device__ __forceinline__ typename Mm<T>::frag frag_of(const u32x4* s, int f) {
     return __builtin_bit_cast(typename Mm<T>::frag, s[f * 64 + (threadIdx.x & 63)]);
 }
 
-// 32 tokens of a channel-first tensor as fragments of form R (second operand).
+// 32 tokens of a channel-first tensor as fragments of form R (second operand).  All
+// loads are issued before one is used: what is behind the last channel is read from it
+// again and counts as 0, and a token behind the last from the last (p: the tensor's
+// first channel at this lane's token, or at the last one).
 template <typename T, int NF>
 __device__ __forceinline__ void load_cols(const T* __restrict__ p, int64_t row, int D, bool in,
                                           typename Mm<T>::frag (&f)[NF]) {
     typedef Mm<T> M;
     const int half = (threadIdx.x & 63) >> 5;
+    T v[NF][M::kPer];
 #pragma unroll
-    for (int i = 0; i < NF; ++i) {
-        T v[M::kPer];
+    for (int i = 0; i < NF; ++i)
 #pragma unroll
         for (int j = 0; j < M::kPer; ++j) {
             const int ch = i * M::kR + half * M::kPer + j;
-            v[j] = in && ch < D ? p[ch * row] : Elt<T>::to_bits(0.f);
+            v[i][j] = p[(ch < D ? ch : D - 1) * row];
         }
-        __builtin_memcpy(&f[i], v, 16);
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+#pragma unroll
+        for (int j = 0; j < M::kPer; ++j)
+            if (!in || i * M::kR + half * M::kPer + j >= D) v[i][j] = Elt<T>::to_bits(0.f);
+        __builtin_memcpy(&f[i], v[i], 16);
     }
 }
 
@@ -367,9 +383,12 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
 
     frag qf[CB][NR];
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
-        load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq + q0 + 32 * c,
-                         a.tq, a.D, q0 + 32 * c < a.tq, qf[c]);
+    for (int c = 0; c < CB; ++c) {
+        const int64_t t = q0 + 32 * c;
+        load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq +
+                             (t < a.tq ? t : a.tq - 1),
+                         a.tq, a.D, t < a.tq, qf[c]);
+    }
 
     f32x16 acc[CB][DB];
     float m[CB], l4[CB][4];  // the running reference and the sum, of this lane's rows
@@ -1271,8 +1290,8 @@ struct AttnPlan {
 
 // Ways to split a long walk: until there are about two workgroups for each CU, but
 // not into pieces of fewer than `least` turns.
-static int splits_for(int64_t groups, int64_t turns, int64_t least) {
-    const int64_t want = 2 * (int64_t)device_cus();
+static int splits_for(int64_t groups, int64_t turns, int64_t least, int per_cu = 2) {
+    const int64_t want = per_cu * (int64_t)device_cus();
     int64_t s = (want + groups / 2) / groups;
     if (s > turns / least) s = turns / least;
     if (s > 256) s = 256;
@@ -1301,7 +1320,10 @@ static int few_stride(const rat3d_attention_desc& d) {  // rows that a workgroup
     return rows <= 2 ? (int)rows : 4;
 }
 
-static AttnPlan attn_plan(const rat3d_attention_desc& d) {
+// masked: whether a mask is given.  Where one is, much of dK/dV's workgroups find no
+// live key (a brain fills about 0.4 of its box), so that walk is cut into twice as
+// many pieces: 4 x 2 x 40 over 12x14x11, 0.38 live, 50 us in 480 workgroups, 31 in 1080.
+static AttnPlan attn_plan(const rat3d_attention_desc& d, bool masked) {
     AttnPlan p = {};
     p.es = d.dtype == RAT3D_BF16 ? 2 : 4;
     p.DB = (d.head_dim + 31) / 32;
@@ -1314,7 +1336,8 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
     const int least = d.dtype == RAT3D_BF16 ? 4 : 1;
     p.fs = splits_for(nq * ceil_div(d.tq, 128 * p.fc), p.tkp / 32, least);
     p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, least);
-    p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), least);
+    p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), least,
+                      masked ? 4 : 2);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         const size_t r = at;
@@ -1355,11 +1378,12 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d) {
 }
 
 size_t attention_ws_bytes(const rat3d_attention_desc& d, int pass) {
-    return attn_plan(d).bytes[pass];
+    const size_t a = attn_plan(d, false).bytes[pass], b = attn_plan(d, true).bytes[pass];
+    return a > b ? a : b;
 }
 
 bool attention_fits(const rat3d_attention_desc& d) {
-    const AttnPlan p = attn_plan(d);
+    const AttnPlan p = attn_plan(d, true);
     const int64_t nq = (int64_t)d.n * d.heads;
     // workgroups of the largest launches (each of 256 threads, 2^32 threads a launch)
     return 2 * nq * ceil_div(d.tq, 64) + 2 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
@@ -1391,6 +1415,22 @@ static AttnArgs attn_args(const rat3d_attention_desc& d, const AttnPlan& p, char
     return a;
 }
 
+#define RAT3D_ATTN(F, dt, DB, ...)                                  \
+    do {                                                            \
+        if ((dt) == RAT3D_BF16) {                                   \
+            if ((DB) == 1) F<bf16, 1>(__VA_ARGS__);                 \
+            else if ((DB) == 2) F<bf16, 2>(__VA_ARGS__);            \
+            else if ((DB) == 3) F<bf16, 3>(__VA_ARGS__);            \
+            else F<bf16, 4>(__VA_ARGS__);                           \
+        } else {                                                    \
+            if ((DB) == 1) F<float, 1>(__VA_ARGS__);                \
+            else if ((DB) == 2) F<float, 2>(__VA_ARGS__);           \
+            else if ((DB) == 3) F<float, 3>(__VA_ARGS__);           \
+            else F<float, 4>(__VA_ARGS__);                          \
+        }                                                           \
+        RAT3D_LAUNCH_CHECK();                                       \
+    } while (0)
+
 // r, t: fragments of the record where forms R and T begin, or -1.
 static PackJob pack_job(const void* src, int64_t stride, int64_t tokens, int heads,
                         const u32x4* rec, int units, int r, int t, const AttnArgs& a, bool keys) {
@@ -1412,15 +1452,17 @@ static PackJob pack_job(const void* src, int64_t stride, int64_t tokens, int hea
     return j;
 }
 
-static rat3d_status pack_launch(PackArgs& pa, int n, rat3d_dtype dt, hipStream_t st) {
+template <typename T, int DB>
+static void pack_kernel(const PackArgs& pa, int64_t blocks, hipStream_t st) {
+    attn_pack_k<T, DB><<<(unsigned)blocks, 256, 0, st>>>(pa);
+}
+static rat3d_status pack_launch(PackArgs& pa, int n, int DB, rat3d_dtype dt, hipStream_t st) {
     int64_t blocks = 0;
     for (int i = 0; i < pa.jobs; ++i) {
         pa.job[i].first = (int)blocks;
         blocks += (int64_t)n * pa.job[i].heads * pa.job[i].tiles;
     }
-    if (dt == RAT3D_BF16) attn_pack_k<bf16><<<(unsigned)blocks, 256, 0, st>>>(pa);
-    else attn_pack_k<float><<<(unsigned)blocks, 256, 0, st>>>(pa);
-    RAT3D_LAUNCH_CHECK();
+    RAT3D_ATTN(pack_kernel, dt, DB, pa, blocks, st);
     return RAT3D_OK;
 }
 
@@ -1477,22 +1519,6 @@ static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
     }
     RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB, 1);
 }
-#define RAT3D_ATTN(F, dt, DB, ...)                                  \
-    do {                                                            \
-        if ((dt) == RAT3D_BF16) {                                   \
-            if ((DB) == 1) F<bf16, 1>(__VA_ARGS__);                 \
-            else if ((DB) == 2) F<bf16, 2>(__VA_ARGS__);            \
-            else if ((DB) == 3) F<bf16, 3>(__VA_ARGS__);            \
-            else F<bf16, 4>(__VA_ARGS__);                           \
-        } else {                                                    \
-            if ((DB) == 1) F<float, 1>(__VA_ARGS__);                \
-            else if ((DB) == 2) F<float, 2>(__VA_ARGS__);           \
-            else if ((DB) == 3) F<float, 3>(__VA_ARGS__);           \
-            else F<float, 4>(__VA_ARGS__);                          \
-        }                                                           \
-        RAT3D_LAUNCH_CHECK();                                       \
-    } while (0)
-
 template <typename T, int VEC>
 static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
     if (f.rows == 1) attn_few_k<T, 1, VEC><<<grid, 256, 0, st>>>(f);
@@ -1503,7 +1529,7 @@ static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
 rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const void* k,
                            const void* v, const uint8_t* mask, void* o, float* lse, void* ws,
                            hipStream_t st) {
-    const AttnPlan p = attn_plan(d);
+    const AttnPlan p = attn_plan(d, mask != nullptr);
     char* w = (char*)ws;
     AttnArgs a = attn_args(d, p, w);
     a.q = q;
@@ -1554,12 +1580,11 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
         ProfScope ps("attn_pack", st, 0.0, 4.0 * nk * d.tk * d.head_dim * p.es);
         PackArgs pa = {};
         pa.D = d.head_dim;
-        pa.DB = p.DB;
         pa.jobs = 2;
         const int nf = 2 * p.DB * p.es / 2;  // fragments of one form
         pa.job[0] = pack_job(k, a.k_stride, d.tk, d.kv_heads, a.kv_rec, 128 * nf, 0, -1, a, true);
         pa.job[1] = pack_job(v, a.v_stride, d.tk, d.kv_heads, a.kv_rec, 128 * nf, -1, nf, a, true);
-        RAT3D_TRY(pack_launch(pa, d.n, d.dtype, st));
+        RAT3D_TRY(pack_launch(pa, d.n, p.DB, d.dtype, st));
     }
     {
         ProfScope ps("attn_fwd", st, 4.0 * nq * d.tq * d.tk * d.head_dim, 0.0);
@@ -1583,7 +1608,7 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
                            const void* k, const void* v, const uint8_t* mask, const void* o,
                            const float* lse, void* dq, void* dk, void* dv, void* ws,
                            hipStream_t st) {
-    const AttnPlan p = attn_plan(d);
+    const AttnPlan p = attn_plan(d, mask != nullptr);
     char* w = (char*)ws;
     AttnArgs a = attn_args(d, p, w);
     a.q_rec = (const u32x4*)(w + p.q_rec);
@@ -1601,7 +1626,6 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
                      (5.0 * nk * d.tk + 7.0 * nq * d.tq) * d.head_dim * p.es);
         PackArgs pa = {};
         pa.D = d.head_dim;
-        pa.DB = p.DB;
         pa.jobs = 4;
         pa.scale = a.scale;
         const int nf = 2 * p.DB * p.es / 2;  // fragments of one form
@@ -1620,7 +1644,7 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
         pa.job[3].lse = lse;
         pa.job[3].lse2 = (float*)(w + p.lse2);
         pa.job[3].delta = (float*)(w + p.delta);
-        RAT3D_TRY(pack_launch(pa, d.n, d.dtype, st));
+        RAT3D_TRY(pack_launch(pa, d.n, p.DB, d.dtype, st));
     }
     const bool bf = d.dtype == RAT3D_BF16;
     {

@@ -554,18 +554,37 @@ __global__ __launch_bounds__(256) void attn_join_k(AttnArgs a) {
     if (qt >= a.tq) return;
     const float* st = a.stat + (int64_t)nh * a.splits * 2 * a.tqp + qt;
     const float* p = a.part + (int64_t)nh * a.splits * a.D * a.tqp + qt;
-    float m = -INFINITY;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) m = fmaxf(m, st[(int64_t)s * 2 * a.tqp]);
-    const float ref = m == -INFINITY ? 0.f : m;
     const int c1 = c0 + sub, c2 = c1 + 4;
-    float l = 0.f, v1 = 0.f, v2 = 0.f;
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(st[(int64_t)s * 2 * a.tqp] - ref);
-        l += st[((int64_t)s * 2 + 1) * a.tqp] * w;
-        if (c1 < a.D) v1 += p[((int64_t)s * a.D + c1) * a.tqp] * w;
-        if (c2 < a.D) v2 += p[((int64_t)s * a.D + c2) * a.tqp] * w;
+    const int64_t d1 = (int64_t)(c1 < a.D ? c1 : a.D - 1) * a.tqp;
+    const int64_t d2 = (int64_t)(c2 < a.D ? c2 : a.D - 1) * a.tqp;
+    float m = -INFINITY, l = 0.f, v1 = 0.f, v2 = 0.f;
+    for (int s0 = 0; s0 < a.splits; s0 += 8) {  // eight splits' loads in flight
+        float ms[8], ls[8], x1[8], x2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t s = s0 + i < a.splits ? s0 + i : a.splits - 1;
+            ms[i] = st[s * 2 * a.tqp];
+            ls[i] = st[(s * 2 + 1) * a.tqp];
+            x1[i] = p[s * a.D * a.tqp + d1];
+            x2[i] = p[s * a.D * a.tqp + d2];
+        }
+        float to = m;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) to = fmaxf(to, ms[i]);
+        const float ref = to == -INFINITY ? 0.f : to;
+        const float f = __builtin_amdgcn_exp2f(m - ref);
+        m = to;
+        l *= f;
+        v1 *= f;
+        v2 *= f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (s0 + i >= a.splits) break;
+            const float w = __builtin_amdgcn_exp2f(ms[i] - ref);
+            l += ls[i] * w;
+            v1 += x1[i] * w;
+            v2 += x2[i] * w;
+        }
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
     const int vol = nh / a.heads, h = nh - vol * a.heads;
@@ -1266,13 +1285,29 @@ __global__ __launch_bounds__(256) void attn_sum_k(SumArgs g) {
     if (t >= (j.count ? j.count[vol] : j.tokens)) return;
     const int64_t tok = j.idx ? j.idx[vol * j.tp + t] : t;
     const float* p = j.part + (int64_t)nh * j.splits * j.rows * j.tp + t;
+    const int64_t d1 = (int64_t)(c0 + sub < j.rows ? c0 + sub : j.rows - 1) * j.tp;
+    const int64_t d2 = (int64_t)(c0 + sub + 4 < j.rows ? c0 + sub + 4 : j.rows - 1) * j.tp;
+    float sum[2] = {0.f, 0.f};
+    for (int s0 = 0; s0 < j.splits; s0 += 8) {  // eight splits' loads in flight
+        float x1[8], x2[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int64_t s = s0 + i < j.splits ? s0 + i : j.splits - 1;
+            x1[i] = p[s * j.rows * j.tp + d1];
+            x2[i] = p[s * j.rows * j.tp + d2];
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            if (s0 + i >= j.splits) break;
+            sum[0] += x1[i];
+            sum[1] += x2[i];
+        }
+    }
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
         const int c = c0 + sub + 4 * k;
         if (c >= j.rows) continue;
-        float v = 0.f;
-#pragma unroll 4
-        for (int s = 0; s < j.splits; ++s) v += p[((int64_t)s * j.rows + c) * j.tp];
+        const float v = sum[k];
         T* to = c < j.D ? (T*)j.a + vol * j.a_stride + ((int64_t)h * j.D + c) * j.tokens
                         : (T*)j.b + vol * j.b_stride + ((int64_t)h * j.D + c - j.D) * j.tokens;
         Elt<T>::st(to + tok, v);

@@ -17,6 +17,8 @@
 // is read in whole cache lines.  The cosines and sines are loaded once for all heads.  The sum
 // over the head's channels goes through LDS.  Rows need no alignment.
 // Bound: HBM, every tensor once.
+#include <type_traits>
+
 #include "kernels.hpp"
 #include "prof.hpp"
 
@@ -54,27 +56,33 @@ struct QkArgs {
 
 constexpr int kQkGroups = 8;  // thread groups along the channel pairs
 
+// TOK tokens of one channel, in words: a row may begin at any element.
 template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Toks {
-    T v[TOK];
+    uint32_t w[TOK * sizeof(T) / 4];
 };
-
-template <typename T, int TOK>
+template <typename T, int TOK, bool ALL>
 __device__ __forceinline__ void ld_tok(const T* p, int left, float (&o)[TOK]) {
-    if (left >= TOK) {
+    if (ALL) {
         const Toks<T, TOK> u = *reinterpret_cast<const Toks<T, TOK>*>(p);
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) o[j] = Elt<T>::from_bits(u.v[j]);
+        for (int j = 0; j < TOK; ++j) {
+            if (sizeof(T) == 4) o[j] = __uint_as_float(u.w[j]);
+            else o[j] = __uint_as_float(j & 1 ? u.w[j / 2] & 0xffff0000u : u.w[j / 2] << 16);
+        }
     } else {
 #pragma unroll
         for (int j = 0; j < TOK; ++j) o[j] = j < left ? Elt<T>::ld(p + j) : 0.f;
     }
 }
-template <typename T, int TOK>
+template <typename T, int TOK, bool ALL>
 __device__ __forceinline__ void st_tok(T* p, int left, const float (&o)[TOK]) {
-    if (left >= TOK) {
+    if (ALL) {
         Toks<T, TOK> u;
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) u.v[j] = Elt<T>::to_bits(o[j]);
+        for (int j = 0; j < TOK; j += sizeof(T) == 4 ? 1 : 2) {
+            if (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
+            else u.w[j / 2] = pack_bf16x2(o[j], o[(j + 1) % TOK]);
+        }
         *reinterpret_cast<Toks<T, TOK>*>(p) = u;
     } else {
 #pragma unroll
@@ -83,11 +91,20 @@ __device__ __forceinline__ void st_tok(T* p, int left, const float (&o)[TOK]) {
     }
 }
 
+// The lower half of a wave gets x of both halves added, the upper half y.
+__device__ __forceinline__ float join_groups(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false,
+                                                    false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
 // PP: pairs per thread, TOK: tokens per thread.
 template <typename T, int PP, int TOK, bool NORM, bool BWD>
 __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
     constexpr int TILE = 32 * TOK;
-    __shared__ float sums[2][BWD ? 2 : 1][kQkGroups][TILE];  // [parity][sum][group][token]
+    // sums over a wave's channels: [parity][sum][wave][token of the lane][lane]
+    __shared__ float sums[2][BWD ? 2 : 1][4][TOK][32];
+    const float inv_d = 1.f / (float)a.pr.head_dim;
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     int bid = blockIdx.x;
     const int tile = bid % a.tiles;
@@ -102,17 +119,24 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
     int ca[PP], cb[PP];
     float cs[PP][TOK], sn[PP][TOK];
     {
+        // one division for the first token (32 bits: a launch holds fewer than 2^31
+        // tokens), steps for its neighbours
         int at[TOK][3];
-        bool row = left == TOK;  // all tokens in one row of the map
+        const uint32_t first = left > 0 ? (uint32_t)t0 : 0u;
+        const uint32_t r0 = first / (uint32_t)a.W;
+        at[0][2] = (int)(first - r0 * (uint32_t)a.W);
+        at[0][0] = (int)(r0 / (uint32_t)a.H);
+        at[0][1] = (int)(r0 - (uint32_t)at[0][0] * (uint32_t)a.H);
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-            const int64_t t = j < left ? t0 + j : 0;
-            const int64_t r = t / a.W;
-            at[j][2] = (int)(t - r * a.W);
-            at[j][0] = (int)(r / a.H);
-            at[j][1] = (int)(r - (int64_t)at[j][0] * a.H);
+        for (int j = 1; j < TOK; ++j) {
+            const bool step = j < left;
+            const bool row_end = step && at[j - 1][2] + 1 == a.W;
+            const bool plane_end = row_end && at[j - 1][1] + 1 == a.H;
+            at[j][2] = row_end ? 0 : at[j - 1][2] + (step ? 1 : 0);
+            at[j][1] = plane_end ? 0 : at[j - 1][1] + (row_end ? 1 : 0);
+            at[j][0] = at[j - 1][0] + (plane_end ? 1 : 0);
         }
-        row = row && at[0][2] + TOK - 1 == at[TOK - 1][2];
+        const bool row = left == TOK && at[0][2] + TOK - 1 == at[TOK - 1][2];  // all in one row
         const int e0 = a.pr.half[0], e1 = e0 + a.pr.half[1], e2 = e1 + a.pr.half[2];
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
@@ -156,12 +180,13 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                 } else {
 #pragma unroll
                     for (int j = 0; j < TOK; j += 2) {
-                        const Toks<float, 4> v =
-                            *reinterpret_cast<const Toks<float, 4>*>(tab + at[0][2] + j);
-                        cs[p][j] = v.v[0];
-                        sn[p][j] = v.v[1];
-                        cs[p][j + 1] = v.v[2];
-                        sn[p][j + 1] = v.v[3];
+                        float v[4];
+                        ld_tok<float, 4, true>(
+                            reinterpret_cast<const float*>(tab + at[0][2] + j), 4, v);
+                        cs[p][j] = v[0];
+                        sn[p][j] = v[1];
+                        cs[p][j + 1] = v[2];
+                        sn[p][j + 1] = v[3];
                     }
                 }
             } else if (tab) {
@@ -205,7 +230,8 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
     }
 
     int par = 0;
-    for (int h = h0; h < h1; ++h, par ^= 1) {
+    auto head = [&](int h, auto all) {
+        constexpr bool kAll = decltype(all)::value;
         const int si = h >= a.heads ? 1 : 0;
         const QkSide& s = a.side[si];
         if (h == h0 || h == a.heads) {
@@ -223,15 +249,26 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
         float xa[PP][TOK], xb[PP][TOK];
         float da[PP][TOK], db[PP][TOK];
         const bool reads = NORM || !BWD;  // without a norm the backward needs dy alone
+        // a channel that is none is read from the head's first and counts as 0
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
-            if (reads) ld_tok<T, TOK>(x + ca[p] * a.V, ca[p] >= 0 ? left : 0, xa[p]);
-            if (reads) ld_tok<T, TOK>(x + cb[p] * a.V, cb[p] >= 0 ? left : 0, xb[p]);
+            const int64_t fa = (ca[p] >= 0 ? ca[p] : 0) * a.V, fb = (cb[p] >= 0 ? cb[p] : 0) * a.V;
+            if (reads) {
+                ld_tok<T, TOK, kAll>(x + fa, left, xa[p]);
+                ld_tok<T, TOK, kAll>(x + fb, left, xb[p]);
+            }
             if (BWD) {
-                ld_tok<T, TOK>(dy + ca[p] * a.V, ca[p] >= 0 ? left : 0, da[p]);
-                ld_tok<T, TOK>(dy + cb[p] * a.V, cb[p] >= 0 ? left : 0, db[p]);
+                ld_tok<T, TOK, kAll>(dy + fa, left, da[p]);
+                ld_tok<T, TOK, kAll>(dy + fb, left, db[p]);
             }
         }
+#pragma unroll
+        for (int p = 0; p < PP; ++p)
+#pragma unroll
+            for (int j = 0; j < TOK; ++j) {
+                if (ca[p] < 0) xa[p][j] = da[p][j] = 0.f;
+                if (cb[p] < 0) xb[p][j] = db[p][j] = 0.f;
+            }
         float rs[TOK], mean[TOK];
         if (BWD) {
 #pragma unroll
@@ -254,24 +291,27 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                     if (BWD) sd[j] += ga[p] * da[p][j] * xa[p][j] + gb[p] * db[p][j] * xb[p][j];
                 }
             }
+            // both groups of a wave, then the four waves through LDS: each half of a wave
+            // writes half of the tokens
+            const int half = grp & 1, wave = grp >> 1;
 #pragma unroll
-            for (int j = 0; j < TOK; ++j) {
-                sums[par][0][grp][j * 32 + lane] = ss[j];
-                if (BWD) sums[par][BWD][grp][j * 32 + lane] = sd[j];
+            for (int j = 0; j < TOK / 2; ++j) {
+                const int k = half * (TOK / 2) + j;
+                sums[par][0][wave][k][lane] = join_groups(ss[j], ss[TOK / 2 + j]);
+                if (BWD) sums[par][BWD][wave][k][lane] = join_groups(sd[j], sd[TOK / 2 + j]);
             }
             // one barrier a head: the next head writes the other half, and this half
             // is written again only behind that head's barrier
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
-                float t = 0.f, d = 0.f;
-#pragma unroll
-                for (int g = 0; g < kQkGroups; ++g) {
-                    t += sums[par][0][g][j * 32 + lane];
-                    if (BWD) d += sums[par][BWD][g][j * 32 + lane];
-                }
-                rs[j] = 1.f / sqrtf(t / (float)D + a.eps);
-                if (BWD) mean[j] = d / (float)D;
+                const float t = (sums[par][0][0][j][lane] + sums[par][0][1][j][lane]) +
+                                (sums[par][0][2][j][lane] + sums[par][0][3][j][lane]);
+                rs[j] = __builtin_amdgcn_rsqf(__builtin_fmaf(t, inv_d, a.eps));
+                if (BWD)
+                    mean[j] = ((sums[par][BWD][0][j][lane] + sums[par][BWD][1][j][lane]) +
+                               (sums[par][BWD][2][j][lane] + sums[par][BWD][3][j][lane])) *
+                              inv_d * (rs[j] * rs[j]);
             }
         }
 #pragma unroll
@@ -281,11 +321,12 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
             for (int j = 0; j < TOK; ++j) {
                 if (BWD) {
                     if (NORM) {
-                        const float r = rs[j], f = r * r * mean[j];
-                        dga[p] += da[p][j] * xa[p][j] * r;
-                        dgb[p] += db[p][j] * xb[p][j] * r;
-                        oa[j] = r * (ga[p] * da[p][j] - xa[p][j] * f);
-                        ob[j] = r * (gb[p] * db[p][j] - xb[p][j] * f);
+                        // x r once, and mean[j] already times r^2
+                        const float r = rs[j], ya = xa[p][j] * r, yb = xb[p][j] * r;
+                        dga[p] = __builtin_fmaf(da[p][j], ya, dga[p]);
+                        dgb[p] = __builtin_fmaf(db[p][j], yb, dgb[p]);
+                        oa[j] = __builtin_fmaf(-ya, mean[j], r * ga[p] * da[p][j]);
+                        ob[j] = __builtin_fmaf(-yb, mean[j], r * gb[p] * db[p][j]);
                     } else {
                         oa[j] = da[p][j];
                         ob[j] = db[p][j];
@@ -297,9 +338,14 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                     ob[j] = za * sn[p][j] + zb * cs[p][j];
                 }
             }
-            st_tok<T, TOK>(out + ca[p] * a.V, ca[p] >= 0 ? left : 0, oa);
-            st_tok<T, TOK>(out + cb[p] * a.V, cb[p] >= 0 ? left : 0, ob);
+            if (ca[p] >= 0) st_tok<T, TOK, kAll>(out + ca[p] * a.V, left, oa);
+            if (cb[p] >= 0) st_tok<T, TOK, kAll>(out + cb[p] * a.V, left, ob);
         }
+    };
+    const bool inside = (int64_t)(tile + 1) * TILE <= a.V;
+    for (int h = h0; h < h1; ++h, par ^= 1) {
+        if (inside) head(h, std::true_type{});
+        else head(h, std::false_type{});
     }
     if (BWD && NORM) put_gains(h1 > a.heads ? 1 : 0);
 }

@@ -317,6 +317,7 @@ template <int U> struct Stage {
 #pragma unroll
         for (int i = 0; i < N; ++i) s[at(i)] = v[i];
     }
+    __device__ __forceinline__ void store(u32x4* s, int i) const { s[at(i)] = v[i]; }
 };
 
 template <typename T>
@@ -360,6 +361,47 @@ __device__ __forceinline__ void split_range(int64_t live, int step, int splits, 
 }
 
 // ------------------------------------------------------------------ forward
+// The result of a lane's query qt leaves: o and lse, or a split's reference, sum and
+// values.  l is the sum over the rows of this lane; the lane 32 away has the others.
+template <typename T, int DB, bool SPLIT>
+__device__ __forceinline__ void fwd_store(const AttnArgs& a, int nh, int sp, int64_t qt, float m,
+                                          float l, const f32x16 (&acc)[DB]) {
+    const int half = (threadIdx.x & 63) >> 5;
+    float la, lb;
+    halves(l, la, lb);
+    l = la + lb;
+    if (qt >= a.tq) return;
+    if (SPLIT) {
+        float* st = a.stat + ((int64_t)nh * a.splits + sp) * 2 * a.tqp + qt;
+        if (half == 0) {
+            st[0] = m;
+            st[a.tqp] = l;
+        }
+        float* to = a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt;
+#pragma unroll
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                if (ch < a.D) to[ch * a.tqp] = acc[e][i];
+            }
+    } else {
+        const int vol = nh / a.heads, h = nh - vol * a.heads;
+        const float inv = l == 0.f ? 0.f : 1.f / l;
+        T* to = (T*)a.o + vol * a.o_stride + (int64_t)h * a.D * a.tq + qt;
+#pragma unroll
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                if (ch < a.D) Elt<T>::st(to + ch * a.tq, acc[e][i] * inv);
+            }
+        if (a.lse && half == 0)
+            a.lse[(int64_t)nh * a.tq + qt] =
+                l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+}
+
 // A workgroup: 128 CB queries of one head, 32 CB a wave as columns; KB x 32 keys a turn.
 template <typename T, int DB, int CB, int KB, bool SPLIT>
 __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k(AttnArgs a) {
@@ -502,43 +544,199 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
         if (b + 1 < b1) next.store(lds[buf ^ 1]);
         __syncthreads();
     }
-    const int half = lane >> 5;
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        float la, lb;
-        halves((l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), la, lb);
-        const float l = la + lb;
-        const int64_t qt = q0 + 32 * c;
-        if (qt >= a.tq) continue;
-        if (SPLIT) {
-            float* st = a.stat + ((int64_t)nh * a.splits + sp) * 2 * a.tqp + qt;
-            if (half == 0) {
-                st[0] = m[c];
-                st[a.tqp] = l;
-            }
-            float* to = a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt;
+    for (int c = 0; c < CB; ++c)
+        fwd_store<T, DB, SPLIT>(a, nh, sp, q0 + 32 * c, m[c],
+                                (l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), acc[c]);
+}
+
+// The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
+// phases of neighbouring turns (32 keys) laid over each other:
+//   X: values of B for turn i - 1, scores of B for turn i   beside   softmax of A, turn i
+//   Y: values of A for turn i, scores of A for turn i + 1   beside   softmax of B, turn i
+// A fragment read from LDS feeds both blocks, and the matrix cores work under the
+// exponentials, which bound the kernel: a score takes a fused multiply-add, an
+// exponential (8 cycles), an addition, half a conversion and half a maximum.  Three LDS
+// buffers, as in attn_dkv2_k.  The last keys, where they do not fill a record, are taken
+// by themselves behind the loop.
+template <int DB, bool SPLIT>
+__global__ __launch_bounds__(256, 2) void attn_fwd2_k(AttnArgs a) {
+    typedef Mm<bf16> M;
+    typedef bf16x8 frag;
+    constexpr int NF = 2 * DB, U = 2 * NF * 64;
+    __shared__ u32x4 lds[3][U];
+    int bid = xcd_remap(blockIdx.x, gridDim.x);
+    const int tile = bid % a.tiles;
+    bid /= a.tiles;
+    const int sp = SPLIT ? bid % a.splits : 0;
+    const int nh = SPLIT ? bid / a.splits : bid;
+    const int vol = nh / a.heads, h = nh - vol * a.heads;
+    const int kvh = vol * a.kv + h / (a.heads / a.kv);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t live = a.count ? a.count[vol] : a.tk;
+    const int64_t q0 = ((int64_t)tile * 4 + wave) * 64 + (lane & 31);
+
+    frag qf[2][NF];
+    f32x16 acc[2][DB], s[2];
+    float m[2], l4[2][4];  // the running reference and the sum, of this lane's rows
+    uint32_t pw[2][8];     // probabilities, two a word
+    frag kf[NF], vf[NF];
 #pragma unroll
-            for (int e = 0; e < DB; ++e)
+    for (int c = 0; c < 2; ++c) {
+        const int64_t t = q0 + 32 * c;
+        load_cols<bf16, NF>((const bf16*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq +
+                                (t < a.tq ? t : a.tq - 1),
+                            a.tq, a.D, t < a.tq, qf[c]);
+        m[c] = -INFINITY;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                    if (ch < a.D) to[ch * a.tqp] = acc[c][e][i];
-                }
-        } else {
-            const float inv = l == 0.f ? 0.f : 1.f / l;
-            T* to = (T*)a.o + vol * a.o_stride + (int64_t)h * a.D * a.tq + qt;
+        for (int i = 0; i < 4; ++i) l4[c][i] = 0.f;
 #pragma unroll
-            for (int e = 0; e < DB; ++e)
+        for (int i = 0; i < 16; ++i) {
+            s[c][i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                    if (ch < a.D) Elt<T>::st(to + ch * a.tq, acc[c][e][i] * inv);
-                }
-            if (a.lse && half == 0)
-                a.lse[(int64_t)nh * a.tq + qt] =
-                    l == 0.f ? -INFINITY : (m[c] + __builtin_amdgcn_logf(l)) * kLn2;
+            for (int e = 0; e < DB; ++e) acc[c][e][i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) pw[c][i] = 0;
+    }
+#pragma unroll
+    for (int f = 0; f < NF; ++f) vf[f] = frag{};
+
+    int b0, b1;
+    split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
+    const int whole = (int)(live / 32);
+    const int i1 = b1 < whole ? b1 : whole;  // records that keys fill
+    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
+    const u32x4* last = rec + (int64_t)(i1 - b0 - 1) * U;
+    Stage<U> next;
+
+    auto value_step = [&](int c, int t) {  // one of the NF products of the values of block c
+        const int w = t / DB, e = t % DB;
+        const u32x4 p = {pw[c][4 * w], pw[c][4 * w + 1], pw[c][4 * w + 2], pw[c][4 * w + 3]};
+        acc[c][e] = M::mul(vf[t], __builtin_bit_cast(frag, p), acc[c][e]);
+    };
+    auto score_step = [&](int c, int t) {  // one of the NF products of the scores of block c
+        const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f,
+                             0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        s[c] = t == 0 ? M::mul(kf[0], qf[c][0], zero) : M::mul(kf[t], qf[c][t], s[c]);
+    };
+    // The reference of the exponentials follows the maximum only where it grew by more
+    // than 8 (in log 2), as in attn_fwd_k.
+    auto top = [&](int c) {
+        float x = s[c][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[c][i]);
+        float xa, xb;
+        halves(x, xa, xb);
+        return fmaxf(xa, xb) * a.c;
+    };
+    auto follow = [&](int c, float t) {
+        if (!__any(t > m[c] + 8.f)) return;
+        const float to = t > m[c] + 8.f ? t : m[c];
+        const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
+        m[c] = to;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) l4[c][i] *= f;
+#pragma unroll
+        for (int e = 0; e < DB; ++e)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[c][e][i] *= f;
+    };
+    // the exponential of register r, and what follows it for register r - 1
+    auto exp_step = [&](int c, int r, float ref) {
+        if (r < 16) s[c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][r], a.c, -ref));
+        if (r == 0) return;
+        l4[c][(r - 1) % 4] += s[c][r - 1];
+        if (!(r & 1)) {
+            pw[c][(r >> 1) - 1] = pack_bf16x2(s[c][r - 2], s[c][r - 1]);
+            // formed here, not where it is used
+            asm volatile("" : "+v"(pw[c][(r >> 1) - 1]));
+        }
+    };
+    // One half of a turn.  C: the block whose probabilities are formed; the products are
+    // the other's, with V of `vb` read behind its values (READV), K of `kb` before its
+    // scores (!READV).
+    auto half_turn = [&](auto block, const u32x4* b) {
+        constexpr int C = decltype(block)::value, O = 1 - C;
+        constexpr bool X = C == 0;
+        // in X the other block's values come first, and its scores use K as it is; in Y
+        // the first values wait for nothing, K of the next record is read under them
+        const float t = top(C);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            if (!X) kf[f] = frag_of<bf16>(b, f);
+            value_step(O, f);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        follow(C, t);
+        const float ref = m[C] == -INFINITY ? 0.f : m[C];
+#pragma unroll
+        for (int r = 0; r < 17; ++r) {
+            if (r % (16 / NF) == 0 && r < 16) score_step(O, r / (16 / NF));
+            if (X && r % (16 / NF) == 0 && r < 16) vf[r / (16 / NF)] = frag_of<bf16>(b, NF + r / (16 / NF));
+            exp_step(C, r, ref);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    if (b0 < i1) {
+        next.load(rec);
+        next.store(lds[0]);
+        next.load(b0 + 1 < i1 ? rec + U : rec);
+        next.store(lds[1]);
+    }
+    __syncthreads();
+    if (b0 < i1) {
+#pragma unroll
+        for (int f = 0; f < NF; ++f) kf[f] = frag_of<bf16>(lds[0], f);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) score_step(0, f);
+    }
+    int u0 = 0, u1 = 1, u2 = 2;  // buffers of records i, i + 1, i + 2
+    for (int i = b0; i < i1; ++i) {
+        // behind the last record it is taken again: what is formed from it is not used
+        next.load(i + 2 < i1 ? rec + 2 * U : last);
+        half_turn(std::integral_constant<int, 0>{}, lds[u0]);
+        half_turn(std::integral_constant<int, 1>{}, lds[u1]);
+        next.store(lds[u2]);
+        __syncthreads();
+        rec += U;
+        const int u = u0;
+        u0 = u1;
+        u1 = u2;
+        u2 = u;
+    }
+#pragma unroll
+    for (int f = 0; f < NF; ++f) value_step(1, f);  // B of the last turn
+    if (i1 < b1) {  // keys that fill no record
+        next.load(a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + i1) * U);
+        next.store(lds[u2]);
+        __syncthreads();
+        const int left = (int)(live - (int64_t)i1 * 32);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            kf[f] = frag_of<bf16>(lds[u2], f);
+            vf[f] = frag_of<bf16>(lds[u2], NF + f);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int f = 0; f < NF; ++f) score_step(c, f);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) s[c][r] = -INFINITY;
+            follow(c, top(c));
+            const float ref = m[c] == -INFINITY ? 0.f : m[c];
+#pragma unroll
+            for (int r = 0; r < 17; ++r) exp_step(c, r, ref);
+#pragma unroll
+            for (int f = 0; f < NF; ++f) value_step(c, f);
         }
     }
+#pragma unroll
+    for (int c = 0; c < 2; ++c)
+        fwd_store<bf16, DB, SPLIT>(a, nh, sp, q0 + 32 * c, m[c],
+                                   (l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), acc[c]);
 }
 
 // Joins the splits of the forward: a workgroup takes 64 queries and 8 channels.
@@ -1094,6 +1292,10 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
         // behind the last record it is taken again, so that no branch divides the turn:
         // what is formed from it is not used
         next.load(i + 2 < i1 ? rec + 2 * U : last);
+        // Reads of LDS are spread over the turn, as far as a fragment's last use before
+        // and its first use behind allow: four waves that read at every step would ask
+        // for all that LDS gives, and stand still for it.
+        constexpr int kEarly = NF;  // fragments of R that X reads, behind its scores' first
         // X
 #pragma unroll
         for (int t = 0; t < N; ++t) {
@@ -1102,19 +1304,20 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
 #pragma unroll
             for (int r = 0; r < 17; ++r)
                 if (r * (N - 2) / 17 + 2 == t) exp_step(0, r);
-            if (t >= N1 && t - N1 < 2 * NF) read_t(lds[b0], t - N1);
+            if (t & 1 && t / 2 < N1) read_t(lds[b0], t / 2);
+            if (!(t & 1) && t >= N1 + 2 && (t - N1 - 2) / 2 < kEarly) read_r(lds[b1], (t - N1 - 2) / 2);
             __builtin_amdgcn_sched_barrier(0);
         }
         // Y
 #pragma unroll
         for (int t = 0; t < N; ++t) {
-            if (t < 2 * NF + 1) read_r(lds[b1], t);
+            if (!(t & 1) && kEarly + t / 2 < 2 * NF + 1) read_r(lds[b1], kEarly + t / 2);
             if (t < N1) grad_step(0, t);
             else score_step(0, t - N1);
 #pragma unroll
             for (int r = 0; r < 17; ++r)
                 if (r * (N - 2) / 17 + 2 == t) exp_step(1, r);
-            if (t == N - 4) next.store(lds[b2]);
+            if (t >= N - 6 && t - (N - 6) < Stage<U>::N) next.store(lds[b2], t - (N - 6));
             __builtin_amdgcn_sched_barrier(0);
         }
         __syncthreads();
@@ -1128,6 +1331,27 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
     for (int t = 0; t < N1; ++t) grad_step(1, t);  // B of the last turn
     dkv_store<bf16, DB, SPLIT>(a, at, kb, dk[0], dv[0]);
     dkv_store<bf16, DB, SPLIT>(a, at, kb + 1, dk[1], dv[1]);
+}
+
+// The sums of 32 queries (block qb) leave: partial sums of a split, or the gradient.
+template <typename T, int DB, bool SPLIT>
+__device__ __forceinline__ void dq_store(const AttnArgs& a, int nh, int sp, int64_t qb,
+                                         const f32x16 (&dq)[DB]) {
+    const int lane = threadIdx.x & 63, half = lane >> 5;
+    const int64_t qt = qb * 32 + (lane & 31);
+    if (qt >= a.tq) return;
+    const int vol = nh / a.heads, h = nh - vol * a.heads;
+    float* tp = SPLIT ? a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt : nullptr;
+    T* to = (T*)a.dq + vol * a.q_stride + (int64_t)h * a.D * a.tq + qt;
+#pragma unroll
+    for (int e = 0; e < DB; ++e)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
+            if (ch >= a.D) continue;
+            if (SPLIT) tp[ch * a.tqp] = dq[e][i] * a.scale;
+            else Elt<T>::st(to + ch * a.tq, dq[e][i] * a.scale);
+        }
 }
 
 // dQ: a workgroup keeps 128 CB queries of one head, 32 CB a wave as columns, and walks
@@ -1238,23 +1462,188 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
         if (b + 1 < b1) next.store(lds[((b - b0) & 1) ^ 1]);
         __syncthreads();
     }
-    const int half = lane >> 5;
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const int64_t qt = (qb + c) * 32 + (lane & 31);
-        if (qt >= a.tq) continue;
-        float* tp = SPLIT ? a.part + ((int64_t)nh * a.splits + sp) * a.D * a.tqp + qt : nullptr;
-        T* to = (T*)a.dq + vol * a.q_stride + (int64_t)h * a.D * a.tq + qt;
+    for (int c = 0; c < CB; ++c) dq_store<T, DB, SPLIT>(a, nh, sp, qb + c, dq[c]);
+}
+
+// The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
+// phases of neighbouring turns laid over each other as in attn_dkv2_k:
+//   X: dQ of B for turn i - 1, scores of B for turn i   beside   exp of A, turn i
+//   Y: dQ of A for turn i, scores of A for turn i + 1   beside   exp of B, turn i
+// -D is added to dO V^T by one more product: ones for every key times the query's
+// constant.  The last keys, where they fill no record, are taken behind the loop.
+template <int DB, bool SPLIT>
+__global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a) {
+    typedef Mm<bf16> M;
+    typedef bf16x8 frag;
+    typedef Rec<bf16, DB> R;
+    constexpr int NF = R::NF, U = R::kKeys;
+    __shared__ u32x4 lds[3][U];
+    int bid = xcd_remap(blockIdx.x, gridDim.x);
+    const int tile = bid % a.tiles;
+    bid /= a.tiles;
+    const int sp = SPLIT ? bid % a.splits : 0;
+    const int nh = SPLIT ? bid / a.splits : bid;
+    const int vol = nh / a.heads, h = nh - vol * a.heads;
+    const int kvh = vol * a.kv + h / (a.heads / a.kv);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t live = a.count ? a.count[vol] : a.tk;
+    const int64_t qb = ((int64_t)tile * 4 + wave) * 2;
+
+    frag qf[2][NF], of[2][NF], low[2];
+    float ls[2];
+    f32x16 dq[2][DB], s[2], dp[2];
+    uint32_t dw[2][8];  // score gradients, two a word
+    frag ka[NF], va[NF], kt[NF];
 #pragma unroll
-        for (int e = 0; e < DB; ++e)
+    for (int c = 0; c < 2; ++c) {
+        const bool have = (qb + c) * 32 < a.tqp;
 #pragma unroll
-            for (int i = 0; i < 16; ++i) {
-                const int ch = e * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                if (ch >= a.D) continue;
-                if (SPLIT) tp[ch * a.tqp] = dq[c][e][i] * a.scale;
-                else Elt<T>::st(to + ch * a.tq, dq[c][e][i] * a.scale);
+        for (int f = 0; f < NF; ++f) {
+            qf[c][f] = frag{};
+            of[c][f] = frag{};
+            if (have) {
+                const u32x4* rec = a.q_rec + ((int64_t)nh * (a.tqp / 32) + qb + c) * R::kQueries;
+                qf[c][f] = frag_of<bf16>(rec, R::kQ + f);
+                of[c][f] = frag_of<bf16>(rec, R::kO + f);
             }
+        }
+        const int64_t at = (int64_t)nh * a.tqp + (qb + c) * 32 + (lane & 31);
+        ls[c] = have ? a.lse2[at] : INFINITY;
+        low[c] = __builtin_bit_cast(frag, M::rows(have ? -a.delta[at] : 0.f, 0.f, lane >> 5));
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            s[c][i] = dp[c][i] = 0.f;
+#pragma unroll
+            for (int e = 0; e < DB; ++e) dq[c][e][i] = 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) dw[c][i] = 0;
     }
+    const frag ones = M::pick(0, lane >> 5);
+#pragma unroll
+    for (int f = 0; f < NF; ++f) kt[f] = frag{};
+
+    int b0, b1;
+    split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
+    const int whole = (int)(live / 32);
+    const int i1 = b1 < whole ? b1 : whole;  // records that keys fill
+    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
+    const u32x4* last = rec + (int64_t)(i1 - b0 - 1) * U;
+    Stage<U> next;
+
+    auto grad_step = [&](int c, int t) {  // one of the NF products of dQ of block c
+        const int w = t / DB, e = t % DB;
+        const u32x4 p = {dw[c][4 * w], dw[c][4 * w + 1], dw[c][4 * w + 2], dw[c][4 * w + 3]};
+        dq[c][e] = M::mul(kt[t], __builtin_bit_cast(frag, p), dq[c][e]);
+    };
+    // one of the 2 NF + 1 products of the scores and of dO V^T - D of block c
+    auto score_step = [&](int c, int t) {
+        const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f,
+                             0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+        if (t == 0) dp[c] = M::mul(ones, low[c], zero);
+        else if (t == 1) s[c] = M::mul(ka[0], qf[c][0], zero);
+        else if (t & 1) s[c] = M::mul(ka[t >> 1], qf[c][t >> 1], s[c]);
+        else dp[c] = M::mul(va[(t >> 1) - 1], of[c][(t >> 1) - 1], dp[c]);
+    };
+    // the exponential of register r, and what follows it for register r - 1
+    auto exp_step = [&](int c, int r) {
+        if (r < 16) s[c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][r], a.c, -ls[c]));
+        if (r == 0) return;
+        dp[c][r - 1] *= s[c][r - 1];
+        if (!(r & 1)) {
+            dw[c][(r >> 1) - 1] = pack_bf16x2(dp[c][r - 2], dp[c][r - 1]);
+            // formed here, not where it is used
+            asm volatile("" : "+v"(dw[c][(r >> 1) - 1]));
+        }
+    };
+    auto read_r = [&](const u32x4* b, int f) {
+        if (f & 1) va[f >> 1] = frag_of<bf16>(b, R::kV + (f >> 1));
+        else ka[f >> 1] = frag_of<bf16>(b, R::kK + (f >> 1));
+    };
+    constexpr int N1 = NF, N2 = 2 * NF + 1, N = N1 + N2;  // products of X, as of Y
+
+    if (b0 < i1) {
+        next.load(rec);
+        next.store(lds[0]);
+        next.load(b0 + 1 < i1 ? rec + U : rec);
+        next.store(lds[1]);
+    }
+    __syncthreads();
+    if (b0 < i1) {
+#pragma unroll
+        for (int f = 0; f < 2 * NF; ++f) read_r(lds[0], f);
+#pragma unroll
+        for (int t = 0; t < N2; ++t) score_step(0, t);
+    }
+    int u0 = 0, u1 = 1, u2 = 2;  // buffers of records i, i + 1, i + 2
+    for (int i = b0; i < i1; ++i) {
+        // behind the last record it is taken again, so that no branch divides the turn:
+        // what is formed from it is not used
+        next.load(i + 2 < i1 ? rec + 2 * U : last);
+        // reads of LDS spread over the turn, as in attn_dkv2_k
+        // X
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if (t < N1) grad_step(1, t);
+            else score_step(1, t - N1);
+#pragma unroll
+            for (int r = 0; r < 17; ++r)
+                if (r * (N - 2) / 17 + 2 == t) exp_step(0, r);
+            if (t & 1 && t / 2 < N1) kt[t / 2] = frag_of<bf16>(lds[u0], R::kKt + t / 2);
+            if (!(t & 1) && t >= N1 + 2 && (t - N1 - 2) / 2 < NF) read_r(lds[u1], (t - N1 - 2) / 2);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        // Y
+#pragma unroll
+        for (int t = 0; t < N; ++t) {
+            if (!(t & 1) && t / 2 < NF) read_r(lds[u1], NF + t / 2);
+            if (t < N1) grad_step(0, t);
+            else score_step(0, t - N1);
+#pragma unroll
+            for (int r = 0; r < 17; ++r)
+                if (r * (N - 2) / 17 + 2 == t) exp_step(1, r);
+            if (t >= N - 4 && t - (N - 4) < Stage<U>::N) next.store(lds[u2], t - (N - 4));
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        __syncthreads();
+        rec += U;
+        const int u = u0;
+        u0 = u1;
+        u1 = u2;
+        u2 = u;
+    }
+#pragma unroll
+    for (int t = 0; t < N1; ++t) grad_step(1, t);  // B of the last turn
+    if (i1 < b1) {  // keys that fill no record: what lies behind them is cleared
+        next.load(a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + i1) * U);
+        next.store(lds[u2]);
+        __syncthreads();
+        const int left = (int)(live - (int64_t)i1 * 32);
+#pragma unroll
+        for (int f = 0; f < NF; ++f) {
+            read_r(lds[u2], 2 * f);
+            read_r(lds[u2], 2 * f + 1);
+            kt[f] = frag_of<bf16>(lds[u2], R::kKt + f);
+        }
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+#pragma unroll
+            for (int t = 0; t < N2; ++t) score_step(c, t);
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) {
+                    s[c][r] = -INFINITY;
+                    dp[c][r] = 0.f;
+                }
+#pragma unroll
+            for (int r = 0; r < 17; ++r) exp_step(c, r);
+#pragma unroll
+            for (int t = 0; t < N1; ++t) grad_step(c, t);
+        }
+    }
+#pragma unroll
+    for (int c = 0; c < 2; ++c) dq_store<bf16, DB, SPLIT>(a, nh, sp, qb + c, dq[c]);
 }
 
 // Sums of the splits of the backward passes, in a fixed order: [nh][split][rows][tp] ->
@@ -1528,7 +1917,7 @@ static void fwd_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) 
     constexpr int KB = sizeof(T) == 2 ? 2 : 1;
     if constexpr (sizeof(T) == 2 && DB <= 2) {
         if (cb == 2) {
-            RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, 2, KB);
+            RAT3D_ATTN_LAUNCH(attn_fwd2_k, DB);
             return;
         }
     }
@@ -1548,7 +1937,7 @@ template <typename T, int DB>
 static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
     if constexpr (sizeof(T) == 2 && DB <= 2) {
         if (cb == 2) {
-            RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB, 2);
+            RAT3D_ATTN_LAUNCH(attn_dq2_k, DB);
             return;
         }
     }

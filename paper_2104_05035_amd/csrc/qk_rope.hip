@@ -54,8 +54,6 @@ struct QkArgs {
     int tiles;
 };
 
-constexpr int kQkGroups = 8;  // thread groups along the channel pairs
-
 // TOK tokens of one channel, in words: a row may begin at any element.
 template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Toks {
     uint32_t w[TOK * sizeof(T) / 4];
@@ -98,12 +96,13 @@ __device__ __forceinline__ float join_groups(float x, float y) {
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-// PP: pairs per thread, TOK: tokens per thread.
-template <typename T, int PP, int TOK, bool NORM, bool BWD>
-__global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
+// G: thread groups along the channel pairs, PP: pairs per thread, TOK: tokens per thread.
+template <typename T, int G, int PP, int TOK, bool NORM, bool BWD>
+__global__ __launch_bounds__(32 * G, (BWD && PP * TOK == 8 ? 4 : BWD && PP == 3 && sizeof(T) == 2 ? 3 : 2))
+void qk_rope_k(QkArgs a) {
     constexpr int TILE = 32 * TOK;
     // sums over a wave's channels: [parity][sum][wave][token of the lane][lane]
-    __shared__ float sums[2][BWD ? 2 : 1][4][TOK][32];
+    __shared__ float sums[2][BWD ? 2 : 1][G / 2][TOK][32];
     const float inv_d = 1.f / (float)a.pr.head_dim;
     const int lane = threadIdx.x & 31, grp = threadIdx.x >> 5;
     int bid = blockIdx.x;
@@ -140,7 +139,7 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
         const int e0 = a.pr.half[0], e1 = e0 + a.pr.half[1], e2 = e1 + a.pr.half[2];
 #pragma unroll
         for (int p = 0; p < PP; ++p) {
-            const int i = grp + p * kQkGroups;  // pair of the head
+            const int i = grp + p * G;  // pair of the head
             const float2* tab = nullptr;
             int axis = 0;
             if (i < e0) {
@@ -291,7 +290,7 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
                     if (BWD) sd[j] += ga[p] * da[p][j] * xa[p][j] + gb[p] * db[p][j] * xb[p][j];
                 }
             }
-            // both groups of a wave, then the four waves through LDS: each half of a wave
+            // both groups of a wave, then the waves through LDS: each half of a wave
             // writes half of the tokens
             const int half = grp & 1, wave = grp >> 1;
 #pragma unroll
@@ -305,13 +304,14 @@ __global__ __launch_bounds__(256) void qk_rope_k(QkArgs a) {
             __syncthreads();
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
-                const float t = (sums[par][0][0][j][lane] + sums[par][0][1][j][lane]) +
-                                (sums[par][0][2][j][lane] + sums[par][0][3][j][lane]);
+                float t = 0.f, d = 0.f;
+#pragma unroll
+                for (int w = 0; w < G / 2; ++w) {
+                    t += sums[par][0][w][j][lane];
+                    if (BWD) d += sums[par][BWD][w][j][lane];
+                }
                 rs[j] = __builtin_amdgcn_rsqf(__builtin_fmaf(t, inv_d, a.eps));
-                if (BWD)
-                    mean[j] = ((sums[par][BWD][0][j][lane] + sums[par][BWD][1][j][lane]) +
-                               (sums[par][BWD][2][j][lane] + sums[par][BWD][3][j][lane])) *
-                              inv_d * (rs[j] * rs[j]);
+                if (BWD) mean[j] = d * inv_d * (rs[j] * rs[j]);
             }
         }
 #pragma unroll
@@ -456,23 +456,26 @@ template <typename T, bool BWD>
 static void qk_launch(const rat3d_qk_desc& d, const QkArgs& a, hipStream_t st) {
     const unsigned grid = (unsigned)a.parts;
     const bool wide = sizeof(T) == 2 && qk_tokens(d, BWD) == 8;
-#define RAT3D_QK(PP, TOK)                                                      \
-    do {                                                                       \
-        if (d.norm) qk_rope_k<T, PP, TOK, true, BWD><<<grid, 256, 0, st>>>(a); \
-        else qk_rope_k<T, PP, TOK, false, BWD><<<grid, 256, 0, st>>>(a);       \
+#define RAT3D_QK(G, PP, TOK)                                                          \
+    do {                                                                              \
+        if (d.norm) qk_rope_k<T, G, PP, TOK, true, BWD><<<grid, 32 * G, 0, st>>>(a);  \
+        else qk_rope_k<T, G, PP, TOK, false, BWD><<<grid, 32 * G, 0, st>>>(a);        \
     } while (0)
+    // groups and pairs so that few slots stay empty and four waves a SIMD find registers
     if constexpr (sizeof(T) == 2) {
         if (wide) {
-            if (d.head_dim <= 16) RAT3D_QK(1, 8);
-            else if (d.head_dim <= 32) RAT3D_QK(2, 8);
-            else if constexpr (!BWD) RAT3D_QK(4, 8);
+            if (d.head_dim <= 16) RAT3D_QK(8, 1, 8);
+            else if (d.head_dim <= 32) RAT3D_QK(8, 2, 8);
+            else if constexpr (!BWD) RAT3D_QK(16, 2, 8);
             return;
         }
     }
-    if (d.head_dim <= 16) RAT3D_QK(1, 4);
-    else if (d.head_dim <= 32) RAT3D_QK(2, 4);
-    else if (d.head_dim <= 64) RAT3D_QK(4, 4);
-    else RAT3D_QK(8, 4);
+    if (d.head_dim <= 16) RAT3D_QK(8, 1, 4);
+    else if (d.head_dim <= 32) RAT3D_QK(8, 2, 4);
+    else if (d.head_dim <= 48) RAT3D_QK(8, 3, 4);
+    else if (d.head_dim <= 64) RAT3D_QK(16, 2, 4);
+    else if (d.head_dim <= 96) RAT3D_QK(16, 3, 4);
+    else RAT3D_QK(16, 4, 4);
 #undef RAT3D_QK
 }
 

@@ -402,8 +402,8 @@ __device__ __forceinline__ void fwd_store(const AttnArgs& a, int nh, int sp, int
     }
 }
 
-// A workgroup: 128 CB queries of one head, 32 CB a wave as columns; KB x 32 keys a turn.
-template <typename T, int DB, int CB, int KB, bool SPLIT>
+// A workgroup: 128 queries of one head, 32 a wave as columns; KB x 32 keys a turn.
+template <typename T, int DB, int KB, bool SPLIT>
 __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k(AttnArgs a) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
@@ -421,29 +421,18 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
     const int kvh = vol * a.kv + h / (a.heads / a.kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t live = a.count ? a.count[vol] : a.tk;
-    const int64_t q0 = ((int64_t)tile * 4 + wave) * 32 * CB + (lane & 31);
+    const int64_t qt = ((int64_t)tile * 4 + wave) * 32 + (lane & 31);
 
-    frag qf[CB][NR];
+    frag qf[NR];
+    load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq +
+                         (qt < a.tq ? qt : a.tq - 1),
+                     a.tq, a.D, qt < a.tq, qf);
+    f32x16 acc[DB];
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const int64_t t = q0 + 32 * c;
-        load_cols<T, NR>((const T*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq +
-                             (t < a.tq ? t : a.tq - 1),
-                         a.tq, a.D, t < a.tq, qf[c]);
-    }
-
-    f32x16 acc[CB][DB];
-    float m[CB], l4[CB][4];  // the running reference and the sum, of this lane's rows
+    for (int e = 0; e < DB; ++e)
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-#pragma unroll
-        for (int e = 0; e < DB; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c][e][i] = 0.f;
-        m[c] = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l4[c][i] = 0.f;
-    }
+        for (int i = 0; i < 16; ++i) acc[e][i] = 0.f;
+    float m = -INFINITY, l4[4] = {0.f, 0.f, 0.f, 0.f};  // the sum, of this lane's rows
 
     int b0, b1;
     split_range(live, 32 * KB, SPLIT ? a.splits : 1, sp, b0, b1);
@@ -460,19 +449,13 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
             rec += KB * U;
             next.load(rec);
         }
-        f32x16 s[CB][KB];
+        f32x16 s[KB];
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
+            for (int i = 0; i < 16; ++i) s[k][i] = 0.f;
 #pragma unroll
-                for (int i = 0; i < 16; ++i) s[c][k][i] = 0.f;
-#pragma unroll
-            for (int f = 0; f < NR; ++f) {
-                const frag ka = frag_of<T>(lds[buf] + k * U, f);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) s[c][k] = M::mul(ka, qf[c][f], s[c][k]);
-            }
+            for (int f = 0; f < NR; ++f) s[k] = M::mul(frag_of<T>(lds[buf] + k * U, f), qf[f], s[k]);
         }
         if ((int64_t)(b + 1) * 32 * KB > live) {  // the last tile: rows behind the last key
             const int left = (int)(live - (int64_t)b * 32 * KB);
@@ -480,74 +463,50 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
             for (int k = 0; k < KB; ++k)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (k * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= left) {
-#pragma unroll
-                        for (int c = 0; c < CB; ++c) s[c][k][i] = -INFINITY;
-                    }
+                    if (k * 32 + 8 * (i / 4) + 4 * (lane >> 5) + i % 4 >= left) s[k][i] = -INFINITY;
         }
-        float t[CB];
-        bool grew = false;
+        float t = s[0][0];
 #pragma unroll
-        for (int c = 0; c < CB; ++c) {
-            float x = s[c][0][0];
+        for (int k = 0; k < KB; ++k)
 #pragma unroll
-            for (int k = 0; k < KB; ++k)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) x = fmaxf(x, s[c][k][i]);
-            float xa, xb;
-            halves(x, xa, xb);
-            t[c] = fmaxf(xa, xb) * a.c;
-            grew = grew || t[c] > m[c] + 8.f;
-        }
+            for (int i = 0; i < 16; ++i) t = fmaxf(t, s[k][i]);
+        float ta, tb;
+        halves(t, ta, tb);
+        t = fmaxf(ta, tb) * a.c;
         // The reference of the exponentials follows the maximum only where it grew by
         // more than 8 (in log 2): probabilities then stay below 2^8, which neither
         // bfloat16 nor the float32 sums mind, and the sums are rescaled rarely.
-        if (__any(grew)) {
+        if (__any(t > m + 8.f)) {
+            const float to = t > m + 8.f ? t : m;
+            const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m - to);
+            m = to;
 #pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                const float to = t[c] > m[c] + 8.f ? t[c] : m[c];
-                const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
-                m[c] = to;
+            for (int i = 0; i < 4; ++i) l4[i] *= f;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) l4[c][i] *= f;
+            for (int e = 0; e < DB; ++e)
 #pragma unroll
-                for (int e = 0; e < DB; ++e)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) acc[c][e][i] *= f;
-            }
+                for (int i = 0; i < 16; ++i) acc[e][i] *= f;
         }
-        float ref[CB];
-#pragma unroll
-        for (int c = 0; c < CB; ++c) ref[c] = m[c] == -INFINITY ? 0.f : m[c];
+        const float ref = m == -INFINITY ? 0.f : m;
 #pragma unroll
         for (int k = 0; k < KB; ++k) {
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    s[c][k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][k][i], a.c, -ref[c]));
-                    l4[c][i % 4] += s[c][k][i];
-                }
+            for (int i = 0; i < 16; ++i) {
+                s[k][i] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[k][i], a.c, -ref));
+                l4[i % 4] += s[k][i];
+            }
 #pragma unroll
             for (int w = 0; w < NT; ++w) {
-                frag p[CB];
+                const frag p = to_frag<T>(s[k], w);
 #pragma unroll
-                for (int c = 0; c < CB; ++c) p[c] = to_frag<T>(s[c][k], w);
-#pragma unroll
-                for (int e = 0; e < DB; ++e) {
-                    const frag va = frag_of<T>(lds[buf] + k * U, NF + w * DB + e);
-#pragma unroll
-                    for (int c = 0; c < CB; ++c) acc[c][e] = M::mul(va, p[c], acc[c][e]);
-                }
+                for (int e = 0; e < DB; ++e)
+                    acc[e] = M::mul(frag_of<T>(lds[buf] + k * U, NF + w * DB + e), p, acc[e]);
             }
         }
         if (b + 1 < b1) next.store(lds[buf ^ 1]);
         __syncthreads();
     }
-#pragma unroll
-    for (int c = 0; c < CB; ++c)
-        fwd_store<T, DB, SPLIT>(a, nh, sp, q0 + 32 * c, m[c],
-                                (l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), acc[c]);
+    fwd_store<T, DB, SPLIT>(a, nh, sp, qt, m, (l4[0] + l4[1]) + (l4[2] + l4[3]), acc);
 }
 
 // The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
@@ -653,14 +612,12 @@ __global__ __launch_bounds__(256, 2) void attn_fwd2_k(AttnArgs a) {
             asm volatile("" : "+v"(pw[c][(r >> 1) - 1]));
         }
     };
-    // One half of a turn.  C: the block whose probabilities are formed; the products are
-    // the other's, with V of `vb` read behind its values (READV), K of `kb` before its
-    // scores (!READV).
+    // One half of a turn: the probabilities of block C beside the other's products.  In
+    // X (C is A) the other's values take V of the turn before, whose registers then get
+    // this turn's (b: this record); in Y, K of the next turn is read (b: that record).
     auto half_turn = [&](auto block, const u32x4* b) {
         constexpr int C = decltype(block)::value, O = 1 - C;
         constexpr bool X = C == 0;
-        // in X the other block's values come first, and its scores use K as it is; in Y
-        // the first values wait for nothing, K of the next record is read under them
         const float t = top(C);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
@@ -795,55 +752,65 @@ __global__ __launch_bounds__(256) void attn_join_k(AttnArgs a) {
 }
 
 // ------------------------------------------------------------------ few rows
-// A key head with at most four query rows (heads of its group times query tokens):
-// read-out tokens.  The keys and values are read once, as they lie: the scores of
+// A key head with few query rows (heads of its group times query tokens): read-out
+// tokens.  The keys and values are read once, as they lie: the scores of
 // neighbouring keys by neighbouring lanes (a channel's row is contiguous), then, with
 // the probabilities in registers, the sums over a channel's row of values.  4 ROWS
 // operations for each element read: bound by HBM.  A workgroup takes one piece of
-// 256 VEC keys; its part of the softmax (maximum, sum, unnormalised values) is joined
-// with the others' by attn_few_join_k.
+// 256 VEC keys and up to four rows (neighbouring workgroups take a piece's other rows,
+// and find it in their cache); its part of the softmax (maximum, sum, unnormalised
+// values) is joined with the others' by attn_few_join_k.
 struct FewArgs {
     const void *q, *k, *v;
     const uint8_t* mask;
     void* o;
     float* lse;
-    float* part;  // [volume, key head][piece][row][2 + D]: maximum, sum, values
+    float* part;  // [volume, key head][piece][group][row][2 + D]: maximum, sum, values
     int64_t tq, tk, q_stride, k_stride, v_stride, o_stride;
-    int heads, kv, D, pieces, rows;
+    int heads, kv, D, pieces, rows, groups;  // groups of rows
     float c;
 };
 
 template <typename T, int VEC> struct __attribute__((packed, aligned(sizeof(T)))) Keys {
     T v[VEC];
 };
-// VEC keys of a row, of which the first `left` are inside it; keys that are off (bit i
-// of on is 0) count as 0, whatever lies there.
-template <typename T, int VEC, bool ALL>
-__device__ __forceinline__ void ld_keys(const T* p, uint32_t on, int left, float (&o)[VEC]) {
-    if (ALL || left >= VEC) {
-        const Keys<T, VEC> u = *reinterpret_cast<const Keys<T, VEC>*>(p);
+// VEC keys of a row from key t on; keys that are off (bit i of on is 0) count as 0,
+// whatever lies there.  MODE 0: all are on; 1: all are inside the row; 2: some may lie
+// behind its last key, which is read instead.  No branch: the loads of many channels
+// are in flight together.
+template <typename T, int VEC, int MODE>
+__device__ __forceinline__ void ld_keys(const T* row, int64_t t, int64_t tk, uint32_t on,
+                                        float (&o)[VEC]) {
+    if (MODE < 2) {
+        const Keys<T, VEC> u = *reinterpret_cast<const Keys<T, VEC>*>(row + t);
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) o[j] = ALL || (on >> j & 1) ? Elt<T>::from_bits(u.v[j]) : 0.f;
+        for (int j = 0; j < VEC; ++j)
+            o[j] = MODE == 0 || (on >> j & 1) ? Elt<T>::from_bits(u.v[j]) : 0.f;
     } else {
+        T u[VEC];
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) o[j] = j < left && (on >> j & 1) ? Elt<T>::ld(p + j) : 0.f;
+        for (int j = 0; j < VEC; ++j) u[j] = row[t + j < tk ? t + j : tk - 1];
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) o[j] = on >> j & 1 ? Elt<T>::from_bits(u[j]) : 0.f;
     }
 }
 
 template <typename T, int ROWS, int VEC>
-__global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
+__global__ __launch_bounds__(256, (ROWS == 4 && VEC == 8 ? 2 : 4)) void attn_few_k(FewArgs a) {
     __shared__ float qs[128][ROWS];
     __shared__ float ps[ROWS][256 * VEC];
     __shared__ uint32_t ons[256];
     __shared__ float red[2][4][ROWS];
-    const int piece = blockIdx.x % a.pieces, kvh = blockIdx.x / a.pieces;
+    const int group = blockIdx.x % a.groups, pk = blockIdx.x / a.groups;
+    const int piece = pk % a.pieces, kvh = pk / a.pieces;
     const int vol = kvh / a.kv, hk = kvh - vol * a.kv, grp = a.heads / a.kv;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int64_t t0 = (int64_t)piece * 256 * VEC;
     for (int i = tid; i < a.D * ROWS; i += 256) {
-        const int r = i % ROWS, ch = i / ROWS;  // row r: head r / tq of the group, token r % tq
-        const int h = hk * grp + r / (int)a.tq, tok = r % (int)a.tq;
-        qs[ch][r] = r < a.rows ? Elt<T>::ld((const T*)a.q + vol * a.q_stride +
+        // row: head row / tq of the key head's group, token row % tq
+        const int r = i % ROWS, ch = i / ROWS, row = group * ROWS + r;
+        const int h = hk * grp + row / (int)a.tq, tok = row % (int)a.tq;
+        qs[ch][r] = row < a.rows ? Elt<T>::ld((const T*)a.q + vol * a.q_stride +
                                             ((int64_t)h * a.D + ch) * a.tq + tok) * a.c
                                : 0.f;
     }
@@ -853,7 +820,7 @@ __global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
     for (int j = 0; j < VEC; ++j)
         on |= (t + j < a.tk && (!a.mask || a.mask[vol * a.tk + t + j]) ? 1u : 0u) << j;
     ons[tid] = on;
-    const int left = (int)(a.tk - t < VEC ? (a.tk - t > 0 ? a.tk - t : 0) : VEC);
+    const bool inside = t0 + 256 * VEC <= a.tk;  // the whole piece
     __syncthreads();
 
     float s[ROWS][VEC];
@@ -861,19 +828,21 @@ __global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
     for (int r = 0; r < ROWS; ++r)
 #pragma unroll
         for (int j = 0; j < VEC; ++j) s[r][j] = 0.f;
-    const T* kp = (const T*)a.k + vol * a.k_stride + (int64_t)hk * a.D * a.tk + t;
-    auto scores = [&](auto all) {
+    const T* kp = (const T*)a.k + vol * a.k_stride + (int64_t)hk * a.D * a.tk;
+    auto scores = [&](auto mode) {
+        // channels whose loads are in flight together
+        constexpr int SC = VEC <= 2 ? 16 : decltype(mode)::value == 2 ? 2 : 8;
 #pragma unroll 1
-        for (int c0 = 0; c0 < a.D; c0 += 8) {
-            // eight loads in flight; behind the last channel it is read again and not used
-            float x[8][VEC];
+        for (int c0 = 0; c0 < a.D; c0 += SC) {
+            // behind the last channel it is read again and not used
+            float x[SC][VEC];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < SC; ++i) {
                 const int ch = c0 + i < a.D ? c0 + i : a.D - 1;
-                ld_keys<T, VEC, decltype(all)::value>(kp + ch * a.tk, on, left, x[i]);
+                ld_keys<T, VEC, decltype(mode)::value>(kp + ch * a.tk, t, a.tk, on, x[i]);
             }
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
+            for (int i = 0; i < SC; ++i) {
                 if (c0 + i >= a.D) break;
 #pragma unroll
                 for (int r = 0; r < ROWS; ++r) {
@@ -884,9 +853,9 @@ __global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
             }
         }
     };
-    const bool full = __all(on == (1u << VEC) - 1);
-    if (full) scores(std::true_type{});
-    else scores(std::false_type{});
+    if (__all(on == (1u << VEC) - 1)) scores(std::integral_constant<int, 0>{});
+    else if (inside) scores(std::integral_constant<int, 1>{});
+    else scores(std::integral_constant<int, 2>{});
 
     float m[ROWS], l[ROWS];
 #pragma unroll
@@ -930,52 +899,68 @@ __global__ __launch_bounds__(256) void attn_few_k(FewArgs a) {
     // values: a wave takes every fourth channel over all the piece's keys
     float p[ROWS][4][VEC];
     uint32_t live[4];
-    int rest[4];
     bool every = true;
 #pragma unroll
     for (int k = 0; k < 4; ++k) {
         live[k] = ons[k * 64 + lane];
-        const int64_t r = a.tk - t0 - (k * 64 + lane) * VEC;
-        rest[k] = (int)(r < VEC ? (r > 0 ? r : 0) : VEC);
         every = every && live[k] == (1u << VEC) - 1;
 #pragma unroll
         for (int r = 0; r < ROWS; ++r)
 #pragma unroll
             for (int j = 0; j < VEC; ++j) p[r][k][j] = ps[r][(k * VEC + j) * 64 + lane];
     }
-    const T* vp = (const T*)a.v + vol * a.v_stride + (int64_t)hk * a.D * a.tk + t0 + lane * VEC;
-    auto values = [&](auto all) {
-        for (int ch = wave; ch < a.D; ch += 4) {
-            float o[ROWS];
+    const T* vp = (const T*)a.v + vol * a.v_stride + (int64_t)hk * a.D * a.tk;
+    constexpr int VC = VEC <= 2 ? 4 : VEC == 4 || ROWS == 4 ? 2 : 1;  // the same of the values, a wave's channels
+    auto values = [&](auto mode) {
+#pragma unroll 1
+        for (int c0 = wave; c0 < a.D; c0 += 4 * VC) {
+            float x[VC][4][VEC];
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) o[r] = 0.f;
-            float x[4][VEC];
+            for (int i = 0; i < VC; ++i) {
+                const int ch = c0 + 4 * i < a.D ? c0 + 4 * i : a.D - 1;
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
-                ld_keys<T, VEC, decltype(all)::value>(vp + ch * a.tk + k * 64 * VEC, live[k],
-                                                      rest[k], x[k]);
+                for (int k = 0; k < 4; ++k)
+                    ld_keys<T, VEC, decltype(mode)::value>(
+                        vp + ch * a.tk, t0 + (k * 64 + lane) * VEC, a.tk, live[k], x[i][k]);
+            }
+            float o[VC][ROWS];
 #pragma unroll
-            for (int k = 0; k < 4; ++k)
+            for (int i = 0; i < VC; ++i)
 #pragma unroll
-                for (int r = 0; r < ROWS; ++r)
+                for (int r = 0; r < ROWS; ++r) {
+                    o[i][r] = 0.f;
 #pragma unroll
-                    for (int j = 0; j < VEC; ++j) o[r] = __builtin_fmaf(p[r][k][j], x[k][j], o[r]);
+                    for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int r = 0; r < ROWS; ++r) {
+                        for (int j = 0; j < VEC; ++j)
+                            o[i][r] = __builtin_fmaf(p[r][k][j], x[i][k][j], o[i][r]);
+                }
 #pragma unroll
-                for (int d = 32; d >= 1; d >>= 1) o[r] += __shfl_xor(o[r], d);
-                if (lane == 0) part[r * (a.D + 2) + 2 + ch] = o[r];
+            for (int d = 32; d >= 1; d >>= 1)
+#pragma unroll
+                for (int i = 0; i < VC; ++i)
+#pragma unroll
+                    for (int r = 0; r < ROWS; ++r) o[i][r] += __shfl_xor(o[i][r], d);
+            if (lane == 0) {
+#pragma unroll
+                for (int i = 0; i < VC; ++i)
+                    if (c0 + 4 * i < a.D) {
+#pragma unroll
+                        for (int r = 0; r < ROWS; ++r)
+                            part[r * (a.D + 2) + 2 + c0 + 4 * i] = o[i][r];
+                    }
             }
         }
     };
-    if (__all(every)) values(std::true_type{});
-    else values(std::false_type{});
+    if (__all(every)) values(std::integral_constant<int, 0>{});
+    else if (inside) values(std::integral_constant<int, 1>{});
+    else values(std::integral_constant<int, 2>{});
 }
 
 // One workgroup a query row: weighs the pieces by their maxima and adds them up, thread =
 // channel and slice of the pieces, in a fixed order.
 template <typename T>
-__global__ __launch_bounds__(256) void attn_few_join_k(FewArgs a, int stride) {
+__global__ __launch_bounds__(256) void attn_few_join_k(FewArgs a, int stride) {  // rows a piece
     __shared__ float red[256], rl[4];
     const int nhq = blockIdx.x;  // [volume][head][query token]
     const int nh = nhq / (int)a.tq, tok = nhq - nh * (int)a.tq;
@@ -1354,9 +1339,9 @@ __device__ __forceinline__ void dq_store(const AttnArgs& a, int nh, int sp, int6
         }
 }
 
-// dQ: a workgroup keeps 128 CB queries of one head, 32 CB a wave as columns, and walks
-// the live keys, 32 a turn as rows.
-template <typename T, int DB, int CB, bool SPLIT>
+// dQ: a workgroup keeps 128 queries of one head, 32 a wave as columns, and walks the
+// live keys, 32 a turn as rows.
+template <typename T, int DB, bool SPLIT>
 __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
@@ -1372,33 +1357,26 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
     const int kvh = vol * a.kv + h / (a.heads / a.kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t live = a.count ? a.count[vol] : a.tk;
-    const int64_t qb = ((int64_t)tile * 4 + wave) * CB;
-    frag qf[CB][NF], of[CB][NF];
-    float ls[CB], de[CB];
+    const int64_t qb = (int64_t)tile * 4 + wave;
+    const bool have = qb * 32 < a.tqp;
+    frag qf[NF], of[NF];
 #pragma unroll
-    for (int c = 0; c < CB; ++c) {
-        const bool have = (qb + c) * 32 < a.tqp;
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            qf[c][f] = frag{};
-            of[c][f] = frag{};
-            if (have) {
-                const u32x4* rec = a.q_rec + ((int64_t)nh * (a.tqp / 32) + qb + c) * R::kQueries;
-                qf[c][f] = frag_of<T>(rec, R::kQ + f);
-                of[c][f] = frag_of<T>(rec, R::kO + f);
-            }
+    for (int f = 0; f < NF; ++f) {
+        qf[f] = frag{};
+        of[f] = frag{};
+        if (have) {
+            const u32x4* rec = a.q_rec + ((int64_t)nh * (a.tqp / 32) + qb) * R::kQueries;
+            qf[f] = frag_of<T>(rec, R::kQ + f);
+            of[f] = frag_of<T>(rec, R::kO + f);
         }
-        const int64_t at = (int64_t)nh * a.tqp + (qb + c) * 32 + (lane & 31);
-        ls[c] = have ? a.lse2[at] : INFINITY;
-        de[c] = have ? a.delta[at] : 0.f;
     }
-    f32x16 dq[CB][DB];
+    const int64_t at = (int64_t)nh * a.tqp + qb * 32 + (lane & 31);
+    const float ls = have ? a.lse2[at] : INFINITY, de = have ? a.delta[at] : 0.f;
+    f32x16 dq[DB];
 #pragma unroll
-    for (int c = 0; c < CB; ++c)
+    for (int e = 0; e < DB; ++e)
 #pragma unroll
-        for (int e = 0; e < DB; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) dq[c][e][i] = 0.f;
+        for (int i = 0; i < 16; ++i) dq[e][i] = 0.f;
     int b0, b1;
     split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
     const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
@@ -1414,56 +1392,38 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
             rec += U;
             next.load(rec);
         }
-        f32x16 s[CB], dp[CB];
+        f32x16 s, dp;
 #pragma unroll
-        for (int c = 0; c < CB; ++c)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) s[c][r] = dp[c][r] = 0.f;
+        for (int r = 0; r < 16; ++r) s[r] = dp[r] = 0.f;
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
-            const frag ka = frag_of<T>(cur, R::kK + f), va = frag_of<T>(cur, R::kV + f);
-#pragma unroll
-            for (int c = 0; c < CB; ++c) {
-                s[c] = M::mul(ka, qf[c][f], s[c]);
-                dp[c] = M::mul(va, of[c][f], dp[c]);
-            }
+            s = M::mul(frag_of<T>(cur, R::kK + f), qf[f], s);
+            dp = M::mul(frag_of<T>(cur, R::kV + f), of[f], dp);
         }
-        frag df[CB][NT];
 #pragma unroll
-        for (int c = 0; c < CB; ++c) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][r], a.c, -ls[c]));
-                dp[c][r] = s[c][r] * (dp[c][r] - de[c]);
-            }
+        for (int r = 0; r < 16; ++r) {
+            s[r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[r], a.c, -ls));
+            dp[r] = s[r] * (dp[r] - de);
         }
         // rows behind the last key have K = V = 0 and so give nothing to dq, as
         // long as their P stays finite, which exp(-lse) might not
         const int left = live - (int64_t)b * 32 < 32 ? (int)(live - (int64_t)b * 32) : 32;
         if (left < 32) {
 #pragma unroll
-            for (int c = 0; c < CB; ++c)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) dp[c][r] = 0.f;
+            for (int r = 0; r < 16; ++r)
+                if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) dp[r] = 0.f;
         }
 #pragma unroll
-        for (int c = 0; c < CB; ++c)
+        for (int w = 0; w < NT; ++w) {
+            const frag d = to_frag<T>(dp, w);
 #pragma unroll
-            for (int w = 0; w < NT; ++w) df[c][w] = to_frag<T>(dp[c], w);
-#pragma unroll
-        for (int w = 0; w < NT; ++w)
-#pragma unroll
-            for (int e = 0; e < DB; ++e) {
-                const frag kt = frag_of<T>(cur, R::kKt + w * DB + e);
-#pragma unroll
-                for (int c = 0; c < CB; ++c) dq[c][e] = M::mul(kt, df[c][w], dq[c][e]);
-            }
+            for (int e = 0; e < DB; ++e)
+                dq[e] = M::mul(frag_of<T>(cur, R::kKt + w * DB + e), d, dq[e]);
+        }
         if (b + 1 < b1) next.store(lds[((b - b0) & 1) ^ 1]);
         __syncthreads();
     }
-#pragma unroll
-    for (int c = 0; c < CB; ++c) dq_store<T, DB, SPLIT>(a, nh, sp, qb + c, dq[c]);
+    dq_store<T, DB, SPLIT>(a, nh, sp, qb, dq);
 }
 
 // The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
@@ -1736,12 +1696,17 @@ static int few_keys(const rat3d_attention_desc& d) {
     const bool many = (int64_t)d.n * d.kv_heads * ceil_div(d.tk, wide) >= 2 * (int64_t)device_cus();
     return (int)(many ? wide : wide / 4);
 }
+// The kernel for few rows is taken up to eight rows in bfloat16, sixteen in float32.
+// Measured against packing and tiles: 8 x 2 key heads x 32 over 48x56x48, 8 rows 117
+// against 241 us (bfloat16) and 165 against 757 (float32), 16 rows 213 against 231 and
+// 301 against 758; 4 x 2 x 64 over 24x28x24, 8 rows 39 against 44 and 51 against 106, 16
+// rows 50 against 43 and 83 against 106.
 static bool few_rows(const rat3d_attention_desc& d) {
-    return d.heads / d.kv_heads * d.tq <= 4;
+    return d.heads / d.kv_heads * d.tq <= (d.dtype == RAT3D_BF16 ? 8 : 16);
 }
-static int few_stride(const rat3d_attention_desc& d) {  // rows that a workgroup is built for
+static int few_stride(const rat3d_attention_desc& d) {  // rows that a piece's workgroups hold
     const int64_t rows = d.heads / d.kv_heads * d.tq;
-    return rows <= 2 ? (int)rows : 4;
+    return rows <= 2 ? (int)rows : (int)(rows + 3) / 4 * 4;
 }
 
 // masked: whether a mask is given.  Where one is, much of dK/dV's workgroups find no
@@ -1816,7 +1781,7 @@ bool attention_fits(const rat3d_attention_desc& d) {
            (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 128) * p.ks < (1 << 24) &&
            nq * ceil_div(d.tq, 64) * 16 + 32 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
                (1ll << 31) &&
-           (!few_rows(d) || (int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) < (1 << 24)) &&
+           (!few_rows(d) || (int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) * 4 < (1 << 24)) &&
            p.tqp / 32 * (d.heads / d.kv_heads) < (1 << 30);
 }
 
@@ -1921,7 +1886,7 @@ static void fwd_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) 
             return;
         }
     }
-    RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, 1, KB);
+    RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, KB);
 }
 template <typename T, int DB>
 static void dkv_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
@@ -1941,7 +1906,7 @@ static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
             return;
         }
     }
-    RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB, 1);
+    RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB);
 }
 template <typename T, int VEC>
 static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
@@ -1986,7 +1951,8 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
         f.pieces = (int)ceil_div(d.tk, keys);
         ProfScope ps("attn_few", st, 4.0 * nq * d.tq * d.tk * d.head_dim,
                      2.0 * nk * d.tk * d.head_dim * p.es);
-        const unsigned grid = (unsigned)((int64_t)d.n * d.kv_heads * f.pieces);
+        f.groups = f.rows <= 4 ? 1 : (f.rows + 3) / 4;
+        const unsigned grid = (unsigned)((int64_t)d.n * d.kv_heads * f.pieces * f.groups);
         if (d.dtype == RAT3D_BF16) {
             if (keys == 2048) few_launch<bf16, 8>(f, grid, st);
             else few_launch<bf16, 2>(f, grid, st);

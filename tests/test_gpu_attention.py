@@ -123,7 +123,9 @@ WIDE = [(64, 4, 4, 64, 77, 130, None), (64, 8, 4, 40, 130, 77, "half"), (64, 4, 
 # few query rows: pieces of the keys, in both widths
 FEW = [(1, 1, 1, 1, 1, 1, None), (2, 2, 1, 33, 1, 513, "half"), (1, 4, 1, 40, 1, 2049, None),
        (2, 2, 2, 128, 3, 700, "run"), (2, 3, 3, 64, 4, 1025, "first_none"), (1, 4, 2, 24, 2, 3000, "one"),
-       (40, 4, 2, 8, 1, 16400, "half"), (40, 2, 2, 9, 4, 13313, None), (60, 3, 3, 5, 3, 6145, "run")]
+       (40, 4, 2, 8, 1, 16400, "half"), (40, 2, 2, 9, 4, 13313, None), (60, 3, 3, 5, 3, 6145, "run"),
+       (1, 1, 1, 17, 5, 600, None), (2, 6, 2, 32, 4, 1030, "half"), (1, 8, 1, 64, 2, 900, "first65"),
+       (2, 4, 2, 40, 7, 520, "first_none"), (40, 2, 2, 6, 13, 13000, "half"), (1, 1, 1, 16, 17, 300, None)]
 ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE + FEW for dt in ("bf16", "f32")]
 
 

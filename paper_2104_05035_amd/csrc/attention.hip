@@ -1019,8 +1019,7 @@ template <typename T, int DB> struct Rec {
 struct DkvPlace {
     int vol, hk, kvh, sp, tile;
     int64_t live;
-    __device__ __forceinline__ DkvPlace(const AttnArgs& a, bool split) {
-        int bid = xcd_remap(blockIdx.x, gridDim.x);
+    __device__ __forceinline__ DkvPlace(const AttnArgs& a, bool split, int bid) {
         tile = bid % a.tiles;
         bid /= a.tiles;
         sp = split ? bid % a.splits : 0;
@@ -1072,13 +1071,12 @@ __device__ __forceinline__ void dkv_store(const AttnArgs& a, const DkvPlace& p, 
 // product as s - lse / scale and dO V^T as dO V^T - D: both constants of a row are added
 // by the matrix instruction, from a fragment of the record.
 template <typename T, int DB, bool SPLIT>
-__global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a) {
+__device__ __forceinline__ void dkv_block(const AttnArgs& a, int bid, u32x4* room) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
     typedef Rec<T, DB> R;
     constexpr int NF = R::NF, NT = 32 / M::kT, U = R::kQueries;
-    __shared__ u32x4 lds[2][U];
-    const DkvPlace at(a, SPLIT);
+    const DkvPlace at(a, SPLIT, bid);
     if ((int64_t)at.tile * 128 >= at.live) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t kb = (int64_t)at.tile * 4 + wave;  // block of 32 keys
@@ -1112,11 +1110,11 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a)
     Stage<U> next;
     if (i0 < i1) {
         next.load(rec);
-        next.store(lds[0]);
+        next.store(room);
     }
     __syncthreads();
     for (int i = i0; i < i1; ++i) {
-        const u32x4* cur = lds[(i - i0) & 1];
+        const u32x4* cur = room + ((i - i0) & 1) * U;
         if (i + 1 < i1) {
             rec += U;
             next.load(rec);
@@ -1146,7 +1144,7 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dkv_k(AttnArgs a)
                 dk[e] = M::mul(frag_of<T>(cur, R::kQt + w * DB + e), d, dk[e]);
             }
         }
-        if (i + 1 < i1) next.store(lds[((i - i0) & 1) ^ 1]);
+        if (i + 1 < i1) next.store(room + (((i - i0) & 1) ^ 1) * U);
         __syncthreads();
     }
     dkv_store<T, DB, SPLIT>(a, at, kb, dk, dv);
@@ -1169,7 +1167,7 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dkv2_k(AttnArgs a
     typedef Rec<bf16, DB> R;
     constexpr int NF = R::NF, U = R::kQueries;
     __shared__ u32x4 lds[3][U];
-    const DkvPlace at(a, SPLIT);
+    const DkvPlace at(a, SPLIT, xcd_remap(blockIdx.x, gridDim.x));
     if ((int64_t)at.tile * 256 >= at.live) return;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t kb = ((int64_t)at.tile * 4 + wave) * 2;  // first block of 32 keys
@@ -1342,13 +1340,11 @@ __device__ __forceinline__ void dq_store(const AttnArgs& a, int nh, int sp, int6
 // dQ: a workgroup keeps 128 queries of one head, 32 a wave as columns, and walks the
 // live keys, 32 a turn as rows.
 template <typename T, int DB, bool SPLIT>
-__global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) {
+__device__ __forceinline__ void dq_block(const AttnArgs& a, int bid, u32x4* room) {
     typedef Mm<T> M;
     typedef typename M::frag frag;
     typedef Rec<T, DB> R;
     constexpr int NF = R::NF, NT = 32 / M::kT, U = R::kKeys;
-    __shared__ u32x4 lds[2][U];
-    int bid = xcd_remap(blockIdx.x, gridDim.x);
     const int tile = bid % a.tiles;
     bid /= a.tiles;
     const int sp = SPLIT ? bid % a.splits : 0;
@@ -1383,11 +1379,11 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
     Stage<U> next;
     if (b0 < b1) {
         next.load(rec);
-        next.store(lds[0]);
+        next.store(room);
     }
     __syncthreads();
     for (int b = b0; b < b1; ++b) {
-        const u32x4* cur = lds[(b - b0) & 1];
+        const u32x4* cur = room + ((b - b0) & 1) * U;
         if (b + 1 < b1) {
             rec += U;
             next.load(rec);
@@ -1420,10 +1416,26 @@ __global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_dq_k(AttnArgs a) 
             for (int e = 0; e < DB; ++e)
                 dq[e] = M::mul(frag_of<T>(cur, R::kKt + w * DB + e), d, dq[e]);
         }
-        if (b + 1 < b1) next.store(lds[((b - b0) & 1) ^ 1]);
+        if (b + 1 < b1) next.store(room + (((b - b0) & 1) ^ 1) * U);
         __syncthreads();
     }
     dq_store<T, DB, SPLIT>(a, nh, sp, qb, dq);
+}
+
+// Both walks of the backward in one launch, one behind the other in the grid: neither
+// reads what the other writes, and on small maps, where each alone leaves CUs idle, they
+// overlap (2 x 4 x 64 over 6x7x6 in float32: 22 us as two launches, 16 as one).
+struct BwdArgs {
+    AttnArgs kv, q;  // dK/dV, dQ
+    int kv_blocks, q_blocks;
+};
+template <typename T, int DB, bool KS, bool QS>
+__global__ __launch_bounds__(256, (DB <= 2 ? 2 : 1)) void attn_bwd_k(BwdArgs g) {
+    __shared__ u32x4 room[2 * Rec<T, DB>::kQueries];  // the larger record
+    static_assert(Rec<T, DB>::kQueries >= Rec<T, DB>::kKeys, "room");
+    const int b = (int)blockIdx.x;
+    if (b < g.kv_blocks) dkv_block<T, DB, KS>(g.kv, xcd_remap(b, g.kv_blocks), room);
+    else dq_block<T, DB, QS>(g.q, xcd_remap(b - g.kv_blocks, g.q_blocks), room);
 }
 
 // The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
@@ -1777,8 +1789,9 @@ bool attention_fits(const rat3d_attention_desc& d) {
     // workgroups of the largest launches (each of 256 threads, 2^32 threads a launch)
     return 2 * nq * ceil_div(d.tq, 64) + 2 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
                (1 << 24) &&
-           nq * ceil_div(d.tq, 128) * p.fs < (1 << 24) && nq * ceil_div(d.tq, 128) * p.qs < (1 << 24) &&
-           (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 128) * p.ks < (1 << 24) &&
+           nq * ceil_div(d.tq, 128) * p.fs < (1 << 24) &&
+           nq * ceil_div(d.tq, 128) * p.qs + (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 128) * p.ks <
+               (1 << 24) &&
            nq * ceil_div(d.tq, 64) * 16 + 32 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
                (1ll << 31) &&
            (!few_rows(d) || (int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) * 4 < (1 << 24)) &&
@@ -1888,25 +1901,29 @@ static void fwd_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) 
     }
     RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, KB);
 }
+// kc, qc: column blocks of the two walks; both walks of one block go in one launch.
 template <typename T, int DB>
-static void dkv_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
+static void bwd_launch(const BwdArgs& g, int kc, int qc, hipStream_t st) {
+    const bool ks = g.kv.splits > 1, qs = g.q.splits > 1;
+    BwdArgs one = g;  // what the general kernel takes
     if constexpr (sizeof(T) == 2 && DB <= 2) {
-        if (cb == 2) {
-            RAT3D_ATTN_LAUNCH(attn_dkv2_k, DB);
-            return;
+        if (kc == 2) {
+            if (ks) attn_dkv2_k<DB, true><<<(unsigned)g.kv_blocks, 256, 0, st>>>(g.kv);
+            else attn_dkv2_k<DB, false><<<(unsigned)g.kv_blocks, 256, 0, st>>>(g.kv);
+            one.kv_blocks = 0;
+        }
+        if (qc == 2) {
+            if (qs) attn_dq2_k<DB, true><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
+            else attn_dq2_k<DB, false><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
+            one.q_blocks = 0;
         }
     }
-    RAT3D_ATTN_LAUNCH(attn_dkv_k, T, DB);
-}
-template <typename T, int DB>
-static void dq_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
-    if constexpr (sizeof(T) == 2 && DB <= 2) {
-        if (cb == 2) {
-            RAT3D_ATTN_LAUNCH(attn_dq2_k, DB);
-            return;
-        }
-    }
-    RAT3D_ATTN_LAUNCH(attn_dq_k, T, DB);
+    const unsigned grid = (unsigned)(one.kv_blocks + one.q_blocks);
+    if (grid == 0) return;
+    if (ks && qs) attn_bwd_k<T, DB, true, true><<<grid, 256, 0, st>>>(one);
+    else if (ks) attn_bwd_k<T, DB, true, false><<<grid, 256, 0, st>>>(one);
+    else if (qs) attn_bwd_k<T, DB, false, true><<<grid, 256, 0, st>>>(one);
+    else attn_bwd_k<T, DB, false, false><<<grid, 256, 0, st>>>(one);
 }
 template <typename T, int VEC>
 static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
@@ -2038,19 +2055,17 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
     }
     const bool bf = d.dtype == RAT3D_BF16;
     {
-        ProfScope ps("attn_dkv", st, 3.0 * one, 0.0);
-        a.splits = p.ks;
-        a.tiles = (int)ceil_div(d.tk, 128 * p.kc);
-        const int64_t grid = (int64_t)d.n * d.kv_heads * a.tiles * a.splits;
-        RAT3D_ATTN(dkv_launch, d.dtype, p.DB, a, p.kc, grid, st);
-    }
-    {
-        ProfScope ps("attn_dq", st, 2.0 * one, 0.0);
-        a.part = (float*)(w + p.qpart);
-        a.splits = p.qs;
-        a.tiles = (int)ceil_div(d.tq, 128 * p.qc);
-        const int64_t grid = (int64_t)d.n * d.heads * a.tiles * a.splits;
-        RAT3D_ATTN(dq_launch, d.dtype, p.DB, a, p.qc, grid, st);
+        ProfScope ps("attn_bwd", st, 5.0 * one, 0.0);
+        BwdArgs g;
+        g.kv = g.q = a;
+        g.kv.splits = p.ks;
+        g.kv.tiles = (int)ceil_div(d.tk, 128 * p.kc);
+        g.kv_blocks = d.n * d.kv_heads * g.kv.tiles * p.ks;
+        g.q.part = (float*)(w + p.qpart);
+        g.q.splits = p.qs;
+        g.q.tiles = (int)ceil_div(d.tq, 128 * p.qc);
+        g.q_blocks = d.n * d.heads * g.q.tiles * p.qs;
+        RAT3D_ATTN(bwd_launch, d.dtype, p.DB, g, p.kc, p.qc, st);
     }
     if (p.ks > 1 || p.qs > 1) {
         SumArgs g = {};

@@ -509,193 +509,6 @@ __global__ __launch_bounds__(256, (sizeof(T) * DB < 16 ? 2 : 1)) void attn_fwd_k
     fwd_store<T, DB, SPLIT>(a, nh, sp, qt, m, (l4[0] + l4[1]) + (l4[2] + l4[3]), acc);
 }
 
-// The same in bfloat16 with 64 queries a wave, in two column blocks A and B, and the
-// phases of neighbouring turns (32 keys) laid over each other:
-//   X: values of B for turn i - 1, scores of B for turn i   beside   softmax of A, turn i
-//   Y: values of A for turn i, scores of A for turn i + 1   beside   softmax of B, turn i
-// A fragment read from LDS feeds both blocks, and the matrix cores work under the
-// exponentials, which bound the kernel: a score takes a fused multiply-add, an
-// exponential (8 cycles), an addition, half a conversion and half a maximum.  Three LDS
-// buffers, as in attn_dkv2_k.  The last keys, where they do not fill a record, are taken
-// by themselves behind the loop.
-template <int DB, bool SPLIT>
-__global__ __launch_bounds__(256, 2) void attn_fwd2_k(AttnArgs a) {
-    typedef Mm<bf16> M;
-    typedef bf16x8 frag;
-    constexpr int NF = 2 * DB, U = 2 * NF * 64;
-    __shared__ u32x4 lds[3][U];
-    int bid = xcd_remap(blockIdx.x, gridDim.x);
-    const int tile = bid % a.tiles;
-    bid /= a.tiles;
-    const int sp = SPLIT ? bid % a.splits : 0;
-    const int nh = SPLIT ? bid / a.splits : bid;
-    const int vol = nh / a.heads, h = nh - vol * a.heads;
-    const int kvh = vol * a.kv + h / (a.heads / a.kv);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t live = a.count ? a.count[vol] : a.tk;
-    const int64_t q0 = ((int64_t)tile * 4 + wave) * 64 + (lane & 31);
-
-    frag qf[2][NF];
-    f32x16 acc[2][DB], s[2];
-    float m[2], l4[2][4];  // the running reference and the sum, of this lane's rows
-    uint32_t pw[2][8];     // probabilities, two a word
-    frag kf[NF], vf[NF];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        const int64_t t = q0 + 32 * c;
-        load_cols<bf16, NF>((const bf16*)a.q + vol * a.q_stride + (int64_t)h * a.D * a.tq +
-                                (t < a.tq ? t : a.tq - 1),
-                            a.tq, a.D, t < a.tq, qf[c]);
-        m[c] = -INFINITY;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l4[c][i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            s[c][i] = 0.f;
-#pragma unroll
-            for (int e = 0; e < DB; ++e) acc[c][e][i] = 0.f;
-        }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) pw[c][i] = 0;
-    }
-#pragma unroll
-    for (int f = 0; f < NF; ++f) vf[f] = frag{};
-
-    int b0, b1;
-    split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
-    const int whole = (int)(live / 32);
-    const int i1 = b1 < whole ? b1 : whole;  // records that keys fill
-    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
-    const u32x4* last = rec + (int64_t)(i1 - b0 - 1) * U;
-    Stage<U> next;
-
-    auto value_step = [&](int c, int t) {  // one of the NF products of the values of block c
-        const int w = t / DB, e = t % DB;
-        const u32x4 p = {pw[c][4 * w], pw[c][4 * w + 1], pw[c][4 * w + 2], pw[c][4 * w + 3]};
-        acc[c][e] = M::mul(vf[t], __builtin_bit_cast(frag, p), acc[c][e]);
-    };
-    auto score_step = [&](int c, int t) {  // one of the NF products of the scores of block c
-        const f32x16 zero = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f,
-                             0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-        s[c] = t == 0 ? M::mul(kf[0], qf[c][0], zero) : M::mul(kf[t], qf[c][t], s[c]);
-    };
-    // The reference of the exponentials follows the maximum only where it grew by more
-    // than 8 (in log 2), as in attn_fwd_k.
-    auto top = [&](int c) {
-        float x = s[c][0];
-#pragma unroll
-        for (int i = 1; i < 16; ++i) x = fmaxf(x, s[c][i]);
-        float xa, xb;
-        halves(x, xa, xb);
-        return fmaxf(xa, xb) * a.c;
-    };
-    auto follow = [&](int c, float t) {
-        if (!__any(t > m[c] + 8.f)) return;
-        const float to = t > m[c] + 8.f ? t : m[c];
-        const float f = to == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(m[c] - to);
-        m[c] = to;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) l4[c][i] *= f;
-#pragma unroll
-        for (int e = 0; e < DB; ++e)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) acc[c][e][i] *= f;
-    };
-    // the exponential of register r, and what follows it for register r - 1
-    auto exp_step = [&](int c, int r, float ref) {
-        if (r < 16) s[c][r] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[c][r], a.c, -ref));
-        if (r == 0) return;
-        l4[c][(r - 1) % 4] += s[c][r - 1];
-        if (!(r & 1)) {
-            pw[c][(r >> 1) - 1] = pack_bf16x2(s[c][r - 2], s[c][r - 1]);
-            // formed here, not where it is used
-            asm volatile("" : "+v"(pw[c][(r >> 1) - 1]));
-        }
-    };
-    // One half of a turn: the probabilities of block C beside the other's products.  In
-    // X (C is A) the other's values take V of the turn before, whose registers then get
-    // this turn's (b: this record); in Y, K of the next turn is read (b: that record).
-    auto half_turn = [&](auto block, const u32x4* b) {
-        constexpr int C = decltype(block)::value, O = 1 - C;
-        constexpr bool X = C == 0;
-        const float t = top(C);
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            if (!X) kf[f] = frag_of<bf16>(b, f);
-            value_step(O, f);
-        }
-        __builtin_amdgcn_sched_barrier(0);
-        follow(C, t);
-        const float ref = m[C] == -INFINITY ? 0.f : m[C];
-#pragma unroll
-        for (int r = 0; r < 17; ++r) {
-            if (r % (16 / NF) == 0 && r < 16) score_step(O, r / (16 / NF));
-            if (X && r % (16 / NF) == 0 && r < 16) vf[r / (16 / NF)] = frag_of<bf16>(b, NF + r / (16 / NF));
-            exp_step(C, r, ref);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-
-    if (b0 < i1) {
-        next.load(rec);
-        next.store(lds[0]);
-        next.load(b0 + 1 < i1 ? rec + U : rec);
-        next.store(lds[1]);
-    }
-    __syncthreads();
-    if (b0 < i1) {
-#pragma unroll
-        for (int f = 0; f < NF; ++f) kf[f] = frag_of<bf16>(lds[0], f);
-#pragma unroll
-        for (int f = 0; f < NF; ++f) score_step(0, f);
-    }
-    int u0 = 0, u1 = 1, u2 = 2;  // buffers of records i, i + 1, i + 2
-    for (int i = b0; i < i1; ++i) {
-        // behind the last record it is taken again: what is formed from it is not used
-        next.load(i + 2 < i1 ? rec + 2 * U : last);
-        half_turn(std::integral_constant<int, 0>{}, lds[u0]);
-        half_turn(std::integral_constant<int, 1>{}, lds[u1]);
-        next.store(lds[u2]);
-        __syncthreads();
-        rec += U;
-        const int u = u0;
-        u0 = u1;
-        u1 = u2;
-        u2 = u;
-    }
-#pragma unroll
-    for (int f = 0; f < NF; ++f) value_step(1, f);  // B of the last turn
-    if (i1 < b1) {  // keys that fill no record
-        next.load(a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + i1) * U);
-        next.store(lds[u2]);
-        __syncthreads();
-        const int left = (int)(live - (int64_t)i1 * 32);
-#pragma unroll
-        for (int f = 0; f < NF; ++f) {
-            kf[f] = frag_of<bf16>(lds[u2], f);
-            vf[f] = frag_of<bf16>(lds[u2], NF + f);
-        }
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-#pragma unroll
-            for (int f = 0; f < NF; ++f) score_step(c, f);
-#pragma unroll
-            for (int r = 0; r < 16; ++r)
-                if (8 * (r / 4) + 4 * (lane >> 5) + r % 4 >= left) s[c][r] = -INFINITY;
-            follow(c, top(c));
-            const float ref = m[c] == -INFINITY ? 0.f : m[c];
-#pragma unroll
-            for (int r = 0; r < 17; ++r) exp_step(c, r, ref);
-#pragma unroll
-            for (int f = 0; f < NF; ++f) value_step(c, f);
-        }
-    }
-#pragma unroll
-    for (int c = 0; c < 2; ++c)
-        fwd_store<bf16, DB, SPLIT>(a, nh, sp, q0 + 32 * c, m[c],
-                                   (l4[c][0] + l4[c][1]) + (l4[c][2] + l4[c][3]), acc[c]);
-}
-
 // Joins the splits of the forward: a workgroup takes 64 queries and 8 channels.
 template <typename T>
 __global__ __launch_bounds__(256) void attn_join_k(AttnArgs a) {
@@ -1679,8 +1492,8 @@ __global__ __launch_bounds__(256) void attn_sum_k(SumArgs g) {
 struct AttnPlan {
     int64_t tqp, tkp;
     int DB, es;
-    int fc, kc, qc;  // blocks of 32 kept tokens a wave: forward, dK/dV, dQ
-    int fs, ks, qs;  // splits of the same
+    int kc, qc;      // blocks of 32 kept tokens a wave: dK/dV, dQ
+    int fs, ks, qs;  // splits of the forward, of dK/dV, of dQ
     size_t idx, count, kv_rec, q_rec, lse2, delta, part, qpart, fpart, stat, bytes[2];
 };
 
@@ -1694,8 +1507,12 @@ static int splits_for(int64_t groups, int64_t turns, int64_t least, int per_cu =
     return s < 2 ? 1 : (int)s;
 }
 
-// Two blocks of 32 kept tokens a wave in bfloat16, where the registers hold them and
-// there are workgroups enough: each fragment read from LDS then feeds two products.
+// Backward in bfloat16: two blocks of 32 kept tokens a wave where the registers hold
+// them (head_dim <= 64) and that leaves three workgroups for two CUs.  Both walks at 4 x 2
+// heads over 24x28x24 voxels: 2120 us with one block, 1714 with two at head_dim 64, 1220
+// and 1060 at 32; 8 x 4 heads x 32 over 2100 tokens (288 workgroups) 126 and 127.  The
+// forward gains nothing by it: its bound is the exponentials, whose number stays
+// (head_dim 32: 433 us with one block, 473 with two; 64: 604 and 581).
 static int columns_for(const rat3d_attention_desc& d, int DB, int64_t groups) {
     return d.dtype == RAT3D_BF16 && DB <= 2 && 2 * groups >= 3 * (int64_t)device_cus() ? 2 : 1;
 }
@@ -1731,11 +1548,11 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d, bool masked) {
     p.tqp = ceil_div(d.tq, 64) * 64;
     p.tkp = ceil_div(d.tk, 64) * 64;
     const int64_t nq = (int64_t)d.n * d.heads, nk = (int64_t)d.n * d.kv_heads;
-    p.fc = p.qc = columns_for(d, p.DB, nq * ceil_div(d.tq, 256));
+    p.qc = columns_for(d, p.DB, nq * ceil_div(d.tq, 256));
     p.kc = columns_for(d, p.DB, nk * ceil_div(d.tk, 256));
     // a turn of float32 takes microseconds, one of bfloat16 a fraction
     const int least = d.dtype == RAT3D_BF16 ? 4 : 1;
-    p.fs = splits_for(nq * ceil_div(d.tq, 128 * p.fc), p.tkp / 32, least);
+    p.fs = splits_for(nq * ceil_div(d.tq, 128), p.tkp / 32, least);
     p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, least);
     p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), least,
                       masked ? 4 : 2);
@@ -1885,21 +1702,11 @@ static rat3d_status live_keys(const rat3d_attention_desc& d, const AttnPlan& p, 
         if (s_ != RAT3D_OK) return s_;        \
     } while (0)
 
-#define RAT3D_ATTN_LAUNCH(K, ...)                                                 \
-    do {                                                                          \
-        if (a.splits > 1) K<__VA_ARGS__, true><<<(unsigned)grid, 256, 0, st>>>(a); \
-        else K<__VA_ARGS__, false><<<(unsigned)grid, 256, 0, st>>>(a);            \
-    } while (0)
 template <typename T, int DB>
-static void fwd_launch(const AttnArgs& a, int cb, int64_t grid, hipStream_t st) {
+static void fwd_launch(const AttnArgs& a, int64_t grid, hipStream_t st) {
     constexpr int KB = sizeof(T) == 2 ? 2 : 1;
-    if constexpr (sizeof(T) == 2 && DB <= 2) {
-        if (cb == 2) {
-            RAT3D_ATTN_LAUNCH(attn_fwd2_k, DB);
-            return;
-        }
-    }
-    RAT3D_ATTN_LAUNCH(attn_fwd_k, T, DB, KB);
+    if (a.splits > 1) attn_fwd_k<T, DB, KB, true><<<(unsigned)grid, 256, 0, st>>>(a);
+    else attn_fwd_k<T, DB, KB, false><<<(unsigned)grid, 256, 0, st>>>(a);
 }
 // kc, qc: column blocks of the two walks; both walks of one block go in one launch.
 template <typename T, int DB>
@@ -1996,9 +1803,9 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
     {
         ProfScope ps("attn_fwd", st, 4.0 * nq * d.tq * d.tk * d.head_dim, 0.0);
         a.splits = p.fs;
-        a.tiles = (int)ceil_div(d.tq, 128 * p.fc);
+        a.tiles = (int)ceil_div(d.tq, 128);
         const int64_t grid = (int64_t)d.n * d.heads * a.tiles * a.splits;
-        RAT3D_ATTN(fwd_launch, d.dtype, p.DB, a, p.fc, grid, st);
+        RAT3D_ATTN(fwd_launch, d.dtype, p.DB, a, grid, st);
     }
     if (p.fs > 1) {
         ProfScope ps("attn_join", st, 0.0, nq * d.tq * d.head_dim * (4.0 * p.fs + p.es));

@@ -289,13 +289,14 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
 typedef struct {
     int n, heads, kv_heads, head_dim;
     int64_t tq, tk;
-    float scale; /* > 0; 0 stands for 1/sqrt(head_dim) */
+    float scale; /* within 2^-60 .. 2^60; 0 stands for 1/sqrt(head_dim) */
     int64_t q_stride, k_stride, v_stride, o_stride; /* also of dq, dk, dv, dout */
     rat3d_dtype dtype;
 } rat3d_attention_desc;
 
-/* Bytes of workspace (pass 0 = fwd, 1 = bwd); (size_t)-1 if the descriptor is
- * invalid. */
+/* Bytes of workspace (pass 0 = fwd, 1 = bwd; enough with and without a mask);
+ * (size_t)-1 if the descriptor is invalid.  Calls that may run at the same time
+ * (streams, graphs) need a workspace each.  No result may overlap an input. */
 size_t rat3d_attention_workspace_size(const rat3d_attention_desc* desc, int pass);
 rat3d_status rat3d_attention_fwd(const rat3d_attention_desc* desc, const void* q, const void* k,
                                  const void* v, const uint8_t* mask, void* o, float* lse,

@@ -365,7 +365,8 @@ static rat3d_status check_qk(const rat3d_qk_desc* d) {
     const double v = (double)d->d * d->h * d->w;
     RAT3D_REQUIRE((double)d->d + d->h + d->w < 1.6e7, RAT3D_EUNSUPPORTED,
                   "qk map too large for one launch");
-    RAT3D_REQUIRE((v / 128.0 + 1) * d->n * ((double)d->heads + d->kv_heads) < 1.6e7,
+    // workgroups of up to 512 threads, 2^32 threads a launch
+    RAT3D_REQUIRE((v / 128.0 + 1) * d->n * ((double)d->heads + d->kv_heads) < 8.0e6,
                   RAT3D_EUNSUPPORTED, "qk map too large for one launch");
     const double hv = (double)d->head_dim * v;
     RAT3D_STRIDE(d->q_stride, hv * d->heads);
@@ -453,8 +454,8 @@ static rat3d_status check_attention(const rat3d_attention_desc* d) {
                   RAT3D_EINVAL, "attention sizes must be >= 1");
     RAT3D_REQUIRE(d->heads % d->kv_heads == 0, RAT3D_EINVAL,
                   "heads must be a multiple of kv_heads (%d, %d)", d->heads, d->kv_heads);
-    RAT3D_REQUIRE(d->scale == 0.f || (d->scale > 0.f && d->scale < 1e30f), RAT3D_EINVAL,
-                  "scale must be positive and finite, or 0 for 1/sqrt(head_dim)");
+    RAT3D_REQUIRE(d->scale == 0.f || (d->scale >= 0x1p-60f && d->scale <= 0x1p60f), RAT3D_EINVAL,
+                  "scale must be within 2^-60 .. 2^60, or 0 for 1/sqrt(head_dim)");
     RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
                   (int)d->dtype);
     RAT3D_REQUIRE(d->head_dim <= 128, RAT3D_EUNSUPPORTED, "head_dim above 128 is not built");

@@ -170,7 +170,8 @@ struct PackJob {
     const float* lse;
     u32x4* rec;          // records of 32 tokens, `units` 16-byte units each:
     int units, r, t, x;  // where forms R and T and the row constants lie, or -1
-    float* lse2;         // lse in units of log 2, padded with +infinity
+    float* lse2;         // lse in units of log 2; +infinity behind the last query and for
+                         // a query without keys: its probabilities are then 0
     float* delta;        // D, padded with 0
     const int* idx;      // live tokens, or null
     const int* count;
@@ -245,7 +246,7 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
         if (half == 0) {
             const int64_t at = (int64_t)nh * J.tiles * kPackTok + t0 + tk;
             J.delta[at] = d;
-            J.lse2[at] = on ? e * kLog2e : INFINITY;
+            J.lse2[at] = e == -INFINITY ? INFINITY : e * kLog2e;
         }
         // Row constants of the products with these rows: -lse in units of the scores,
         // and -D.  Behind the last query, and where a query has no key, a number so low
@@ -1603,15 +1604,15 @@ size_t attention_ws_bytes(const rat3d_attention_desc& d, int pass) {
 bool attention_fits(const rat3d_attention_desc& d) {
     const AttnPlan p = attn_plan(d, true);
     const int64_t nq = (int64_t)d.n * d.heads;
-    // workgroups of the largest launches (each of 256 threads, 2^32 threads a launch)
+    // workgroups of the largest launches (each of 256 threads, 2^32 threads a launch);
+    // joins and sums follow splits alone, which few workgroups get
     return 2 * nq * ceil_div(d.tq, 64) + 2 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
                (1 << 24) &&
            nq * ceil_div(d.tq, 128) * p.fs < (1 << 24) &&
            nq * ceil_div(d.tq, 128) * p.qs + (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 128) * p.ks <
                (1 << 24) &&
-           nq * ceil_div(d.tq, 64) * 16 + 32 * (int64_t)d.n * d.kv_heads * ceil_div(d.tk, 64) <
-               (1ll << 31) &&
-           (!few_rows(d) || (int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) * 4 < (1 << 24)) &&
+           (!few_rows(d) || ((int64_t)d.n * d.kv_heads * ceil_div(d.tk, few_keys(d)) * 4 < (1 << 24) &&
+                             nq * d.tq < (1 << 24))) &&
            p.tqp / 32 * (d.heads / d.kv_heads) < (1 << 30);
 }
 

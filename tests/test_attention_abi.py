@@ -28,11 +28,11 @@ def _att(**kw):
     (dict(heads=3), R.EINVAL), (dict(head_dim=0), R.EINVAL), (dict(tq=0), R.EINVAL),
     (dict(tk=0), R.EINVAL), (dict(tk=-5), R.EINVAL), (dict(head_dim=129), R.EUNSUPPORTED),
     (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(scale=-1.0), R.EINVAL),
-    (dict(scale=float("nan")), R.EINVAL), (dict(scale=float("inf")), R.EINVAL),
+    (dict(scale=1e-30), R.EINVAL), (dict(scale=1e30), R.EINVAL), (dict(scale=float("nan")), R.EINVAL), (dict(scale=float("inf")), R.EINVAL),
     (dict(q_stride=4 * 32 * 50 - 1), R.EINVAL), (dict(k_stride=1), R.EINVAL),
     (dict(v_stride=-1), R.EINVAL), (dict(o_stride=5), R.EINVAL),
     (dict(tk=(1 << 28) + 1), R.EUNSUPPORTED), (dict(n=1 << 30), R.EUNSUPPORTED),
-    (dict(n=4096, tq=1 << 20), R.EUNSUPPORTED), (dict(heads=1 << 30), R.EUNSUPPORTED),
+    (dict(n=4096, tq=1 << 20), R.EUNSUPPORTED), (dict(n=1 << 21, tq=2, tk=1), R.EUNSUPPORTED), (dict(heads=1 << 30), R.EUNSUPPORTED),
 ])
 def test_attention_descriptor(kw, status):
     d = _att(**kw)
@@ -77,6 +77,7 @@ def _qk(**kw):
     (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(q_stride=1), R.EINVAL),
     (dict(ok_stride=2 * 32 * 60 - 1), R.EINVAL), (dict(d=1 << 20, h=1 << 20), R.EUNSUPPORTED),
     (dict(n=1 << 30), R.EUNSUPPORTED), (dict(d=1 << 30), R.EUNSUPPORTED),
+    (dict(n=1 << 21), R.EUNSUPPORTED),
 ])
 def test_qk_descriptor(kw, status):
     d = _qk(**kw)

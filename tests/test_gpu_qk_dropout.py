@@ -170,6 +170,30 @@ def test_qk_ranges_in_place(dt):
     del torch
 
 
+def test_qk_offsets_beyond_32_bits():
+    """Volumes more than 2^31 elements apart."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, heads, kv, hd, grid, v, wide = 2, 2, 1, 16, (3, 5, 9), 135, (1 << 31) + 4097
+    rng = _rng("far")
+    x, xr = U.dev_input(rng.standard_normal((n, (heads + kv) * hd, v)), "bf16")
+    g, gr = U.dev_input(1 + 0.3 * rng.standard_normal(hd), "f32")
+    big = torch.empty(wide + x[0].numel() + 64, dtype=torch.bfloat16, device="cuda:0")
+    rows = [big[i * wide + 5:i * wide + 5 + x[0].numel()].view(-1, v) for i in range(n)]
+    for i in range(n):
+        rows[i].copy_(x[i])
+    desc = R.qk_desc(n, heads, kv, hd, *grid, R.BF16, rot=(4, 4, 4), q_stride=wide, k_stride=wide)
+    table = _ws(R.rat3d_rope_table_size(desc))
+    R.rat3d_rope_table(desc, table)
+    y, z = U.empty((n, heads * hd, v), "bf16"), U.empty((n, kv * hd, v), "bf16")
+    p = big.data_ptr() + 10
+    R.rat3d_qk_norm_rope_fwd(desc, p, p + 2 * heads * hd * v, g, g, table, y, z)
+    U.sync()
+    turn = A.rotation(hd, grid, (4, 4, 4), (0, 0, 0), 100.0)
+    AU.within(U.f64(y), _qk_bounds("bf16", xr[:, :heads * hd], heads, gr, turn, 1e-6), "q")
+    AU.within(U.f64(z), _qk_bounds("bf16", xr[:, heads * hd:], kv, gr, turn, 1e-6), "k")
+
+
 # ------------------------------------------------------------------ dropout
 DROP = [(1, 1, 0.5), (7, 1, 0.3), (8, 1, 0.1), (9, 1, 0.9), (4099, 1, 0.25), (4100, 3, 0.5),
         (4100, 7, 0.5), (4103, 8, 0.5), (6000, 75, 0.4), (6001, 75, 0.4), (9000, 3000, 0.5),

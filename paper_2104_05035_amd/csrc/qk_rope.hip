@@ -54,12 +54,15 @@ struct QkArgs {
     int tiles;
 };
 
-// TOK tokens of one channel, in words: a row may begin at any element.
+// TOK tokens of one channel, in words: a row may begin at any element.  Without ALL only
+// `left` of them are in the row, whose last token lies at p[end] (end may be negative):
+// it is read in the others' place, without a branch, and they count as 0.  (The
+// backward branches instead: its registers are full.)
 template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Toks {
     uint32_t w[TOK * sizeof(T) / 4];
 };
-template <typename T, int TOK, bool ALL>
-__device__ __forceinline__ void ld_tok(const T* p, int left, float (&o)[TOK]) {
+template <typename T, int TOK, bool ALL, bool BRANCH>
+__device__ __forceinline__ void ld_tok(const T* p, int left, int end, float (&o)[TOK]) {
     if (ALL) {
         const Toks<T, TOK> u = *reinterpret_cast<const Toks<T, TOK>*>(p);
 #pragma unroll
@@ -67,14 +70,20 @@ __device__ __forceinline__ void ld_tok(const T* p, int left, float (&o)[TOK]) {
             if (sizeof(T) == 4) o[j] = __uint_as_float(u.w[j]);
             else o[j] = __uint_as_float(j & 1 ? u.w[j / 2] & 0xffff0000u : u.w[j / 2] << 16);
         }
-    } else {
+    } else if (BRANCH) {
 #pragma unroll
         for (int j = 0; j < TOK; ++j) o[j] = j < left ? Elt<T>::ld(p + j) : 0.f;
+    } else {
+        T u[TOK];
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) u[j] = p[j < end ? j : end];
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) o[j] = j < left ? Elt<T>::from_bits(u[j]) : 0.f;
     }
 }
 template <typename T, int TOK, bool ALL>
 __device__ __forceinline__ void st_tok(T* p, int left, const float (&o)[TOK]) {
-    if (ALL) {
+    if (ALL || left == TOK) {
         Toks<T, TOK> u;
 #pragma unroll
         for (int j = 0; j < TOK; j += sizeof(T) == 4 ? 1 : 2) {
@@ -97,8 +106,13 @@ __device__ __forceinline__ float join_groups(float x, float y) {
 }
 
 // G: thread groups along the channel pairs, PP: pairs per thread, TOK: tokens per thread.
+// The backward's waves a SIMD are held to what measured best at 8 x (4 + 2) heads over
+// 24x28x24 voxels: head_dim 64 (16 groups of 2 pairs) 93 -> 73 us in bfloat16 at four;
+// 40 (8 of 3) 50 -> 46 at three, but 81 -> 85 in float32, which is left alone.
 template <typename T, int G, int PP, int TOK, bool NORM, bool BWD>
-__global__ __launch_bounds__(32 * G, (BWD && PP * TOK == 8 ? 4 : BWD && PP == 3 && sizeof(T) == 2 ? 3 : 2))
+__global__ __launch_bounds__(32 * G, (BWD && PP * TOK == 8                        ? 4
+                                      : BWD && G == 8 && PP == 3 && sizeof(T) == 2 ? 3
+                                                                                   : 2))
 void qk_rope_k(QkArgs a) {
     constexpr int TILE = 32 * TOK;
     // sums over a wave's channels: [parity][sum][wave][token of the lane][lane]
@@ -112,6 +126,7 @@ void qk_rope_k(QkArgs a) {
     const int vol = bid / a.chunks;
     const int64_t t0 = (int64_t)tile * TILE + lane * TOK;
     const int left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
+    const int end = (int)(a.V - 1 - t0 < TOK ? a.V - 1 - t0 : TOK);
     const int D = a.pr.head_dim;
 
     // this thread's channels and their cosines and sines, the same for every head
@@ -167,7 +182,22 @@ void qk_rope_k(QkArgs a) {
                 cs[p][j] = 1.f;
                 sn[p][j] = 0.f;
             }
-            if (tab && row) {
+            if (TOK == 4) {
+                // without a branch, so that every load is in flight at once: small maps
+                // wait for little else
+                if (a.table) {
+                    const float2* t = tab ? tab : a.table;
+                    float2 v[TOK];
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j)
+                        v[j] = t[!tab ? 0 : axis == 0 ? at[j][0] : axis == 1 ? at[j][1] : at[j][2]];
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) {
+                        cs[p][j] = tab ? v[j].x : 1.f;
+                        sn[p][j] = tab ? v[j].y : 0.f;
+                    }
+                }
+            } else if (tab && row) {
                 // one row: one place on the first two axes, neighbours on the third
                 if (axis < 2) {
                     const float2 v = tab[axis == 0 ? at[0][0] : at[0][1]];
@@ -180,8 +210,8 @@ void qk_rope_k(QkArgs a) {
 #pragma unroll
                     for (int j = 0; j < TOK; j += 2) {
                         float v[4];
-                        ld_tok<float, 4, true>(
-                            reinterpret_cast<const float*>(tab + at[0][2] + j), 4, v);
+                        ld_tok<float, 4, true, false>(
+                            reinterpret_cast<const float*>(tab + at[0][2] + j), 4, 3, v);
                         cs[p][j] = v[0];
                         sn[p][j] = v[1];
                         cs[p][j + 1] = v[2];
@@ -253,12 +283,12 @@ void qk_rope_k(QkArgs a) {
         for (int p = 0; p < PP; ++p) {
             const int64_t fa = (ca[p] >= 0 ? ca[p] : 0) * a.V, fb = (cb[p] >= 0 ? cb[p] : 0) * a.V;
             if (reads) {
-                ld_tok<T, TOK, kAll>(x + fa, left, xa[p]);
-                ld_tok<T, TOK, kAll>(x + fb, left, xb[p]);
+                ld_tok<T, TOK, kAll, BWD>(x + fa, left, end, xa[p]);
+                ld_tok<T, TOK, kAll, BWD>(x + fb, left, end, xb[p]);
             }
             if (BWD) {
-                ld_tok<T, TOK, kAll>(dy + fa, left, da[p]);
-                ld_tok<T, TOK, kAll>(dy + fb, left, db[p]);
+                ld_tok<T, TOK, kAll, BWD>(dy + fa, left, end, da[p]);
+                ld_tok<T, TOK, kAll, BWD>(dy + fb, left, end, db[p]);
             }
         }
 #pragma unroll

@@ -5,8 +5,8 @@
 // logarithm of the sum (lse) and D_i = do_i . o_i:
 //   P = exp(S - lse), dV = P^T dO, dS = P (dO V^T - D), dQ = scale dS K,
 //   dK = scale dS^T Q,
-// in two kernels, one that keeps keys and walks the queries (dK, dV), one that
-// keeps queries and walks the keys (dQ): S is formed three times in a training
+// in two walks, one that keeps keys and goes over the queries (dK, dV), one that
+// keeps queries and goes over the keys (dQ): S is formed three times in a training
 // step, and no sum is shared between workgroups, so nothing is atomic and every
 // result has the same bits each time.
 //
@@ -991,7 +991,7 @@ __device__ __forceinline__ void dkv_block(const AttnArgs& a, int bid, u32x4* roo
 //   X: dV, dK of B for turn i - 1, scores of B for turn i   beside   exp of A, turn i
 //   Y: dV, dK of A for turn i, scores of A for turn i + 1   beside   exp of B, turn i
 // A fragment read from LDS feeds both blocks (it stays in registers from Y to X, or
-// from X to Y): 8 (D <= 64: 17) reads for 20 (36) products of 32 cycles, where one
+// from X to Y): 9 (D <= 64: 17) reads for 20 (36) products of 32 cycles, where one
 // block a wave would ask LDS for as many cycles as the products take.  One wave a SIMD
 // holds all this (two at D <= 32); the order of instructions is pinned step by step.
 // Three LDS buffers: turn i reads T of record i and R of i + 1 and writes record i + 2.

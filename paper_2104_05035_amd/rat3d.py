@@ -211,11 +211,29 @@ def _p(t):
     return t.data_ptr()
 
 
+def _find_current_stream():
+    """A function that returns the handle of the current device's current stream.
+    torch.cuda.current_stream() builds an object for it, 2.8 us a call; the handle
+    alone takes 0.1 us (a whole call without a stream argument: 6.8 -> 4.5 us)."""
+    import torch
+    try:
+        raw, device = torch._C._cuda_getCurrentRawStream, torch.cuda.current_device
+        device()  # initialises the runtime, as current_stream() would
+        return lambda: raw(device())
+    except AttributeError:
+        return lambda: torch.cuda.current_stream().cuda_stream
+
+
+_current_stream = None
+
+
 def _stream(stream):
+    global _current_stream
     if stream is not None:
         return stream
-    import torch
-    return torch.cuda.current_stream().cuda_stream
+    if _current_stream is None:
+        _current_stream = _find_current_stream()
+    return _current_stream()
 
 
 def dtype_code(torch_dtype):

@@ -402,3 +402,23 @@ def test_read_out_of_a_very_long_row():
     off = float((o[0, :, 0].double() - want).norm() / want.norm())
     assert off <= 2.0 ** -8 + 1e-4, off
     assert abs(float(lse) - float(torch.logsumexp(s, 0))) <= 1e-4
+
+
+def test_calls_follow_the_current_stream():
+    """Without a stream argument a call goes to the stream that is current then."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    other = torch.cuda.Stream()
+    assert R._stream(None) == torch.cuda.current_stream().cuda_stream
+    with torch.cuda.stream(other):
+        assert R._stream(None) == other.cuda_stream
+        # a call that waits for work of that stream only if it is enqueued there
+        x = torch.ones(1 << 24, device="cuda:0")
+        for _ in range(20):
+            x.mul_(1.5).div_(1.5)
+        y = torch.empty_like(x)
+        R.rat3d_dropout_fwd(R.dropout_desc(x.numel(), 0.0, R.F32), 0, None, x, None, y)
+    other.synchronize()
+    assert torch.equal(x, y)
+    assert R._stream(None) == torch.cuda.current_stream().cuda_stream != other.cuda_stream
+    assert R._stream(123) == 123

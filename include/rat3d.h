@@ -230,7 +230,7 @@ rat3d_status rat3d_softmask_bwd(int64_t count, rat3d_dtype dtype, const void* do
 
 /* Norm of each head's query and key vector and rotation by the voxel's place, in
  * one pass:
- *   z = x * gamma / sqrt(mean(x^2) + eps)        (norm != 0; else z = x)
+ *   z = x * gamma / sqrt(mean(x^2) + eps)        (norm != 0; else z = x; eps >= 2^-126)
  * over the head_dim channels of one head and token, and then, for each axis a of
  * d, h, w in that order, the next rot_a channels of the head are turned in pairs
  * (i, i + rot_a/2), i < rot_a/2, by the angle
@@ -254,7 +254,7 @@ typedef struct {
 
 /* The cosines and sines of a descriptor's grid (angles are formed in float64):
  * bytes, and the call that fills them.  They depend on d, h, w, rot, origin and
- * base only and are made once; 0 bytes without rotation (table may then be NULL).
+ * base only and are made once; 0 bytes without rotation (table is then not read).
  * (size_t)-1 if the descriptor is invalid. */
 size_t rat3d_rope_table_size(const rat3d_qk_desc* desc);
 rat3d_status rat3d_rope_table(const rat3d_qk_desc* desc, void* table, void* stream);

@@ -358,8 +358,9 @@ static rat3d_status check_qk(const rat3d_qk_desc* d) {
     RAT3D_REQUIRE(all <= d->head_dim, RAT3D_EINVAL, "more rotated channels than head_dim");
     RAT3D_REQUIRE(all == 0 || (d->base > 0.f && d->base < 1e30f), RAT3D_EINVAL,
                   "rotation needs a positive, finite base");
-    RAT3D_REQUIRE(!d->norm || (d->eps > 0.f && d->eps < 1e30f), RAT3D_EINVAL,
-                  "the norm needs a positive, finite eps");
+    // the root of a smaller one is infinite on the device, and a token of zeros then NaN
+    RAT3D_REQUIRE(!d->norm || (d->eps >= 0x1p-126f && d->eps < 1e30f), RAT3D_EINVAL,
+                  "the norm needs a finite eps of at least 2^-126");
     RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
                   (int)d->dtype);
     const double v = (double)d->d * d->h * d->w;

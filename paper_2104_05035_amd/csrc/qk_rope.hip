@@ -520,7 +520,7 @@ rat3d_status qk_rope_fwd(const rat3d_qk_desc& d, const void* q, const void* k, c
     int64_t total;
     a.pr = make_pairs(d, &total);
     qk_plan(d, false, &a);
-    a.table = (const float2*)table;
+    a.table = total ? (const float2*)table : nullptr;
     a.side[0].x = q;
     a.side[0].out = oq;
     a.side[0].gamma = gq;
@@ -546,7 +546,7 @@ rat3d_status qk_rope_bwd(const rat3d_qk_desc& d, const void* doq, const void* do
     int64_t total;
     a.pr = make_pairs(d, &total);
     qk_plan(d, true, &a);
-    a.table = (const float2*)table;
+    a.table = total ? (const float2*)table : nullptr;
     a.part = (float*)ws;
     a.side[0].x = q;
     a.side[0].dy = doq;

@@ -72,7 +72,7 @@ def _qk(**kw):
     (dict(rot=(3, 2, 2)), R.EINVAL), (dict(rot=(-2, 2, 2)), R.EINVAL),
     (dict(rot=(16, 16, 2)), R.EINVAL), (dict(rot=(2 ** 30, 2 ** 30, 2 ** 30)), R.EINVAL),
     (dict(origin=(1 << 25, 0, 0)), R.EINVAL), (dict(base=0.0), R.EINVAL),
-    (dict(base=float("nan")), R.EINVAL), (dict(eps=0.0), R.EINVAL),
+    (dict(base=float("nan")), R.EINVAL), (dict(eps=0.0), R.EINVAL), (dict(eps=1e-40), R.EINVAL),
     (dict(eps=float("inf")), R.EINVAL), (dict(head_dim=130), R.EUNSUPPORTED),
     (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(q_stride=1), R.EINVAL),
     (dict(ok_stride=2 * 32 * 60 - 1), R.EINVAL), (dict(d=1 << 20, h=1 << 20), R.EUNSUPPORTED),

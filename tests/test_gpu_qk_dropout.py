@@ -359,3 +359,33 @@ def test_self_attention_block(dt):
             s[i][e] -= 2 * h
             diff = (up - f(*s)) / (2 * h)
             assert float(U.f64(got[name])[e]) == pytest.approx(diff, rel=1e-3), name
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_qk_smallest_eps_and_no_rotation(dt):
+    """At the smallest eps a token of zeros stays zero and its gradient finite; without
+    rotation a table that is given all the same changes nothing."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    hd, v = 24, 10
+    desc = R.qk_desc(1, 1, 0, hd, 1, 2, 5, U.code(dt), rot=(0, 0, 0), eps=2.0 ** -126, norm=True)
+    x, xr = U.dev_input(_rng(("eps", dt)).standard_normal((1, hd, v)), dt)
+    x[0, :, 3] = 0
+    xr[0, :, 3] = 0
+    dy, _ = U.dev_input(np.ones((1, hd, v)), dt)
+    g, gr = U.dev_input(np.ones(hd), "f32")
+    table = torch.full((2,), float("nan"), device="cuda:0")
+    y, dx = torch.empty_like(x), torch.empty_like(x)
+    dg = torch.empty(hd, device="cuda:0")
+    need = R.rat3d_qk_norm_rope_workspace_size(desc)
+    R.rat3d_qk_norm_rope_fwd(desc, x, None, g, None, table, y, None)
+    R.rat3d_qk_norm_rope_bwd(desc, dy, None, x, None, g, None, table, dx, None, dg, None, 0,
+                             _ws(need), need)
+    U.sync()
+    want = _qk_bounds(dt, xr, 1, gr, A.rotation(hd, (1, 2, 5), (0, 0, 0), (0, 0, 0), 100.0),
+                      2.0 ** -126)
+    AU.within(U.f64(y), want, "y")
+    assert bool((y[0, :, 3] == 0).all())
+    # r = 2^63 there: dx = dy r, a power of two
+    assert bool((dx[0, :, 3].float() == 2.0 ** 63).all())
+    assert bool(torch.isfinite(dg).all())

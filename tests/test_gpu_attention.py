@@ -126,7 +126,10 @@ FEW = [(1, 1, 1, 1, 1, 1, None), (2, 2, 1, 33, 1, 513, "half"), (1, 4, 1, 40, 1,
        (40, 4, 2, 8, 1, 16400, "half"), (40, 2, 2, 9, 4, 13313, None), (60, 3, 3, 5, 3, 6145, "run"),
        (1, 1, 1, 17, 5, 600, None), (2, 6, 2, 32, 4, 1030, "half"), (1, 8, 1, 64, 2, 900, "first65"),
        (2, 4, 2, 40, 7, 520, "first_none"), (40, 2, 2, 6, 13, 13000, "half"), (1, 1, 1, 16, 17, 300, None)]
-ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE + FEW for dt in ("bf16", "f32")]
+# around the length up to which the packing itself finds the live keys
+LISTS = [(2, 2, 2, 16, 40, tk, mk) for tk, mk in (
+    (2047, "half"), (2048, "run"), (2049, "half"), (1001, "first65"), (9, "half"), (7, "half"))]
+ALL = [c + (dt,) for c in HEAD_DIMS + TOKENS + HEADS + MASKS + WIDE + FEW + LISTS for dt in ("bf16", "f32")]
 
 
 @pytest.mark.parametrize("case", ALL, ids=lambda c: "n%d_h%d_%d_d%d_q%d_k%d_%s_%s" % c)

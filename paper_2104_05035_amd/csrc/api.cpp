@@ -366,8 +366,8 @@ static rat3d_status check_qk(const rat3d_qk_desc* d) {
     const double v = (double)d->d * d->h * d->w;
     RAT3D_REQUIRE((double)d->d + d->h + d->w < 1.6e7, RAT3D_EUNSUPPORTED,
                   "qk map too large for one launch");
-    // workgroups of up to 512 threads, 2^32 threads a launch
-    RAT3D_REQUIRE((v / 128.0 + 1) * d->n * ((double)d->heads + d->kv_heads) < 8.0e6,
+    // workgroups of up to 768 threads, 2^32 threads a launch
+    RAT3D_REQUIRE((v / 128.0 + 1) * d->n * ((double)d->heads + d->kv_heads) < 5.5e6,
                   RAT3D_EUNSUPPORTED, "qk map too large for one launch");
     const double hv = (double)d->head_dim * v;
     RAT3D_STRIDE(d->q_stride, hv * d->heads);

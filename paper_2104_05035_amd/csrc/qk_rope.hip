@@ -12,7 +12,7 @@
 //
 // Layout: a workgroup takes 128 or 256 neighbouring tokens of one head after another,
 // queries' heads and then keys': 32 lanes along the tokens, four or eight tokens each
-// (one 8- or 16-byte access a channel), by eight groups of threads along the head's
+// (one 8- or 16-byte access a channel), by 8 to 24 groups of threads along the head's
 // channel pairs, so that both halves of a pair are in one thread and a channel's row
 // is read in whole cache lines.  The cosines and sines are loaded once for all heads.  The sum
 // over the head's channels goes through LDS.  Rows need no alignment.
@@ -449,10 +449,12 @@ rat3d_status rope_table(const rat3d_qk_desc& d, void* table, hipStream_t st) {
 
 // Tokens per thread: eight of bfloat16 (one 16-byte access a channel) where their
 // values and angles fit the registers of two waves a SIMD and there are tiles enough
-// to fill the GPU, else four.
+// to fill the GPU, else four.  24 x (4 + 2) heads over 24x28x24 voxels, four and eight
+// tokens: forward at head_dim 96 349 and 183 us, backward at 48 218 and 193, at 64 216
+// and 207; where they do not fit, forward at 128 260 and 428, backward at 96 325 and 429.
 static int qk_tokens(const rat3d_qk_desc& d, bool bwd) {
     const int64_t V = (int64_t)d.d * d.h * d.w;
-    const bool fits = d.dtype == RAT3D_BF16 && d.head_dim <= (bwd ? 32 : 64);
+    const bool fits = d.dtype == RAT3D_BF16 && d.head_dim <= (bwd ? 64 : 96);
     return fits && ceil_div(V, 256) * d.n >= 4 * (int64_t)device_cus() ? 8 : 4;
 }
 
@@ -488,15 +490,18 @@ static void qk_launch(const rat3d_qk_desc& d, const QkArgs& a, hipStream_t st) {
     const bool wide = sizeof(T) == 2 && qk_tokens(d, BWD) == 8;
 #define RAT3D_QK(G, PP, TOK)                                                          \
     do {                                                                              \
-        if (d.norm) qk_rope_k<T, G, PP, TOK, true, BWD><<<grid, 32 * G, 0, st>>>(a);  \
-        else qk_rope_k<T, G, PP, TOK, false, BWD><<<grid, 32 * G, 0, st>>>(a);        \
+        if (d.norm) qk_rope_k<T, G, PP, TOK, true, BWD><<<grid, 32 * (G), 0, st>>>(a);  \
+        else qk_rope_k<T, G, PP, TOK, false, BWD><<<grid, 32 * (G), 0, st>>>(a);        \
     } while (0)
     // groups and pairs so that few slots stay empty and four waves a SIMD find registers
+    // (forward at head_dim 96, 8 x 6 heads over 24x28x24 voxels in bfloat16: 16 groups of
+    // 3 pairs 124 us, 24 of 2 85; backward 128 and 129)
     if constexpr (sizeof(T) == 2) {
         if (wide) {
             if (d.head_dim <= 16) RAT3D_QK(8, 1, 8);
             else if (d.head_dim <= 32) RAT3D_QK(8, 2, 8);
-            else if constexpr (!BWD) RAT3D_QK(16, 2, 8);
+            else if (d.head_dim <= 64) RAT3D_QK(16, 2, 8);
+            else if constexpr (!BWD) RAT3D_QK(24, 2, 8);
             return;
         }
     }
@@ -504,7 +509,7 @@ static void qk_launch(const rat3d_qk_desc& d, const QkArgs& a, hipStream_t st) {
     else if (d.head_dim <= 32) RAT3D_QK(8, 2, 4);
     else if (d.head_dim <= 48) RAT3D_QK(8, 3, 4);
     else if (d.head_dim <= 64) RAT3D_QK(16, 2, 4);
-    else if (d.head_dim <= 96) RAT3D_QK(16, 3, 4);
+    else if (d.head_dim <= 96) RAT3D_QK(BWD ? 16 : 24, BWD ? 3 : 2, 4);
     else RAT3D_QK(16, 4, 4);
 #undef RAT3D_QK
 }

@@ -39,6 +39,12 @@ QK = [
     (2, 0, 2, 24, (4, 5, 13), (8, 8, 8), (0, 0, 0), False),
     (1, 70, 30, 8, (2, 2, 40), (2, 2, 2), (0, 0, 0), True),
     (40, 9, 3, 20, (5, 6, 7), (6, 6, 6), (0, 0, 0), True),
+    # tiles enough for eight tokens a thread in bfloat16
+    (1030, 1, 1, 16, (3, 5, 3), (4, 6, 4), (0, 0, 0), True),
+    (520, 1, 1, 40, (5, 6, 9), (12, 12, 12), (0, 0, 0), True),
+    (1030, 1, 0, 64, (2, 4, 5), (20, 20, 20), (3, 0, 0), True),
+    (520, 1, 1, 72, (1, 2, 130), (24, 24, 24), (0, 0, 0), True),
+    (1030, 1, 1, 96, (1, 3, 11), (32, 32, 32), (0, 0, 7), False),
 ]
 
 

@@ -447,14 +447,16 @@ rat3d_status rope_table(const rat3d_qk_desc& d, void* table, hipStream_t st) {
     return RAT3D_OK;
 }
 
-// Tokens per thread: eight of bfloat16 (one 16-byte access a channel) where their
-// values and angles fit the registers of two waves a SIMD and there are tiles enough
-// to fill the GPU, else four.  24 x (4 + 2) heads over 24x28x24 voxels, four and eight
-// tokens: forward at head_dim 96 349 and 183 us, backward at 48 218 and 193, at 64 216
-// and 207; where they do not fit, forward at 128 260 and 428, backward at 96 325 and 429.
+// Tokens per thread: eight of bfloat16 (one 16-byte access a channel) where that is
+// faster and there are tiles enough to fill the GPU, else four.  24 x (4 + 2) heads over
+// 24x28x24 voxels, four and eight tokens: forward at head_dim 96 222 and 181 us, at 80
+// 321 and 156, but at 48 89 and 101, at 64 119 and 127, at 128 260 and 428 (registers);
+// backward at 48 214 and 165, at 64 218 and 204, but at 96 325 and 429.
 static int qk_tokens(const rat3d_qk_desc& d, bool bwd) {
     const int64_t V = (int64_t)d.d * d.h * d.w;
-    const bool fits = d.dtype == RAT3D_BF16 && d.head_dim <= (bwd ? 64 : 96);
+    const bool fits = d.dtype == RAT3D_BF16 &&
+                      (d.head_dim <= 32 || (bwd ? d.head_dim <= 64
+                                                : d.head_dim > 64 && d.head_dim <= 96));
     return fits && ceil_div(V, 256) * d.n >= 4 * (int64_t)device_cus() ? 8 : 4;
 }
 
@@ -493,22 +495,25 @@ static void qk_launch(const rat3d_qk_desc& d, const QkArgs& a, hipStream_t st) {
         if (d.norm) qk_rope_k<T, G, PP, TOK, true, BWD><<<grid, 32 * (G), 0, st>>>(a);  \
         else qk_rope_k<T, G, PP, TOK, false, BWD><<<grid, 32 * (G), 0, st>>>(a);        \
     } while (0)
+    constexpr bool kFew = sizeof(T) == 2 && !BWD;
     // groups and pairs so that few slots stay empty and four waves a SIMD find registers
-    // (forward at head_dim 96, 8 x 6 heads over 24x28x24 voxels in bfloat16: 16 groups of
-    // 3 pairs 124 us, 24 of 2 85; backward 128 and 129)
+    // (8 x 6 heads over 24x28x24 voxels in bfloat16, forward: at head_dim 96 16 groups of
+    // 3 pairs 124 us, 24 of 2 85, backward 128 and 129; at 64 16 of 2 42, 8 of 4 36, in
+    // float32 76 and 78)
     if constexpr (sizeof(T) == 2) {
         if (wide) {
             if (d.head_dim <= 16) RAT3D_QK(8, 1, 8);
             else if (d.head_dim <= 32) RAT3D_QK(8, 2, 8);
-            else if (d.head_dim <= 64) RAT3D_QK(16, 2, 8);
             else if constexpr (!BWD) RAT3D_QK(24, 2, 8);
+            else if (d.head_dim <= 48) RAT3D_QK(12, 2, 8);
+            else RAT3D_QK(16, 2, 8);
             return;
         }
     }
     if (d.head_dim <= 16) RAT3D_QK(8, 1, 4);
     else if (d.head_dim <= 32) RAT3D_QK(8, 2, 4);
     else if (d.head_dim <= 48) RAT3D_QK(8, 3, 4);
-    else if (d.head_dim <= 64) RAT3D_QK(16, 2, 4);
+    else if (d.head_dim <= 64) RAT3D_QK(kFew ? 8 : 16, kFew ? 4 : 2, 4);
     else if (d.head_dim <= 96) RAT3D_QK(BWD ? 16 : 24, BWD ? 3 : 2, 4);
     else RAT3D_QK(16, 4, 4);
 #undef RAT3D_QK

@@ -404,12 +404,12 @@ rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, co
     if (desc->heads) {
         RAT3D_ELT(q, es, "q");
         RAT3D_ELT(oq, es, "oq");
-        RAT3D_REQUIRE(!desc->norm || gamma_q, RAT3D_EINVAL, "gamma_q must not be NULL");
+        if (desc->norm) RAT3D_ELT(gamma_q, sizeof(float), "gamma_q");
     }
     if (desc->kv_heads) {
         RAT3D_ELT(k, es, "k");
         RAT3D_ELT(ok, es, "ok");
-        RAT3D_REQUIRE(!desc->norm || gamma_k, RAT3D_EINVAL, "gamma_k must not be NULL");
+        if (desc->norm) RAT3D_ELT(gamma_k, sizeof(float), "gamma_k");
     }
     if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
     return qk_rope_fwd(*desc, q, k, gamma_q, gamma_k, table, oq, ok, (hipStream_t)stream);
@@ -428,8 +428,8 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
         RAT3D_ELT(dq, es, "dq");
         if (desc->norm) {
             RAT3D_ELT(q, es, "q");
-            RAT3D_REQUIRE(gamma_q && dgamma_q, RAT3D_EINVAL,
-                          "gamma_q and dgamma_q must not be NULL");
+            RAT3D_ELT(gamma_q, sizeof(float), "gamma_q");
+            RAT3D_ELT(dgamma_q, sizeof(float), "dgamma_q");
         }
     }
     if (desc->kv_heads) {
@@ -437,8 +437,8 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
         RAT3D_ELT(dk, es, "dk");
         if (desc->norm) {
             RAT3D_ELT(k, es, "k");
-            RAT3D_REQUIRE(gamma_k && dgamma_k, RAT3D_EINVAL,
-                          "gamma_k and dgamma_k must not be NULL");
+            RAT3D_ELT(gamma_k, sizeof(float), "gamma_k");
+            RAT3D_ELT(dgamma_k, sizeof(float), "dgamma_k");
         }
     }
     if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
@@ -488,6 +488,7 @@ rat3d_status rat3d_attention_fwd(const rat3d_attention_desc* desc, const void* q
     RAT3D_ELT(k, es, "k");
     RAT3D_ELT(v, es, "v");
     RAT3D_ELT(o, es, "o");
+    if (lse) RAT3D_ELT(lse, sizeof(float), "lse");
     s = check_ws(ws, ws_bytes, attention_ws_bytes(*desc, 0));
     if (s != RAT3D_OK) return s;
     return attention_fwd(*desc, q, k, v, mask, o, lse, ws, (hipStream_t)stream);
@@ -508,7 +509,7 @@ rat3d_status rat3d_attention_bwd(const rat3d_attention_desc* desc, const void* d
     RAT3D_ELT(dq, es, "dq");
     RAT3D_ELT(dk, es, "dk");
     RAT3D_ELT(dv, es, "dv");
-    RAT3D_REQUIRE(lse != nullptr, RAT3D_EINVAL, "lse must not be NULL");
+    RAT3D_ELT(lse, sizeof(float), "lse");
     s = check_ws(ws, ws_bytes, attention_ws_bytes(*desc, 1));
     if (s != RAT3D_OK) return s;
     return attention_bwd(*desc, dout, q, k, v, mask, o, lse, dq, dk, dv, ws,

@@ -1,0 +1,42 @@
+"""Calls of the voxel self-attention that the library refuses on the host because
+their result would be wrong: float32 operands between two elements."""
+import pytest
+
+from paper_2104_05035_amd import rat3d as R
+
+FAKE = 0x10000  # aligned, never read: every call here is refused first
+
+
+def _refused(status, f, *a):
+    with pytest.raises(R.Rat3dError) as e:
+        f(*a, stream=0)
+    assert e.value.status == status
+    assert str(e.value).split(": ", 1)[1]
+
+
+def _with(args, at, value):
+    return args[:at] + [value] + args[at + 1:]
+
+
+def _qk(**kw):
+    d = dict(n=2, heads=4, kv_heads=2, head_dim=32, d=3, h=4, w=5, dtype=R.BF16, rot=(8, 8, 8))
+    d.update(kw)
+    return R.qk_desc(**d)
+
+
+@pytest.mark.parametrize("off", [1, 2, 3])
+def test_float32_operands_are_aligned(off):
+    # gains: operands 2 and 3 of the forward, 4, 5 and (gradients) 9, 10 of the backward
+    d = _qk()
+    need = R.rat3d_qk_norm_rope_workspace_size(d)
+    for i in (2, 3):
+        _refused(R.EALIGN, R.rat3d_qk_norm_rope_fwd, d, *_with([FAKE] * 7, i, FAKE + off))
+    for i in (4, 5, 9, 10):
+        _refused(R.EALIGN, R.rat3d_qk_norm_rope_bwd, d, *_with([FAKE] * 11, i, FAKE + off), 0,
+                 FAKE, need)
+    a = R.attention_desc(2, 4, 2, 32, 50, 60, R.BF16)
+    need = [R.rat3d_attention_workspace_size(a, i) for i in (0, 1)]
+    _refused(R.EALIGN, R.rat3d_attention_fwd, a, FAKE, FAKE, FAKE, None, FAKE, FAKE + off, FAKE,
+             need[0])
+    _refused(R.EALIGN, R.rat3d_attention_bwd, a, FAKE, FAKE, FAKE, FAKE, None, FAKE, FAKE + off,
+             FAKE, FAKE, FAKE, FAKE, need[1])

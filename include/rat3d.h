@@ -269,7 +269,8 @@ rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, co
 /* Backward: from doq, dok and the forward's inputs q, k the gradients dq, dk
  * (which may be doq, dok if their strides agree) and dgamma_q, dgamma_k float32
  * [head_dim], summed over volumes, heads and voxels (written, or added to when
- * accumulate != 0; ignored without norm). */
+ * accumulate != 0; ignored without norm).  They must not overlap, also where
+ * gamma_q and gamma_k are one gain. */
 size_t rat3d_qk_norm_rope_workspace_size(const rat3d_qk_desc* desc);
 rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, const void* dok,
                                     const void* q, const void* k, const float* gamma_q,

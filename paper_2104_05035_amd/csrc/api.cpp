@@ -444,6 +444,12 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
     if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
     s = check_ws(ws, ws_bytes, qk_ws_bytes(*desc));
     if (s != RAT3D_OK) return s;
+    if (desc->norm && desc->heads && desc->kv_heads) {
+        // each side writes, or adds to, its own
+        const uintptr_t a = (uintptr_t)dgamma_q, b = (uintptr_t)dgamma_k;
+        RAT3D_REQUIRE((a < b ? b - a : a - b) >= desc->head_dim * sizeof(float), RAT3D_EINVAL,
+                      "dgamma_q and dgamma_k must not overlap");
+    }
     return qk_rope_bwd(*desc, doq, dok, q, k, gamma_q, gamma_k, table, dq, dk, dgamma_q, dgamma_k,
                        accumulate ? 1 : 0, ws, (hipStream_t)stream);
 }

@@ -40,3 +40,15 @@ def test_float32_operands_are_aligned(off):
              need[0])
     _refused(R.EALIGN, R.rat3d_attention_bwd, a, FAKE, FAKE, FAKE, FAKE, None, FAKE, FAKE + off,
              FAKE, FAKE, FAKE, FAKE, need[1])
+
+
+@pytest.mark.parametrize("apart", [0, 1, 31, -31])
+def test_gain_gradients_have_a_place_each(apart):
+    """One gain for queries and keys is fine, one gradient for both is not: each side
+    writes its own (or adds to it), and the sum would be lost."""
+    d = _qk()
+    need = R.rat3d_qk_norm_rope_workspace_size(d)
+    _refused(R.EINVAL, R.rat3d_qk_norm_rope_bwd, d, *[FAKE] * 9, FAKE, FAKE + 4 * apart, 0, FAKE,
+             need)
+    _refused(R.EINVAL, R.rat3d_qk_norm_rope_bwd, d, *[FAKE] * 9, FAKE, FAKE + 4 * apart, 1, FAKE,
+             need)

@@ -377,6 +377,16 @@ static rat3d_status check_qk(const rat3d_qk_desc* d) {
     return RAT3D_OK;
 }
 
+// A result over its input: in every volume, or it would overwrite another's.
+static rat3d_status check_in_place(const rat3d_qk_desc* d, const void* x, const void* y, int heads,
+                                   int64_t x_stride, int64_t y_stride, const char* name) {
+    const int64_t packed = (int64_t)heads * d->head_dim * d->d * d->h * d->w;
+    RAT3D_REQUIRE(x != y || heads == 0 || d->n == 1 ||
+                      (x_stride ? x_stride : packed) == (y_stride ? y_stride : packed),
+                  RAT3D_EINVAL, "%s over its input needs the input's stride", name);
+    return RAT3D_OK;
+}
+
 size_t rat3d_rope_table_size(const rat3d_qk_desc* desc) {
     if (check_qk(desc) != RAT3D_OK) return (size_t)-1;
     return rope_table_bytes(*desc);
@@ -412,6 +422,10 @@ rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, co
         if (desc->norm) RAT3D_ELT(gamma_k, sizeof(float), "gamma_k");
     }
     if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
+    s = check_in_place(desc, q, oq, desc->heads, desc->q_stride, desc->oq_stride, "oq");
+    if (s != RAT3D_OK) return s;
+    s = check_in_place(desc, k, ok, desc->kv_heads, desc->k_stride, desc->ok_stride, "ok");
+    if (s != RAT3D_OK) return s;
     return qk_rope_fwd(*desc, q, k, gamma_q, gamma_k, table, oq, ok, (hipStream_t)stream);
 }
 
@@ -443,6 +457,10 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
     }
     if (rope_table_bytes(*desc)) RAT3D_ACT(table, "table");
     s = check_ws(ws, ws_bytes, qk_ws_bytes(*desc));
+    if (s != RAT3D_OK) return s;
+    s = check_in_place(desc, doq, dq, desc->heads, desc->oq_stride, desc->q_stride, "dq");
+    if (s != RAT3D_OK) return s;
+    s = check_in_place(desc, dok, dk, desc->kv_heads, desc->ok_stride, desc->k_stride, "dk");
     if (s != RAT3D_OK) return s;
     if (desc->norm && desc->heads && desc->kv_heads) {
         // each side writes, or adds to, its own

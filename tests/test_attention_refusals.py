@@ -52,3 +52,17 @@ def test_gain_gradients_have_a_place_each(apart):
              need)
     _refused(R.EINVAL, R.rat3d_qk_norm_rope_bwd, d, *[FAKE] * 9, FAKE, FAKE + 4 * apart, 1, FAKE,
              need)
+
+
+def test_in_place_needs_equal_strides():
+    """Over its input a result has to lie where the input lies, in every volume."""
+    packed = 4 * 32 * 60
+    for kw in (dict(q_stride=packed + 8), dict(oq_stride=packed + 8), dict(k_stride=packed),
+               dict(ok_stride=packed)):
+        d = _qk(**kw)
+        need = R.rat3d_qk_norm_rope_workspace_size(d)
+        q = kw.keys() & {"q_stride", "oq_stride"}
+        fwd = [FAKE, FAKE * 2, FAKE, FAKE, FAKE] + ([FAKE, FAKE * 3] if q else [FAKE * 3, FAKE * 2])
+        _refused(R.EINVAL, R.rat3d_qk_norm_rope_fwd, d, *fwd)
+        bwd = [FAKE, FAKE * 2] + [FAKE * 5] * 5 + fwd[5:] + [FAKE * 6, FAKE * 7]
+        _refused(R.EINVAL, R.rat3d_qk_norm_rope_bwd, d, *bwd, 0, FAKE, need)

@@ -216,6 +216,7 @@ struct PackJob {
     const float* lse;
     u32x4* rec;          // records of 32 tokens, `units` 16-byte units each:
     int units, r, t, x;  // where forms R and T and the row constants lie, or -1
+    int again;           // behind the last token stands: 0, zeros; 1, that token again
     float* lse2;         // lse in units of log 2; +infinity behind the last query and for
                          // a query without keys: its probabilities are then 0
     float* delta;        // D, padded with 0
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     }
     if (J.count && t0 >= live) return;  // never read: kernels stop at the live keys
     const bool in = t0 + col < live;
-    const int64_t tok = !in      ? 0
+    const int64_t tok = !in      ? (J.again ? J.tokens - 1 : 0)
                         : J.scan ? pick[col]
                         : J.idx  ? J.idx[vol * (int64_t)J.tiles * kPackTok + t0 + col]
                                  : t0 + col;
@@ -287,7 +288,7 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
     }
 #pragma unroll
     for (int i = 0; i < 8 * DB; ++i) {
-        const bool on = in && sub + 4 * i < a.D;
+        const bool on = (in || J.again) && sub + 4 * i < a.D;
         if (!on) v[i] = Elt<T>::to_bits(0.f);
         if (oth && on) d += Elt<T>::from_bits(v[i]) * Elt<T>::from_bits(o[i]);
         tile[(sub + 4 * i) * ROW + col] = v[i];
@@ -307,9 +308,12 @@ __global__ __launch_bounds__(256) void attn_pack_k(PackArgs a) {
         }
         // Row constants of the products with these rows: -lse in units of the scores,
         // and -D.  Behind the last query, and where a query has no key, a number so low
-        // that its probabilities are 0, finite because it is multiplied by 0 elsewhere.
+        // that its probabilities are 0 at any score, finite because it is multiplied by 0
+        // elsewhere.  What stands behind the last query is that query again (`again`):
+        // zeros would score 0 * infinity at a key that holds one, NaN, where every
+        // query has -infinity and so the probability 0.
         J.rec[(blk0 + (tk >> 5)) * J.units + J.x + half * 32 + (tk & 31)] =
-            M::rows(e == -INFINITY ? -1e30f : -e / a.scale, -d, half);
+            M::rows(e == -INFINITY ? -3e38f : -e / a.scale, -d, half);
     }
     // fragments: 2 blocks of 32 tokens x Dp, 16 bytes a lane
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1952,6 +1956,7 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
             pa.job[1].zero = dv;
         }
         pa.job[2] = pack_job(q, a.q_stride, d.tq, d.heads, a.q_rec, qu, 0, 2 * nf + 1, a, false);
+        pa.job[2].again = 1;
         pa.job[3] = pack_job(dout, a.o_stride, d.tq, d.heads, a.q_rec, qu, nf, 3 * nf + 1, a, false);
         pa.job[3].x = 2 * nf * 64;
         pa.job[3].other = o;

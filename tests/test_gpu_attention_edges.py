@@ -1,4 +1,5 @@
-"""Voxel self-attention on inputs at the edge of what it takes: infinite keys."""
+"""Voxel self-attention on inputs at the edge of what it takes: infinite keys, sums over
+very many voxels."""
 import zlib
 
 import numpy as np
@@ -76,3 +77,26 @@ def test_minus_infinity_in_a_key(case, dt):
     g = U.f64(dq)
     assert np.all(np.isnan(g[:, first]))
     AU.within(g[:, ~first], tuple(t[:, ~first] for t in want["dq"]), "dq")
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_gain_gradient_of_a_very_large_map(dt):
+    """2^27 voxels with equal terms: the parts' float32 sums would drift by 4e-5
+    (float32) and 4.7e-6 (bfloat16).  Terms: the norm and the product, head_dim + 16
+    roundings as in the other tests; a thread adds up to 8 tokens and joins 32 threads
+    in 5 steps; the parts are added in float64 and rounded once."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    hd, grid = 2, (512, 512, 512)
+    v = 512 ** 3
+    desc = R.qk_desc(1, 1, 0, hd, *grid, U.code(dt), eps=1e-5)
+    x = torch.ones((1, hd, v), dtype=U.tdtype(dt), device="cuda:0")
+    dy = torch.full_like(x, 0.55)
+    c = float(dy[0, 0, 0])
+    g, dg = torch.ones(hd, device="cuda:0"), torch.zeros(hd, device="cuda:0")
+    need = R.rat3d_qk_norm_rope_workspace_size(desc)
+    dx = torch.empty_like(x)
+    R.rat3d_qk_norm_rope_bwd(desc, dy, None, x, None, g, None, None, dx, None, dg, None, 0,
+                             _ws(need), need)
+    U.sync()
+    want = np.full(hd, c / np.sqrt(1 + np.float64(np.float32(1e-5))) * v)
+    AU.within(U.f64(dg), (want, (hd + 16 + 8 + 5 + 1) * AU.F * want), "dgamma")

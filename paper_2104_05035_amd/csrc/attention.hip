@@ -1344,18 +1344,17 @@ __global__ __launch_bounds__(256, (DB <= 2 || sizeof(T) == 2 ? 2 : 1)) void attn
 //   Y: dQ of A for turn i, scores of A for turn i + 1   beside   exp of B, turn i
 // -D is added to dO V^T by one more product: ones for every key times the query's
 // constant.  The last keys, where they fill no record, are taken behind the loop.
-template <int DB, bool SPLIT>
+// Never split: it is taken only where the queries alone fill the GPU.
+template <int DB>
 __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a) {
     typedef Mm<bf16> M;
     typedef bf16x8 frag;
     typedef Rec<bf16, DB> R;
     constexpr int NF = R::NF, U = R::kKeys;
     __shared__ u32x4 lds[3][U];
-    int bid = xcd_remap(blockIdx.x, gridDim.x);
+    const int bid = xcd_remap(blockIdx.x, gridDim.x);
     const int tile = bid % a.tiles;
-    bid /= a.tiles;
-    const int sp = SPLIT ? bid % a.splits : 0;
-    const int nh = SPLIT ? bid / a.splits : bid;
+    const int nh = bid / a.tiles;
     const int vol = nh / a.heads, h = nh - vol * a.heads;
     const int kvh = vol * a.kv + h / (a.heads / a.kv);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -1396,12 +1395,11 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a)
 #pragma unroll
     for (int f = 0; f < NF; ++f) kt[f] = frag{};
 
-    int b0, b1;
-    split_range(live, 32, SPLIT ? a.splits : 1, sp, b0, b1);
-    const int whole = (int)(live / 32);
-    const int i1 = b1 < whole ? b1 : whole;  // records that keys fill
-    const u32x4* rec = a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + b0) * U;
-    const u32x4* last = rec + (int64_t)(i1 - b0 - 1) * U;
+    const int whole = (int)(live / 32);  // records that keys fill
+    const int left = (int)(live - (int64_t)whole * 32);  // keys behind them
+    const u32x4* const first = a.kv_rec + (int64_t)kvh * (a.tkp / 32) * U;
+    const u32x4* rec = first;
+    const u32x4* last = rec + (int64_t)(whole - 1) * U;
     Stage<U> next;
 
     auto grad_step = [&](int c, int t) {  // one of the NF products of dQ of block c
@@ -1435,24 +1433,24 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a)
     };
     constexpr int N1 = NF, N2 = 2 * NF + 1, N = N1 + N2;  // products of X, as of Y
 
-    if (b0 < i1) {
+    if (whole > 0) {
         next.load(rec);
         next.store(lds[0]);
-        next.load(b0 + 1 < i1 ? rec + U : rec);
+        next.load(whole > 1 ? rec + U : rec);
         next.store(lds[1]);
     }
     __syncthreads();
-    if (b0 < i1) {
+    if (whole > 0) {
 #pragma unroll
         for (int f = 0; f < 2 * NF; ++f) read_r(lds[0], f);
 #pragma unroll
         for (int t = 0; t < N2; ++t) score_step(0, t);
     }
     int u0 = 0, u1 = 1, u2 = 2;  // buffers of records i, i + 1, i + 2
-    for (int i = b0; i < i1; ++i) {
+    for (int i = 0; i < whole; ++i) {
         // behind the last record it is taken again, so that no branch divides the turn:
         // what is formed from it is not used
-        next.load(i + 2 < i1 ? rec + 2 * U : last);
+        next.load(i + 2 < whole ? rec + 2 * U : last);
         // reads of LDS spread over the turn, as in attn_dkv2_k
         // X
 #pragma unroll
@@ -1487,11 +1485,10 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a)
     }
 #pragma unroll
     for (int t = 0; t < N1; ++t) grad_step(1, t);  // B of the last turn
-    if (i1 < b1) {  // keys that fill no record: what lies behind them is cleared
-        next.load(a.kv_rec + ((int64_t)kvh * (a.tkp / 32) + i1) * U);
+    if (left > 0) {  // keys that fill no record: what lies behind them is cleared
+        next.load(first + (int64_t)whole * U);
         next.store(lds[u2]);
         __syncthreads();
-        const int left = (int)(live - (int64_t)i1 * 32);
 #pragma unroll
         for (int f = 0; f < NF; ++f) {
             read_r(lds[u2], 2 * f);
@@ -1515,7 +1512,7 @@ __global__ __launch_bounds__(256, (DB == 1 ? 2 : 1)) void attn_dq2_k(AttnArgs a)
         }
     }
 #pragma unroll
-    for (int c = 0; c < 2; ++c) dq_store<bf16, DB, SPLIT>(a, nh, sp, qb + c, dq[c]);
+    for (int c = 0; c < 2; ++c) dq_store<bf16, DB, false>(a, nh, 0, qb + c, dq[c]);
 }
 
 // Sums of the splits of the backward passes, in a fixed order: [nh][split][rows][tp] ->
@@ -1640,7 +1637,8 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d, bool masked) {
     // a turn of float32 takes microseconds, one of bfloat16 a fraction
     const int least = d.dtype == RAT3D_BF16 ? 4 : 1;
     p.fs = splits_for(nq * ceil_div(d.tq, 128), p.tkp / 32, least);
-    p.qs = splits_for(nq * ceil_div(d.tq, 128 * p.qc), p.tkp / 32, least);
+    // two column blocks are taken from 1.5 workgroups a CU on, where there is nothing to split
+    p.qs = p.qc == 2 ? 1 : splits_for(nq * ceil_div(d.tq, 128), p.tkp / 32, least);
     p.ks = splits_for(nk * ceil_div(d.tk, 128 * p.kc), p.tqp / 32 * (d.heads / d.kv_heads), least,
                       masked ? 4 : 2);
     size_t at = 0;
@@ -1825,8 +1823,7 @@ static void bwd_launch(const BwdArgs& g, int kc, int qc, hipStream_t st) {
             one.kv_blocks = 0;
         }
         if (qc == 2) {
-            if (qs) attn_dq2_k<DB, true><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
-            else attn_dq2_k<DB, false><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
+            attn_dq2_k<DB><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
             one.q_blocks = 0;
         }
     }

@@ -1578,7 +1578,7 @@ struct AttnPlan {
     int DB, es;
     int kc, qc;      // blocks of 32 kept tokens a wave: dK/dV, dQ
     int fs, ks, qs;  // splits of the forward, of dK/dV, of dQ
-    size_t idx, count, kv_rec, q_rec, lse2, delta, part, qpart, fpart, stat, bytes[2];
+    size_t few, idx, count, kv_rec, q_rec, lse2, delta, part, qpart, fpart, stat, bytes[2];
 };
 
 // Ways to split a long walk: until there are about two workgroups for each CU, but
@@ -1649,23 +1649,24 @@ static AttnPlan attn_plan(const rat3d_attention_desc& d, bool masked) {
     };
     const size_t qb = (size_t)nq * p.tqp * p.DB * 32 * p.es;  // one form of the queries
     const size_t kb = (size_t)nk * p.tkp * p.DB * 32 * p.es;
+    if (few_rows(d)) {  // reads the mask itself: its sums alone
+        p.few = take((size_t)nk * ceil_div(d.tk, few_keys(d)) * few_stride(d) * (d.head_dim + 2) *
+                     sizeof(float));
+        p.bytes[0] = at;
+        at = 0;
+    }
     p.idx = take((size_t)d.n * p.tkp * sizeof(int));
     p.count = take((size_t)d.n * sizeof(int));
     const size_t both = at;
-    // forward
     p.kv_rec = at;
-    if (few_rows(d)) {
-        take((size_t)nk * ceil_div(d.tk, few_keys(d)) * few_stride(d) * (d.head_dim + 2) *
-             sizeof(float));
-        p.bytes[0] = at;
-    } else {
+    if (!few_rows(d)) {  // forward: records of two forms
         take(2 * kb);
+        if (p.fs > 1) {
+            p.stat = take((size_t)nq * p.fs * 2 * p.tqp * sizeof(float));
+            p.fpart = take((size_t)nq * p.fs * d.head_dim * p.tqp * sizeof(float));
+        }
+        p.bytes[0] = at;
     }
-    if (p.fs > 1 && !few_rows(d)) {
-        p.stat = take((size_t)nq * p.fs * 2 * p.tqp * sizeof(float));
-        p.fpart = take((size_t)nq * p.fs * d.head_dim * p.tqp * sizeof(float));
-    }
-    p.bytes[0] = at;
     // backward: records of three forms, and of four and the row constants
     at = both;
     take(3 * kb);
@@ -1861,7 +1862,7 @@ rat3d_status attention_fwd(const rat3d_attention_desc& d, const void* q, const v
         f.mask = mask;
         f.o = o;
         f.lse = lse;
-        f.part = (float*)(w + p.kv_rec);
+        f.part = (float*)(w + p.few);
         f.tq = d.tq;
         f.tk = d.tk;
         f.q_stride = a.q_stride;

@@ -17,3 +17,15 @@ def test_no_two_block_dq_over_split_keys():
     for cus in (1, 8, 64, 256, 304):
         for groups in range((3 * cus + 1) // 2, 6 * cus):
             assert (2 * cus + groups // 2) // groups <= 1
+
+
+def test_read_out_workspace_holds_its_sums_alone():
+    """A forward of few query rows reads the mask itself: its workspace is the pieces'
+    maxima, sums and values, with no list of live keys (4 bytes a key)."""
+    for n, heads, kv, hd, tq, tk, dt, rows in ((1, 1, 1, 128, 1, 20_000_003, R.BF16, 1),
+                                               (3, 4, 2, 40, 1, 5_000_001, R.F32, 2),
+                                               (2, 6, 2, 32, 2, 3_000_000, R.F32, 8)):
+        d = R.attention_desc(n, heads, kv, hd, tq, tk, dt)
+        piece = 2048 if dt == R.BF16 else 1024  # keys
+        sums = n * kv * -(-tk // piece) * rows * (hd + 2) * 4
+        assert R.rat3d_attention_workspace_size(d, 0) == -(-sums // 256) * 256

@@ -1812,28 +1812,32 @@ static void fwd_launch(const AttnArgs& a, int64_t grid, hipStream_t st) {
     if (a.splits > 1) attn_fwd_k<T, DB, KB, true><<<(unsigned)grid, 256, 0, st>>>(a);
     else attn_fwd_k<T, DB, KB, false><<<(unsigned)grid, 256, 0, st>>>(a);
 }
-// kc, qc: column blocks of the two walks; both walks of one block go in one launch.
+// kc, qc: column blocks of the two walks; both walks of one block go in one launch.  `one`:
+// operations of one product over all keys, of which dK and dV need four and dQ the fifth.
 template <typename T, int DB>
-static void bwd_launch(const BwdArgs& g, int kc, int qc, hipStream_t st) {
+static void bwd_launch(const BwdArgs& g, int kc, int qc, double one, hipStream_t st) {
     const bool ks = g.kv.splits > 1, qs = g.q.splits > 1;
-    BwdArgs one = g;  // what the general kernel takes
+    BwdArgs rest = g;  // what the general kernel takes
     if constexpr (sizeof(T) == 2 && DB <= 2) {
         if (kc == 2) {
+            ProfScope ps("attn_dkv2", st, 4.0 * one, 0.0);
             if (ks) attn_dkv2_k<DB, true><<<(unsigned)g.kv_blocks, 256, 0, st>>>(g.kv);
             else attn_dkv2_k<DB, false><<<(unsigned)g.kv_blocks, 256, 0, st>>>(g.kv);
-            one.kv_blocks = 0;
+            rest.kv_blocks = 0;
         }
         if (qc == 2) {
+            ProfScope ps("attn_dq2", st, one, 0.0);
             attn_dq2_k<DB><<<(unsigned)g.q_blocks, 256, 0, st>>>(g.q);
-            one.q_blocks = 0;
+            rest.q_blocks = 0;
         }
     }
-    const unsigned grid = (unsigned)(one.kv_blocks + one.q_blocks);
+    const unsigned grid = (unsigned)(rest.kv_blocks + rest.q_blocks);
     if (grid == 0) return;
-    if (ks && qs) attn_bwd_k<T, DB, true, true><<<grid, 256, 0, st>>>(one);
-    else if (ks) attn_bwd_k<T, DB, true, false><<<grid, 256, 0, st>>>(one);
-    else if (qs) attn_bwd_k<T, DB, false, true><<<grid, 256, 0, st>>>(one);
-    else attn_bwd_k<T, DB, false, false><<<grid, 256, 0, st>>>(one);
+    ProfScope ps("attn_bwd", st, ((rest.kv_blocks ? 4 : 0) + (rest.q_blocks ? 1 : 0)) * one, 0.0);
+    if (ks && qs) attn_bwd_k<T, DB, true, true><<<grid, 256, 0, st>>>(rest);
+    else if (ks) attn_bwd_k<T, DB, true, false><<<grid, 256, 0, st>>>(rest);
+    else if (qs) attn_bwd_k<T, DB, false, true><<<grid, 256, 0, st>>>(rest);
+    else attn_bwd_k<T, DB, false, false><<<grid, 256, 0, st>>>(rest);
 }
 template <typename T, int VEC>
 static void few_launch(const FewArgs& f, unsigned grid, hipStream_t st) {
@@ -1967,7 +1971,6 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
     }
     const bool bf = d.dtype == RAT3D_BF16;
     {
-        ProfScope ps("attn_bwd", st, 5.0 * one, 0.0);
         BwdArgs g;
         g.kv = g.q = a;
         g.kv.splits = p.ks;
@@ -1977,7 +1980,7 @@ rat3d_status attention_bwd(const rat3d_attention_desc& d, const void* dout, cons
         g.q.splits = p.qs;
         g.q.tiles = (int)ceil_div(d.tq, 128 * p.qc);
         g.q_blocks = d.n * d.heads * g.q.tiles * p.qs;
-        RAT3D_ATTN(bwd_launch, d.dtype, p.DB, g, p.kc, p.qc, st);
+        RAT3D_ATTN(bwd_launch, d.dtype, p.DB, g, p.kc, p.qc, one, st);
     }
     if (p.ks > 1 || p.qs > 1) {
         SumArgs g = {};

@@ -544,7 +544,7 @@ rat3d_status qk_rope_fwd(const rat3d_qk_desc& d, const void* q, const void* k, c
     a.side[1].gamma = gk;
     a.side[1].x_stride = d.k_stride ? d.k_stride : (int64_t)d.kv_heads * d.head_dim * a.V;
     a.side[1].y_stride = d.ok_stride ? d.ok_stride : (int64_t)d.kv_heads * d.head_dim * a.V;
-    ProfScope ps("qk_rope_fwd", st, 0.0, qk_bytes(d, 2));
+    ProfScope ps(qk_tokens(d, false) == 8 ? "qk_rope_fwd_8" : "qk_rope_fwd", st, 0.0, qk_bytes(d, 2));
     if (d.dtype == RAT3D_BF16) qk_launch<bf16, false>(d, a, st);
     else qk_launch<float, false>(d, a, st);
     RAT3D_LAUNCH_CHECK();
@@ -574,7 +574,8 @@ rat3d_status qk_rope_bwd(const rat3d_qk_desc& d, const void* doq, const void* do
     a.side[1].x_stride = d.k_stride ? d.k_stride : (int64_t)d.kv_heads * d.head_dim * a.V;
     a.side[1].y_stride = d.ok_stride ? d.ok_stride : (int64_t)d.kv_heads * d.head_dim * a.V;
     {
-        ProfScope ps("qk_rope_bwd", st, 0.0, qk_bytes(d, 3));
+        ProfScope ps(qk_tokens(d, true) == 8 ? "qk_rope_bwd_8" : "qk_rope_bwd", st, 0.0,
+                     qk_bytes(d, 3));
         if (d.dtype == RAT3D_BF16) qk_launch<bf16, true>(d, a, st);
         else qk_launch<float, true>(d, a, st);
         RAT3D_LAUNCH_CHECK();

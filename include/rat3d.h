@@ -25,6 +25,8 @@
  *     tensors (x, y, dx, dy, residual, z, t, out, m) and workspaces must be
  *     16-byte aligned (RAT3D_EALIGN otherwise); weights and per-channel
  *     float32 vectors need only their natural alignment.
+ *   - A call runs on the device that is current; its stream and every pointer
+ *     belong to that device.
  *   - `stream` is a hipStream_t (NULL = the default stream).  Calls only
  *     enqueue work; they return before it runs.  Argument errors are detected
  *     on the host and returned before anything is enqueued.
@@ -52,7 +54,8 @@ typedef enum {
     RAT3D_OK = 0,
     RAT3D_EINVAL = -1,       /* a size, count or pointer argument is invalid */
     RAT3D_EUNSUPPORTED = -2, /* valid, but this shape/dtype combination is not built */
-    RAT3D_EALIGN = -3,       /* a device pointer is not 16-byte aligned */
+    RAT3D_EALIGN = -3,       /* a device pointer is not aligned as the call asks (16 bytes,
+                                or an element where that is enough) */
     RAT3D_EWORKSPACE = -4,   /* workspace smaller than the *_workspace_size query */
     RAT3D_EHIP = -5          /* the HIP runtime reported an error at launch */
 } rat3d_status;
@@ -231,7 +234,8 @@ rat3d_status rat3d_softmask_bwd(int64_t count, rat3d_dtype dtype, const void* do
 /* Norm of each head's query and key vector and rotation by the voxel's place, in
  * one pass:
  *   z = x * gamma / sqrt(mean(x^2) + eps)        (norm != 0; else z = x; eps >= 2^-126)
- * over the head_dim channels of one head and token, and then, for each axis a of
+ * over the head_dim channels of one head and token (x^2 is summed in float32: beyond
+ * |x| of about 10^18 the sum is infinite and z is 0), and then, for each axis a of
  * d, h, w in that order, the next rot_a channels of the head are turned in pairs
  * (i, i + rot_a/2), i < rot_a/2, by the angle
  *   (origin_a + place of the voxel on a) * base^(-2 i / rot_a);
@@ -261,7 +265,8 @@ rat3d_status rat3d_rope_table(const rat3d_qk_desc* desc, void* table, void* stre
 
 /* oq, ok = the norm and rotation of q [n][heads*head_dim][d*h*w] and of k
  * [n][kv_heads*head_dim][d*h*w]; gamma_q, gamma_k float32 [head_dim] (ignored
- * without norm).  oq may be q and ok may be k (same strides). */
+ * without norm).  oq may be q and ok may be k, with the same strides (other strides
+ * over the input are RAT3D_EINVAL). */
 rat3d_status rat3d_qk_norm_rope_fwd(const rat3d_qk_desc* desc, const void* q, const void* k,
                                     const float* gamma_q, const float* gamma_k,
                                     const void* table, void* oq, void* ok, void* stream);
@@ -285,8 +290,10 @@ rat3d_status rat3d_qk_norm_rope_bwd(const rat3d_qk_desc* desc, const void* doq, 
  * [tk], 1 <= tq, tk <= 2^28, head_dim <= 128.  lse float32 [n][heads][tq]
  * (nullable) receives log sum_j exp(scale q_i . k_j), which the backward reads.
  * A query without keys has o = 0 and lse = -infinity, and no part in any
- * gradient.  Masked keys and values are not read into a result, whatever they
- * hold; their gradients are 0. */
+ * gradient.  In RAT3D_BF16 probabilities and their gradients are rounded to bfloat16
+ * for the products behind them (tq times the group's heads above 8, and every
+ * gradient); maxima, sums and accumulators are float32.  Masked keys and values
+ * are not read into a result, whatever they hold; their gradients are 0. */
 typedef struct {
     int n, heads, kv_heads, head_dim;
     int64_t tq, tk;

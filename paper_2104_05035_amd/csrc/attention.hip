@@ -97,7 +97,10 @@ template <> struct Mm<float> {
 // Accumulator register i of a lane is row 8 (i / 4) + 4 (lane / 32) + i % 4.
 // Registers i .. i + kPer - 1 as an operand of contraction kT.  Probabilities and
 // score gradients are rounded to the storage type here, as the matrix instruction
-// takes them; the sums over them stay in float32.
+// takes them; the sums over them stay in float32.  In bfloat16 this is a second rounding
+// beside the result's own: sqrt(2) times its error (norm-wise 1.7e-3 -> 2.4e-3).  Unrounded
+// they would need the float32 instructions, at a sixteenth of the rate, or a second
+// product for what the rounding leaves.
 template <typename T>
 __device__ __forceinline__ typename Mm<T>::frag to_frag(const f32x16& p, int u);
 template <>
@@ -212,7 +215,9 @@ __device__ __forceinline__ int live_tokens(const uint8_t* __restrict__ m, int T,
 // ------------------------------------------------------------------ packing
 struct PackJob {
     const void* src;     // [n][heads * D][tokens], volumes `stride` apart
-    const void* other;   // o, where src is dout: D = sum over channels of src * other
+    const void* other;   // o, where src is dout: D = sum over channels of src * other; o as
+                         // stored, whose rounding is in dq and dk by sqrt(sum p^2) of what
+                         // that of the score gradients gives (some ten live keys: 2.7e-3 in all)
     const float* lse;
     u32x4* rec;          // records of 32 tokens, `units` 16-byte units each:
     int units, r, t, x;  // where forms R and T and the row constants lie, or -1
@@ -1591,8 +1596,9 @@ static int splits_for(int64_t groups, int64_t turns, int64_t least, int per_cu =
     return s < 2 ? 1 : (int)s;
 }
 
-// Backward in bfloat16: two blocks of 32 kept tokens a wave where the registers hold
-// them (head_dim <= 64) and that leaves three workgroups for two CUs.  Both walks at 4 x 2
+// Backward in bfloat16: two blocks of 32 kept tokens a wave up to head_dim 64, where that
+// leaves three workgroups for two CUs.  Above 64 it is not built: dQ would find registers
+// up to 128, dK/dV would spill 10 at 96 and 308 at 128; neither was timed.  Both walks at 4 x 2
 // heads over 24x28x24 voxels: 2120 us with one block, 1714 with two at head_dim 64, 1220
 // and 1060 at 32; 8 x 4 heads x 32 over 2100 tokens (288 workgroups) 126 and 127.  The
 // forward gains nothing by it: its bound is the exponentials, whose number stays

@@ -23,7 +23,7 @@
 //   T: rows are 32 channels, the contraction runs over 32 tokens, in the order of
 //      the accumulator's rows.
 // Head sizes are filled up with zeros to a multiple of 32, token counts to one of
-// 64.  Masked keys are left out: the live ones move up (an index list, made from
+// 64 (the backward's queries with the last query, see attn_pack_k).  Masked keys are left out: the live ones move up (an index list, made from
 // the mask), so masked voxels cost nothing and what they hold is never read.
 #include <math.h>
 

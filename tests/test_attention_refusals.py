@@ -1,5 +1,6 @@
 """Calls of the voxel self-attention that the library refuses on the host because
-their result would be wrong: float32 operands between two elements."""
+their result would be wrong: float32 operands between two elements, one gradient for
+two gains, results that lie over another volume's input."""
 import pytest
 
 from paper_2104_05035_amd import rat3d as R

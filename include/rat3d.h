@@ -350,6 +350,119 @@ rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
                                int accumulate, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Recurrent blocks over the voxels of a map (token mixing that is linear in the
+ * voxels, beside the attention above).  A map [n][c][d][h][w] is a sequence of
+ * v = d*h*w tokens a volume, in memory order.  With the 1^3 convolutions a block is
+ *   u = pre_norm(x); r, i, t, g = conv(u); h = recurrence(r, i, t);
+ *   z = conv(h);     y, u' = post_norm(x, z, g), u' the next block's u.
+ * Tensors may be channel ranges of larger ones: their pointers need only the alignment
+ * of an element, and the *_stride fields say how many elements lie between one volume
+ * and the next (0: packed, c * v); a gradient lies as the tensor it belongs to.
+ * mask is uint8 [n][v], or NULL: all voxels.  What a masked voxel's inputs hold is not
+ * read into a result, but for the residual's.
+ * A result may be one of the call's inputs of the same shape (the same pointer and, for
+ * n > 1, the same stride); any other overlap of a result with an input or another
+ * result is RAT3D_EINVAL.
+ * ------------------------------------------------------------------------ */
+
+typedef enum {
+    RAT3D_GATE_NONE = 0,
+    RAT3D_GATE_SIGMOID = 1, /* phi(g) = 1 / (1 + exp(-g)) */
+    RAT3D_GATE_SILU = 2     /* phi(g) = g / (1 + exp(-g)) */
+} rat3d_gate;
+
+/* Norms over a voxel's channels, N(x) = x / sqrt(mean_c x^2 + eps), x^2 summed in
+ * float32 (beyond |x| of about 10^18 the sum is infinite and N(x) is 0):
+ *   before a block   u = gamma N(x)
+ *   behind a block   y = x + scale phi(g) gamma N(z)        one rounding, and
+ *                    u = gamma_next N(y), y before its rounding (gamma_next != NULL)
+ * Masked voxels: u = 0, y = x.  2^-126 <= eps < 10^30; c <= 2^20. */
+typedef struct {
+    int n, c;
+    int64_t v;
+    rat3d_gate gate;  /* behind a block */
+    float eps;
+    int64_t x_stride; /* x and dx; before a block also dres */
+    int64_t z_stride, g_stride, y_stride, u_stride; /* also of dz, dg, dy, du */
+    rat3d_dtype dtype;
+} rat3d_norm_desc;
+
+/* gamma float32 [c]; gate, z_stride, g_stride and y_stride are ignored. */
+rat3d_status rat3d_pre_norm_fwd(const rat3d_norm_desc* desc, const void* x, const float* gamma,
+                                const uint8_t* mask, void* u, void* stream);
+
+/* gamma, scale (nullable: 1), gamma_next float32 [c]; g is read iff gate is not
+ * RAT3D_GATE_NONE, u is written iff gamma_next is given. */
+rat3d_status rat3d_post_norm_fwd(const rat3d_norm_desc* desc, const void* x, const void* z,
+                                 const void* g, const float* gamma, const float* scale,
+                                 const float* gamma_next, const uint8_t* mask, void* y, void* u,
+                                 void* stream);
+
+/* Bytes of workspace of either backward; (size_t)-1 if the descriptor is invalid.
+ * Calls that may run at the same time (streams, graphs) need a workspace each. */
+size_t rat3d_norm_workspace_size(const rat3d_norm_desc* desc);
+
+/* dx = [dres +] the gradient of x; dres (nullable) is the gradient that reaches x past
+ * the block, added before the one rounding.  Masked voxels: dx = dres, or 0.  dgamma
+ * float32 [c]: written, or added to when accumulate != 0. */
+rat3d_status rat3d_pre_norm_bwd(const rat3d_norm_desc* desc, const void* du, const void* x,
+                                const float* gamma, const uint8_t* mask, const void* dres,
+                                void* dx, float* dgamma, int accumulate, void* ws,
+                                size_t ws_bytes, void* stream);
+
+/* Gradients from dy and, iff gamma_next is given, du and the forward's y:
+ *   dx = dy + the gradient of y from du      (dx may be NULL without gamma_next: it is dy)
+ *   dz, dg (iff gated)                       0 at masked voxels, where dx = dy
+ *   dgamma, dscale (nullable), dgamma_next (iff gamma_next) float32 [c]: written, or
+ *   added to when accumulate != 0. */
+rat3d_status rat3d_post_norm_bwd(const rat3d_norm_desc* desc, const void* dy, const void* du,
+                                 const void* y, const void* z, const void* g, const float* gamma,
+                                 const float* scale, const float* gamma_next, const uint8_t* mask,
+                                 void* dx, void* dz, void* dg, float* dgamma, float* dscale,
+                                 float* dgamma_next, int accumulate, void* ws, size_t ws_bytes,
+                                 void* stream);
+
+/* Gated linear recurrence along the tokens, one state for each volume and channel
+ * (De et al. 2024, arXiv 2402.19427, equations 1 to 4):
+ *   a_t = exp(-rate softplus(lambda_c) sigmoid(r_t))
+ *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y = h
+ * from the first token to the last, or from the last to the first if reverse; h before
+ * the walk is h0 (nullable: 0).  A masked token hands the state on unchanged and has
+ * y = 0.  States, decays and sums are float32.  One token from a kept state is a call
+ * with len = 1 whose h_last is its h0. */
+typedef struct {
+    int n, c;
+    int64_t len;      /* tokens, 1 .. 2^38 */
+    int reverse;
+    float rate;       /* 2^-20 .. 2^20 */
+    int64_t r_stride, i_stride, x_stride, y_stride; /* also of dr, di, dx, dy */
+    rat3d_dtype dtype;
+} rat3d_recurrence_desc;
+
+/* Bytes of the states that the forward saves for the backward, and of workspace (pass 0
+ * = fwd, 1 = bwd); (size_t)-1 if the descriptor is invalid. */
+size_t rat3d_recurrence_carry_size(const rat3d_recurrence_desc* desc);
+size_t rat3d_recurrence_workspace_size(const rat3d_recurrence_desc* desc, int pass);
+
+/* r, i, x, y [n][c][len]; lambda float32 [c]; h0, h_last (nullable) float32 [n][c];
+ * h_last receives the state behind the walk.  carry (nullable) receives what the
+ * backward of the same descriptor needs. */
+rat3d_status rat3d_recurrence_fwd(const rat3d_recurrence_desc* desc, const void* r,
+                                  const void* i, const void* x, const float* lambda,
+                                  const uint8_t* mask, const float* h0, void* y, float* h_last,
+                                  float* carry, void* ws, size_t ws_bytes, void* stream);
+
+/* Gradients from dy and dh_last (nullable: 0), the forward's inputs and its carry: dr,
+ * di, dx (0 at masked tokens), dlambda float32 [c] (written, or added to when accumulate
+ * != 0) and dh0 float32 [n][c] (nullable, written). */
+rat3d_status rat3d_recurrence_bwd(const rat3d_recurrence_desc* desc, const void* dy,
+                                  const float* dh_last, const void* r, const void* i,
+                                  const void* x, const float* lambda, const uint8_t* mask,
+                                  const float* carry, void* dr, void* di, void* dx,
+                                  float* dlambda, float* dh0, int accumulate, void* ws,
+                                  size_t ws_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Classifier head and update (experiments section: cross-entropy, SGD).
  * ------------------------------------------------------------------------ */
 

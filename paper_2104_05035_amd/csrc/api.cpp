@@ -576,6 +576,327 @@ rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
                    accumulate ? dx : nullptr, dx, (hipStream_t)stream);
 }
 
+// Tensors of n parts of `held` bytes, `stride` bytes apart: what a call writes must not
+// lie over another of its tensors, unless the two are one.
+struct Span {
+    const void* p;
+    int64_t stride, held;
+    const char* name;
+};
+
+static bool spans_meet(const Span& a, const Span& b, int64_t n) {
+    const int64_t pa = (int64_t)(uintptr_t)a.p, pb = (int64_t)(uintptr_t)b.p;
+    if (pa + (n - 1) * a.stride + a.held <= pb || pb + (n - 1) * b.stride + b.held <= pa)
+        return false;
+    if (a.stride == b.stride) {  // one distance for all parts, up to whole strides
+        const int64_t m = (pb - pa) / a.stride;
+        for (int64_t k = m - 1; k <= m + 1; ++k) {
+            const int64_t off = pb - pa - k * a.stride;
+            if (k > -n && k < n && off < a.held && -off < b.held) return true;
+        }
+        return false;
+    }
+    for (int64_t k = 0; k < n; ++k) {
+        const int64_t lo = pa + k * a.stride, d = lo - b.held - pb;
+        const int64_t j = d < 0 ? 0 : d / b.stride + 1;  // b's first part that ends behind lo
+        if (j < n && pb + j * b.stride < lo + a.held) return true;
+    }
+    return false;
+}
+
+// outs must not meet one another, nor an input, unless it is that input.
+static rat3d_status check_spans(const Span* outs, int n_outs, const Span* ins, int n_ins, int64_t n,
+                                bool in_place) {
+    for (int o = 0; o < n_outs; ++o) {
+        if (!outs[o].p) continue;
+        for (int k = o + 1; k < n_outs; ++k)
+            RAT3D_REQUIRE(!outs[k].p || !spans_meet(outs[o], outs[k], n), RAT3D_EINVAL,
+                          "%s and %s must not overlap", outs[o].name, outs[k].name);
+        for (int k = 0; k < n_ins; ++k) {
+            const bool same = in_place && outs[o].p == ins[k].p &&
+                              (n == 1 || outs[o].stride == ins[k].stride);
+            RAT3D_REQUIRE(!ins[k].p || same || !spans_meet(outs[o], ins[k], n), RAT3D_EINVAL,
+                          "%s must not overlap %s", outs[o].name, ins[k].name);
+        }
+    }
+    return RAT3D_OK;
+}
+
+static rat3d_status check_norm(const rat3d_norm_desc* d) {
+    RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "norm descriptor is NULL");
+    RAT3D_REQUIRE(d->n >= 1 && d->c >= 1 && d->v >= 1, RAT3D_EINVAL, "norm sizes must be >= 1");
+    RAT3D_REQUIRE(d->gate == RAT3D_GATE_NONE || d->gate == RAT3D_GATE_SIGMOID ||
+                      d->gate == RAT3D_GATE_SILU,
+                  RAT3D_EINVAL, "unknown gate %d", (int)d->gate);
+    // the root of a smaller one is infinite on the device, and a token of zeros then NaN
+    RAT3D_REQUIRE(d->eps >= 0x1p-126f && d->eps < 1e30f, RAT3D_EINVAL,
+                  "the norm needs a finite eps of at least 2^-126");
+    RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
+                  (int)d->dtype);
+    RAT3D_REQUIRE(d->c <= 1 << 20, RAT3D_EUNSUPPORTED, "more than 2^20 channels");
+    RAT3D_REQUIRE(d->v <= (int64_t)1 << 36 && (double)d->c * d->v < 1.0e15, RAT3D_EUNSUPPORTED,
+                  "map too large");
+    const double held = (double)d->c * d->v;
+    RAT3D_STRIDE(d->x_stride, held);
+    RAT3D_STRIDE(d->z_stride, held);
+    RAT3D_STRIDE(d->g_stride, held);
+    RAT3D_STRIDE(d->y_stride, held);
+    RAT3D_STRIDE(d->u_stride, held);
+    return RAT3D_OK;
+}
+
+// A tensor of the map's shape, and a float32 vector of its channels.
+static Span map_span(const void* p, int64_t stride, int64_t packed, size_t es, const char* name) {
+    return {p, (int64_t)es * (stride ? stride : packed), (int64_t)es * packed, name};
+}
+static Span vec_span(const void* p, int64_t count, const char* name) {
+    return {p, 4 * count, 4 * count, name};
+}
+
+size_t rat3d_norm_workspace_size(const rat3d_norm_desc* desc) {
+    if (check_norm(desc) != RAT3D_OK) return (size_t)-1;
+    return norm_ws_bytes(*desc);
+}
+
+rat3d_status rat3d_pre_norm_fwd(const rat3d_norm_desc* desc, const void* x, const float* gamma,
+                                const uint8_t* mask, void* u, void* stream) {
+    rat3d_status s = check_norm(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(x, es, "x");
+    RAT3D_ELT(gamma, sizeof(float), "gamma");
+    RAT3D_ELT(u, es, "u");
+    const int64_t packed = desc->c * desc->v;
+    const Span outs[] = {map_span(u, desc->u_stride, packed, es, "u")};
+    const Span ins[] = {map_span(x, desc->x_stride, packed, es, "x")};
+    s = check_spans(outs, 1, ins, 1, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    return pre_norm_fwd(*desc, x, gamma, mask, u, (hipStream_t)stream);
+}
+
+rat3d_status rat3d_pre_norm_bwd(const rat3d_norm_desc* desc, const void* du, const void* x,
+                                const float* gamma, const uint8_t* mask, const void* dres,
+                                void* dx, float* dgamma, int accumulate, void* ws,
+                                size_t ws_bytes, void* stream) {
+    rat3d_status s = check_norm(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(du, es, "du");
+    RAT3D_ELT(x, es, "x");
+    RAT3D_ELT(gamma, sizeof(float), "gamma");
+    if (dres) RAT3D_ELT(dres, es, "dres");
+    RAT3D_ELT(dx, es, "dx");
+    RAT3D_ELT(dgamma, sizeof(float), "dgamma");
+    s = check_ws(ws, ws_bytes, norm_ws_bytes(*desc));
+    if (s != RAT3D_OK) return s;
+    const int64_t packed = desc->c * desc->v;
+    const Span outs[] = {map_span(dx, desc->x_stride, packed, es, "dx")};
+    const Span ins[] = {map_span(du, desc->u_stride, packed, es, "du"),
+                        map_span(x, desc->x_stride, packed, es, "x"),
+                        map_span(dres, desc->x_stride, packed, es, "dres")};
+    s = check_spans(outs, 1, ins, 3, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    const Span vec[] = {vec_span(dgamma, desc->c, "dgamma"), vec_span(gamma, desc->c, "gamma")};
+    s = check_spans(vec, 1, vec + 1, 1, 1, false);
+    if (s != RAT3D_OK) return s;
+    return pre_norm_bwd(*desc, du, x, gamma, mask, dres, dx, dgamma, accumulate ? 1 : 0, ws,
+                        (hipStream_t)stream);
+}
+
+rat3d_status rat3d_post_norm_fwd(const rat3d_norm_desc* desc, const void* x, const void* z,
+                                 const void* g, const float* gamma, const float* scale,
+                                 const float* gamma_next, const uint8_t* mask, void* y, void* u,
+                                 void* stream) {
+    rat3d_status s = check_norm(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(x, es, "x");
+    RAT3D_ELT(z, es, "z");
+    if (desc->gate) RAT3D_ELT(g, es, "g");
+    RAT3D_ELT(gamma, sizeof(float), "gamma");
+    if (scale) RAT3D_ELT(scale, sizeof(float), "scale");
+    RAT3D_ELT(y, es, "y");
+    if (gamma_next) {
+        RAT3D_ELT(gamma_next, sizeof(float), "gamma_next");
+        RAT3D_ELT(u, es, "u");
+    }
+    const int64_t packed = desc->c * desc->v;
+    const Span outs[] = {map_span(y, desc->y_stride, packed, es, "y"),
+                         map_span(gamma_next ? u : nullptr, desc->u_stride, packed, es, "u")};
+    const Span ins[] = {map_span(x, desc->x_stride, packed, es, "x"),
+                        map_span(z, desc->z_stride, packed, es, "z"),
+                        map_span(desc->gate ? g : nullptr, desc->g_stride, packed, es, "g")};
+    s = check_spans(outs, 2, ins, 3, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    return post_norm_fwd(*desc, x, z, g, gamma, scale, gamma_next, mask, y, u,
+                         (hipStream_t)stream);
+}
+
+rat3d_status rat3d_post_norm_bwd(const rat3d_norm_desc* desc, const void* dy, const void* du,
+                                 const void* y, const void* z, const void* g, const float* gamma,
+                                 const float* scale, const float* gamma_next, const uint8_t* mask,
+                                 void* dx, void* dz, void* dg, float* dgamma, float* dscale,
+                                 float* dgamma_next, int accumulate, void* ws, size_t ws_bytes,
+                                 void* stream) {
+    rat3d_status s = check_norm(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(dy, es, "dy");
+    RAT3D_ELT(z, es, "z");
+    RAT3D_ELT(dz, es, "dz");
+    if (desc->gate) {
+        RAT3D_ELT(g, es, "g");
+        RAT3D_ELT(dg, es, "dg");
+    }
+    RAT3D_ELT(gamma, sizeof(float), "gamma");
+    RAT3D_ELT(dgamma, sizeof(float), "dgamma");
+    if (scale) RAT3D_ELT(scale, sizeof(float), "scale");
+    if (dscale) RAT3D_ELT(dscale, sizeof(float), "dscale");
+    if (gamma_next) {
+        RAT3D_ELT(du, es, "du");
+        RAT3D_ELT(y, es, "y");
+        RAT3D_ELT(gamma_next, sizeof(float), "gamma_next");
+        RAT3D_ELT(dgamma_next, sizeof(float), "dgamma_next");
+        RAT3D_ELT(dx, es, "dx");
+    } else if (dx) {
+        RAT3D_ELT(dx, es, "dx");
+    }
+    s = check_ws(ws, ws_bytes, norm_ws_bytes(*desc));
+    if (s != RAT3D_OK) return s;
+    const bool gated = desc->gate != RAT3D_GATE_NONE;
+    const int64_t packed = desc->c * desc->v, c = desc->c;
+    const Span outs[] = {map_span(dx, desc->x_stride, packed, es, "dx"),
+                         map_span(dz, desc->z_stride, packed, es, "dz"),
+                         map_span(gated ? dg : nullptr, desc->g_stride, packed, es, "dg")};
+    const Span ins[] = {map_span(dy, desc->y_stride, packed, es, "dy"),
+                        map_span(gamma_next ? du : nullptr, desc->u_stride, packed, es, "du"),
+                        map_span(gamma_next ? y : nullptr, desc->y_stride, packed, es, "y"),
+                        map_span(z, desc->z_stride, packed, es, "z"),
+                        map_span(gated ? g : nullptr, desc->g_stride, packed, es, "g")};
+    s = check_spans(outs, 3, ins, 5, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    const Span vec[] = {vec_span(dgamma, c, "dgamma"), vec_span(dscale, c, "dscale"),
+                        vec_span(gamma_next ? dgamma_next : nullptr, c, "dgamma_next"),
+                        vec_span(gamma, c, "gamma"), vec_span(scale, c, "scale"),
+                        vec_span(gamma_next, c, "gamma_next")};
+    s = check_spans(vec, 3, vec + 3, 3, 1, false);
+    if (s != RAT3D_OK) return s;
+    return post_norm_bwd(*desc, dy, du, y, z, g, gamma, scale, gamma_next, mask, dx, dz, dg, dgamma,
+                         dscale, gamma_next ? dgamma_next : nullptr, accumulate ? 1 : 0, ws,
+                         (hipStream_t)stream);
+}
+
+static rat3d_status check_recurrence(const rat3d_recurrence_desc* d) {
+    RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "recurrence descriptor is NULL");
+    RAT3D_REQUIRE(d->n >= 1 && d->c >= 1 && d->len >= 1, RAT3D_EINVAL,
+                  "recurrence sizes must be >= 1");
+    RAT3D_REQUIRE(d->rate >= 0x1p-20f && d->rate <= 0x1p20f, RAT3D_EINVAL,
+                  "rate must be within 2^-20 .. 2^20");
+    RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
+                  (int)d->dtype);
+    // workgroups of up to 1024 threads, 2^32 threads a launch
+    RAT3D_REQUIRE((double)d->n * d->c < 4.0e6 && d->len <= (int64_t)1 << 38 &&
+                      (double)d->c * d->len < 1.0e15,
+                  RAT3D_EUNSUPPORTED, "recurrence too large for one launch");
+    const double held = (double)d->c * d->len;
+    RAT3D_STRIDE(d->r_stride, held);
+    RAT3D_STRIDE(d->i_stride, held);
+    RAT3D_STRIDE(d->x_stride, held);
+    RAT3D_STRIDE(d->y_stride, held);
+    return RAT3D_OK;
+}
+
+size_t rat3d_recurrence_carry_size(const rat3d_recurrence_desc* desc) {
+    if (check_recurrence(desc) != RAT3D_OK) return (size_t)-1;
+    return recurrence_carry_bytes(*desc);
+}
+
+size_t rat3d_recurrence_workspace_size(const rat3d_recurrence_desc* desc, int pass) {
+    if (check_recurrence(desc) != RAT3D_OK || pass < 0 || pass > 1) return (size_t)-1;
+    return recurrence_ws_bytes(*desc, pass);
+}
+
+rat3d_status rat3d_recurrence_fwd(const rat3d_recurrence_desc* desc, const void* r,
+                                  const void* i, const void* x, const float* lambda,
+                                  const uint8_t* mask, const float* h0, void* y, float* h_last,
+                                  float* carry, void* ws, size_t ws_bytes, void* stream) {
+    rat3d_status s = check_recurrence(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(r, es, "r");
+    RAT3D_ELT(i, es, "i");
+    RAT3D_ELT(x, es, "x");
+    RAT3D_ELT(lambda, sizeof(float), "lambda");
+    if (h0) RAT3D_ELT(h0, sizeof(float), "h0");
+    RAT3D_ELT(y, es, "y");
+    if (h_last) RAT3D_ELT(h_last, sizeof(float), "h_last");
+    if (carry) RAT3D_ELT(carry, sizeof(float), "carry");
+    s = check_ws(ws, ws_bytes, recurrence_ws_bytes(*desc, 0));
+    if (s != RAT3D_OK) return s;
+    const int64_t packed = desc->c * desc->len, rows = (int64_t)desc->n * desc->c;
+    const Span outs[] = {map_span(y, desc->y_stride, packed, es, "y")};
+    const Span ins[] = {map_span(r, desc->r_stride, packed, es, "r"),
+                        map_span(i, desc->i_stride, packed, es, "i"),
+                        map_span(x, desc->x_stride, packed, es, "x")};
+    s = check_spans(outs, 1, ins, 3, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    const Span vec[] = {vec_span(h_last, rows, "h_last"),
+                        vec_span(carry, (int64_t)recurrence_carry_bytes(*desc) / 4, "carry"),
+                        vec_span(lambda, desc->c, "lambda"),
+                        vec_span(h_last == h0 ? nullptr : h0, rows, "h0"),
+                        vec_span(h0, rows, "h0")};
+    s = check_spans(vec, 2, vec + 2, 2, 1, false);
+    if (s == RAT3D_OK) s = check_spans(vec + 1, 1, vec + 4, 1, 1, false);
+    if (s != RAT3D_OK) return s;
+    return recurrence_fwd(*desc, r, i, x, lambda, mask, h0, y, h_last, carry, ws,
+                          (hipStream_t)stream);
+}
+
+rat3d_status rat3d_recurrence_bwd(const rat3d_recurrence_desc* desc, const void* dy,
+                                  const float* dh_last, const void* r, const void* i,
+                                  const void* x, const float* lambda, const uint8_t* mask,
+                                  const float* carry, void* dr, void* di, void* dx,
+                                  float* dlambda, float* dh0, int accumulate, void* ws,
+                                  size_t ws_bytes, void* stream) {
+    rat3d_status s = check_recurrence(desc);
+    if (s != RAT3D_OK) return s;
+    const size_t es = esize(desc->dtype);
+    RAT3D_ELT(dy, es, "dy");
+    if (dh_last) RAT3D_ELT(dh_last, sizeof(float), "dh_last");
+    RAT3D_ELT(r, es, "r");
+    RAT3D_ELT(i, es, "i");
+    RAT3D_ELT(x, es, "x");
+    RAT3D_ELT(lambda, sizeof(float), "lambda");
+    RAT3D_ELT(carry, sizeof(float), "carry");
+    RAT3D_ELT(dr, es, "dr");
+    RAT3D_ELT(di, es, "di");
+    RAT3D_ELT(dx, es, "dx");
+    RAT3D_ELT(dlambda, sizeof(float), "dlambda");
+    if (dh0) RAT3D_ELT(dh0, sizeof(float), "dh0");
+    s = check_ws(ws, ws_bytes, recurrence_ws_bytes(*desc, 1));
+    if (s != RAT3D_OK) return s;
+    const int64_t packed = desc->c * desc->len, rows = (int64_t)desc->n * desc->c;
+    const Span outs[] = {map_span(dr, desc->r_stride, packed, es, "dr"),
+                         map_span(di, desc->i_stride, packed, es, "di"),
+                         map_span(dx, desc->x_stride, packed, es, "dx")};
+    const Span ins[] = {map_span(dy, desc->y_stride, packed, es, "dy"),
+                        map_span(r, desc->r_stride, packed, es, "r"),
+                        map_span(i, desc->i_stride, packed, es, "i"),
+                        map_span(x, desc->x_stride, packed, es, "x")};
+    s = check_spans(outs, 3, ins, 4, desc->n, true);
+    if (s != RAT3D_OK) return s;
+    const Span vec[] = {vec_span(dlambda, desc->c, "dlambda"), vec_span(dh0, rows, "dh0"),
+                        vec_span(lambda, desc->c, "lambda"),
+                        vec_span(carry, (int64_t)recurrence_carry_bytes(*desc) / 4, "carry"),
+                        vec_span(dh_last == dh0 ? nullptr : dh_last, rows, "dh_last"),
+                        vec_span(dh_last, rows, "dh_last")};
+    s = check_spans(vec, 2, vec + 2, 3, 1, false);
+    if (s == RAT3D_OK) s = check_spans(vec, 1, vec + 5, 1, 1, false);
+    if (s != RAT3D_OK) return s;
+    return recurrence_bwd(*desc, dy, dh_last, r, i, x, lambda, mask, carry, dr, di, dx, dlambda,
+                          dh0, accumulate ? 1 : 0, ws, (hipStream_t)stream);
+}
+
 size_t rat3d_head_workspace_size(int n, int c, int classes) {
     if (n < 1 || c < 1 || classes < 1) return (size_t)-1;
     return head_ws_bytes(n, c, classes);

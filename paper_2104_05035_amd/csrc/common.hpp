@@ -30,6 +30,18 @@ __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
 // that a mask recomputed elsewhere has the same bits.
 __device__ __forceinline__ float sigmoidf(float z) { return 1.f / (1.f + expf(-z)); }
 
+// sigmoid(v) and 1 - sigmoid(v), the latter as exp(-v) sigmoid(v) so that it keeps its
+// digits; from exp(-v) = 2^126 on it is 1.
+struct Sig {
+    float s, rest;
+    __device__ __forceinline__ explicit Sig(float v) {
+        const float t = -v * 1.44269504f;
+        const float e = __builtin_amdgcn_exp2f(t);
+        s = __builtin_amdgcn_rcpf(1.f + e);
+        rest = t > 126.f ? 1.f : e * s;
+    }
+};
+
 // Storage-type traits: load as float, store from float.
 template <typename T> struct Elt;
 template <> struct Elt<float> {

@@ -266,6 +266,31 @@ rat3d_status dropout(int64_t count, int64_t unit, double p, uint64_t seed, uint6
                      const uint64_t* step_dev, rat3d_dtype dt, const void* x, const void* res,
                      void* y, hipStream_t st);
 
+// ---- recurrent blocks (block_norm.hip, recurrence.hip) ------------------
+size_t norm_ws_bytes(const rat3d_norm_desc& d);
+rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* gamma,
+                          const uint8_t* mask, void* u, hipStream_t st);
+rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* x,
+                          const float* gamma, const uint8_t* mask, const void* dres, void* dx,
+                          float* dgamma, int accumulate, void* ws, hipStream_t st);
+rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* z, const void* g,
+                           const float* gamma, const float* scale, const float* next,
+                           const uint8_t* mask, void* y, void* u, hipStream_t st);
+rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void* du, const void* y,
+                           const void* z, const void* g, const float* gamma, const float* scale,
+                           const float* next, const uint8_t* mask, void* dx, void* dz, void* dg,
+                           float* dgamma, float* dscale, float* dnext, int accumulate, void* ws,
+                           hipStream_t st);
+size_t recurrence_carry_bytes(const rat3d_recurrence_desc& d);
+size_t recurrence_ws_bytes(const rat3d_recurrence_desc& d, int pass);
+rat3d_status recurrence_fwd(const rat3d_recurrence_desc& d, const void* r, const void* i,
+                            const void* x, const float* lam, const uint8_t* mask, const float* h0,
+                            void* y, float* h_last, float* carry, void* ws, hipStream_t st);
+rat3d_status recurrence_bwd(const rat3d_recurrence_desc& d, const void* dy, const float* dh_last,
+                            const void* r, const void* i, const void* x, const float* lam,
+                            const uint8_t* mask, const float* carry, void* dr, void* di, void* dx,
+                            float* dlam, float* dh0, int accumulate, void* ws, hipStream_t st);
+
 // ---- head, update, casts (head.hip) ------------------------------------
 size_t head_ws_bytes(int N, int C, int classes);
 rat3d_status head_fwd_bwd(int N, int C, int64_t V, int classes, rat3d_dtype dt, const void* x,

@@ -16,6 +16,7 @@ HEADER = os.path.join(os.path.dirname(HERE), "include", "rat3d.h")
 
 OK, EINVAL, EUNSUPPORTED, EALIGN, EWORKSPACE, EHIP = 0, -1, -2, -3, -4, -5
 F32, BF16, U8 = 0, 1, 2
+GATE_NONE, GATE_SIGMOID, GATE_SILU = 0, 1, 2
 NET_RESUNIT, NET_ATTN, NET_RESATTNET, NET_PARTITION1 = 1, 2, 3, 4
 
 
@@ -76,6 +77,21 @@ class DropoutDesc(ctypes.Structure):
                 ("seed", ctypes.c_uint64), ("dtype", ctypes.c_int)]
 
 
+class NormDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("c", ctypes.c_int), ("v", ctypes.c_int64),
+                ("gate", ctypes.c_int), ("eps", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("x_stride", "z_stride", "g_stride", "y_stride",
+                                              "u_stride")] + \
+               [("dtype", ctypes.c_int)]
+
+
+class RecurrenceDesc(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int), ("c", ctypes.c_int), ("len", ctypes.c_int64),
+                ("reverse", ctypes.c_int), ("rate", ctypes.c_float)] + \
+               [(n, ctypes.c_int64) for n in ("r_stride", "i_stride", "x_stride", "y_stride")] + \
+               [("dtype", ctypes.c_int)]
+
+
 class GabraParams(ctypes.Structure):
     _fields_ = [("population", ctypes.c_int), ("generations", ctypes.c_int),
                 ("crossover_p", ctypes.c_double), ("seed", ctypes.c_uint64),
@@ -125,6 +141,16 @@ _SIGS = {
     "rat3d_attention_bwd": (_I, [ctypes.POINTER(AttentionDesc)] + [_VP] * 11 + [_SZ, _VP]),
     "rat3d_dropout_fwd": (_I, [ctypes.POINTER(DropoutDesc), _U64] + [_VP] * 5),
     "rat3d_dropout_bwd": (_I, [ctypes.POINTER(DropoutDesc), _U64] + [_VP] * 3 + [_I, _VP]),
+    "rat3d_norm_workspace_size": (_SZ, [ctypes.POINTER(NormDesc)]),
+    "rat3d_pre_norm_fwd": (_I, [ctypes.POINTER(NormDesc)] + [_VP] * 5),
+    "rat3d_pre_norm_bwd": (_I, [ctypes.POINTER(NormDesc)] + [_VP] * 7 + [_I, _VP, _SZ, _VP]),
+    "rat3d_post_norm_fwd": (_I, [ctypes.POINTER(NormDesc)] + [_VP] * 10),
+    "rat3d_post_norm_bwd": (_I, [ctypes.POINTER(NormDesc)] + [_VP] * 15 + [_I, _VP, _SZ, _VP]),
+    "rat3d_recurrence_carry_size": (_SZ, [ctypes.POINTER(RecurrenceDesc)]),
+    "rat3d_recurrence_workspace_size": (_SZ, [ctypes.POINTER(RecurrenceDesc), _I]),
+    "rat3d_recurrence_fwd": (_I, [ctypes.POINTER(RecurrenceDesc)] + [_VP] * 10 + [_SZ, _VP]),
+    "rat3d_recurrence_bwd": (_I, [ctypes.POINTER(RecurrenceDesc)] + [_VP] * 13 +
+                             [_I, _VP, _SZ, _VP]),
     "rat3d_head_workspace_size": (_SZ, [_I, _I, _I]),
     "rat3d_head_fwd_bwd": (_I, [_I, _I, _I64, _I, _I] + [_VP] * 9 + [_I, _VP, _SZ, _VP]),
     "rat3d_sgd": (_I, [_I64, _F, _VP, _VP, _VP]),
@@ -396,6 +422,71 @@ def rat3d_dropout_fwd(desc, step, step_dev, x, residual, y, stream=None):
 def rat3d_dropout_bwd(desc, step, step_dev, dy, dx, accumulate, stream=None):
     _check(lib().rat3d_dropout_bwd(ctypes.byref(desc), step, _p(step_dev), _p(dy), _p(dx),
                                    int(accumulate), _stream(stream)))
+
+
+# ---------------------------------------------------------------- recurrent blocks
+def norm_desc(n, c, v, dtype, gate=GATE_NONE, eps=1e-6, x_stride=0, z_stride=0, g_stride=0,
+              y_stride=0, u_stride=0):
+    return NormDesc(n, c, v, gate, eps, x_stride, z_stride, g_stride, y_stride, u_stride, dtype)
+
+
+def rat3d_norm_workspace_size(desc):
+    return lib().rat3d_norm_workspace_size(ctypes.byref(desc))
+
+
+def rat3d_pre_norm_fwd(desc, x, gamma, mask, u, stream=None):
+    _check(lib().rat3d_pre_norm_fwd(ctypes.byref(desc), _p(x), _p(gamma), _p(mask), _p(u),
+                                    _stream(stream)))
+
+
+def rat3d_pre_norm_bwd(desc, du, x, gamma, mask, dres, dx, dgamma, accumulate, ws, ws_bytes,
+                       stream=None):
+    _check(lib().rat3d_pre_norm_bwd(ctypes.byref(desc), _p(du), _p(x), _p(gamma), _p(mask),
+                                    _p(dres), _p(dx), _p(dgamma), int(accumulate), _p(ws),
+                                    ws_bytes, _stream(stream)))
+
+
+def rat3d_post_norm_fwd(desc, x, z, g, gamma, scale, gamma_next, mask, y, u, stream=None):
+    _check(lib().rat3d_post_norm_fwd(ctypes.byref(desc), _p(x), _p(z), _p(g), _p(gamma),
+                                     _p(scale), _p(gamma_next), _p(mask), _p(y), _p(u),
+                                     _stream(stream)))
+
+
+def rat3d_post_norm_bwd(desc, dy, du, y, z, g, gamma, scale, gamma_next, mask, dx, dz, dg, dgamma,
+                        dscale, dgamma_next, accumulate, ws, ws_bytes, stream=None):
+    _check(lib().rat3d_post_norm_bwd(ctypes.byref(desc), _p(dy), _p(du), _p(y), _p(z), _p(g),
+                                     _p(gamma), _p(scale), _p(gamma_next), _p(mask), _p(dx),
+                                     _p(dz), _p(dg), _p(dgamma), _p(dscale), _p(dgamma_next),
+                                     int(accumulate), _p(ws), ws_bytes, _stream(stream)))
+
+
+def recurrence_desc(n, c, length, dtype, reverse=False, rate=8.0, r_stride=0, i_stride=0,
+                    x_stride=0, y_stride=0):
+    return RecurrenceDesc(n, c, length, int(reverse), rate, r_stride, i_stride, x_stride, y_stride,
+                          dtype)
+
+
+def rat3d_recurrence_carry_size(desc):
+    return lib().rat3d_recurrence_carry_size(ctypes.byref(desc))
+
+
+def rat3d_recurrence_workspace_size(desc, pass_):
+    return lib().rat3d_recurrence_workspace_size(ctypes.byref(desc), pass_)
+
+
+def rat3d_recurrence_fwd(desc, r, i, x, lam, mask, h0, y, h_last, carry, ws, ws_bytes,
+                         stream=None):
+    _check(lib().rat3d_recurrence_fwd(ctypes.byref(desc), _p(r), _p(i), _p(x), _p(lam), _p(mask),
+                                      _p(h0), _p(y), _p(h_last), _p(carry), _p(ws), ws_bytes,
+                                      _stream(stream)))
+
+
+def rat3d_recurrence_bwd(desc, dy, dh_last, r, i, x, lam, mask, carry, dr, di, dx, dlam, dh0,
+                         accumulate, ws, ws_bytes, stream=None):
+    _check(lib().rat3d_recurrence_bwd(ctypes.byref(desc), _p(dy), _p(dh_last), _p(r), _p(i),
+                                      _p(x), _p(lam), _p(mask), _p(carry), _p(dr), _p(di), _p(dx),
+                                      _p(dlam), _p(dh0), int(accumulate), _p(ws), ws_bytes,
+                                      _stream(stream)))
 
 
 # ---------------------------------------------------------------- head, sgd

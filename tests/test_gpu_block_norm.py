@@ -1,0 +1,380 @@
+"""rat3d_pre_norm_* and rat3d_post_norm_* against their float64 definitions."""
+import zlib
+
+import numpy as np
+import pytest
+
+from tests import gpu_util as U
+from tests import recurrent_util as RU
+
+pytestmark = pytest.mark.gpu
+
+GATES = {None: 0, "sigmoid": 1, "silu": 2}
+EPS = 1e-5
+
+
+def _rng(case):
+    return np.random.default_rng(zlib.crc32(repr(case).encode()))
+
+
+def _ws(nbytes):
+    torch = U.torch_mod()
+    return torch.full((max(int(nbytes), 16),), 0xFF, dtype=torch.uint8, device="cuda:0")
+
+
+def _mask(rng, n, v, kind):
+    """uint8 [n][v] or None; "holes" has a volume that is masked as a whole if n > 1."""
+    if kind is None:
+        return None
+    m = (rng.random((n, v)) < 0.6).astype(np.uint8) * rng.integers(1, 256, (n, v), dtype=np.uint8)
+    if n > 1:
+        m[n // 2] = 0
+    return m
+
+
+def _dev(mask):
+    return None if mask is None else U.torch_mod().from_numpy(mask).to("cuda:0")
+
+
+def _spoil(t, mask):
+    """NaN and infinities at masked voxels of the device tensor."""
+    if mask is not None:
+        torch = U.torch_mod()
+        off = torch.from_numpy(mask == 0).to("cuda:0")[:, None, :].expand(t.shape)
+        bad = torch.tensor([float("nan"), float("inf"), float("-inf")], device="cuda:0")
+        t[off] = bad[torch.arange(int(off.sum()), device="cuda:0") % 3].to(t.dtype)
+
+
+class Norms:
+    """Inputs of one case on the device and their exact values, the results guarded."""
+
+    def __init__(self, case, dt, amp=1.0):
+        from paper_2104_05035_amd import rat3d as R
+        self.R, self.dt = R, dt
+        self.n, self.c, self.v, self.kind, self.nxt, mask = case
+        rng = _rng((case, dt))
+        n, c, v = self.n, self.c, self.v
+        self.mask = _mask(rng, n, v, mask)
+        self.dmask = _dev(self.mask)
+        self.ref = {}
+        for name, a in (("x", 2.0), ("z", 1.5), ("g", 2.0), ("dy", 1.0), ("du", 1.0), ("dres", 1.0)):
+            val = rng.standard_normal((n, c, v)) * a * amp
+            t, self.ref[name] = U.dev_input(val, dt)
+            if v > 2 and name in "xz":  # a token of zeros: eps keeps the norm finite
+                t[0, :, 1] = 0
+                self.ref[name][0, :, 1] = 0
+            if name in ("z", "g", "du"):  # what else is masked is the residual's
+                _spoil(t, self.mask)
+            setattr(self, name, t)
+        for name in ("gamma", "scale", "gnext", "i0", "i1", "i2"):
+            t, self.ref[name] = U.dev_input(1 + 0.4 * rng.standard_normal(c), "f32")
+            setattr(self, name, t)
+        self.desc = R.norm_desc(n, c, v, U.code(dt), gate=GATES[self.kind], eps=EPS)
+        self.need = R.rat3d_norm_workspace_size(self.desc)
+        self.guards = []
+
+    def out(self, shape=None, dt=None):
+        t, buf = U.guarded(shape or (self.n, self.c, self.v), dt or self.dt)
+        self.guards.append(buf)
+        return t
+
+    def intact(self):
+        for b in self.guards:
+            U.guard_intact(b)
+
+
+def _check(got, want, names):
+    for k in names:
+        RU.within(U.f64(got[k]), want[k], k)
+
+
+# n, c, voxels, gate, next norm, mask
+CASES = [
+    (1, 1, 1, "silu", True, None), (1, 64, 1, None, True, None), (3, 256, 1, "silu", True, None),
+    (2, 5, 2, "sigmoid", False, "holes"), (2, 16, 7, "silu", True, "holes"),
+    (1, 33, 130, None, False, None), (2, 32, 257, "silu", True, None),
+    (2, 64, 1000, "sigmoid", True, "holes"), (1, 48, 1024, "silu", False, None),
+    (3, 100, 319, None, True, "holes"), (1, 128, 512, "silu", True, None),
+    (2, 200, 77, "sigmoid", True, None), (1, 256, 252, "silu", True, "holes"),
+    (1, 300, 129, "silu", True, None), (1, 512, 96, None, True, None),
+    (1, 700, 65, "sigmoid", True, "holes"), (1, 1500, 20, "silu", True, None),
+    (40, 3, 300, "silu", True, None), (5, 17, 4097, "silu", True, "holes"),
+]
+
+
+def _id(c):
+    return c if isinstance(c, str) else "n%d_c%d_v%d_%s%s%s" % (
+        c[0], c[1], c[2], c[3] or "plain", "_next" if c[4] else "", "_mask" if c[5] else "")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=_id)
+def test_pre_norm(case, dt):
+    print("pre_norm", case, dt, flush=True)
+    s = Norms(case, dt)
+    torch, R, x = U.torch_mod(), s.R, s.x.clone()
+    _spoil(x, s.mask)  # before a block the residual stream itself is read only where live
+    u, dx, dx0, dg = s.out(), s.out(), s.out(), s.out((s.c,), "f32")
+    R.rat3d_pre_norm_fwd(s.desc, x, s.gamma, s.dmask, u)
+    R.rat3d_pre_norm_bwd(s.desc, s.du, x, s.gamma, s.dmask, s.dres, dx, dg, 0, _ws(s.need), s.need)
+    U.sync()
+    args = (s.ref["x"], s.ref["gamma"], s.mask, EPS, dt, s.ref["du"])
+    _check(dict(u=u, dx=dx, dgamma=dg), RU.pre_norm_refs(*args, s.ref["dres"]),
+           ("u", "dx", "dgamma"))
+    acc = s.i0.clone()
+    R.rat3d_pre_norm_bwd(s.desc, s.du, x, s.gamma, s.dmask, None, dx0, acc, 1, _ws(s.need), s.need)
+    U.sync()
+    _check(dict(dx=dx0), RU.pre_norm_refs(*args), ("dx",))
+    assert torch.equal(acc, s.i0 + dg)
+    s.intact()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=_id)
+def test_post_norm(case, dt):
+    print("post_norm", case, dt, flush=True)
+    s = Norms(case, dt)
+    torch, R, r = U.torch_mod(), s.R, s.ref
+    g = s.g if s.kind else None
+    gn, gnr = (s.gnext, r["gnext"]) if s.nxt else (None, None)
+    for scale, sr in ((s.scale, r["scale"]), (None, None)):
+        y, u = s.out(), s.out() if s.nxt else None
+        R.rat3d_post_norm_fwd(s.desc, s.x, s.z, g, s.gamma, scale, gn, s.dmask, y, u)
+        U.sync()
+        want = RU.post_norm_refs(r["x"], r["z"], r["g"], s.kind, r["gamma"], sr, gnr, s.mask, EPS, dt)
+        _check(dict(y=y, u=u), want, want)
+        # the backward reads a stored y: here the forward's x, so that its values are known
+        yin = s.x.clone()
+        _spoil(yin, s.mask)
+        dx = s.out()
+        dz, dg = s.out(), s.out() if s.kind else None
+        vec = [s.out((s.c,), "f32") for _ in range(3)]
+        names = ("dgamma",) + (("dscale",) if scale is not None else ()) + \
+            (("dgamma_next",) if s.nxt else ())
+        back = lambda dgs, acc, dx: R.rat3d_post_norm_bwd(  # noqa: E731
+            s.desc, s.dy, s.du if s.nxt else None, yin if s.nxt else None, s.z, g, s.gamma, scale,
+            gn, s.dmask, dx, dz, dg, dgs[0], dgs[1] if scale is not None else None,
+            dgs[2] if s.nxt else None, acc, _ws(s.need), s.need)
+        back(vec, 0, dx)
+        U.sync()
+        want = RU.post_norm_bwd_refs(r["dy"], r["du"], r["x"], r["z"], r["g"], s.kind, r["gamma"],
+                                     sr, gnr, s.mask, EPS, dt)
+        got = dict(dx=dx, dz=dz, dg=dg, dgamma=vec[0], dscale=vec[1], dgamma_next=vec[2])
+        _check(got, want, ("dx", "dz") + (("dg",) if s.kind else ()) + names)
+        # added to what is there; without a next norm dx is dy itself and may be left out
+        first, acc = dz.clone(), [s.i0.clone(), s.i1.clone(), s.i2.clone()]
+        back(acc, 1, dx if s.nxt else None)
+        U.sync()
+        assert torch.equal(dz, first)
+        for a, i, t, k in zip(acc, (s.i0, s.i1, s.i2), vec, ("dgamma", "dscale", "dgamma_next")):
+            if k in names:
+                assert torch.equal(a, i + t), k
+    s.intact()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [24, 64, 300, 600])
+def test_ranges_of_wider_tensors(c, dt):
+    """Every tensor a channel range of a larger one at its own stride and odd element;
+    nothing beside the results changes."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, v = 3, 131
+    held = c * v
+    rng = _rng((c, dt, "ranges"))
+    strides = dict(x=held + 7, z=2 * held + 1, g=held + 13, y=held + 2, u=3 * held)
+    desc = R.norm_desc(n, c, v, U.code(dt), gate=R.GATE_SILU, eps=EPS,
+                       **{k + "_stride": s for k, s in strides.items()})
+    need = R.rat3d_norm_workspace_size(desc)
+    big, ref, ptr = {}, {}, {}
+
+    def place(name, like, at):
+        s = strides[like]
+        t, r = U.dev_input(rng.standard_normal(n * s + 64), dt)
+        big[name], ref[name] = t, np.stack([r[at + i * s:at + i * s + held] for i in range(n)])
+        ref[name] = ref[name].reshape(n, c, v)
+        ptr[name] = t.data_ptr() + at * t.element_size()
+
+    for k, (name, like) in enumerate((("x", "x"), ("z", "z"), ("g", "g"), ("y", "y"), ("u", "u"),
+                                      ("dy", "y"), ("du", "u"), ("yin", "y"), ("dx", "x"),
+                                      ("dz", "z"), ("dg", "g"), ("pre", "u"), ("pdx", "x"))):
+        place(name, like, (3 * k + 1) % 11)
+    like = dict(y="y", u="u", dx="x", dz="z", dg="g", pre="u", pdx="x")
+    before = {k: big[k].clone() for k in like}
+    gamma, gr = U.dev_input(1 + 0.3 * rng.standard_normal(c), "f32")
+    scale, sr = U.dev_input(1 + 0.3 * rng.standard_normal(c), "f32")
+    vec = [U.zeros_f32(c) for _ in range(3)]
+    R.rat3d_post_norm_fwd(desc, ptr["x"], ptr["z"], ptr["g"], gamma, scale, gamma, None, ptr["y"],
+                          ptr["u"])
+    R.rat3d_post_norm_bwd(desc, ptr["dy"], ptr["du"], ptr["yin"], ptr["z"], ptr["g"], gamma, scale,
+                          gamma, None, ptr["dx"], ptr["dz"], ptr["dg"], *vec, 0, _ws(need), need)
+    R.rat3d_pre_norm_fwd(desc, ptr["x"], gamma, None, ptr["pre"])
+    R.rat3d_pre_norm_bwd(desc, ptr["du"], ptr["x"], gamma, None, None, ptr["pdx"], vec[0], 0,
+                         _ws(need), need)
+    U.sync()
+    want = RU.post_norm_refs(ref["x"], ref["z"], ref["g"], "silu", gr, sr, gr, None, EPS, dt)
+    want.update(RU.post_norm_bwd_refs(ref["dy"], ref["du"], ref["yin"], ref["z"], ref["g"], "silu",
+                                      gr, sr, gr, None, EPS, dt))
+    pre = RU.pre_norm_refs(ref["x"], gr, None, EPS, dt, ref["du"])
+    want.update(pre=pre["u"], pdx=pre["dx"])
+    for k, (name, w) in enumerate(like.items()):
+        s = strides[w]
+        at = (ptr[name] - big[name].data_ptr()) // big[name].element_size()
+        mine = torch.zeros_like(big[name], dtype=torch.bool)
+        for i in range(n):
+            mine[at + i * s:at + i * s + held] = True
+        assert torch.equal(big[name][~mine], before[name][~mine]), name
+        RU.within(U.f64(big[name][mine]).reshape(n, c, v), want[name], name)
+
+
+def test_offsets_beyond_32_bits():
+    """Volumes more than 2^31 elements apart."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, c, v, wide = 2, 20, 133, (1 << 31) + 4097
+    rng = _rng("far")
+    x, xr = U.dev_input(rng.standard_normal((n, c, v)), "bf16")
+    z, zr = U.dev_input(rng.standard_normal((n, c, v)), "bf16")
+    g, gr = U.dev_input(1 + 0.3 * rng.standard_normal(c), "f32")
+    big = torch.empty(wide + c * v + 64, dtype=torch.bfloat16, device="cuda:0")
+    for i in range(n):
+        big[i * wide + 5:i * wide + 5 + c * v].copy_(x[i].view(-1))
+    desc = R.norm_desc(n, c, v, R.BF16, eps=EPS, x_stride=wide, y_stride=wide)
+    p = big.data_ptr() + 10
+    R.rat3d_post_norm_fwd(desc, p, z, None, g, None, None, None, p, None)
+    U.sync()
+    got = torch.stack([big[i * wide + 5:i * wide + 5 + c * v].view(c, v) for i in range(n)])
+    RU.within(U.f64(got), RU.post_norm_refs(xr, zr, None, None, gr, None, None, None, EPS,
+                                            "bf16")["y"], "y")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [40, 128, 400, 900])
+def test_results_over_inputs(c, dt):
+    """The same bits as into tensors of their own."""
+    case = (2, c, 203, "sigmoid", True, "holes")
+    s = Norms(case, dt)
+    torch, R = U.torch_mod(), s.R
+    E = lambda: torch.empty_like(s.x)  # noqa: E731
+    V = lambda: torch.empty(c, device="cuda:0")  # noqa: E731
+
+    def run(y, u, dx, dz, dg, pre, pdx, t):
+        v = [V(), V(), V(), V()]
+        R.rat3d_post_norm_fwd(s.desc, t["x"], t["z"], t["g"], s.gamma, s.scale, s.gnext, s.dmask, y,
+                              u)
+        R.rat3d_post_norm_bwd(s.desc, t["dy"], t["du"], t["yin"], t["z2"], t["g2"], s.gamma,
+                              s.scale, s.gnext, s.dmask, dx, dz, dg, *v[:3], 0, _ws(s.need), s.need)
+        R.rat3d_pre_norm_fwd(s.desc, t["x2"], s.gamma, s.dmask, pre)
+        R.rat3d_pre_norm_bwd(s.desc, t["du2"], t["x3"], s.gamma, s.dmask, t["dres"], pdx, v[3], 0,
+                             _ws(s.need), s.need)
+        U.sync()
+        return [y, u, dx, dz, dg, pre, pdx] + v
+
+    src = dict(x=s.x, z=s.z, g=s.g, dy=s.dy, du=s.du, yin=s.x, z2=s.z, g2=s.g, x2=s.x, du2=s.du,
+               x3=s.x, dres=s.dres)
+    own = run(*[E() for _ in range(7)], {k: t.clone() for k, t in src.items()})
+    for over in (("x", "z", "dy", "z2", "g2", "x2", "dres"), ("g", "x", "du", "yin", "dy", "x2", "du2"),
+                 ("z", "g", "yin", "g2", "du", "x2", "x3")):
+        t = {k: a.clone() for k, a in src.items()}
+        for a, b in zip(own, run(*[t[k] for k in over], t)):
+            assert torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float())), over
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c", [32, 700])
+def test_captured_and_replayed(c, dt):
+    """All four calls in a HIP graph, replayed on new inputs, with eager work between."""
+    case = (2, c, 517, "silu", True, "holes")
+    s = Norms(case, dt)
+    torch, R = U.torch_mod(), s.R
+    ws = _ws(s.need)
+    out = [torch.empty_like(s.x) for _ in range(7)] + [torch.empty(c, device="cuda:0")
+                                                       for _ in range(4)]
+    y, u, dx, dz, dg, pre, pdx, v0, v1, v2, v3 = out
+
+    def all_():
+        R.rat3d_pre_norm_fwd(s.desc, s.x, s.gamma, s.dmask, pre)
+        R.rat3d_post_norm_fwd(s.desc, s.x, s.z, s.g, s.gamma, s.scale, s.gnext, s.dmask, y, u)
+        R.rat3d_post_norm_bwd(s.desc, s.dy, s.du, y, s.z, s.g, s.gamma, s.scale, s.gnext, s.dmask,
+                              dx, dz, dg, v0, v1, v2, 0, ws, s.need)
+        R.rat3d_pre_norm_bwd(s.desc, s.du, s.x, s.gamma, s.dmask, dx, pdx, v3, 0, ws, s.need)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        all_()
+    U.sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        all_()
+    for i in range(3):
+        g = torch.Generator(device="cuda:0").manual_seed(60 + i)
+        for t in (s.x, s.z, s.g, s.dy, s.du):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda:0"))
+        ws.fill_(0xFF)
+        U.sync()
+        graph.replay()
+        U.sync()
+        got = [t.clone() for t in out]
+        for t in out:
+            t.fill_(55.0)
+        all_()
+        U.sync()
+        assert all(torch.equal(a, b) for a, b in zip(got, out))
+
+
+def test_two_streams_at_once():
+    """Backward calls on two streams, a workspace each: the bits of one after another."""
+    torch = U.torch_mod()
+    s = [Norms((2, 64, 9000, "silu", True, None), "bf16"),
+         Norms((3, 64, 7001, "sigmoid", True, "holes"), "bf16")]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def run(t, stream):
+        o = [torch.empty_like(t.x) for _ in range(3)] + [torch.empty(t.c, device="cuda:0")
+                                                         for _ in range(3)]
+        ws = _ws(t.need)
+        U.sync()
+        t.R.rat3d_post_norm_bwd(t.desc, t.dy, t.du, t.x, t.z, t.g, t.gamma, t.scale, t.gnext,
+                                t.dmask, *o, 0, ws, t.need, stream=stream.cuda_stream)
+        return o, ws
+
+    alone = []
+    for t, st in zip(s, streams):
+        alone.append(run(t, st)[0])
+        U.sync()
+    for _ in range(3):
+        both = [run(t, st) for t, st in zip(s, streams)]
+        U.sync()
+        for (o, _), a in zip(both, alone):
+            assert all(torch.equal(p, q) for p, q in zip(o, a))
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_smallest_eps_and_large_values(dt):
+    """At the smallest eps a token of zeros stays zero and its gradient finite; an infinite
+    sum of squares gives zeros; gates far out are shut or open."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    c, v = 24, 6
+    desc = R.norm_desc(1, c, v, U.code(dt), gate=R.GATE_SIGMOID, eps=2.0 ** -126)
+    z = torch.ones((1, c, v), dtype=U.tdtype(dt), device="cuda:0")
+    z[0, :, 1] = 0
+    z[0, :, 2] = 1e30
+    g = torch.zeros_like(z)
+    g[0, :, 3], g[0, :, 4] = 1e30, -1e30
+    x = torch.full_like(z, 2.0)
+    one = torch.ones(c, device="cuda:0")
+    y, dz, dg = (torch.empty_like(z) for _ in range(3))
+    dv = [torch.empty(c, device="cuda:0") for _ in range(2)]
+    need = R.rat3d_norm_workspace_size(desc)
+    R.rat3d_post_norm_fwd(desc, x, z, g, one, one, None, None, y, None)
+    R.rat3d_post_norm_bwd(desc, x, None, None, z, g, one, one, None, None, None, dz, dg, *dv, None,
+                          0, _ws(need), need)
+    U.sync()
+    assert torch.equal(y[0].float(), torch.tensor([2.5, 2.0, 2.0, 3.0, 2.0, 2.5],
+                                                  device="cuda:0").expand(c, v))
+    for t in [dz, dg] + dv:
+        assert bool(torch.isfinite(t).all())
+    assert bool((dz[0, :, 1].float() == 2.0 ** 63).all())  # dy phi r
+    assert bool((dg[0, :, 3:5] == 0).all())

@@ -1,0 +1,465 @@
+"""rat3d_recurrence_* against its float64 definition, and a whole recurrent block."""
+import numpy as np
+import pytest
+
+from oracle import recurrent as Q
+from tests import gpu_util as U
+from tests import recurrent_util as RU
+from tests.test_gpu_block_norm import _dev, _mask, _rng, _spoil, _ws
+
+pytestmark = pytest.mark.gpu
+
+
+class Walk:
+    """Inputs of one case on the device and their exact values."""
+
+    def __init__(self, case, dt):
+        from paper_2104_05035_amd import rat3d as R
+        self.R, self.dt = R, dt
+        self.n, self.c, self.v, self.reverse, mask, amp, rate = case
+        rng = _rng((case, dt))
+        n, c, v = self.n, self.c, self.v
+        self.mask = _mask(rng, n, v, mask)
+        self.dmask = _dev(self.mask)
+        self.ref = {}
+        for name, a in (("r", amp), ("i", amp), ("x", 1.0), ("dy", 1.0)):
+            t, self.ref[name] = U.dev_input(rng.standard_normal((n, c, v)) * a, dt)
+            _spoil(t, self.mask)
+            setattr(self, name, t)
+        for name, shape in (("lam", (c,)), ("h0", (n, c)), ("dh", (n, c)), ("init", (c,))):
+            val = rng.standard_normal(shape) * (2.0 if name == "lam" else 1.0)
+            t, self.ref[name] = U.dev_input(val - (2.0 if name == "lam" else 0.0), "f32")
+            setattr(self, name, t)
+        self.rate = rate
+        self.desc = R.recurrence_desc(n, c, v, U.code(dt), reverse=self.reverse, rate=rate)
+        self.need = [R.rat3d_recurrence_workspace_size(self.desc, p) for p in (0, 1)]
+        self.carry = _ws(R.rat3d_recurrence_carry_size(self.desc))
+        self.guards = []
+
+    def out(self, shape=None, dt=None):
+        t, buf = U.guarded(shape or (self.n, self.c, self.v), dt or self.dt)
+        self.guards.append(buf)
+        return t
+
+    def results(self):
+        f = lambda *s: self.out(s, "f32")  # noqa: E731
+        return dict(y=self.out(), h_last=f(self.n, self.c), dr=self.out(), di=self.out(),
+                    dx=self.out(), dlam=f(self.c), dh0=f(self.n, self.c))
+
+    def fwd(self, o, h0=True, save=True):
+        self.R.rat3d_recurrence_fwd(self.desc, self.r, self.i, self.x, self.lam, self.dmask,
+                                    self.h0 if h0 else None, o["y"], o.get("h_last"),
+                                    self.carry if save else None, _ws(self.need[0]), self.need[0])
+
+    def bwd(self, o, dh=True, acc=0):
+        self.R.rat3d_recurrence_bwd(self.desc, self.dy, self.dh if dh else None, self.r, self.i,
+                                    self.x, self.lam, self.dmask, self.carry, o["dr"], o["di"],
+                                    o["dx"], o["dlam"], o.get("dh0"), acc, _ws(self.need[1]),
+                                    self.need[1])
+
+    def refs(self, ends=True):
+        r = self.ref
+        return RU.recurrence_refs(r["r"], r["i"], r["x"], r["lam"], self.mask,
+                                  r["h0"] if ends else None, self.rate, self.reverse, self.dt,
+                                  r["dy"], r["dh"] if ends else None)
+
+
+# n, c, tokens, reverse, mask, gates' amplitude, rate
+CASES = [
+    (1, 1, 1, False, None, 1.0, 8.0), (8, 256, 1, True, None, 1.0, 8.0),
+    (3, 5, 1, False, "holes", 1.0, 8.0), (2, 3, 2, True, "holes", 1.0, 8.0),
+    (5, 7, 7, False, None, 1.0, 8.0), (2, 64, 8, True, None, 1.0, 1.0),
+    (3, 11, 9, False, "holes", 2.0, 8.0), (2, 30, 16, True, "holes", 1.0, 8.0),
+    (2, 33, 31, False, None, 1.0, 8.0), (2, 20, 64, True, None, 1.0, 8.0),
+    (1, 70, 65, False, "holes", 1.0, 8.0), (2, 9, 127, True, "holes", 3.0, 8.0),
+    (1, 256, 252, False, "holes", 1.0, 8.0), (2, 5, 300, True, None, 1.0, 0.5),
+    (2, 5, 511, False, None, 1.0, 8.0), (2, 5, 512, True, "holes", 1.0, 8.0),
+    (2, 5, 513, False, None, 10.0, 8.0), (2, 5, 1024, True, None, 1.0, 8.0),
+    (3, 4, 1500, False, "holes", 1.0, 8.0), (2, 3, 4096, True, "holes", 1.0, 8.0),
+    (1, 3, 4097, False, None, 1.0, 8.0), (2, 2, 9001, True, "holes", 1.0, 8.0),
+    (1, 2, 20000, False, None, 1.0, 8.0), (1, 1, 70001, True, "holes", 1.0, 8.0),
+    (1, 1, 300000, False, None, 1.0, 8.0), (300, 3, 1100, True, "holes", 1.0, 8.0),
+]
+
+
+def _id(c):
+    return c if isinstance(c, str) else "n%d_c%d_v%d%s%s_a%g_r%g" % (
+        c[0], c[1], c[2], "_back" if c[3] else "", "_mask" if c[4] else "", c[5], c[6])
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("case", CASES, ids=_id)
+def test_recurrence(case, dt):
+    print("recurrence", case, dt, flush=True)
+    torch = U.torch_mod()
+    s = Walk(case, dt)
+    o = s.results()
+    s.fwd(o)
+    s.bwd(o)
+    U.sync()
+    want = s.refs()
+    for k in want:
+        RU.within(U.f64(o[k]), want[k], k)
+    # added to what is there, and without what may be left out
+    p = s.results()
+    p.pop("dh0")
+    p["dlam"].copy_(s.init)
+    s.bwd(p, acc=1)
+    q = s.results()
+    q.pop("h_last")
+    s.fwd(q, save=False)
+    U.sync()
+    assert torch.equal(p["dlam"], s.init + o["dlam"])
+    for k in ("dr", "di", "dx"):
+        assert torch.equal(p[k], o[k])
+    assert torch.equal(q["y"], o["y"])
+    s.fwd(q, h0=False)
+    s.bwd(q, dh=False)
+    U.sync()
+    want = s.refs(ends=False)
+    want.pop("h_last")
+    for k in want:
+        RU.within(U.f64(q[k]), want[k], k)
+    for b in s.guards:
+        U.guard_intact(b)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", [(5, 1), (6, 37), (4, 700), (2, 9003)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_ranges_of_wider_tensors(c, v, reverse, dt):
+    """Every tensor a channel range of a larger one at its own stride and odd element;
+    nothing beside the results changes."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, held = 3, c * v
+    rng = _rng((c, v, reverse, dt))
+    strides = dict(r=held + 3, i=2 * held + 1, x=held, y=held + 5)
+    desc = R.recurrence_desc(n, c, v, U.code(dt), reverse=reverse,
+                             **{k + "_stride": t for k, t in strides.items()})
+    big, ref, at = {}, {}, {}
+    for k, (name, like) in enumerate((("r", "r"), ("i", "i"), ("x", "x"), ("y", "y"), ("dy", "y"),
+                                      ("dr", "r"), ("di", "i"), ("dx", "x"))):
+        s, at[name] = strides[like], (5 * k + 1) % 9
+        big[name], t = U.dev_input(rng.standard_normal(n * s + 16), dt)
+        ref[name] = np.stack([t[at[name] + j * s:at[name] + j * s + held] for j in range(n)])
+        ref[name] = ref[name].reshape(n, c, v)
+    ptr = {k: t.data_ptr() + at[k] * t.element_size() for k, t in big.items()}
+    like = dict(y="y", dr="r", di="i", dx="x")
+    before = {k: big[k].clone() for k in like}
+    lam, lr = U.dev_input(rng.standard_normal(c) - 2, "f32")
+    need = [R.rat3d_recurrence_workspace_size(desc, p) for p in (0, 1)]
+    carry, dlam = _ws(R.rat3d_recurrence_carry_size(desc)), U.zeros_f32(c)
+    R.rat3d_recurrence_fwd(desc, ptr["r"], ptr["i"], ptr["x"], lam, None, None, ptr["y"], None,
+                           carry, _ws(need[0]), need[0])
+    R.rat3d_recurrence_bwd(desc, ptr["dy"], None, ptr["r"], ptr["i"], ptr["x"], lam, None, carry,
+                           ptr["dr"], ptr["di"], ptr["dx"], dlam, None, 0, _ws(need[1]), need[1])
+    U.sync()
+    want = RU.recurrence_refs(ref["r"], ref["i"], ref["x"], lr, None, None, 8.0, reverse, dt,
+                              ref["dy"])
+    RU.within(U.f64(dlam), want["dlam"], "dlam")
+    for name, w in like.items():
+        mine = torch.zeros_like(big[name], dtype=torch.bool)
+        for j in range(n):
+            mine[at[name] + j * strides[w]:at[name] + j * strides[w] + held] = True
+        assert torch.equal(big[name][~mine], before[name][~mine]), name
+        RU.within(U.f64(big[name][mine]).reshape(n, c, v), want[name], name)
+
+
+def test_offsets_beyond_32_bits():
+    """Volumes more than 2^31 elements apart."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, c, v, wide = 2, 3, 1300, (1 << 31) + 4097
+    rng = _rng("far")
+    dev = {}
+    ref = {}
+    for k in ("r", "i", "x"):
+        dev[k], ref[k] = U.dev_input(rng.standard_normal((n, c, v)), "bf16")
+    big = torch.empty(wide + c * v + 64, dtype=torch.bfloat16, device="cuda:0")
+    for j in range(n):
+        big[j * wide + 3:j * wide + 3 + c * v].copy_(dev["x"][j].view(-1))
+    lam, lr = U.dev_input(rng.standard_normal(c) - 2, "f32")
+    desc = R.recurrence_desc(n, c, v, R.BF16, x_stride=wide, y_stride=wide)
+    need = R.rat3d_recurrence_workspace_size(desc, 0)
+    p = big.data_ptr() + 6
+    R.rat3d_recurrence_fwd(desc, dev["r"], dev["i"], p, lam, None, None, p, None, None, _ws(need),
+                           need)
+    U.sync()
+    got = torch.stack([big[j * wide + 3:j * wide + 3 + c * v].view(c, v) for j in range(n)])
+    RU.within(U.f64(got), RU.recurrence_refs(ref["r"], ref["i"], ref["x"], lr, None, None, 8.0, False,
+                                             "bf16")["y"], "y")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", [(5, 1), (6, 37), (4, 700), (2, 9003), (1, 70000)])
+def test_results_over_inputs(c, v, dt):
+    """The same bits as into tensors of their own; the state kept in place."""
+    torch = U.torch_mod()
+    a = Walk((2, c, v, False, "holes", 1.0, 8.0), dt)
+    o = a.results()
+    a.fwd(o)
+    a.bwd(o)
+    U.sync()
+    for over in "rix":
+        b = Walk((2, c, v, False, "holes", 1.0, 8.0), dt)
+        b.fwd(dict(y=getattr(b, over), h_last=b.h0))
+        U.sync()
+        assert torch.equal(getattr(b, over), o["y"]) and torch.equal(b.h0, o["h_last"])
+    for over in (("r", "i", "x"), ("dy", "x", "r"), ("x", "dy", "i"), ("i", "r", "dy")):
+        b = Walk((2, c, v, False, "holes", 1.0, 8.0), dt)
+        p = b.results()
+        b.fwd(p)
+        p.update({k: getattr(b, t) for k, t in zip(("dr", "di", "dx"), over)}, dh0=b.dh)
+        b.bwd(p)
+        U.sync()
+        for k in o:
+            assert torch.equal(p[k], o[k]), (over, k)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_token_by_token(reverse, dt):
+    """A sequence one token a call from the kept state, in pieces, and as a whole."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, c, v = 2, 37, 12
+    s = Walk((n, c, v, reverse, "holes", 1.0, 8.0), dt)
+    want = s.refs()
+    order = list(range(v - 1, -1, -1) if reverse else range(v))
+    for size in (1, 5):
+        state, y = s.h0.clone(), torch.empty_like(s.x)
+        for first in range(0, v, size):
+            part = sorted(order[first:first + size])
+            cut = lambda t: t[..., part].contiguous()  # noqa: E731
+            desc = R.recurrence_desc(n, c, len(part), U.code(dt), reverse=reverse)
+            need = R.rat3d_recurrence_workspace_size(desc, 0)
+            o = torch.empty((n, c, len(part)), dtype=s.x.dtype, device="cuda:0")
+            R.rat3d_recurrence_fwd(desc, cut(s.r), cut(s.i), cut(s.x), s.lam, cut(s.dmask), state,
+                                   o, state, None, _ws(need), need)
+            y[..., part] = o
+        U.sync()
+        RU.within(U.f64(y), want["y"], "y")
+        RU.within(U.f64(state), want["h_last"], "h_last")
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("n,c,v", [(2, 6, 37), (3, 4, 1100), (1, 2, 70000)])
+def test_captured_and_replayed(n, c, v, dt):
+    """Forward and backward in a HIP graph, replayed on new inputs, with eager work
+    between the replays."""
+    torch = U.torch_mod()
+    s = Walk((n, c, v, True, "holes", 1.0, 8.0), dt)
+    ws = [_ws(b) for b in s.need]
+    o = s.results()
+
+    def both():
+        s.R.rat3d_recurrence_fwd(s.desc, s.r, s.i, s.x, s.lam, s.dmask, s.h0, o["y"], o["h_last"],
+                                 s.carry, ws[0], s.need[0])
+        s.R.rat3d_recurrence_bwd(s.desc, s.dy, s.dh, s.r, s.i, s.x, s.lam, s.dmask, s.carry,
+                                 o["dr"], o["di"], o["dx"], o["dlam"], o["dh0"], 0, ws[1],
+                                 s.need[1])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        both()
+    U.sync()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        both()
+    for k in range(3):
+        g = torch.Generator(device="cuda:0").manual_seed(70 + k)
+        for t in (s.r, s.i, s.x, s.dy):
+            t.copy_(torch.randn(t.shape, generator=g, device="cuda:0"))
+        for t in ws + [s.carry]:
+            t.fill_(0xFF)
+        U.sync()
+        graph.replay()
+        U.sync()
+        got = {k: t.clone() for k, t in o.items()}
+        for t in o.values():
+            t.fill_(55.0)
+        both()
+        U.sync()
+        assert all(torch.equal(got[k], o[k]) for k in o)
+
+
+def test_two_streams_at_once():
+    """Two walks on two streams, workspaces each: the bits of one after another."""
+    torch = U.torch_mod()
+    s = [Walk((1, 4, 50000, False, None, 1.0, 8.0), "bf16"),
+         Walk((2, 3, 60001, True, "holes", 1.0, 8.0), "bf16")]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def run(t, stream):
+        o = t.results()
+        with torch.cuda.stream(stream):
+            t.fwd(o)
+            t.bwd(o)
+        return o
+
+    alone = []
+    for t, st in zip(s, streams):
+        U.sync()
+        alone.append(run(t, st))
+        U.sync()
+    for _ in range(3):
+        U.sync()
+        both = [run(t, st) for t, st in zip(s, streams)]
+        U.sync()
+        for o, a in zip(both, alone):
+            assert all(torch.equal(o[k], a[k]) for k in a)
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+def test_shut_and_open_gates(dt):
+    """Gates far out: shut, the state stays as it is to the bit and the inputs get no
+    gradient; open with a fast decay, nothing is kept."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n, c, v = 1, 3, 1700
+    code = U.code(dt)
+    full = lambda a: torch.full((n, c, v), a, dtype=U.tdtype(dt), device="cuda:0")  # noqa: E731
+    x, dy = full(3.0), full(0.0)
+    h0 = torch.tensor([[0.5, -2.0, 7.0]], device="cuda:0")
+    dh = torch.tensor([[1.0, 2.0, -3.0]], device="cuda:0")
+    for r, lam, shut in ((-1e30, 5.0, True), (1e30, 50.0, False), (0.0, -200.0, True)):
+        desc = R.recurrence_desc(n, c, v, code)
+        lamt = torch.full((c,), lam, device="cuda:0")
+        need = max(R.rat3d_recurrence_workspace_size(desc, p) for p in (0, 1))
+        carry, ws = _ws(R.rat3d_recurrence_carry_size(desc)), _ws(need)
+        y, dr, di, dx = (full(9.0) for _ in range(4))
+        last, dlam, dh0 = torch.empty_like(h0), torch.empty(c, device="cuda:0"), torch.empty_like(h0)
+        R.rat3d_recurrence_fwd(desc, full(r), full(0.0), x, lamt, None, h0, y, last, carry, ws, need)
+        R.rat3d_recurrence_bwd(desc, dy, dh, full(r), full(0.0), x, lamt, None, carry, dr, di, dx,
+                               dlam, dh0, 0, ws, need)
+        U.sync()
+        for t in (y, last, dr, di, dx, dlam, dh0):
+            assert bool(torch.isfinite(t).all())
+        if shut:  # what a gate that is not quite shut lets through is below 2^-50 a token
+            assert float((last - h0).abs().max()) <= v * 3 * 2.0 ** -49
+            assert float((dh0 - dh).abs().max()) <= 2.0 ** -20
+            assert float(dx.float().abs().max()) <= 2.0 ** -47
+        else:
+            assert bool((y.float() == 1.5).all()) and bool((last == 1.5).all())
+            assert bool((dh0 == 0).all()) and bool((dr == 0).all())
+
+
+def test_nan_stays_in_its_row():
+    """A live NaN reaches every later voxel of its channel and nothing else."""
+    torch = U.torch_mod()
+    s = Walk((2, 3, 1300, False, None, 1.0, 8.0), "f32")
+    o, p = s.results(), s.results()
+    s.fwd(o)
+    s.r[1, 1, 600] = float("nan")
+    s.fwd(p)
+    U.sync()
+    assert bool(torch.isnan(p["y"][1, 1, 600:]).all())
+    p["y"][1, 1, 600:] = o["y"][1, 1, 600:]
+    assert torch.equal(p["y"], o["y"])
+
+
+# ------------------------------------------------------------------ the block
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+def test_recurrent_block(dt):
+    """u = norm(x); r, i, t, g = conv(u); h = recurrence(r, i, t) there and back;
+    z = conv(h); y, u' = x + gate(g) norm(z), norm(y) as a program runs it, in one tensor
+    for the gates and values, forward and backward, against float64 and, in float32,
+    against differences of the float64 block."""
+    from paper_2104_05035_amd import rat3d as R
+    n, c, grid, rate, eps = 2, 24, (4, 5, 6), 8.0, 1e-5
+    v = 120
+    rng = _rng(("block", dt))
+    code = U.code(dt)
+    x, xr = U.dev_input(rng.standard_normal((n, c, v)), dt)
+    w1, w1r = U.dev_input(rng.standard_normal((4 * c, c)) / np.sqrt(c), dt)
+    w2, w2r = U.dev_input(rng.standard_normal((c, 2 * c)) / np.sqrt(2 * c), dt)
+    vec, vr = {}, {}
+    for k in ("g0", "g1", "sc", "g2"):
+        vec[k], vr[k] = U.dev_input(1 + 0.2 * rng.standard_normal(c), "f32")
+    vec["lam"], vr["lam"] = U.dev_input(rng.standard_normal(c) - 3, "f32")
+    dy, dyr = U.dev_input(rng.standard_normal((n, c, v)), dt)
+    du, dur = U.dev_input(rng.standard_normal((n, c, v)), dt)
+    mask = (rng.random((n, v)) < 0.7).astype(np.uint8)
+    m = _dev(mask)
+    wide = 4 * c * v
+    c1 = R.conv_desc(n, c, 4 * c, *grid, 1, 1, 0, False, code)
+    c2 = R.conv_desc(n, 2 * c, c, *grid, 1, 1, 0, False, code)
+    nd = R.norm_desc(n, c, v, code, gate=R.GATE_SILU, eps=eps, g_stride=wide)
+    rd = [R.recurrence_desc(n, c, v, code, reverse=b, rate=rate, r_stride=wide, i_stride=wide,
+                            x_stride=wide, y_stride=2 * c * v) for b in (False, True)]
+    need = max([R.rat3d_conv3d_workspace_size(d, i) for d in (c1, c2) for i in range(3)] +
+               [R.rat3d_recurrence_workspace_size(rd[0], i) for i in (0, 1)] +
+               [R.rat3d_norm_workspace_size(nd)])
+    ws = _ws(need)
+    E = lambda ch: U.empty((n, ch, v), dt)  # noqa: E731
+    Z = U.zeros_f32
+    u0, t, h, z, y, u = E(c), E(4 * c), E(2 * c), E(c), E(c), E(c)
+    r_, i_, t_, g_ = (t[:, k * c:(k + 1) * c] for k in range(4))
+    carry = [_ws(R.rat3d_recurrence_carry_size(d)) for d in rd]
+    R.rat3d_pre_norm_fwd(nd, x, vec["g0"], m, u0)
+    R.rat3d_conv3d_fwd(c1, u0, w1, None, t, ws, need)
+    for k in range(2):  # the first half of h walks forth, the second back
+        R.rat3d_recurrence_fwd(rd[k], r_, i_, t_, vec["lam"], m, None, h[:, k * c:], None, carry[k],
+                               ws, need)
+    R.rat3d_conv3d_fwd(c2, h, w2, None, z, ws, need)
+    R.rat3d_post_norm_fwd(nd, x, z, g_, vec["g1"], vec["sc"], vec["g2"], m, y, u)
+    dxr_, dz, dh, dt1, dt2, du0, dx = E(c), E(c), E(2 * c), E(4 * c), E(4 * c), E(c), E(c)
+    d = {k: Z(c) for k in ("dg0", "dg1", "dsc", "dg2", "dlam")}
+    dw1, dw2 = Z((4 * c, c)), Z((c, 2 * c))
+    R.rat3d_post_norm_bwd(nd, dy, du, y, z, g_, vec["g1"], vec["sc"], vec["g2"], m, dxr_, dz,
+                          dt1[:, 3 * c:], d["dg1"], d["dsc"], d["dg2"], 0, ws, need)
+    R.rat3d_conv3d_wgrad(c2, h, dz, dw2, None, 0, ws, need)
+    R.rat3d_conv3d_dgrad(c2, dz, w2, dh, 0, ws, need)
+    dt2.zero_()
+    for k, to in ((0, dt1), (1, dt2)):
+        R.rat3d_recurrence_bwd(rd[k], dh[:, k * c:], None, r_, i_, t_, vec["lam"], m, carry[k],
+                               to[:, :c], to[:, c:2 * c], to[:, 2 * c:3 * c], d["dlam"], None, k, ws,
+                               need)
+    dt1 += dt2
+    R.rat3d_conv3d_wgrad(c1, u0, dt1, dw1, None, 0, ws, need)
+    R.rat3d_conv3d_dgrad(c1, dt1, w1, du0, 0, ws, need)
+    R.rat3d_pre_norm_bwd(nd, du0, x, vec["g0"], m, dxr_, dx, d["dg0"], 0, ws, need)
+    U.sync()
+
+    def forward(xr, w1r, w2r, p):
+        us = Q.pre_norm(xr, p["g0"], mask, eps)
+        ts = np.matmul(w1r, us)
+        rs, is_, vs, gs = (ts[:, k * c:(k + 1) * c] for k in range(4))
+        walks = [Q.recurrence(rs, is_, vs, p["lam"], mask, None, rate, b) for b in (False, True)]
+        hs = np.concatenate([w[0] for w in walks], axis=1)
+        zs = np.matmul(w2r, hs)
+        ys, un = Q.post_norm(xr, zs, gs, "silu", p["g1"], p["sc"], p["g2"], mask, eps)
+        return us, ts, walks, hs, zs, ys, un
+
+    us, ts, walks, hs, zs, ys, un = forward(xr, w1r, w2r, vr)
+    rs, is_, vs, gs = (ts[:, k * c:(k + 1) * c] for k in range(4))
+    p = Q.post_norm_bwd(dyr, dur, ys, zs, gs, "silu", vr["g1"], vr["sc"], vr["g2"], mask, eps)
+    dhs = np.matmul(w2r.T, p["dz"])
+    b = [Q.recurrence_bwd(dhs[:, k * c:(k + 1) * c], None, rs, is_, vs, vr["lam"], mask,
+                          walks[k][2], rate, bool(k)) for k in range(2)]
+    dts = np.concatenate([b[0][k] + b[1][k] for k in ("dr", "di", "dx")] + [p["dg"]], axis=1)
+    more, dg0 = Q.pre_norm_bwd(np.matmul(w1r.T, dts), xr, vr["g0"], mask, eps)
+    want = dict(y=ys, u=un, dx=p["dx"] + more, dw1=np.matmul(dts, us.swapaxes(1, 2)).sum(0),
+                dw2=np.matmul(p["dz"], hs.swapaxes(1, 2)).sum(0), dg0=dg0, dg1=p["dgamma"],
+                dsc=p["dscale"], dg2=p["dgamma_next"], dlam=b[0]["dlam"] + b[1]["dlam"])
+    got = dict(y=y, u=u, dx=dx, dw1=dw1, dw2=dw2, **d)
+    for name in want:
+        e = U.rel(U.f64(got[name]), want[name])
+        print(name, e, flush=True)
+        # the stated tolerances of the composites: 1e-4 in float32, 2e-2 in bfloat16
+        assert e <= U.TOL[dt], (name, e)
+    if dt == "f32":
+        def value(*s):
+            o = forward(*s[:3], dict(zip(("g0", "g1", "sc", "g2", "lam"), s[3:])))
+            return float((o[5] * dyr).sum() + (o[6] * dur).sum())
+        args = [xr, w1r, w2r] + [vr[k] for k in ("g0", "g1", "sc", "g2", "lam")]
+        for k, name in enumerate(("dx", "dw1", "dw2", "dg0", "dg1", "dsc", "dg2", "dlam")):
+            e = tuple(np.unravel_index(int(np.argmax(np.abs(want[name]))), want[name].shape))
+            s = [a.copy() for a in args]
+            s[k][e] += 1e-5
+            up = value(*s)
+            s[k][e] -= 2e-5
+            diff = (up - value(*s)) / 2e-5
+            assert float(U.f64(got[name])[e]) == pytest.approx(diff, rel=1e-3), name

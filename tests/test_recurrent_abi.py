@@ -1,0 +1,194 @@
+"""The recurrent block's calls refuse what they do not take, on the host, before
+anything is enqueued; sizes follow the descriptor."""
+import ctypes
+
+import pytest
+
+from paper_2104_05035_amd import rat3d as R
+
+FAKE = 0x100000  # aligned, never read: every call here is refused first
+BAD = ctypes.c_size_t(-1).value
+BIG = 1 << 44
+
+
+def _refused(status, f, *a):
+    with pytest.raises(R.Rat3dError) as e:
+        f(*a, stream=0)
+    assert e.value.status == status
+    assert str(e.value).split(": ", 1)[1]
+
+
+def _apart(k):
+    """k addresses that no two tensors of these tests share."""
+    return [FAKE * (i + 1) for i in range(k)]
+
+
+def _with(args, at, value):
+    return args[:at] + [value] + args[at + 1:]
+
+
+def _norm(**kw):
+    d = dict(n=2, c=24, v=60, dtype=R.BF16, gate=R.GATE_SILU)
+    d.update(kw)
+    return R.norm_desc(**d)
+
+
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n=0), R.EINVAL), (dict(c=0), R.EINVAL), (dict(v=0), R.EINVAL), (dict(v=-4), R.EINVAL),
+    (dict(gate=3), R.EINVAL), (dict(gate=-1), R.EINVAL), (dict(eps=0.0), R.EINVAL),
+    (dict(eps=1e-40), R.EINVAL), (dict(eps=-1.0), R.EINVAL), (dict(eps=NAN), R.EINVAL),
+    (dict(eps=INF), R.EINVAL), (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(dtype=9), R.EUNSUPPORTED),
+    (dict(c=(1 << 20) + 1), R.EUNSUPPORTED), (dict(v=(1 << 36) + 1), R.EUNSUPPORTED),
+    (dict(c=1 << 20, v=1 << 36), R.EUNSUPPORTED), (dict(x_stride=24 * 60 - 1), R.EINVAL),
+    (dict(z_stride=1), R.EINVAL), (dict(g_stride=-1), R.EINVAL), (dict(y_stride=5), R.EINVAL),
+    (dict(u_stride=1 << 60), R.EINVAL),
+])
+def test_norm_descriptor(kw, status):
+    d = _norm(**kw)
+    assert R.rat3d_norm_workspace_size(d) == BAD
+    p = _apart(15)
+    _refused(status, R.rat3d_pre_norm_fwd, d, *p[:2], None, p[2])
+    _refused(status, R.rat3d_pre_norm_bwd, d, *p[:3], None, *p[3:6], 0, FAKE, BIG)
+    _refused(status, R.rat3d_post_norm_fwd, d, *p[:6], None, *p[6:8])
+    _refused(status, R.rat3d_post_norm_bwd, d, *p[:8], None, *p[8:14], 0, FAKE, BIG)
+
+
+def test_norm_pointers():
+    d = _norm()
+    need = R.rat3d_norm_workspace_size(d)
+    assert 0 < need < BAD
+    p = _apart(16)
+    ws = p[15]
+    pre = [p[0], p[1], None, p[2]]
+    for i in (0, 1, 3):
+        _refused(R.EINVAL, R.rat3d_pre_norm_fwd, d, *_with(pre, i, None))
+        _refused(R.EALIGN, R.rat3d_pre_norm_fwd, d, *_with(pre, i, FAKE + 1))
+    _refused(R.EALIGN, R.rat3d_pre_norm_fwd, d, *_with(pre, 1, FAKE + 2))
+    bwd = [p[0], p[1], p[2], None, p[3], p[4], p[5]]  # du, x, gamma, mask, dres, dx, dgamma
+    for i in (0, 1, 2, 5, 6):
+        _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, i, None), 0, ws, need)
+    for i in (0, 1, 2, 4, 5, 6):
+        _refused(R.EALIGN, R.rat3d_pre_norm_bwd, d, *_with(bwd, i, p[i] + 1), 0, ws, need)
+    _refused(R.EWORKSPACE, R.rat3d_pre_norm_bwd, d, *bwd, 0, ws, need - 1)
+    _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *bwd, 0, None, need)
+    _refused(R.EALIGN, R.rat3d_pre_norm_bwd, d, *bwd, 0, ws + 8, need)
+    post = p[:6] + [None] + p[6:8]  # x, z, g, gamma, scale, gamma_next, mask, y, u
+    for i in (0, 1, 2, 3, 7, 8):
+        _refused(R.EINVAL, R.rat3d_post_norm_fwd, d, *_with(post, i, None))
+    for i in (0, 1, 2, 3, 4, 5, 7, 8):
+        _refused(R.EALIGN, R.rat3d_post_norm_fwd, d, *_with(post, i, post[i] + 1))
+    # dy, du, y, z, g, gamma, scale, gamma_next, mask, dx, dz, dg, dgamma, dscale, dgamma_next
+    back = p[:8] + [None] + p[8:14]
+    for i in (0, 1, 2, 3, 4, 5, 9, 10, 11, 12, 14):
+        _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, i, None), 0, ws, need)
+    for i in (0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11, 12, 13, 14):
+        _refused(R.EALIGN, R.rat3d_post_norm_bwd, d, *_with(back, i, back[i] + 1), 0, ws, need)
+    _refused(R.EWORKSPACE, R.rat3d_post_norm_bwd, d, *back, 0, ws, need - 1)
+
+
+def test_norm_overlaps():
+    """A result over an input is that input, or lies nowhere in it; results are apart."""
+    d = _norm()
+    held = 24 * 60 * 2
+    need = R.rat3d_norm_workspace_size(d)
+    p = _apart(16)
+    ws = p[15]
+    for off in (2, held - 2, -2, held * 2 - 2, 2 - held * 2):
+        _refused(R.EINVAL, R.rat3d_pre_norm_fwd, d, p[0], p[1], None, p[0] + off)
+    _refused(R.EINVAL, R.rat3d_pre_norm_fwd, _norm(u_stride=24 * 60 + 1), p[0], p[1], None, p[0])
+    post = p[:6] + [None] + p[6:8]
+    _refused(R.EINVAL, R.rat3d_post_norm_fwd, d, *_with(post, 8, post[7]))  # u over y
+    _refused(R.EINVAL, R.rat3d_post_norm_fwd, d, *_with(post, 8, post[7] + held))
+    for i in (0, 1, 2):
+        _refused(R.EINVAL, R.rat3d_post_norm_fwd, d, *_with(post, 7, post[i] + held))
+    back = p[:8] + [None] + p[8:14]
+    for i, k in ((9, 10), (9, 11), (10, 11), (12, 13), (12, 14), (13, 14), (12, 5), (13, 6),
+                 (14, 7), (12, 6)):
+        _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, i, back[k]), 0, ws, need)
+        _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, i, back[k] + 4), 0, ws, need)
+    for k in (0, 1, 2, 3, 4):
+        _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, 10, back[k] + 2), 0, ws, need)
+    bwd = [p[0], p[1], p[2], None, p[3], p[4], p[5]]
+    _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, 6, p[2] + 4), 0, ws, need)
+    for k in (0, 1, 4):
+        _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, 5, bwd[k] + 2), 0, ws, need)
+
+
+def _rec(**kw):
+    d = dict(n=2, c=24, length=60, dtype=R.BF16)
+    d.update(kw)
+    return R.recurrence_desc(**d)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(n=0), R.EINVAL), (dict(c=0), R.EINVAL), (dict(length=0), R.EINVAL),
+    (dict(length=-1), R.EINVAL), (dict(rate=0.0), R.EINVAL), (dict(rate=-8.0), R.EINVAL),
+    (dict(rate=NAN), R.EINVAL), (dict(rate=INF), R.EINVAL), (dict(rate=1e7), R.EINVAL),
+    (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(n=1 << 20, c=4), R.EUNSUPPORTED),
+    (dict(length=(1 << 38) + 1), R.EUNSUPPORTED), (dict(c=1 << 20, length=1 << 36), R.EUNSUPPORTED),
+    (dict(r_stride=24 * 60 - 1), R.EINVAL), (dict(i_stride=-2), R.EINVAL),
+    (dict(x_stride=1), R.EINVAL), (dict(y_stride=7), R.EINVAL),
+])
+def test_recurrence_descriptor(kw, status):
+    d = _rec(**kw)
+    assert R.rat3d_recurrence_carry_size(d) == BAD
+    for i in (0, 1):
+        assert R.rat3d_recurrence_workspace_size(d, i) == BAD
+    p = _apart(13)
+    _refused(status, R.rat3d_recurrence_fwd, d, *p[:4], None, *p[4:8], p[8], BIG)
+    _refused(status, R.rat3d_recurrence_bwd, d, *p[:6], None, *p[6:12], 0, p[12], BIG)
+
+
+def test_recurrence_pointers():
+    d = _rec()
+    need = [R.rat3d_recurrence_workspace_size(d, i) for i in (0, 1)]
+    assert need[1] < BAD and R.rat3d_recurrence_workspace_size(d, 2) == BAD
+    assert R.rat3d_recurrence_carry_size(d) >= 4 * 2 * 24
+    p = _apart(14)
+    ws = p[13]
+    fwd = p[:4] + [None] + p[4:8]  # r, i, x, lambda, mask, h0, y, h_last, carry
+    for i in (0, 1, 2, 3, 6):
+        _refused(R.EINVAL, R.rat3d_recurrence_fwd, d, *_with(fwd, i, None), ws, need[0])
+    for i in (0, 1, 2, 3, 5, 6, 7, 8):
+        _refused(R.EALIGN, R.rat3d_recurrence_fwd, d, *_with(fwd, i, fwd[i] + 1), ws, need[0])
+    # dy, dh_last, r, i, x, lambda, mask, carry, dr, di, dx, dlambda, dh0
+    bwd = p[:6] + [None] + p[6:12]
+    for i in (0, 2, 3, 4, 5, 7, 8, 9, 10, 11):
+        _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(bwd, i, None), 0, ws, need[1])
+    for i in (0, 1, 2, 3, 4, 5, 7, 8, 9, 10, 11, 12):
+        _refused(R.EALIGN, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[i] + 1), 0, ws, need[1])
+    _refused(R.EWORKSPACE, R.rat3d_recurrence_bwd, d, *bwd, 0, ws, need[1] - 1)
+    _refused(R.EALIGN, R.rat3d_recurrence_bwd, d, *bwd, 0, ws + 4, need[1])
+
+
+def test_recurrence_overlaps():
+    d = _rec()
+    held = 24 * 60 * 2
+    p = _apart(14)
+    ws = p[13]
+    fwd = p[:4] + [None] + p[4:8]
+    for i in (0, 1, 2):
+        for off in (2, -held, held):
+            _refused(R.EINVAL, R.rat3d_recurrence_fwd, d, *_with(fwd, 6, fwd[i] + off), ws, BIG)
+    for i, k, off in ((7, 5, 4), (7, 3, 0), (8, 5, 0), (8, 3, 0), (7, 8, 0), (7, 8, 4)):
+        _refused(R.EINVAL, R.rat3d_recurrence_fwd, d, *_with(fwd, i, fwd[k] + off), ws, BIG)
+    bwd = p[:6] + [None] + p[6:12]
+    for i, k, off in ((8, 9, 0), (8, 10, 0), (9, 10, 0), (8, 9, held), (8, 0, 2), (9, 2, 2),
+                      (10, 3, held), (8, 4, -2), (11, 5, 0), (11, 12, 0), (11, 7, 0), (12, 7, 0),
+                      (12, 1, 4), (11, 1, 0), (12, 5, 4)):
+        _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[k] + off), 0, ws, BIG)
+    # the gates and values side by side in one tensor: ranges between one another's volumes
+    w = 3 * 24 * 60
+    d = _rec(r_stride=w, i_stride=w, x_stride=w)
+    side = [FAKE, FAKE + held, FAKE + 2 * held]
+    grads = [FAKE * 2, FAKE * 2 + held, FAKE * 2 + 2 * held]
+    bwd = [p[8], None] + side + [p[9], None, p[10]] + grads + [p[11], None]
+    for i in (8, 9, 10):
+        _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[i] + 2), 0, ws, BIG)
+        _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[i] - 2), 0, ws, BIG)
+    # as they are only the workspace is missing
+    need = R.rat3d_recurrence_workspace_size(d, 1)
+    _refused(R.EWORKSPACE, R.rat3d_recurrence_bwd, d, *bwd, 0, ws, need - 1)

@@ -13,8 +13,11 @@
 //
 // Layout: 16 lanes along the voxels, 16 bytes each, by groups of threads along the
 // channels, so a channel's row is read in pieces of 256 bytes; a group takes the
-// channels grp, grp + groups, ... Sums over a voxel's channels are joined by lane swaps
-// and through LDS.
+// channels grp, grp + groups, ... Up to 512 channels a thread keeps what it has read of
+// its channels (4, or 8 of half as many voxels) in registers, so every tensor passes
+// once; beyond, each sum reads its tensors again.  Sums over a voxel's channels are
+// joined by lane swaps that leave each of a wave's four groups a quarter of the voxels,
+// and through LDS.  Rows need no alignment.
 // Bound: HBM.
 #include <type_traits>
 
@@ -34,7 +37,7 @@ struct NormArgs {
     void *oy, *ou, *dx, *dz, *dg;
     const float *gamma, *scale, *next;
     const uint8_t* mask;
-    float* part;  // [workgroup][gain][channel]
+    float* part;  // [gain][channel][workgroup]
     int64_t sx, sz, sg, sy, su;  // from one volume to the next
     int64_t V;
     int c, groups, tiles, gate;  // tiles of one volume
@@ -42,244 +45,411 @@ struct NormArgs {
     float eps;
 };
 
-// Sum over a voxel's channels of K values of each token: the four groups of a wave by
-// lane swaps that leave every group a quarter of the tokens, the waves through LDS.
+// Half of a wave's rows of 16 lanes get x of their and the neighbouring row (or half of
+// the wave) added, the others y.
+__device__ __forceinline__ float join32(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(y), false,
+                                                    false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ float join16(float x, float y) {
+    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(y), false,
+                                                    false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Sums over a voxel's channels of K values of each token, to all of the voxel's threads:
+// in a wave, then through LDS [value][wave][lane][token].
 template <int TOK, int K>
 __device__ __forceinline__ void channel_sums(float (&s)[K][TOK], float* lds, int waves) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, at = lane & 15, row = lane >> 4;
 #pragma unroll
     for (int k = 0; k < K; ++k) {
+        float* to = lds + ((k * waves + wave) * kLanes + at) * TOK;
+        if constexpr (TOK == 1) {
+            const float h = join32(s[k][0], s[k][0]);
+            const float v = join16(h, h);
+            if (row == 0) *to = v;
+        } else {
+            constexpr int PART = TOK / 4;  // tokens that one group of a wave sums up
+            float h[TOK / 2];
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) {
-            s[k][j] += __shfl_xor(s[k][j], 16);
-            s[k][j] += __shfl_xor(s[k][j], 32);
-        }
-        if (lane < kLanes) {
+            for (int j = 0; j < TOK / 2; ++j) h[j] = join32(s[k][j], s[k][TOK / 2 + j]);
+            // rows 0 and 1 keep the first half of the tokens, rows 0 and 2 its first half
+            to += (row >> 1) * (TOK / 2) + (row & 1) * PART;
 #pragma unroll
-            for (int j = 0; j < TOK; ++j) lds[((wave * K + k) * kLanes + at) * TOK + j] = s[k][j];
+            for (int j = 0; j < PART; ++j) to[j] = join16(h[j], h[PART + j]);
         }
     }
     __syncthreads();
 #pragma unroll
-    for (int k = 0; k < K; ++k)
+    for (int k = 0; k < K; ++k) {
+        const float* from = lds + (k * waves * kLanes + at) * TOK;
 #pragma unroll
-        for (int j = 0; j < TOK; ++j) s[k][j] = 0.f;
-    for (int w = 0; w < waves; ++w)
+        for (int j = 0; j < TOK; ++j) s[k][j] = from[j];
+        for (int w = 1; w < waves; ++w)
 #pragma unroll
-        for (int k = 0; k < K; ++k)
-#pragma unroll
-            for (int j = 0; j < TOK; ++j) s[k][j] += lds[((w * K + k) * kLanes + at) * TOK + j];
+            for (int j = 0; j < TOK; ++j) s[k][j] += from[w * kLanes * TOK + j];
+    }
 }
 
 __device__ __forceinline__ float rsqrt_of(float sum, float inv_c, float eps) {
     return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_c, eps));
 }
 
-template <typename T, int TOK, NormMode MODE, bool GATED, bool NEXT>
-__global__ __launch_bounds__(256) void block_norm_k(NormArgs a) {
+// A thread's tokens of one channel, as they lie.
+template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Words {
+    typename std::conditional<TOK * sizeof(T) < 4, uint16_t, uint32_t>::type
+        w[TOK * sizeof(T) < 4 ? 1 : TOK * sizeof(T) / 4];
+};
+template <typename T, int TOK> struct Toks {
+    Words<T, TOK> u;
+    __device__ __forceinline__ float operator[](int j) const {
+        if constexpr (sizeof(T) == 4) return __uint_as_float(u.w[j]);
+        else if constexpr (TOK == 1) return Elt<T>::from_bits(u.w[0]);
+        else return __uint_as_float(j & 1 ? u.w[j / 2] & 0xffff0000u : u.w[j / 2] << 16);
+    }
+    // The tokens at p, or without ALL, where p is `over` tokens (0 .. TOK) before its place
+    // so that none lies behind the row's end, those from `over` on.
+    template <bool ALL> __device__ __forceinline__ void load(const T* p, int over) {
+        u = *reinterpret_cast<const Words<T, TOK>*>(p);
+        if constexpr (!ALL && TOK > 1) {
+            constexpr int N = TOK * sizeof(T) / 4;
+            const int words = over * (int)sizeof(T) / 4;
+#pragma unroll
+            for (int m = N; m >= 1; m >>= 1)
+#pragma unroll
+                for (int i = 0; i < N; ++i) u.w[i] = words & m ? (i + m < N ? u.w[i + m] : 0u) : u.w[i];
+            if constexpr (sizeof(T) == 2) {
+                const uint32_t bits = over & 1 ? 16u : 0u;
+#pragma unroll
+                for (int i = 0; i < N; ++i)
+                    u.w[i] = __builtin_amdgcn_alignbit(i + 1 < N ? u.w[i + 1] : 0u, u.w[i], bits);
+            }
+        }
+    }
+};
+template <typename T, int TOK, bool ALL>
+__device__ __forceinline__ void put_tokens(T* p, int left, const float (&o)[TOK]) {
+    if (ALL || left == TOK) {
+        Words<T, TOK> u;
+#pragma unroll
+        for (int j = 0; j < TOK; j += 4 / (int)sizeof(T)) {
+            if constexpr (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
+            else if constexpr (TOK == 1) u.w[0] = Elt<T>::to_bits(o[0]);
+            else u.w[j / 2] = pack_bf16x2(o[j], o[j + 1]);
+        }
+        *reinterpret_cast<Words<T, TOK>*>(p) = u;
+    } else {
+#pragma unroll
+        for (int j = 0; j < TOK; ++j)
+            if (j < left) Elt<T>::st(p + j, o[j]);
+    }
+}
+
+// PC: channels a thread, held in registers, c <= PC * groups; 0: any number, read again
+// for every sum.
+template <typename T, int TOK, int PC, NormMode MODE, bool GATED, bool NEXT, int THREADS>
+__global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr bool kPost = MODE == POST_FWD || MODE == POST_BWD;
-    constexpr int TILE = kLanes * TOK;
-    __shared__ float lds[2][4 * 3 * kLanes * TOK];
+    constexpr bool kNext = kBwd ? MODE == PRE_BWD || NEXT : NEXT;  // a norm of y
+    constexpr int TILE = kLanes * TOK, NP = PC ? PC : 1;
+    constexpr int K = !kBwd ? 1 : kNext && kPost ? 3 : kNext ? 2 : 1;
+    typedef Toks<T, TOK> V;
+    __shared__ float lds[2][K * (THREADS / 64) * kLanes * TOK];
     const int at = threadIdx.x & 15, grp = threadIdx.x >> 4;
     const int waves = (a.groups * kLanes + 63) >> 6;
+    const int rounds = PC ? 1 : (a.c + a.groups - 1) / a.groups;
     const float inv_c = 1.f / (float)a.c;
+    const float* gn = MODE == PRE_BWD ? a.gamma : a.next;
 
-    for (int64_t t = blockIdx.x; t < a.all; t += gridDim.x) {
-        const int64_t vol = t / a.tiles;
-        const int64_t t0 = (t - vol * a.tiles) * TILE + at * TOK;
-        const int left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
-        uint32_t on = (1u << left) - 1u;
-        if (a.mask)
+    double sum_n[NP], sum_t[NP];  // PC: the gains' gradients over this workgroup's tiles
 #pragma unroll
-            for (int j = 0; j < TOK; ++j)
-                if (j < left && !a.mask[vol * a.V + t0 + j]) on &= ~(1u << j);
-        auto rd = [&](const void* p, int64_t stride, int ch, float (&o)[TOK], bool live) {
-            const T* q = (const T*)p + vol * stride + (int64_t)ch * a.V + t0;
+    for (int p = 0; p < NP; ++p) sum_n[p] = sum_t[p] = 0.0;
+    auto put_gain = [&](int which, int ch, double v, bool more) {
 #pragma unroll
-            for (int j = 0; j < TOK; ++j)
-                o[j] = (live ? on >> j & 1u : j < left) ? Elt<T>::ld(q + j) : 0.f;
-        };
-        auto wr = [&](void* p, int64_t stride, int ch, const float (&o)[TOK]) {
-            T* q = (T*)p + vol * stride + (int64_t)ch * a.V + t0;
-#pragma unroll
-            for (int j = 0; j < TOK; ++j)
-                if (j < left) Elt<T>::st(q + j, o[j]);
-        };
-        // the gate's value and slope
-        auto gate = [&](float g, float& phi, float& slope) {
-            const Sig sg(g);
-            phi = a.gate == RAT3D_GATE_SILU ? g * sg.s : sg.s;
-            slope = a.gate == RAT3D_GATE_SILU ? sg.s * (1.f + g * sg.rest) : sg.s * sg.rest;
-        };
-        auto gain = [&](int ch) { return a.gamma[ch] * (a.scale ? a.scale[ch] : 1.f); };
-        float s[3][TOK], e[1][TOK];
-#pragma unroll
-        for (int j = 0; j < TOK; ++j) s[0][j] = s[1][j] = s[2][j] = e[0][j] = 0.f;
-
-        if constexpr (MODE == PRE_FWD) {
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float x[TOK];
-                rd(a.x, a.sx, ch, x, true);
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) e[0][j] += x[j] * x[j];
-            }
-            channel_sums(e, lds[0], waves);
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float x[TOK];
-                rd(a.x, a.sx, ch, x, true);
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) x[j] *= rsqrt_of(e[0][j], inv_c, a.eps) * a.gamma[ch];
-                wr(a.ou, a.su, ch, x);
-            }
+        for (int m = 8; m >= 1; m >>= 1) v += __shfl_xor(v, m);
+        if (at == 0 && ch < a.c) {
+            float* to = a.part + ((int64_t)which * a.c + ch) * gridDim.x + blockIdx.x;
+            *to = more ? *to + (float)v : (float)v;
         }
-        if constexpr (MODE == POST_FWD) {
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float z[TOK];
-                rd(a.z, a.sz, ch, z, true);
+    };
+
+    auto tile = [&](int64_t t, int64_t vol, int64_t first, auto all_) {
+        constexpr bool kAll = decltype(all_)::value;  // every token and channel is there
+        const int64_t t0 = first + at * TOK;
+        int left = TOK, over = 0;
+        uint32_t live = (1u << TOK) - 1u;
+        if (!kAll) {
+            left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
+            over = TOK - left;
+            live = (1u << left) - 1u;
+            if (a.mask)
 #pragma unroll
-                for (int j = 0; j < TOK; ++j) e[0][j] += z[j] * z[j];
+                for (int j = 0; j < TOK; ++j)
+                    if (j < left && !a.mask[vol * a.V + t0 + j]) live &= ~(1u << j);
+        }
+        // where the thread's tokens of its first channel lie, from its last row's end
+        // counted back where they do not fill it
+        const int64_t at0 = kAll || left == TOK ? t0 : a.V - TOK;
+        const int64_t step = (int64_t)a.groups * a.V;
+        V X[NP], Z[NP], G[NP], Y[NP], DU[NP];  // backward: X is dy (before a block dres)
+        uint32_t on[NP];
+        int ch[NP];
+        auto load = [&](int k) {
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                const int c = grp + (k + p) * a.groups;
+                ch[p] = c;
+                on[p] = c < a.c ? live : 0u;
             }
-            channel_sums(e, lds[0], waves);
-            float rz[TOK];
+            auto get = [&](V(&to)[NP], const void* q, int64_t stride) {
+                const T* from = (const T*)q + vol * stride + at0;
 #pragma unroll
-            for (int j = 0; j < TOK; ++j) rz[j] = rsqrt_of(e[0][j], inv_c, a.eps);
-            auto value = [&](int ch, float (&y)[TOK]) {
-                float z[TOK], g[TOK];
-                rd(a.z, a.sz, ch, z, true);
-                if (GATED) rd(a.g, a.sg, ch, g, true);
-                rd(a.x, a.sx, ch, y, false);
-                const float k = gain(ch);
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) {
-                    float phi = 1.f, slope;
-                    if (GATED) gate(g[j], phi, slope);
-                    if (on >> j & 1u) y[j] += k * phi * (z[j] * rz[j]);
-                }
+                for (int p = 0; p < NP; ++p)
+                    to[p].template load<kAll>(
+                        from + (kAll ? grp * a.V + (k + p) * step : (int64_t)(ch[p] < a.c ? ch[p] : a.c - 1) * a.V),
+                        over);
             };
-            if (NEXT) {
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) e[0][j] = 0.f;
-                for (int ch = grp; ch < a.c; ch += a.groups) {
-                    float y[TOK];
-                    value(ch, y);
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j) e[0][j] += on >> j & 1u ? y[j] * y[j] : 0.f;
-                }
-                channel_sums(e, lds[1], waves);
+            if (kBwd && kNext) {
+                get(Y, a.y, a.sy);
+                get(DU, a.du, a.su);
             }
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float y[TOK];
-                value(ch, y);
-                wr(a.oy, a.sy, ch, y);
-                if (NEXT) {
+            if (kPost) get(Z, a.z, a.sz);
+            if (GATED) get(G, a.g, a.sg);
+            if (!kBwd) get(X, a.x, a.sx);
+            else if (MODE == POST_BWD) get(X, a.dy, a.sy);
+            else if (a.dy) get(X, a.dy, a.sx);
+        };
+        // a masked token's value is 0, whatever it holds
+        auto val = [&](const V& v, int p, int j) { return kAll || on[p] >> j & 1u ? v[j] : 0.f; };
+        auto put = [&](void* q, int64_t stride, int p, const float (&o)[TOK]) {
+            if (kAll || ch[p] < a.c)
+                put_tokens<T, TOK, kAll>((T*)q + vol * stride + (int64_t)ch[p] * a.V + t0, left, o);
+        };
+        // What is formed from a held value is formed again behind a barrier, not held too:
+        // the registers are what limits the waves.
+        auto forget = [&](V& v) {
 #pragma unroll
-                    for (int j = 0; j < TOK; ++j)
-                        y[j] = on >> j & 1u ? y[j] * rsqrt_of(e[0][j], inv_c, a.eps) * a.next[ch] : 0.f;
-                    wr(a.ou, a.su, ch, y);
+            for (auto& w : v.u.w) asm volatile("" : "+v"(w));
+        };
+        auto again = [&]() {
+            if (PC == 0) return;
+#pragma unroll
+            for (int p = 0; p < NP; ++p) {
+                if (kBwd && kNext) {
+                    forget(Y[p]);
+                    forget(DU[p]);
+                }
+                if (kPost) forget(Z[p]);
+                if (GATED) forget(G[p]);
+                forget(X[p]);
+            }
+        };
+        // all of the thread's channels
+        auto each = [&](auto f) {
+            for (int k = 0; k < rounds; ++k) {
+                if (!PC) load(k);
+#pragma unroll
+                for (int p = 0; p < NP; ++p) {
+                    f(p);
+                    __builtin_amdgcn_sched_barrier(0);  // a channel's registers for the next
                 }
             }
-        }
-        if constexpr (kBwd) {
-            constexpr bool kNext = MODE == PRE_BWD || NEXT;
-            const float* gn = MODE == PRE_BWD ? a.gamma : a.next;
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float y[TOK], du[TOK], z[TOK];
-                if (kNext) {
-                    rd(a.y, a.sy, ch, y, true);
-                    rd(a.du, a.su, ch, du, true);
-                }
-                if (kPost) rd(a.z, a.sz, ch, z, true);
+        };
+        auto of = [&](const float* v, int p) { return v[kAll || ch[p] < a.c ? ch[p] : 0]; };
+        auto gain = [&](int p) { return of(a.gamma, p) * (a.scale ? of(a.scale, p) : 1.f); };
+        // the gate's value and slope
+        auto gate = [&](int p, int j, float& phi, float& slope) {
+            phi = 1.f;
+            slope = 0.f;
+            if (GATED) {
+                const float g = val(G[p], p, j);
+                const Sig sg(g);
+                phi = a.gate == RAT3D_GATE_SILU ? g * sg.s : sg.s;
+                slope = sg.s * (a.gate == RAT3D_GATE_SILU ? 1.f + g * sg.rest : sg.rest);
+            }
+        };
+        if (PC) load(0);
+        float s[K][TOK], e[1][TOK];
+        auto clear = [&](auto& v) {
+            for (auto& row : v)
+                for (float& x : row) x = 0.f;
+        };
+
+        if constexpr (!kBwd) {
+            clear(e);
+            each([&](int p) {
 #pragma unroll
                 for (int j = 0; j < TOK; ++j) {
-                    if (kNext) {
-                        s[0][j] += y[j] * y[j];
-                        s[1][j] += gn[ch] * du[j] * y[j];
+                    const float v = val(kPost ? Z[p] : X[p], p, j);
+                    e[0][j] += v * v;
+                }
+            });
+            channel_sums(e, lds[0], waves);
+            again();
+            float r[TOK];
+#pragma unroll
+            for (int j = 0; j < TOK; ++j) r[j] = rsqrt_of(e[0][j], inv_c, a.eps);
+            if constexpr (MODE == PRE_FWD) {
+                each([&](int p) {
+                    const float k = of(a.gamma, p);
+                    float u[TOK];
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) u[j] = k * (val(X[p], p, j) * r[j]);
+                    put(a.ou, a.su, p, u);
+                });
+            } else {
+                auto value = [&](int p, float (&y)[TOK]) {
+                    const float k = gain(p);
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) {
+                        float phi, slope;
+                        gate(p, j, phi, slope);
+                        const float b = k * phi * (val(Z[p], p, j) * r[j]);
+                        y[j] = X[p][j] + (kAll || on[p] >> j & 1u ? b : 0.f);
                     }
-                    if (kPost) s[2][j] += z[j] * z[j];
+                };
+                if constexpr (!NEXT) {
+                    each([&](int p) {
+                        float y[TOK];
+                        value(p, y);
+                        put(a.oy, a.sy, p, y);
+                    });
+                } else {
+                    clear(e);
+                    each([&](int p) {
+                        float y[TOK];
+                        value(p, y);
+#pragma unroll
+                        for (int j = 0; j < TOK; ++j) {
+                            const float v = kAll || on[p] >> j & 1u ? y[j] : 0.f;
+                            e[0][j] += v * v;
+                        }
+                    });
+                    channel_sums(e, lds[1], waves);
+                    again();
+                    float ry[TOK];
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) ry[j] = rsqrt_of(e[0][j], inv_c, a.eps);
+                    each([&](int p) {
+                        float y[TOK];
+                        value(p, y);
+                        put(a.oy, a.sy, p, y);
+                        const float k = of(a.next, p);
+#pragma unroll
+                        for (int j = 0; j < TOK; ++j)
+                            y[j] = kAll || on[p] >> j & 1u ? k * (y[j] * ry[j]) : 0.f;
+                        put(a.ou, a.su, p, y);
+                    });
                 }
             }
+        } else {
+            clear(s);
+            each([&](int p) {
+                const float k = kNext ? of(gn, p) : 0.f;
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) {
+                    if constexpr (kPost) {
+                        const float z = val(Z[p], p, j);
+                        s[0][j] += z * z;
+                    }
+                    if constexpr (kNext) {
+                        const float y = val(Y[p], p, j);
+                        s[K - 2][j] += y * y;
+                        s[K - 1][j] += k * val(DU[p], p, j) * y;
+                    }
+                }
+            });
             channel_sums(s, lds[0], waves);
+            again();
             float ry[TOK], my[TOK], rz[TOK], mz[TOK];
 #pragma unroll
             for (int j = 0; j < TOK; ++j) {
-                ry[j] = rsqrt_of(s[0][j], inv_c, a.eps);
-                my[j] = s[1][j] * inv_c * (ry[j] * ry[j]);
-                rz[j] = rsqrt_of(s[2][j], inv_c, a.eps);
-            }
-            // dY, and what it leaves to the branch (0 where masked)
-            auto residual = [&](int ch, float (&dY)[TOK], float (&du)[TOK], float (&y)[TOK]) {
-                if (a.dy) rd(a.dy, MODE == PRE_BWD ? a.sx : a.sy, ch, dY, false);
-                else
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j) dY[j] = 0.f;
-                if (kNext) {
-                    rd(a.y, a.sy, ch, y, true);
-                    rd(a.du, a.su, ch, du, true);
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j)
-                        if (on >> j & 1u) dY[j] += ry[j] * (gn[ch] * du[j] - y[j] * my[j]);
+                if constexpr (kNext) {
+                    ry[j] = rsqrt_of(s[K - 2][j], inv_c, a.eps);
+                    my[j] = s[K - 1][j] * inv_c * (ry[j] * ry[j]);
                 }
+                if constexpr (kPost) rz[j] = rsqrt_of(s[0][j], inv_c, a.eps);
+            }
+            // dY
+            auto total = [&](int p, int j, float k) {
+                float d = MODE == POST_BWD || a.dy ? X[p][j] : 0.f;
+                if constexpr (kNext)
+                    if (kAll || on[p] >> j & 1u)
+                        d += ry[j] * (k * DU[p][j] - Y[p][j] * my[j]);
+                return d;
             };
-            if (kPost) {
-                for (int ch = grp; ch < a.c; ch += a.groups) {
-                    float dY[TOK], du[TOK], y[TOK], z[TOK], g[TOK];
-                    residual(ch, dY, du, y);
-                    rd(a.z, a.sz, ch, z, true);
-                    if (GATED) rd(a.g, a.sg, ch, g, true);
-                    const float k = gain(ch);
+            if constexpr (kPost) {
+                clear(e);
+                each([&](int p) {
+                    const float k = kNext ? of(gn, p) : 0.f, w = gain(p);
 #pragma unroll
                     for (int j = 0; j < TOK; ++j) {
-                        float phi = 1.f, slope;
-                        if (GATED) gate(g[j], phi, slope);
-                        if (on >> j & 1u) e[0][j] += dY[j] * k * phi * z[j];
+                        float phi, slope;
+                        gate(p, j, phi, slope);
+                        const float d = total(p, j, k);
+                        e[0][j] += (kAll || on[p] >> j & 1u ? d : 0.f) * w * phi * val(Z[p], p, j);
                     }
-                }
+                });
                 channel_sums(e, lds[1], waves);
+                again();
 #pragma unroll
                 for (int j = 0; j < TOK; ++j) mz[j] = e[0][j] * inv_c * (rz[j] * rz[j]);
             }
-            for (int ch = grp; ch < a.c; ch += a.groups) {
-                float dY[TOK], du[TOK], y[TOK];
-                residual(ch, dY, du, y);
-                float sum_n = 0.f, sum_t = 0.f;
-                if (kNext) {
+            each([&](int p) {
+                const float k = kNext ? of(gn, p) : 0.f;
+                float dY[TOK], n = 0.f, q = 0.f;
 #pragma unroll
-                    for (int j = 0; j < TOK; ++j) sum_n += du[j] * y[j] * ry[j];
+                for (int j = 0; j < TOK; ++j) {
+                    dY[j] = total(p, j, k);
+                    if constexpr (kNext) n += val(DU[p], p, j) * (val(Y[p], p, j) * ry[j]);
                 }
-                if (kPost) {
-                    float z[TOK], g[TOK], dz[TOK], dg[TOK];
-                    rd(a.z, a.sz, ch, z, true);
-                    if (GATED) rd(a.g, a.sg, ch, g, true);
-                    const float k = gain(ch);
+                if constexpr (kPost) {
+                    const float w = gain(p);
+                    float dz[TOK], dg[TOK];
 #pragma unroll
                     for (int j = 0; j < TOK; ++j) {
-                        float phi = 1.f, slope = 0.f;
-                        if (GATED) gate(g[j], phi, slope);
-                        const float d = on >> j & 1u ? dY[j] : 0.f, zr = z[j] * rz[j];
-                        sum_t += d * phi * zr;
-                        dz[j] = rz[j] * (d * k * phi - z[j] * mz[j]);
-                        dg[j] = d * k * zr * slope;
+                        float phi, slope;
+                        gate(p, j, phi, slope);
+                        const float z = val(Z[p], p, j), zr = z * rz[j];
+                        const float d = kAll || on[p] >> j & 1u ? dY[j] : 0.f;
+                        q += d * phi * zr;
+                        dz[j] = rz[j] * (d * w * phi - z * mz[j]);
+                        dg[j] = d * w * zr * slope;
                     }
-                    wr(a.dz, a.sz, ch, dz);
-                    if (GATED) wr(a.dg, a.sg, ch, dg);
+                    put(a.dz, a.sz, p, dz);
+                    if (GATED) put(a.dg, a.sg, p, dg);
                 }
-                if (a.dx) wr(a.dx, a.sx, ch, dY);
-                // gains: over the lanes, then this workgroup's tiles
-#pragma unroll
-                for (int m = 8; m >= 1; m >>= 1) {
-                    sum_n += __shfl_xor(sum_n, m);
-                    sum_t += __shfl_xor(sum_t, m);
-                }
-                if (at == 0) {
-                    float* to = a.part + (int64_t)blockIdx.x * 2 * a.c;
+                if (MODE == PRE_BWD || kNext || a.dx) put(a.dx, a.sx, p, dY);
+                if constexpr (PC != 0) {
+                    sum_n[p] += (double)n;
+                    sum_t[p] += (double)q;
+                } else {
                     const bool more = t != blockIdx.x;
-                    if (kNext) to[ch] = more ? to[ch] + sum_n : sum_n;
-                    if (kPost) to[a.c + ch] = more ? to[a.c + ch] + sum_t : sum_t;
+                    if (kNext) put_gain(0, ch[p], (double)n, more);
+                    if (kPost) put_gain(1, ch[p], (double)q, more);
                 }
-            }
+            });
         }
-        __syncthreads();  // LDS is written again
+        // the first sums are written again only behind the barrier of the second, the
+        // second only behind that of the next first
+        if constexpr (!(kPost && (kBwd || NEXT))) __syncthreads();
+    };
+
+    for (int64_t t = blockIdx.x; t < a.all; t += gridDim.x) {
+        const int64_t vol = t / a.tiles, first = (t - vol * a.tiles) * TILE;
+        if (a.mask || first + TILE > a.V || a.c != NP * rounds * a.groups)
+            tile(t, vol, first, std::false_type{});
+        else tile(t, vol, first, std::true_type{});
+    }
+    if constexpr (kBwd && PC != 0) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            if (kNext) put_gain(0, grp + p * a.groups, sum_n[p], false);
+            if (kPost) put_gain(1, grp + p * a.groups, sum_t[p], false);
+        }
     }
 }
 
@@ -292,7 +462,7 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
     const int ch = blockIdx.x, which = blockIdx.y;  // 0: the norm read by du, 1: the branch's
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256)
-        s += (double)part[((int64_t)i * 2 + which) * c + ch];
+        s += (double)part[((int64_t)which * c + ch) * parts + i];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -312,8 +482,20 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 }
 
 // ------------------------------------------------------------------ host
+// Tokens and channels a thread: 16 bytes of 4 channels up to 256 of them, 8 bytes of 8 up
+// to 512, beyond that nothing is held.
+struct NormShape {
+    int tok, pc;
+};
+static NormShape norm_shape(const rat3d_norm_desc& d) {
+    const int tok = d.dtype == RAT3D_BF16 ? 8 : 4;
+    if (d.v < tok) return {1, d.c <= 256 ? 4 : 0};
+    return {tok, d.c <= 256 ? 4 : 0};
+}
+
 static void norm_plan(const rat3d_norm_desc& d, NormArgs* a) {
     const int64_t packed = (int64_t)d.c * d.v;
+    const NormShape shape = norm_shape(d);
     a->sx = d.x_stride ? d.x_stride : packed;
     a->sz = d.z_stride ? d.z_stride : packed;
     a->sg = d.g_stride ? d.g_stride : packed;
@@ -323,28 +505,41 @@ static void norm_plan(const rat3d_norm_desc& d, NormArgs* a) {
     a->c = d.c;
     a->eps = d.eps;
     a->gate = d.gate;
-    a->groups = 16;
-    const int tile = kLanes * 16 / (d.dtype == RAT3D_BF16 ? 2 : 4);
-    a->tiles = (int)ceil_div(d.v, tile);
+    // whole waves
+    a->groups = shape.pc ? (int)ceil_div(ceil_div(d.c, shape.pc), 4) * 4 : 16;
+    a->tiles = (int)ceil_div(d.v, kLanes * shape.tok);
     a->all = (int64_t)a->tiles * d.n;
 }
 
-static int norm_grid(const NormArgs& a) {
-    const int64_t most = 8 * (int64_t)device_cus();
+static int norm_grid(const NormArgs& a, bool bwd) {
+    const int64_t most = bwd ? 8 * (int64_t)device_cus() : 1 << 24;
     return (int)(a.all < most ? a.all : most);
 }
 
 size_t norm_ws_bytes(const rat3d_norm_desc& d) {
     NormArgs a = {};
     norm_plan(d, &a);
-    return (size_t)norm_grid(a) * 2 * d.c * sizeof(float);
+    return (size_t)norm_grid(a, true) * 2 * d.c * sizeof(float);
 }
 
 template <NormMode MODE, bool GATED, bool NEXT>
 static void norm_launch(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
-    const int grid = norm_grid(a);
-    if (d.dtype == RAT3D_BF16) block_norm_k<bf16, 8, MODE, GATED, NEXT><<<grid, 256, 0, st>>>(a);
-    else block_norm_k<float, 4, MODE, GATED, NEXT><<<grid, 256, 0, st>>>(a);
+    const int grid = norm_grid(a, MODE == PRE_BWD || MODE == POST_BWD), threads = a.groups * kLanes;
+    const NormShape shape = norm_shape(d);
+#define RAT3D_NORM(T, TOK, PC, THREADS) \
+    block_norm_k<T, TOK, PC, MODE, GATED, NEXT, THREADS><<<grid, threads, 0, st>>>(a)
+#define RAT3D_NORM_T(T, TOK)                                     \
+    do {                                                         \
+        if (shape.tok == 1 && shape.pc) RAT3D_NORM(T, 1, 4, 1024); \
+        else if (shape.tok == 1) RAT3D_NORM(T, 1, 0, 256);       \
+        else if (shape.pc == 0) RAT3D_NORM(T, TOK, 0, 256);      \
+        else if (threads <= 256) RAT3D_NORM(T, TOK, 4, 256);     \
+        else RAT3D_NORM(T, TOK, 4, 1024);                        \
+    } while (0)
+    if (d.dtype == RAT3D_BF16) RAT3D_NORM_T(bf16, 8);
+    else RAT3D_NORM_T(float, 4);
+#undef RAT3D_NORM_T
+#undef RAT3D_NORM
 }
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
@@ -390,7 +585,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
 
 static rat3d_status norm_gains(const NormArgs& a, float* dnext, float* dgamma, float* dscale,
                                int accumulate, hipStream_t st) {
-    const int parts = norm_grid(a);
+    const int parts = norm_grid(a, true);
     ProfScope ps("norm_gain", st, 0.0, 8.0 * a.c * parts);
     norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
                                               dscale, accumulate);

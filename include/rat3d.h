@@ -376,7 +376,7 @@ typedef enum {
  *   before a block   u = gamma N(x)
  *   behind a block   y = x + scale phi(g) gamma N(z)        one rounding, and
  *                    u = gamma_next N(y), y before its rounding (gamma_next != NULL)
- * Masked voxels: u = 0, y = x.  2^-126 <= eps < 10^30; c <= 2^20. */
+ * Masked voxels: u = 0, y = x.  2^-126 <= eps < 10^30; c <= 2^20; v <= 2^28. */
 typedef struct {
     int n, c;
     int64_t v;
@@ -411,7 +411,8 @@ rat3d_status rat3d_pre_norm_bwd(const rat3d_norm_desc* desc, const void* du, con
                                 size_t ws_bytes, void* stream);
 
 /* Gradients from dy and, iff gamma_next is given, du and the forward's y:
- *   dx = dy + the gradient of y from du      (dx may be NULL without gamma_next: it is dy)
+ *   dx = dy + the gradient of y from du      (without gamma_next dx is dy itself, and the
+ *                                             argument must be NULL)
  *   dz, dg (iff gated)                       0 at masked voxels, where dx = dy
  *   dgamma, dscale (nullable), dgamma_next (iff gamma_next) float32 [c]: written, or
  *   added to when accumulate != 0. */

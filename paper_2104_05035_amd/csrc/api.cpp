@@ -634,8 +634,8 @@ static rat3d_status check_norm(const rat3d_norm_desc* d) {
     RAT3D_REQUIRE(valid_dtype(d->dtype), RAT3D_EUNSUPPORTED, "unsupported dtype %d",
                   (int)d->dtype);
     RAT3D_REQUIRE(d->c <= 1 << 20, RAT3D_EUNSUPPORTED, "more than 2^20 channels");
-    RAT3D_REQUIRE(d->v <= (int64_t)1 << 36 && (double)d->c * d->v < 1.0e15, RAT3D_EUNSUPPORTED,
-                  "map too large");
+    RAT3D_REQUIRE(d->v <= (int64_t)1 << 28 && ((double)d->v / 16 + 1) * d->n < 2.0e9,
+                  RAT3D_EUNSUPPORTED, "map too large for one launch");
     const double held = (double)d->c * d->v;
     RAT3D_STRIDE(d->x_stride, held);
     RAT3D_STRIDE(d->z_stride, held);
@@ -758,8 +758,8 @@ rat3d_status rat3d_post_norm_bwd(const rat3d_norm_desc* desc, const void* dy, co
         RAT3D_ELT(gamma_next, sizeof(float), "gamma_next");
         RAT3D_ELT(dgamma_next, sizeof(float), "dgamma_next");
         RAT3D_ELT(dx, es, "dx");
-    } else if (dx) {
-        RAT3D_ELT(dx, es, "dx");
+    } else {
+        RAT3D_REQUIRE(dx == nullptr, RAT3D_EINVAL, "without gamma_next dx is dy: it must be NULL");
     }
     s = check_ws(ws, ws_bytes, norm_ws_bytes(*desc));
     if (s != RAT3D_OK) return s;

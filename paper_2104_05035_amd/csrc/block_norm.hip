@@ -40,8 +40,8 @@ struct NormArgs {
     float* part;  // [gain][channel][workgroup]
     int64_t sx, sz, sg, sy, su;  // from one volume to the next
     int64_t V;
-    int c, groups, tiles, gate;  // tiles of one volume
-    int64_t all;                 // tiles of all volumes
+    int c, groups, gate, stream;
+    uint32_t tiles, all;  // of one volume, of all (below 2^31)
     float eps;
 };
 
@@ -87,14 +87,11 @@ __device__ __forceinline__ void channel_sums(float (&s)[K][TOK], float* lds, int
         const float* from = lds + (k * waves * kLanes + at) * TOK;
 #pragma unroll
         for (int j = 0; j < TOK; ++j) s[k][j] = from[j];
+#pragma unroll 2
         for (int w = 1; w < waves; ++w)
 #pragma unroll
             for (int j = 0; j < TOK; ++j) s[k][j] += from[w * kLanes * TOK + j];
     }
-}
-
-__device__ __forceinline__ float rsqrt_of(float sum, float inv_c, float eps) {
-    return __builtin_amdgcn_rsqf(__builtin_fmaf(sum, inv_c, eps));
 }
 
 // A thread's tokens of one channel, as they lie.
@@ -103,18 +100,33 @@ template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))
         w[TOK * sizeof(T) < 4 ? 1 : TOK * sizeof(T) / 4];
 };
 template <typename T, int TOK> struct Toks {
+    static constexpr int N = sizeof(Words<T, TOK>) / sizeof(Words<T, TOK>::w[0]);
     Words<T, TOK> u;
+    // all bits of the tokens whose bit is set
+    __device__ __forceinline__ static Words<T, TOK> bits(uint32_t on) {
+        Words<T, TOK> m;
+        if constexpr (sizeof(T) == 4 || TOK == 1) {
+#pragma unroll
+            for (int j = 0; j < TOK; ++j) m.w[j] = on >> j & 1u ? ~0u : 0u;
+        } else {
+#pragma unroll
+            for (int j = 0; j < TOK; j += 2)
+                m.w[j / 2] = (on >> j & 1u ? 0xffffu : 0u) | (on >> j & 2u ? 0xffff0000u : 0u);
+        }
+        return m;
+    }
     __device__ __forceinline__ float operator[](int j) const {
         if constexpr (sizeof(T) == 4) return __uint_as_float(u.w[j]);
         else if constexpr (TOK == 1) return Elt<T>::from_bits(u.w[0]);
         else return __uint_as_float(j & 1 ? u.w[j / 2] & 0xffff0000u : u.w[j / 2] << 16);
     }
-    // The tokens at p, or without ALL, where p is `over` tokens (0 .. TOK) before its place
-    // so that none lies behind the row's end, those from `over` on.
-    template <bool ALL> __device__ __forceinline__ void load(const T* p, int over) {
-        u = *reinterpret_cast<const Words<T, TOK>*>(p);
-        if constexpr (!ALL && TOK > 1) {
-            constexpr int N = TOK * sizeof(T) / 4;
+    // The tokens `off` bytes behind base, which is the same for a workgroup.
+    __device__ __forceinline__ void load(const T* base, uint32_t off) {
+        u = *reinterpret_cast<const Words<T, TOK>*>((const char*)base + off);
+    }
+    // The tokens from `over` (0 .. TOK) on.
+    __device__ __forceinline__ void shift(int over) {
+        if constexpr (TOK > 1) {
             const int words = over * (int)sizeof(T) / 4;
 #pragma unroll
             for (int m = N; m >= 1; m >>= 1)
@@ -130,7 +142,9 @@ template <typename T, int TOK> struct Toks {
     }
 };
 template <typename T, int TOK, bool ALL>
-__device__ __forceinline__ void put_tokens(T* p, int left, const float (&o)[TOK]) {
+__device__ __forceinline__ void put_tokens(T* base, uint32_t off, int left,
+                                           const float (&o)[TOK], bool stream) {
+    T* p = (T*)((char*)base + off);
     if (ALL || left == TOK) {
         Words<T, TOK> u;
 #pragma unroll
@@ -138,6 +152,14 @@ __device__ __forceinline__ void put_tokens(T* p, int left, const float (&o)[TOK]
             if constexpr (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
             else if constexpr (TOK == 1) u.w[0] = Elt<T>::to_bits(o[0]);
             else u.w[j / 2] = pack_bf16x2(o[j], o[j + 1]);
+        }
+        if constexpr (TOK * sizeof(T) == 16) {
+            if (stream) {
+                typedef uint32_t __attribute__((ext_vector_type(4))) u4;
+                typedef u4 __attribute__((aligned(2))) u4_any;
+                __builtin_nontemporal_store(u4{u.w[0], u.w[1], u.w[2], u.w[3]}, (u4_any*)p);
+                return;
+            }
         }
         *reinterpret_cast<Words<T, TOK>*>(p) = u;
     } else {
@@ -148,8 +170,9 @@ __device__ __forceinline__ void put_tokens(T* p, int left, const float (&o)[TOK]
 }
 
 // PC: channels a thread, held in registers, c <= PC * groups; 0: any number, read again
-// for every sum.
-template <typename T, int TOK, int PC, NormMode MODE, bool GATED, bool NEXT, int THREADS>
+// for every sum.  ALL: no mask, whole tiles, c = PC * groups (in kernels of their own, for
+// what the other case needs is formed before the loop and takes registers).
+template <typename T, int TOK, int PC, NormMode MODE, bool GATED, bool NEXT, bool ALL, int THREADS>
 __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr bool kPost = MODE == POST_FWD || MODE == POST_BWD;
@@ -176,274 +199,341 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
         }
     };
 
-    auto tile = [&](int64_t t, int64_t vol, int64_t first, auto all_) {
-        constexpr bool kAll = decltype(all_)::value;  // every token and channel is there
+    // the gains of the held channels: gamma scale, and that of the norm of y
+    float wgt[NP], nxt[NP];
+    auto gains = [&](int round) {
+#pragma unroll
+        for (int p = 0; p < NP; ++p) {
+            const int c = grp + (round + p) * a.groups, at_c = ALL || c < a.c ? c : 0;
+            if (MODE != PRE_BWD) wgt[p] = a.gamma[at_c] * (kPost && a.scale ? a.scale[at_c] : 1.f);
+            if (kNext) nxt[p] = gn[at_c];
+        }
+    };
+    if (PC) gains(0);
+
+    auto tile = [&](uint32_t t, int64_t vol, int64_t first) {
+        constexpr bool kAll = ALL;
+        const bool ragged = !ALL && first + TILE > a.V;
         const int64_t t0 = first + at * TOK;
         int left = TOK, over = 0;
         uint32_t live = (1u << TOK) - 1u;
+        Words<T, TOK> keep;  // all bits of live tokens
         if (!kAll) {
-            left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
-            over = TOK - left;
-            live = (1u << left) - 1u;
-            if (a.mask)
+            if (ragged) {
+                left = (int)(a.V - t0 < TOK ? (a.V - t0 > 0 ? a.V - t0 : 0) : TOK);
+                over = TOK - left;
+                live = (1u << left) - 1u;
+            }
+            if (a.mask) {
+                uint8_t m[TOK];
+#pragma unroll
+                for (int j = 0; j < TOK; ++j)  // read without a branch
+                    m[j] = a.mask[vol * a.V + (t0 + j < a.V ? t0 + j : a.V - 1)];
 #pragma unroll
                 for (int j = 0; j < TOK; ++j)
-                    if (j < left && !a.mask[vol * a.V + t0 + j]) live &= ~(1u << j);
+                    if (!m[j]) live &= ~(1u << j);
+            }
+            keep = V::bits(live);
         }
-        // where the thread's tokens of its first channel lie, from its last row's end
-        // counted back where they do not fill it
-        const int64_t at0 = kAll || left == TOK ? t0 : a.V - TOK;
-        const int64_t step = (int64_t)a.groups * a.V;
+        // Bytes from a volume's channel ch[p] - grp, which is the same for a workgroup, to
+        // the thread's tokens; counted back from the row's end where they do not fill it.
+        const uint32_t es = sizeof(T);
+        const uint32_t off = (uint32_t)((int64_t)grp * a.V + t0) * es;
         V X[NP], Z[NP], G[NP], Y[NP], DU[NP];  // backward: X is dy (before a block dres)
-        uint32_t on[NP];
         int ch[NP];
+        // Masked tokens, and channels that are none, come as 0 but for X.
         auto load = [&](int k) {
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                const int c = grp + (k + p) * a.groups;
-                ch[p] = c;
-                on[p] = c < a.c ? live : 0u;
-            }
-            auto get = [&](V(&to)[NP], const void* q, int64_t stride) {
-                const T* from = (const T*)q + vol * stride + at0;
+            for (int p = 0; p < NP; ++p) ch[p] = grp + (k + p) * a.groups;
+            auto get = [&](V(&to)[NP], const void* q, int64_t stride, bool masked) {
+                const T* from = (const T*)q + vol * stride;
 #pragma unroll
-                for (int p = 0; p < NP; ++p)
-                    to[p].template load<kAll>(
-                        from + (kAll ? grp * a.V + (k + p) * step : (int64_t)(ch[p] < a.c ? ch[p] : a.c - 1) * a.V),
-                        over);
+                for (int p = 0; p < NP; ++p) {
+                    const int64_t first_ch = (int64_t)(k + p) * a.groups;
+                    if (kAll) {
+                        to[p].load(from + first_ch * a.V, off);
+                    } else {
+                        const int64_t base = first_ch < a.c ? first_ch : a.c - 1;
+                        const int64_t row = grp < a.c - base ? grp : a.c - base - 1;
+                        const int64_t at0 = left == TOK ? t0 : a.V - TOK;
+                        to[p].load(from + base * a.V, (uint32_t)(row * a.V + at0) * es);
+                        if (ragged) to[p].shift(over);
+                        if (masked)
+#pragma unroll
+                            for (int i = 0; i < V::N; ++i)
+                                to[p].u.w[i] &= ch[p] < a.c ? keep.w[i] : 0;
+                    }
+                }
             };
             if (kBwd && kNext) {
-                get(Y, a.y, a.sy);
-                get(DU, a.du, a.su);
+                get(Y, a.y, a.sy, true);
+                get(DU, a.du, a.su, true);
             }
-            if (kPost) get(Z, a.z, a.sz);
-            if (GATED) get(G, a.g, a.sg);
-            if (!kBwd) get(X, a.x, a.sx);
-            else if (MODE == POST_BWD) get(X, a.dy, a.sy);
-            else if (a.dy) get(X, a.dy, a.sx);
+            if (kPost) get(Z, a.z, a.sz, true);
+            if (GATED) get(G, a.g, a.sg, true);
+            if (!kBwd) get(X, a.x, a.sx, !kPost);
+            else if (MODE == POST_BWD) get(X, a.dy, a.sy, false);
+            else if (a.dy) get(X, a.dy, a.sx, false);
         };
-        // a masked token's value is 0, whatever it holds
-        auto val = [&](const V& v, int p, int j) { return kAll || on[p] >> j & 1u ? v[j] : 0.f; };
+        int round = 0;
         auto put = [&](void* q, int64_t stride, int p, const float (&o)[TOK]) {
             if (kAll || ch[p] < a.c)
-                put_tokens<T, TOK, kAll>((T*)q + vol * stride + (int64_t)ch[p] * a.V + t0, left, o);
+                put_tokens<T, TOK, kAll>(
+                    (T*)q + vol * stride + (int64_t)(round + p) * a.groups * a.V, off, left, o,
+                    a.stream);
         };
-        // What is formed from a held value is formed again behind a barrier, not held too:
-        // the registers are what limits the waves.
-        auto forget = [&](V& v) {
+        // What is formed from a held value is formed again behind a barrier, not held too.
+        auto forget = [&](V(&v)[NP]) {
+            if (PC)
 #pragma unroll
-            for (auto& w : v.u.w) asm volatile("" : "+v"(w));
-        };
-        auto again = [&]() {
-            if (PC == 0) return;
+                for (int p = 0; p < NP; ++p)
 #pragma unroll
-            for (int p = 0; p < NP; ++p) {
-                if (kBwd && kNext) {
-                    forget(Y[p]);
-                    forget(DU[p]);
-                }
-                if (kPost) forget(Z[p]);
-                if (GATED) forget(G[p]);
-                forget(X[p]);
-            }
+                    for (auto& w : v[p].u.w) asm volatile("" : "+v"(w));
         };
-        // all of the thread's channels
+        // formed here, not where it is used
+        auto pin = [&](float(&v)[TOK]) {
+            if (PC)
+#pragma unroll
+                for (float& x : v) asm volatile("" : "+v"(x));
+        };
+        // All of the thread's channels, one after another: the order keeps a channel's
+        // registers free for the next.
         auto each = [&](auto f) {
-            for (int k = 0; k < rounds; ++k) {
-                if (!PC) load(k);
+            for (round = 0; round < rounds; ++round) {
+                if (!PC) {
+                    load(round);
+                    gains(round);
+                }
 #pragma unroll
                 for (int p = 0; p < NP; ++p) {
                     f(p);
-                    __builtin_amdgcn_sched_barrier(0);  // a channel's registers for the next
+                    __builtin_amdgcn_sched_barrier(0);
                 }
+                if (PC) break;
             }
+            round = 0;
         };
-        auto of = [&](const float* v, int p) { return v[kAll || ch[p] < a.c ? ch[p] : 0]; };
-        auto gain = [&](int p) { return of(a.gamma, p) * (a.scale ? of(a.scale, p) : 1.f); };
+        auto is_live = [&](int p, int j) { return kAll || (ch[p] < a.c && (live >> j & 1u)); };
         // the gate's value and slope
         auto gate = [&](int p, int j, float& phi, float& slope) {
             phi = 1.f;
             slope = 0.f;
             if (GATED) {
-                const float g = val(G[p], p, j);
+                const float g = G[p][j];
                 const Sig sg(g);
                 phi = a.gate == RAT3D_GATE_SILU ? g * sg.s : sg.s;
                 slope = sg.s * (a.gate == RAT3D_GATE_SILU ? 1.f + g * sg.rest : sg.rest);
             }
         };
-        if (PC) load(0);
-        float s[K][TOK], e[1][TOK];
+        auto root = [&](float (&r)[TOK], const float (&sum)[TOK]) {
+#pragma unroll
+            for (int j = 0; j < TOK; ++j)
+                r[j] = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[j], inv_c, a.eps));
+        };
         auto clear = [&](auto& v) {
             for (auto& row : v)
                 for (float& x : row) x = 0.f;
         };
+        if (PC) load(0);
+        float e[1][TOK];
+        clear(e);
 
-        if constexpr (!kBwd) {
-            clear(e);
+        if constexpr (MODE == PRE_FWD) {
             each([&](int p) {
 #pragma unroll
+                for (int j = 0; j < TOK; ++j) e[0][j] += X[p][j] * X[p][j];
+            });
+            channel_sums(e, lds[0], waves);
+            forget(X);
+            float r[TOK];
+            root(r, e[0]);
+            each([&](int p) {
+                const float k = wgt[p];
+                float u[TOK];
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) u[j] = k * (X[p][j] * r[j]);
+                put(a.ou, a.su, p, u);
+            });
+        }
+        if constexpr (MODE == POST_FWD) {
+            // held in the place of z and g: the branch without its root, then y
+            float b[NP][TOK], r[TOK];
+            auto branch = [&](int p) {
+                const float k = wgt[p];
+#pragma unroll
                 for (int j = 0; j < TOK; ++j) {
-                    const float v = val(kPost ? Z[p] : X[p], p, j);
-                    e[0][j] += v * v;
+                    float phi, slope;
+                    gate(p, j, phi, slope);
+                    b[p][j] = k * phi * Z[p][j];
+                }
+            };
+            auto sum = [&](int p) {
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) b[p][j] = __builtin_fmaf(b[p][j], r[j], X[p][j]);
+            };
+            each([&](int p) {
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) e[0][j] += Z[p][j] * Z[p][j];
+                if (PC) {
+                    branch(p);
+                    pin(b[p]);
+                    pin(e[0]);
                 }
             });
             channel_sums(e, lds[0], waves);
-            again();
-            float r[TOK];
-#pragma unroll
-            for (int j = 0; j < TOK; ++j) r[j] = rsqrt_of(e[0][j], inv_c, a.eps);
-            if constexpr (MODE == PRE_FWD) {
-                each([&](int p) {
-                    const float k = of(a.gamma, p);
-                    float u[TOK];
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j) u[j] = k * (val(X[p], p, j) * r[j]);
-                    put(a.ou, a.su, p, u);
-                });
-            } else {
-                auto value = [&](int p, float (&y)[TOK]) {
-                    const float k = gain(p);
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j) {
-                        float phi, slope;
-                        gate(p, j, phi, slope);
-                        const float b = k * phi * (val(Z[p], p, j) * r[j]);
-                        y[j] = X[p][j] + (kAll || on[p] >> j & 1u ? b : 0.f);
-                    }
-                };
-                if constexpr (!NEXT) {
-                    each([&](int p) {
-                        float y[TOK];
-                        value(p, y);
-                        put(a.oy, a.sy, p, y);
-                    });
-                } else {
-                    clear(e);
-                    each([&](int p) {
-                        float y[TOK];
-                        value(p, y);
-#pragma unroll
-                        for (int j = 0; j < TOK; ++j) {
-                            const float v = kAll || on[p] >> j & 1u ? y[j] : 0.f;
-                            e[0][j] += v * v;
-                        }
-                    });
-                    channel_sums(e, lds[1], waves);
-                    again();
-                    float ry[TOK];
-#pragma unroll
-                    for (int j = 0; j < TOK; ++j) ry[j] = rsqrt_of(e[0][j], inv_c, a.eps);
-                    each([&](int p) {
-                        float y[TOK];
-                        value(p, y);
-                        put(a.oy, a.sy, p, y);
-                        const float k = of(a.next, p);
-#pragma unroll
-                        for (int j = 0; j < TOK; ++j)
-                            y[j] = kAll || on[p] >> j & 1u ? k * (y[j] * ry[j]) : 0.f;
-                        put(a.ou, a.su, p, y);
-                    });
-                }
-            }
-        } else {
-            clear(s);
-            each([&](int p) {
-                const float k = kNext ? of(gn, p) : 0.f;
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) {
-                    if constexpr (kPost) {
-                        const float z = val(Z[p], p, j);
-                        s[0][j] += z * z;
-                    }
-                    if constexpr (kNext) {
-                        const float y = val(Y[p], p, j);
-                        s[K - 2][j] += y * y;
-                        s[K - 1][j] += k * val(DU[p], p, j) * y;
-                    }
-                }
-            });
-            channel_sums(s, lds[0], waves);
-            again();
-            float ry[TOK], my[TOK], rz[TOK], mz[TOK];
-#pragma unroll
-            for (int j = 0; j < TOK; ++j) {
-                if constexpr (kNext) {
-                    ry[j] = rsqrt_of(s[K - 2][j], inv_c, a.eps);
-                    my[j] = s[K - 1][j] * inv_c * (ry[j] * ry[j]);
-                }
-                if constexpr (kPost) rz[j] = rsqrt_of(s[0][j], inv_c, a.eps);
-            }
-            // dY
-            auto total = [&](int p, int j, float k) {
-                float d = MODE == POST_BWD || a.dy ? X[p][j] : 0.f;
-                if constexpr (kNext)
-                    if (kAll || on[p] >> j & 1u)
-                        d += ry[j] * (k * DU[p][j] - Y[p][j] * my[j]);
-                return d;
-            };
-            if constexpr (kPost) {
+            forget(X);
+            root(r, e[0]);
+            float ry[TOK];
+            if constexpr (NEXT) {
                 clear(e);
                 each([&](int p) {
-                    const float k = kNext ? of(gn, p) : 0.f, w = gain(p);
+                    if (!PC) branch(p);
+                    sum(p);
+                    if (PC) put(a.oy, a.sy, p, b[p]);
+                    const bool is = kAll || ch[p] < a.c;
 #pragma unroll
-                    for (int j = 0; j < TOK; ++j) {
-                        float phi, slope;
-                        gate(p, j, phi, slope);
-                        const float d = total(p, j, k);
-                        e[0][j] += (kAll || on[p] >> j & 1u ? d : 0.f) * w * phi * val(Z[p], p, j);
-                    }
+                    for (int j = 0; j < TOK; ++j) e[0][j] += is ? b[p][j] * b[p][j] : 0.f;
+                    pin(b[p]);
+                    pin(e[0]);
                 });
                 channel_sums(e, lds[1], waves);
-                again();
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) mz[j] = e[0][j] * inv_c * (rz[j] * rz[j]);
+                root(ry, e[0]);
             }
             each([&](int p) {
-                const float k = kNext ? of(gn, p) : 0.f;
-                float dY[TOK], n = 0.f, q = 0.f;
-#pragma unroll
-                for (int j = 0; j < TOK; ++j) {
-                    dY[j] = total(p, j, k);
-                    if constexpr (kNext) n += val(DU[p], p, j) * (val(Y[p], p, j) * ry[j]);
+                if (!PC) branch(p);
+                if (!PC || !NEXT) {
+                    sum(p);
+                    put(a.oy, a.sy, p, b[p]);
                 }
-                if constexpr (kPost) {
-                    const float w = gain(p);
-                    float dz[TOK], dg[TOK];
+                if constexpr (NEXT) {
+                    const float k = nxt[p];
 #pragma unroll
-                    for (int j = 0; j < TOK; ++j) {
-                        float phi, slope;
-                        gate(p, j, phi, slope);
-                        const float z = val(Z[p], p, j), zr = z * rz[j];
-                        const float d = kAll || on[p] >> j & 1u ? dY[j] : 0.f;
-                        q += d * phi * zr;
-                        dz[j] = rz[j] * (d * w * phi - z * mz[j]);
-                        dg[j] = d * w * zr * slope;
-                    }
-                    put(a.dz, a.sz, p, dz);
-                    if (GATED) put(a.dg, a.sg, p, dg);
-                }
-                if (MODE == PRE_BWD || kNext || a.dx) put(a.dx, a.sx, p, dY);
-                if constexpr (PC != 0) {
-                    sum_n[p] += (double)n;
-                    sum_t[p] += (double)q;
-                } else {
-                    const bool more = t != blockIdx.x;
-                    if (kNext) put_gain(0, ch[p], (double)n, more);
-                    if (kPost) put_gain(1, ch[p], (double)q, more);
+                    for (int j = 0; j < TOK; ++j)
+                        b[p][j] = is_live(p, j) ? k * (b[p][j] * ry[j]) : 0.f;
+                    put(a.ou, a.su, p, b[p]);
                 }
             });
         }
+        if constexpr (kBwd) {
+            float s[K][TOK];
+            clear(s);
+            each([&](int p) {
+                const float k = kNext ? nxt[p] : 0.f;
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) {
+                    if constexpr (kPost) s[0][j] += Z[p][j] * Z[p][j];
+                    if constexpr (kNext) {
+                        const float y = Y[p][j];
+                        s[K - 2][j] += y * y;
+                        s[K - 1][j] += k * DU[p][j] * y;
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < K; ++k) pin(s[k]);
+            });
+            channel_sums(s, lds[0], waves);
+            forget(X);
+            if (kNext) {
+                forget(Y);
+                forget(DU);
+            }
+            if (kPost) forget(Z);
+            if (GATED) forget(G);
+            float ry[TOK], my[TOK], rz[TOK];
+            if constexpr (kNext) {
+                root(ry, s[K - 2]);
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) my[j] = s[K - 1][j] * inv_c * (ry[j] * ry[j]);
+            }
+            if constexpr (kPost) root(rz, s[0]);
+            // dY, and its part in the next norm's gain
+            auto residual = [&](int p, float (&d)[TOK]) {
+                const float k = kNext ? nxt[p] : 0.f;
+                float n = 0.f;
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) {
+                    d[j] = MODE == POST_BWD || a.dy ? X[p][j] : 0.f;
+                    if constexpr (kNext) {
+                        const float y = Y[p][j], du = DU[p][j];
+                        d[j] += ry[j] * (k * du - y * my[j]);
+                        n += du * (y * ry[j]);
+                    }
+                }
+                return n;
+            };
+            auto add_n = [&](int p, float n) {
+                asm volatile("" : "+v"(n));
+                if constexpr (PC != 0) sum_n[p] += (double)n;
+                else if (kNext) put_gain(0, ch[p], (double)n, t != blockIdx.x);
+            };
+            auto add_t = [&](int p, float q) {
+                asm volatile("" : "+v"(q));
+                if constexpr (PC != 0) sum_t[p] += (double)q;
+                else put_gain(1, ch[p], (double)q, t != blockIdx.x);
+            };
+            if constexpr (!kPost) {
+                each([&](int p) {
+                    float d[TOK];
+                    add_n(p, residual(p, d));
+                    put(a.dx, a.sx, p, d);
+                });
+            } else {
+                // e = dY s gamma phi, held in the place of what it is formed from; where
+                // nothing is held, results wait for the last pass, which reads all again
+                float E[NP][TOK], mz[TOK];
+                auto middle = [&](int p, bool out) {
+                    const float w = wgt[p];
+                    const float n = residual(p, E[p]);
+                    if (out) {
+                        add_n(p, n);
+                        if (kNext) put(a.dx, a.sx, p, E[p]);
+                    }
+                    float dg[TOK], q = 0.f;
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) {
+                        float phi, slope;
+                        gate(p, j, phi, slope);
+                        const float d = is_live(p, j) ? E[p][j] : 0.f, zr = Z[p][j] * rz[j];
+                        q += d * phi * zr;
+                        dg[j] = d * w * zr * slope;
+                        E[p][j] = d * w * phi;
+                    }
+                    if (out) {
+                        add_t(p, q);
+                        if (GATED) put(a.dg, a.sg, p, dg);
+                    }
+                };
+                each([&](int p) {
+                    middle(p, PC != 0);
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) e[0][j] += E[p][j] * Z[p][j];
+                    pin(E[p]);
+                    pin(e[0]);
+                });
+                channel_sums(e, lds[1], waves);
+                forget(Z);
+#pragma unroll
+                for (int j = 0; j < TOK; ++j) mz[j] = e[0][j] * inv_c * (rz[j] * rz[j]);
+                each([&](int p) {
+                    if (!PC) middle(p, true);
+#pragma unroll
+                    for (int j = 0; j < TOK; ++j) E[p][j] = rz[j] * (E[p][j] - Z[p][j] * mz[j]);
+                    put(a.dz, a.sz, p, E[p]);
+                });
+            }
+        }
         // the first sums are written again only behind the barrier of the second, the
         // second only behind that of the next first
-        if constexpr (!(kPost && (kBwd || NEXT))) __syncthreads();
+        if constexpr (MODE == PRE_BWD) __syncthreads();
     };
 
-    for (int64_t t = blockIdx.x; t < a.all; t += gridDim.x) {
-        const int64_t vol = t / a.tiles, first = (t - vol * a.tiles) * TILE;
-        if (a.mask || first + TILE > a.V || a.c != NP * rounds * a.groups)
-            tile(t, vol, first, std::false_type{});
-        else tile(t, vol, first, std::true_type{});
-    }
+    // backward: several tiles a workgroup, so that the gains' parts stay few
+    uint32_t t = blockIdx.x;
+    do {
+        const uint32_t vol = t / a.tiles;
+        tile(t, vol, (int64_t)(t - vol * a.tiles) * TILE);
+        t += gridDim.x;
+    } while (kBwd && t < a.all);
     if constexpr (kBwd && PC != 0) {
 #pragma unroll
         for (int p = 0; p < NP; ++p) {
@@ -482,20 +572,31 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 }
 
 // ------------------------------------------------------------------ host
-// Tokens and channels a thread: 16 bytes of 4 channels up to 256 of them, 8 bytes of 8 up
-// to 512, beyond that nothing is held.
+// Tokens and channels a thread, and groups of threads along the channels (whole waves).
+// Beyond 128 channels of bfloat16 the backward keeps half as many tokens of twice the
+// channels, so that a workgroup has 512 threads and their registers: 4 x 256 channels over
+// 64512 voxels 546 -> 280 us behind a block, 146 -> 136 before one; the forward does not
+// gain (145 and 153 us).
 struct NormShape {
-    int tok, pc;
+    int tok, pc, groups;
 };
-static NormShape norm_shape(const rat3d_norm_desc& d) {
-    const int tok = d.dtype == RAT3D_BF16 ? 8 : 4;
-    if (d.v < tok) return {1, d.c <= 256 ? 4 : 0};
-    return {tok, d.c <= 256 ? 4 : 0};
+static NormShape norm_shape(const rat3d_norm_desc& d, bool bwd) {
+    const int es = d.dtype == RAT3D_BF16 ? 2 : 4, tok = d.v < 16 / es ? 1 : 16 / es;
+    // a group's rows are reached with 32 bits: at least 4 of them up to 2^28 tokens
+    const int64_t most = ((int64_t)1 << 32) / (d.v * es);
+    if (d.c <= 256) {
+        const bool half = bwd && tok == 8 && d.c > 128;
+        const int pc = half ? 8 : 4, groups = (int)ceil_div(d.c, 4 * pc) * 4;
+        if (groups <= most) return {half ? 4 : tok, pc, groups};
+    }
+    int groups = 16;
+    while (groups > most) groups /= 2;
+    return {tok, 0, groups};
 }
 
-static void norm_plan(const rat3d_norm_desc& d, NormArgs* a) {
+static void norm_plan(const rat3d_norm_desc& d, bool bwd, NormArgs* a) {
     const int64_t packed = (int64_t)d.c * d.v;
-    const NormShape shape = norm_shape(d);
+    const NormShape shape = norm_shape(d, bwd);
     a->sx = d.x_stride ? d.x_stride : packed;
     a->sz = d.z_stride ? d.z_stride : packed;
     a->sg = d.g_stride ? d.g_stride : packed;
@@ -505,41 +606,65 @@ static void norm_plan(const rat3d_norm_desc& d, NormArgs* a) {
     a->c = d.c;
     a->eps = d.eps;
     a->gate = d.gate;
-    // whole waves
-    a->groups = shape.pc ? (int)ceil_div(ceil_div(d.c, shape.pc), 4) * 4 : 16;
-    a->tiles = (int)ceil_div(d.v, kLanes * shape.tok);
-    a->all = (int64_t)a->tiles * d.n;
+    // Results larger than the memory-side cache (256 MB) do not wait there for their
+    // reader; stored past it they leave it to the inputs (16 x 64 channels over 48x56x48:
+    // 261 -> 255 us behind a block, its gradient 447 -> 434).
+    a->stream = (double)d.n * d.c * d.v * (d.dtype == RAT3D_BF16 ? 2 : 4) > 256e6;
+    a->groups = shape.groups;
+    a->tiles = (uint32_t)ceil_div(d.v, kLanes * shape.tok);
+    a->all = a->tiles * d.n;
 }
 
-static int norm_grid(const NormArgs& a, bool bwd) {
-    const int64_t most = bwd ? 8 * (int64_t)device_cus() : 1 << 24;
-    return (int)(a.all < most ? a.all : most);
+// Backward: a few tiles a workgroup, so that the gains' parts stay few (2 to 32 workgroups
+// a CU take the same time within 3 % at 64 channels, 239 to 265 us at 128).
+static uint32_t norm_grid(const NormArgs& a, bool bwd) {
+    const uint32_t most = 4 * device_cus();
+    return bwd && a.all > most ? most : a.all;
 }
 
 size_t norm_ws_bytes(const rat3d_norm_desc& d) {
     NormArgs a = {};
-    norm_plan(d, &a);
+    norm_plan(d, true, &a);
     return (size_t)norm_grid(a, true) * 2 * d.c * sizeof(float);
+}
+
+template <typename T, NormMode MODE, bool GATED, bool NEXT>
+static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
+    constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
+    constexpr int TOK = 16 / (int)sizeof(T);
+    const NormShape shape = norm_shape(d, kBwd);
+    const unsigned grid = norm_grid(a, kBwd);
+    const int threads = a.groups * kLanes;
+    const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
+                     d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
+#define RAT3D_NORM1(TOK, PC, ALL, THREADS) \
+    block_norm_k<T, TOK, PC, MODE, GATED, NEXT, ALL, THREADS><<<grid, threads, 0, st>>>(a)
+#define RAT3D_NORM(TOK, PC, THREADS)                  \
+    do {                                              \
+        if (all) RAT3D_NORM1(TOK, PC, true, THREADS); \
+        else RAT3D_NORM1(TOK, PC, false, THREADS);    \
+    } while (0)
+    if (shape.tok == 1) {
+        if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
+        else RAT3D_NORM1(1, 0, false, 256);
+    } else if (shape.pc == 0) {
+        RAT3D_NORM(TOK, 0, 256);
+    } else if constexpr (!kBwd) {
+        RAT3D_NORM(TOK, 4, 1024);  // 128 registers are enough
+    } else {
+        if (threads <= 256 && shape.pc == 4) RAT3D_NORM(TOK, 4, 256);
+        else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(TOK, 4, 512);
+        else if constexpr (sizeof(T) == 2) RAT3D_NORM(4, 8, 512);
+        else RAT3D_NORM(4, 4, 1024);
+    }
+#undef RAT3D_NORM
+#undef RAT3D_NORM1
 }
 
 template <NormMode MODE, bool GATED, bool NEXT>
 static void norm_launch(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
-    const int grid = norm_grid(a, MODE == PRE_BWD || MODE == POST_BWD), threads = a.groups * kLanes;
-    const NormShape shape = norm_shape(d);
-#define RAT3D_NORM(T, TOK, PC, THREADS) \
-    block_norm_k<T, TOK, PC, MODE, GATED, NEXT, THREADS><<<grid, threads, 0, st>>>(a)
-#define RAT3D_NORM_T(T, TOK)                                     \
-    do {                                                         \
-        if (shape.tok == 1 && shape.pc) RAT3D_NORM(T, 1, 4, 1024); \
-        else if (shape.tok == 1) RAT3D_NORM(T, 1, 0, 256);       \
-        else if (shape.pc == 0) RAT3D_NORM(T, TOK, 0, 256);      \
-        else if (threads <= 256) RAT3D_NORM(T, TOK, 4, 256);     \
-        else RAT3D_NORM(T, TOK, 4, 1024);                        \
-    } while (0)
-    if (d.dtype == RAT3D_BF16) RAT3D_NORM_T(bf16, 8);
-    else RAT3D_NORM_T(float, 4);
-#undef RAT3D_NORM_T
-#undef RAT3D_NORM
+    if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, a, st);
+    else norm_launch_t<float, MODE, GATED, NEXT>(d, a, st);
 }
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
@@ -549,7 +674,7 @@ static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
 rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* gamma,
                           const uint8_t* mask, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, &a);
+    norm_plan(d, false, &a);
     a.x = x;
     a.gamma = gamma;
     a.mask = mask;
@@ -564,7 +689,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
                            const float* gamma, const float* scale, const float* next,
                            const uint8_t* mask, void* y, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, &a);
+    norm_plan(d, false, &a);
     a.x = x;
     a.z = z;
     a.g = g;
@@ -585,7 +710,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
 
 static rat3d_status norm_gains(const NormArgs& a, float* dnext, float* dgamma, float* dscale,
                                int accumulate, hipStream_t st) {
-    const int parts = norm_grid(a, true);
+    const int parts = (int)norm_grid(a, true);
     ProfScope ps("norm_gain", st, 0.0, 8.0 * a.c * parts);
     norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
                                               dscale, accumulate);
@@ -597,7 +722,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
                           const float* gamma, const uint8_t* mask, const void* dres, void* dx,
                           float* dgamma, int accumulate, void* ws, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, &a);
+    norm_plan(d, true, &a);
     a.du = du;
     a.y = x;
     a.sy = a.sx;
@@ -620,7 +745,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
                            float* dgamma, float* dscale, float* dnext, int accumulate, void* ws,
                            hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, &a);
+    norm_plan(d, true, &a);
     a.dy = dy;
     a.du = du;
     a.y = y;
@@ -636,7 +761,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.part = (float*)ws;
     {
         ProfScope ps("post_norm_bwd", st, 0.0,
-                     norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : dx ? 1 : 0)));
+                     norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
         if (d.gate && next) norm_launch<POST_BWD, true, true>(d, a, st);
         else if (d.gate) norm_launch<POST_BWD, true, false>(d, a, st);
         else if (next) norm_launch<POST_BWD, false, true>(d, a, st);

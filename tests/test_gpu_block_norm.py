@@ -146,24 +146,24 @@ def test_post_norm(case, dt):
         # the backward reads a stored y: here the forward's x, so that its values are known
         yin = s.x.clone()
         _spoil(yin, s.mask)
-        dx = s.out()
+        dx = s.out() if s.nxt else None  # without a next norm it is dy itself
         dz, dg = s.out(), s.out() if s.kind else None
         vec = [s.out((s.c,), "f32") for _ in range(3)]
         names = ("dgamma",) + (("dscale",) if scale is not None else ()) + \
             (("dgamma_next",) if s.nxt else ())
-        back = lambda dgs, acc, dx: R.rat3d_post_norm_bwd(  # noqa: E731
+        back = lambda dgs, acc: R.rat3d_post_norm_bwd(  # noqa: E731
             s.desc, s.dy, s.du if s.nxt else None, yin if s.nxt else None, s.z, g, s.gamma, scale,
             gn, s.dmask, dx, dz, dg, dgs[0], dgs[1] if scale is not None else None,
             dgs[2] if s.nxt else None, acc, _ws(s.need), s.need)
-        back(vec, 0, dx)
+        back(vec, 0)
         U.sync()
         want = RU.post_norm_bwd_refs(r["dy"], r["du"], r["x"], r["z"], r["g"], s.kind, r["gamma"],
                                      sr, gnr, s.mask, EPS, dt)
         got = dict(dx=dx, dz=dz, dg=dg, dgamma=vec[0], dscale=vec[1], dgamma_next=vec[2])
-        _check(got, want, ("dx", "dz") + (("dg",) if s.kind else ()) + names)
-        # added to what is there; without a next norm dx is dy itself and may be left out
+        _check(got, want, (("dx",) if s.nxt else ()) + ("dz",) + (("dg",) if s.kind else ()) + names)
+        # added to what is there
         first, acc = dz.clone(), [s.i0.clone(), s.i1.clone(), s.i2.clone()]
-        back(acc, 1, dx if s.nxt else None)
+        back(acc, 1)
         U.sync()
         assert torch.equal(dz, first)
         for a, i, t, k in zip(acc, (s.i0, s.i1, s.i2), vec, ("dgamma", "dscale", "dgamma_next")):

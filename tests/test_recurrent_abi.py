@@ -41,8 +41,8 @@ NAN, INF = float("nan"), float("inf")
     (dict(gate=3), R.EINVAL), (dict(gate=-1), R.EINVAL), (dict(eps=0.0), R.EINVAL),
     (dict(eps=1e-40), R.EINVAL), (dict(eps=-1.0), R.EINVAL), (dict(eps=NAN), R.EINVAL),
     (dict(eps=INF), R.EINVAL), (dict(dtype=R.U8), R.EUNSUPPORTED), (dict(dtype=9), R.EUNSUPPORTED),
-    (dict(c=(1 << 20) + 1), R.EUNSUPPORTED), (dict(v=(1 << 36) + 1), R.EUNSUPPORTED),
-    (dict(c=1 << 20, v=1 << 36), R.EUNSUPPORTED), (dict(x_stride=24 * 60 - 1), R.EINVAL),
+    (dict(c=(1 << 20) + 1), R.EUNSUPPORTED), (dict(v=(1 << 28) + 1), R.EUNSUPPORTED),
+    (dict(n=1 << 30, v=1 << 8), R.EUNSUPPORTED), (dict(x_stride=24 * 60 - 1), R.EINVAL),
     (dict(z_stride=1), R.EINVAL), (dict(g_stride=-1), R.EINVAL), (dict(y_stride=5), R.EINVAL),
     (dict(u_stride=1 << 60), R.EINVAL),
 ])
@@ -87,6 +87,8 @@ def test_norm_pointers():
     for i in (0, 1, 2, 3, 4, 5, 6, 7, 9, 10, 11, 12, 13, 14):
         _refused(R.EALIGN, R.rat3d_post_norm_bwd, d, *_with(back, i, back[i] + 1), 0, ws, need)
     _refused(R.EWORKSPACE, R.rat3d_post_norm_bwd, d, *back, 0, ws, need - 1)
+    # without a next norm dx is dy itself
+    _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, 7, None), 0, ws, need)
 
 
 def test_norm_overlaps():

@@ -19,11 +19,9 @@
 // joined by lane swaps that leave each of a wave's four groups a quarter of the voxels,
 // and through LDS.  Rows need no alignment.
 // Bound: HBM.
-#include <type_traits>
-
 #include "kernels.hpp"
 #include "prof.hpp"
-#include "vec.hpp"
+#include "tokens.hpp"
 
 namespace rat3d {
 
@@ -40,7 +38,8 @@ struct NormArgs {
     float* part;  // [gain][channel][workgroup]
     int64_t sx, sz, sg, sy, su;  // from one volume to the next
     int64_t V;
-    int c, groups, gate, stream;
+    int c, groups, gate;
+    int stream, near;  // stores past the cache; neighbouring tiles on one XCD
     uint32_t tiles, all;  // of one volume, of all (below 2^31)
     float eps;
 };
@@ -94,81 +93,6 @@ __device__ __forceinline__ void channel_sums(float (&s)[K][TOK], float* lds, int
     }
 }
 
-// A thread's tokens of one channel, as they lie.
-template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Words {
-    typename std::conditional<TOK * sizeof(T) < 4, uint16_t, uint32_t>::type
-        w[TOK * sizeof(T) < 4 ? 1 : TOK * sizeof(T) / 4];
-};
-template <typename T, int TOK> struct Toks {
-    static constexpr int N = sizeof(Words<T, TOK>) / sizeof(Words<T, TOK>::w[0]);
-    Words<T, TOK> u;
-    // all bits of the tokens whose bit is set
-    __device__ __forceinline__ static Words<T, TOK> bits(uint32_t on) {
-        Words<T, TOK> m;
-        if constexpr (sizeof(T) == 4 || TOK == 1) {
-#pragma unroll
-            for (int j = 0; j < TOK; ++j) m.w[j] = on >> j & 1u ? ~0u : 0u;
-        } else {
-#pragma unroll
-            for (int j = 0; j < TOK; j += 2)
-                m.w[j / 2] = (on >> j & 1u ? 0xffffu : 0u) | (on >> j & 2u ? 0xffff0000u : 0u);
-        }
-        return m;
-    }
-    __device__ __forceinline__ float operator[](int j) const {
-        if constexpr (sizeof(T) == 4) return __uint_as_float(u.w[j]);
-        else if constexpr (TOK == 1) return Elt<T>::from_bits(u.w[0]);
-        else return __uint_as_float(j & 1 ? u.w[j / 2] & 0xffff0000u : u.w[j / 2] << 16);
-    }
-    // The tokens `off` bytes behind base, which is the same for a workgroup.
-    __device__ __forceinline__ void load(const T* base, uint32_t off) {
-        u = *reinterpret_cast<const Words<T, TOK>*>((const char*)base + off);
-    }
-    // The tokens from `over` (0 .. TOK) on.
-    __device__ __forceinline__ void shift(int over) {
-        if constexpr (TOK > 1) {
-            const int words = over * (int)sizeof(T) / 4;
-#pragma unroll
-            for (int m = N; m >= 1; m >>= 1)
-#pragma unroll
-                for (int i = 0; i < N; ++i) u.w[i] = words & m ? (i + m < N ? u.w[i + m] : 0u) : u.w[i];
-            if constexpr (sizeof(T) == 2) {
-                const uint32_t bits = over & 1 ? 16u : 0u;
-#pragma unroll
-                for (int i = 0; i < N; ++i)
-                    u.w[i] = __builtin_amdgcn_alignbit(i + 1 < N ? u.w[i + 1] : 0u, u.w[i], bits);
-            }
-        }
-    }
-};
-template <typename T, int TOK, bool ALL>
-__device__ __forceinline__ void put_tokens(T* base, uint32_t off, int left,
-                                           const float (&o)[TOK], bool stream) {
-    T* p = (T*)((char*)base + off);
-    if (ALL || left == TOK) {
-        Words<T, TOK> u;
-#pragma unroll
-        for (int j = 0; j < TOK; j += 4 / (int)sizeof(T)) {
-            if constexpr (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
-            else if constexpr (TOK == 1) u.w[0] = Elt<T>::to_bits(o[0]);
-            else u.w[j / 2] = pack_bf16x2(o[j], o[j + 1]);
-        }
-        if constexpr (TOK * sizeof(T) == 16) {
-            if (stream) {
-                typedef uint32_t __attribute__((ext_vector_type(4))) u4;
-                typedef u4 __attribute__((aligned(2))) u4_any;
-                __builtin_nontemporal_store(u4{u.w[0], u.w[1], u.w[2], u.w[3]}, (u4_any*)p);
-                return;
-            }
-        }
-        *reinterpret_cast<Words<T, TOK>*>(p) = u;
-    } else {
-#pragma unroll
-        for (int j = 0; j < TOK; ++j)
-            if (j < left) Elt<T>::st(p + j, o[j]);
-    }
-}
-
 // PC: channels a thread, held in registers, c <= PC * groups; 0: any number, read again
 // for every sum.  ALL: no mask, whole tiles, c = PC * groups (in kernels of their own, for
 // what the other case needs is formed before the loop and takes registers).
@@ -211,7 +135,8 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     };
     if (PC) gains(0);
 
-    auto tile = [&](uint32_t t, int64_t vol, int64_t first) {
+    // more: not this workgroup's first tile
+    auto tile = [&](bool more, int64_t vol, int64_t first) {
         constexpr bool kAll = ALL;
         const bool ragged = !ALL && first + TILE > a.V;
         const int64_t t0 = first + at * TOK;
@@ -464,12 +389,12 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
             auto add_n = [&](int p, float n) {
                 asm volatile("" : "+v"(n));
                 if constexpr (PC != 0) sum_n[p] += (double)n;
-                else if (kNext) put_gain(0, ch[p], (double)n, t != blockIdx.x);
+                else if (kNext) put_gain(0, ch[p], (double)n, more);
             };
             auto add_t = [&](int p, float q) {
                 asm volatile("" : "+v"(q));
                 if constexpr (PC != 0) sum_t[p] += (double)q;
-                else put_gain(1, ch[p], (double)q, t != blockIdx.x);
+                else put_gain(1, ch[p], (double)q, more);
             };
             if constexpr (!kPost) {
                 each([&](int p) {
@@ -528,10 +453,11 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     };
 
     // backward: several tiles a workgroup, so that the gains' parts stay few
-    uint32_t t = blockIdx.x;
+    const uint32_t t0 = a.near ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
+    uint32_t t = t0;
     do {
         const uint32_t vol = t / a.tiles;
-        tile(t, vol, (int64_t)(t - vol * a.tiles) * TILE);
+        tile(t != t0, vol, (int64_t)(t - vol * a.tiles) * TILE);
         t += gridDim.x;
     } while (kBwd && t < a.all);
     if constexpr (kBwd && PC != 0) {
@@ -628,6 +554,22 @@ size_t norm_ws_bytes(const rat3d_norm_desc& d) {
     return (size_t)norm_grid(a, true) * 2 * d.c * sizeof(float);
 }
 
+// Rows that begin inside a cache line: neighbouring tiles share lines, and one XCD's
+// L2 should see both (16 x 64 channels of 129023 voxels: 407 -> 348 us behind a block,
+// its gradient 692 -> 544; whole lines are 2 to 4 % faster dealt out).  Streaming stores
+// would write the shared lines twice.
+static void norm_lines(const rat3d_norm_desc& d, NormArgs* a) {
+    const int64_t es = d.dtype == RAT3D_BF16 ? 2 : 4;
+    uintptr_t any = (uintptr_t)(d.v * es);
+    for (int64_t s : {a->sx, a->sz, a->sg, a->sy, a->su}) any |= (uintptr_t)(s * es);
+    for (const void* p : {a->x, a->z, a->g, a->y, a->dy, a->du, (const void*)a->oy,
+                          (const void*)a->ou, (const void*)a->dx, (const void*)a->dz,
+                          (const void*)a->dg})
+        any |= (uintptr_t)p;
+    a->near = any % 128 != 0;
+    if (a->near) a->stream = 0;
+}
+
 template <typename T, NormMode MODE, bool GATED, bool NEXT>
 static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
@@ -662,7 +604,8 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream
 }
 
 template <NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
+static void norm_launch(const rat3d_norm_desc& d, NormArgs& a, hipStream_t st) {
+    norm_lines(d, &a);
     if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, a, st);
     else norm_launch_t<float, MODE, GATED, NEXT>(d, a, st);
 }

@@ -8,30 +8,43 @@
 //   K = D la (a h_{t-1} - sigmoid(i) x a^2 / beta),  la = -w sigmoid(r),
 //   dr = K (1 - sigmoid(r)),  dlambda = sigmoid(lambda) / softplus(lambda) sum K
 // Both directions are linear recurrences, whose steps (a, b) join associatively:
-// (a, b) behind (a', b') is (a a', a b' + b).  h_{t-1} is formed again from the states
-// that the forward left every kBlock voxels, in float32.
+// (a, b) behind (a', b') is (a a', a b' + b).
+//
+// Layout: 16 bytes of neighbouring voxels a lane, in the order of memory, so a wave holds
+// one block of a row; the walk goes up or down through the lanes.  A lane joins its own
+// steps, the 16 lanes of a DPP row theirs, the four rows of a wave are joined by values
+// read from single lanes, the waves of a workgroup through LDS: a workgroup takes as many
+// blocks at once as it has waves, one barrier a turn, the next turn's loads in flight.
+// h_{t-1} is formed again in the backward from the states that the forward left before
+// every block, in float32.  Rows of up to 16 lanes share a wave.  Few rows are cut into
+// segments: a first launch joins each segment's steps, the second begins each segment
+// with the joined steps before it.
 //
 // beta: 1 - a^2 is -expm1(-2 w sigmoid(r)), by its series where the argument is small.
 // Bound: HBM.
 #include "kernels.hpp"
 #include "prof.hpp"
-#include "vec.hpp"
+#include "tokens.hpp"
 
 namespace rat3d {
 
-constexpr int kTok = 8;              // voxels a lane
-constexpr int kBlock = 64 * kTok;    // voxels between two saved states
+template <typename T> constexpr int tok() { return 16 / (int)sizeof(T); }  // voxels a lane
+template <typename T> constexpr int block() { return 64 * tok<T>(); }      // voxels a wave
+constexpr int kWaves = 8;   // of a workgroup, at most
+constexpr int kSegs = 64;   // segments of a row, at most
 
 struct RecArgs {
     const void *r, *i, *x, *dy;
     const float* lam;
     const uint8_t* mask;
-    const float* h0;
-    const float* dh;
+    const float* h0;   // the state (backward: its gradient) that the walk begins with
     void *y, *dr, *di, *dx;
-    float *h_last, *carry, *dh0, *part;
+    float *h_last;     // what it ends with
+    float *carry, *part;
+    float* joined;     // [row][segment] (a, b) of each segment, then [row] the walk's first state
     int64_t sr, si, sx, sy, len;
-    int c, blocks, reverse;
+    int64_t rows;
+    int c, blocks, segs, lanes, stream;  // of a row; lanes: of a short row
     float rate;
 };
 
@@ -41,190 +54,572 @@ __device__ __forceinline__ float softplusf(float v) {
 
 // One voxel's step.
 struct Step {
-    float rest, la, a, p, inv;  // rest = 1 - sigmoid(r), p = 1 - a^2, inv = 1 / sqrt(p)
+    float rest, la, a, p;  // rest = 1 - sigmoid(r), p = 1 - a^2
     __device__ __forceinline__ Step(float r, float w) {
         const Sig g(r);
         rest = g.rest;
         la = -w * g.s;
-        a = expf(la);
-        p = -expm1f(2.f * la);
-        // at p = 0 (a shut gate) la inv and p inv come out as 0, their limits
-        inv = __builtin_amdgcn_rsqf(p < 0x1p-100f ? 0x1p-100f : p);
+        a = __builtin_amdgcn_exp2f(la * 1.44269504f);
+        // -expm1(-t): five terms are off by less than t^5 / 720 = 4e-8 at 1/8, from where
+        // on 1 - a^2 is off by 1.5e-6 at most
+        const float t = -2.f * la;
+        float s = __builtin_fmaf(t, 1.f / 120.f, -1.f / 24.f);
+        s = __builtin_fmaf(t, s, 1.f / 6.f);
+        s = __builtin_fmaf(t, s, -0.5f);
+        s = t * __builtin_fmaf(t, s, 1.f);
+        p = t < 0.125f ? s : __builtin_fmaf(-a, a, 1.f);
     }
 };
 
-// (a, b) of this lane and of all lanes before it, joined; lanes behind in the walk's
-// order have higher ids.
-__device__ __forceinline__ void scan_wave(float& a, float& b) {
-    const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int m = 1; m < 64; m <<= 1) {
-        const float pa = __shfl_up(a, m), pb = __shfl_up(b, m);
-        if (lane >= m) {
-            b = __builtin_fmaf(a, pb, b);
-            a *= pa;
-        }
-    }
+template <int CTRL> __device__ __forceinline__ float dpp_or(float old, float v) {
+    return __uint_as_float(__builtin_amdgcn_update_dpp(__float_as_uint(old), __float_as_uint(v),
+                                                       CTRL, 0xf, 0xf, false));
+}
+__device__ __forceinline__ float lane_of(float v, int lane) {
+    return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane));
 }
 
-// One wave a row.  The walk's step k takes the voxels k * kBlock and up in its order;
-// voxel v of the order lies at v, or from the end if REV.
-template <typename T, bool REV>
-__global__ __launch_bounds__(64) void recurrence_fwd_k(RecArgs q) {
-    const int lane = threadIdx.x;
-    const int64_t row = blockIdx.x;
-    const int64_t vol = row / q.c;
-    const int ch = (int)(row - vol * q.c);
-    const float w = q.rate * softplusf(q.lam[ch]);
-    const T* r = (const T*)q.r + vol * q.sr + (int64_t)ch * q.len;
-    const T* g = (const T*)q.i + vol * q.si + (int64_t)ch * q.len;
-    const T* x = (const T*)q.x + vol * q.sx + (int64_t)ch * q.len;
-    T* y = (T*)q.y + vol * q.sy + (int64_t)ch * q.len;
-    const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
-    float state = q.h0 ? q.h0[row] : 0.f;
-    for (int k = 0; k < q.blocks; ++k) {
-        if (q.carry && lane == 0) q.carry[row * q.blocks + k] = state;
-        float a[kTok], b[kTok];
-        float A = 1.f, B = 0.f;
-        const int64_t v0 = (int64_t)k * kBlock + lane * kTok;
+// The steps of a wave's lanes joined in the order of a walk up (or DOWN) the lanes.
+template <bool DOWN> struct WaveWalk {
+    float a, b;        // this lane's and all before it in its row of 16
+    float ra[4], rb[4];  // the rows, in the walk's order
+    __device__ __forceinline__ WaveWalk(float a_, float b_) : a(a_), b(b_) {
+        constexpr int SH = DOWN ? 0x100 : 0x110;  // row_shl, row_shr
+        join<SH + 1>();
+        join<SH + 2>();
+        join<SH + 4>();
+        join<SH + 8>();
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const int last = DOWN ? 16 * (3 - k) : 16 * k + 15;
+            ra[k] = lane_of(a, last);
+            rb[k] = lane_of(b, last);
+        }
+    }
+    template <int CTRL> __device__ __forceinline__ void join() {
+        const float pa = dpp_or<CTRL>(1.f, a), pb = dpp_or<CTRL>(0.f, b);
+        b = __builtin_fmaf(a, pb, b);
+        a *= pa;
+    }
+    // the whole wave
+    __device__ __forceinline__ float2 all() const {
+        float A = ra[0], B = rb[0];
+#pragma unroll
+        for (int k = 1; k < 4; ++k) {
+            B = __builtin_fmaf(ra[k], B, rb[k]);
+            A *= ra[k];
+        }
+        return make_float2(A, B);
+    }
+    // what this lane begins with, if the wave begins with s
+    __device__ __forceinline__ float begin(float s) const {
+        const int row = (threadIdx.x >> 4) & 3, k = DOWN ? 3 - row : row;
+        float t = s;
+#pragma unroll
+        for (int j = 0; j < 3; ++j) {
+            s = __builtin_fmaf(ra[j], s, rb[j]);
+            t = k > j ? s : t;
+        }
+        constexpr int BY1 = DOWN ? 0x101 : 0x111;
+        return __builtin_fmaf(dpp_or<BY1>(1.f, a), t, dpp_or<BY1>(0.f, b));
+    }
+};
+
+// A lane's voxels of a row, `at` the first of them, `over` of them behind the row's end.
+// They are read from `from` on, no further than the end (a row has at least as many), and
+// shifted; stores leave them out.
+template <typename T> struct Place {
+    int64_t at, from;
+    int over;
+    uint32_t live;  // bit j: voxel at + j is there and not masked
+    template <bool ALL> __device__ __forceinline__ void find(int64_t v, int64_t len) {
+        constexpr int TOK = tok<T>();
+        at = from = v;
+        over = 0;
+        live = (1u << TOK) - 1u;
+        if (!ALL && v + TOK > len) {
+            from = len - TOK;
+            over = v >= len ? TOK : (int)(v - from);
+            live >>= over;
+        }
+    }
+    template <bool ALL>
+    __device__ __forceinline__ Toks<T, tok<T>()> load(const T* row) const {
+        Toks<T, tok<T>()> t;
+        t.load(row + (ALL ? at : from), 0);
+        if (!ALL) t.shift(over);
+        return t;
+    }
+    __device__ __forceinline__ void apply(const uint8_t* mask) {
+        constexpr int TOK = tok<T>();
+        struct __attribute__((packed, aligned(1))) Bytes { uint32_t w[TOK / 4]; };
+        const Bytes m = *reinterpret_cast<const Bytes*>(mask + from);
         uint32_t on = 0;
 #pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-            const int64_t v = v0 + j, at = REV ? q.len - 1 - v : v;
-            a[j] = 1.f;
-            b[j] = 0.f;
-            if (v < q.len && (!mask || mask[at])) {
-                on |= 1u << j;
-                const Step s(Elt<T>::ld(r + at), w);
-                a[j] = s.a;
-                b[j] = s.p * s.inv * Sig(Elt<T>::ld(g + at)).s * Elt<T>::ld(x + at);
-            }
+        for (int j = 0; j < TOK; ++j) on |= (m.w[j / 4] >> (8 * (j & 3)) & 0xffu ? 1u : 0u) << j;
+        live &= on >> over;
+    }
+    // 0 where nothing is to be stored but a zero
+    __device__ __forceinline__ void clear(float (&o)[tok<T>()]) const {
+#pragma unroll
+        for (int j = 0; j < tok<T>(); ++j) o[j] = live >> j & 1u ? o[j] : 0.f;
+    }
+};
+
+// Raw inputs of a lane's voxels.  A row shorter than a lane's voxels is read by elements.
+template <typename T, int N> struct Raw {
+    Toks<T, tok<T>()> t[N];
+    Place<T> at;
+};
+template <typename T, int N, bool ALL>
+__device__ __forceinline__ void read(Raw<T, N>& d, const T* const (&row)[N], const uint8_t* mask,
+                                     int64_t v, int64_t len) {
+    d.at.template find<ALL>(v, len);
+#pragma unroll
+    for (int i = 0; i < N; ++i) d.t[i] = d.at.template load<ALL>(row[i]);
+    if (!ALL && mask) d.at.apply(mask);
+}
+
+// What the forward needs of a lane's voxels: the steps.
+template <typename T> struct Steps {
+    static constexpr int TOK = tok<T>();
+    float a[TOK], b[TOK];
+    // r, i, x as they lie; ALL: every voxel counts
+    template <bool ALL> __device__ __forceinline__ void form(const Raw<T, 3>& d, float w) {
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) {
+            const Step s(d.t[0][j], w);
+            const bool is = ALL || d.at.live >> j & 1u;
+            a[j] = is ? s.a : 1.f;
+            b[j] = is ? __builtin_amdgcn_sqrtf(s.p) * Sig(d.t[1][j]).s * d.t[2][j] : 0.f;
+        }
+    }
+    template <bool DOWN> __device__ __forceinline__ float2 all() const {
+        float A = 1.f, B = 0.f;
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) {
+            const int j = DOWN ? TOK - 1 - k : k;
             B = __builtin_fmaf(a[j], B, b[j]);
             A *= a[j];
         }
-        scan_wave(A, B);
-        float pa = __shfl_up(A, 1), pb = __shfl_up(B, 1);
-        if (lane == 0) {
-            pa = 1.f;
-            pb = 0.f;
-        }
-        float h = __builtin_fmaf(pa, state, pb);
-#pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-            const int64_t v = v0 + j, at = REV ? q.len - 1 - v : v;
-            h = __builtin_fmaf(a[j], h, b[j]);
-            if (v < q.len) Elt<T>::st(y + at, on >> j & 1u ? h : 0.f);
-        }
-        state = __shfl(h, 63);
+        return make_float2(A, B);
     }
-    if (q.h_last && lane == 0) q.h_last[row] = state;
+    // the states behind a lane's voxels, from that before them
+    template <bool DOWN> __device__ __forceinline__ void states(float h, float (&o)[TOK]) const {
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) {
+            const int j = DOWN ? TOK - 1 - k : k;
+            h = __builtin_fmaf(a[j], h, b[j]);
+            o[j] = h;
+        }
+    }
+};
+
+// What the backward needs: the steps, and the factors of the gradients.  DOWN is the way
+// of the gradient's walk, against the forward's.
+template <typename T, bool DOWN> struct GradSteps {
+    static constexpr int TOK = tok<T>();
+    float a[TOK], la[TOK], m[TOK], g[TOK], rr[TOK], ri[TOK], x[TOK], d[TOK];
+    // r, i, x, dy as they lie
+    template <bool ALL> __device__ __forceinline__ void form(const Raw<T, 4>& q, float w) {
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) {
+            const Step s(q.t[0][j], w);
+            const Sig gi(q.t[1][j]);
+            // at p = 0 (a shut gate) la inv and p inv come out as 0, their limits
+            const float inv = __builtin_amdgcn_rsqf(s.p < 0x1p-100f ? 0x1p-100f : s.p);
+            const bool is = ALL || q.at.live >> j & 1u;
+            a[j] = is ? s.a : 1.f;
+            la[j] = is ? s.la * s.a : 0.f;                        // by the past state
+            m[j] = is ? gi.s * (s.a * s.a) * (s.la * inv) : 0.f;  // by x
+            g[j] = is ? s.p * inv * gi.s : 0.f;                   // beta sigmoid(i)
+            rr[j] = is ? s.rest : 0.f;
+            ri[j] = is ? gi.rest : 0.f;
+            x[j] = is ? q.t[2][j] : 0.f;
+            d[j] = is ? q.t[3][j] : 0.f;
+        }
+    }
+    // the lane's steps of the gradient's walk, and the inhomogeneous part of the forward's
+    __device__ __forceinline__ void all(float& A, float& B, float& F) const {
+        A = 1.f;
+        B = F = 0.f;
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) {
+            const int j = DOWN ? TOK - 1 - k : k, i = DOWN ? k : TOK - 1 - k;
+            A *= a[j];
+            B = a[j] * (d[j] + B);
+            F = __builtin_fmaf(a[i], F, g[i] * x[i]);
+        }
+    }
+    // dr, di, dx from E behind the lane's voxels and h before them; returns the sum of K
+    __device__ __forceinline__ float grads(float E, float h, float (&dr)[TOK], float (&di)[TOK],
+                                           float (&dx)[TOK]) const {
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) {  // dr holds la a h_{t-1} first
+            const int j = DOWN ? k : TOK - 1 - k;
+            dr[j] = la[j] * h;
+            h = __builtin_fmaf(a[j], h, g[j] * x[j]);
+        }
+        float sum = 0.f;
+#pragma unroll
+        for (int k = 0; k < TOK; ++k) {
+            const int j = DOWN ? TOK - 1 - k : k;
+            const float D = d[j] + E;
+            E = a[j] * D;
+            const float K = D * __builtin_fmaf(-m[j], x[j], dr[j]);
+            sum += K;
+            dr[j] = K * rr[j];
+            dx[j] = D * g[j];
+            di[j] = dx[j] * x[j] * ri[j];
+        }
+        return sum;
+    }
+};
+
+// The walk's state at the beginning of a segment: the segments before it joined.
+__device__ __forceinline__ float segment_begin(const RecArgs& q, int64_t row, int seg) {
+    if (q.segs == 1) return q.h0 ? q.h0[row] : 0.f;
+    const float2* join = (const float2*)q.joined + row * q.segs;
+    float s = q.joined[2 * q.rows * q.segs + row];
+    for (int k = 0; k < seg; ++k) s = __builtin_fmaf(join[k].x, s, join[k].y);
+    return s;
 }
 
-template <typename T, bool REV>
-__global__ __launch_bounds__(64) void recurrence_bwd_k(RecArgs q) {
-    const int lane = threadIdx.x;
-    const int64_t row = blockIdx.x;
+// The blocks of a segment, first to last in the order of the walk.
+struct Segment {
+    int first, count;  // `first` counted in the walk's order
+    __device__ __forceinline__ Segment(const RecArgs& q, int seg) {
+        const int size = (q.blocks + q.segs - 1) / q.segs;
+        first = seg * size;
+        count = q.blocks - first < size ? q.blocks - first : size;
+        if (count < 0) count = 0;
+    }
+};
+
+// Rows beyond 16 lanes: a workgroup a segment of a row.  JOIN: only the segments' steps.
+template <typename T, bool DOWN, bool JOIN>
+__global__ __launch_bounds__(64 * kWaves) void recurrence_fwd_k(RecArgs q) {
+    constexpr int TOK = tok<T>(), BLOCK = block<T>();
+    __shared__ float2 tot[2][kWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int64_t row = blockIdx.x / q.segs;
+    const int seg = blockIdx.x - (int)(row * q.segs);
     const int64_t vol = row / q.c;
     const int ch = (int)(row - vol * q.c);
     const float w = q.rate * softplusf(q.lam[ch]);
-    const T* r = (const T*)q.r + vol * q.sr + (int64_t)ch * q.len;
-    const T* g = (const T*)q.i + vol * q.si + (int64_t)ch * q.len;
-    const T* x = (const T*)q.x + vol * q.sx + (int64_t)ch * q.len;
-    const T* dy = (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len;
+    const T* const in[3] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len};
+    T* y = (T*)q.y + vol * q.sy + (int64_t)ch * q.len;
+    const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
+    const Segment sg(q, seg);
+    float state = JOIN ? 0.f : segment_begin(q, row, seg), prod = 1.f;
+
+    auto place = [&](int k) {  // the block in memory of the walk's k-th
+        return DOWN ? q.blocks - 1 - (sg.first + k) : sg.first + k;
+    };
+    auto whole = [&](int k) { return !mask && (int64_t)(place(k) + 1) * BLOCK <= q.len; };
+    Raw<T, 3> cur, nxt;
+    auto fetch = [&](Raw<T, 3>& d, int k) {
+        if (k >= sg.count) return;
+        const int64_t v = (int64_t)place(k) * BLOCK + lane * TOK;
+        if (whole(k)) read<T, 3, true>(d, in, mask, v, q.len);
+        else read<T, 3, false>(d, in, mask, v, q.len);
+    };
+    fetch(cur, wave);
+    int par = 0;
+    for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
+        const int k = k0 + wave;
+        fetch(nxt, k + waves);
+        const bool all = k < sg.count && whole(k);
+        Steps<T> s;
+        if (k >= sg.count) cur.at.live = 0;  // steps that change nothing
+        if (all) s.template form<true>(cur, w);
+        else s.template form<false>(cur, w);
+        const float2 mine = s.template all<DOWN>();
+        const WaveWalk<DOWN> walk(mine.x, mine.y);
+        if (lane == 0) tot[par][wave] = walk.all();
+        __syncthreads();  // one a turn: the next turn writes the other half
+        float begin = state;
+        for (int j = 0; j < waves; ++j) {
+            const float2 o = tot[par][j];
+            if (j == wave) begin = state;
+            state = __builtin_fmaf(o.x, state, o.y);
+            if (JOIN) prod *= o.x;
+        }
+        if (!JOIN && k < sg.count) {
+            if (q.carry && lane == 0) q.carry[row * q.blocks + place(k)] = begin;
+            float o[TOK];
+            s.template states<DOWN>(walk.begin(begin), o);
+            if (all) {
+                put_tokens<T, TOK, true>(y + cur.at.at, 0, TOK, o, q.stream);
+            } else {
+                cur.at.clear(o);
+                put_tokens<T, TOK, false>(y + cur.at.at, 0, TOK - cur.at.over, o, q.stream);
+            }
+        }
+        cur = nxt;
+    }
+    if (threadIdx.x == 0) {
+        if (JOIN) {
+            ((float2*)q.joined)[row * q.segs + seg] = make_float2(prod, state);
+            // kept, for the walk's last state may take the first one's place
+            if (seg == 0) q.joined[2 * q.rows * q.segs + row] = q.h0 ? q.h0[row] : 0.f;
+        } else if (q.h_last && seg == q.segs - 1) {
+            q.h_last[row] = state;
+        }
+    }
+}
+
+// DOWN: the way of the gradient's walk, against that of the forward.
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_k(RecArgs q) {
+    constexpr int TOK = tok<T>(), BLOCK = block<T>();
+    __shared__ float2 tot[2][kWaves];
+    __shared__ double sums[kWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int64_t row = blockIdx.x / q.segs;
+    const int seg = blockIdx.x - (int)(row * q.segs);
+    const int64_t vol = row / q.c;
+    const int ch = (int)(row - vol * q.c);
+    const float w = q.rate * softplusf(q.lam[ch]);
+    const T* const in[4] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len,
+                            (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
     T* dr = (T*)q.dr + vol * q.sr + (int64_t)ch * q.len;
     T* di = (T*)q.di + vol * q.si + (int64_t)ch * q.len;
     T* dx = (T*)q.dx + vol * q.sx + (int64_t)ch * q.len;
     const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
-    float end = q.dh ? q.dh[row] : 0.f;  // E behind the block
+    const Segment sg(q, seg);
+    float state = segment_begin(q, row, seg);  // E
     double sum = 0.0;
-    for (int k = q.blocks - 1; k >= 0; --k) {
-        float a[kTok], b[kTok], la[kTok], rr[kTok], inv[kTok], p[kTok], si[kTok], ri[kTok], xv[kTok],
-            d[kTok];
-        const int64_t v0 = (int64_t)k * kBlock + lane * kTok;
-        uint32_t on = 0;
-        float A = 1.f, B = 0.f;
-#pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-            const int64_t v = v0 + j, at = REV ? q.len - 1 - v : v;
-            a[j] = 1.f;
-            b[j] = la[j] = rr[j] = inv[j] = p[j] = si[j] = ri[j] = xv[j] = d[j] = 0.f;
-            if (v < q.len && (!mask || mask[at])) {
-                on |= 1u << j;
-                const Step s(Elt<T>::ld(r + at), w);
-                a[j] = s.a;
-                la[j] = s.la;
-                rr[j] = s.rest;
-                p[j] = s.p;
-                inv[j] = s.inv;
-                const Sig gi(Elt<T>::ld(g + at));
-                si[j] = gi.s;
-                ri[j] = gi.rest;
-                xv[j] = Elt<T>::ld(x + at);
-                d[j] = Elt<T>::ld(dy + at);
-                b[j] = p[j] * inv[j] * si[j] * xv[j];
-            }
-            B = __builtin_fmaf(a[j], B, b[j]);
-            A *= a[j];
+
+    auto place = [&](int k) { return DOWN ? q.blocks - 1 - (sg.first + k) : sg.first + k; };
+    auto whole = [&](int k) { return !mask && (int64_t)(place(k) + 1) * BLOCK <= q.len; };
+    Raw<T, 4> cur, nxt;
+    float past0 = 0.f, past1 = 0.f;  // the states before the blocks
+    auto fetch = [&](Raw<T, 4>& d, float& past, int k) {
+        if (k >= sg.count) return;
+        past = q.carry[row * q.blocks + place(k)];
+        const int64_t v = (int64_t)place(k) * BLOCK + lane * TOK;
+        if (whole(k)) read<T, 4, true>(d, in, mask, v, q.len);
+        else read<T, 4, false>(d, in, mask, v, q.len);
+    };
+    fetch(cur, past0, wave);
+    int par = 0;
+    for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
+        const int k = k0 + wave;
+        fetch(nxt, past1, k + waves);
+        const bool all = k < sg.count && whole(k);
+        GradSteps<T, DOWN> s;
+        if (k >= sg.count) cur.at.live = 0;
+        if (all) s.template form<true>(cur, w);
+        else s.template form<false>(cur, w);
+        float A, B, F;
+        s.all(A, B, F);
+        const WaveWalk<DOWN> walk(A, B);
+        if (lane == 0) tot[par][wave] = walk.all();
+        const float h = WaveWalk<!DOWN>(A, F).begin(past0);
+        __syncthreads();
+        float begin = state;
+        for (int j = 0; j < waves; ++j) {
+            const float2 o = tot[par][j];
+            if (j == wave) begin = state;
+            state = __builtin_fmaf(o.x, state, o.y);
         }
-        scan_wave(A, B);
-        float pa = __shfl_up(A, 1), pb = __shfl_up(B, 1);
-        if (lane == 0) {
-            pa = 1.f;
-            pb = 0.f;
+        if (k < sg.count) {
+            float o[3][TOK];
+            sum += (double)s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+            auto put = [&](auto all) {
+                constexpr bool ALL = decltype(all)::value;
+                const int left = TOK - cur.at.over;
+                if (!ALL)
+                    for (auto& v : o) cur.at.clear(v);
+                put_tokens<T, TOK, ALL>(dr + cur.at.at, 0, left, o[0], q.stream);
+                put_tokens<T, TOK, ALL>(di + cur.at.at, 0, left, o[1], q.stream);
+                put_tokens<T, TOK, ALL>(dx + cur.at.at, 0, left, o[2], q.stream);
+            };
+            if (all) put(std::true_type{});
+            else put(std::false_type{});
         }
-        float h = __builtin_fmaf(pa, q.carry[row * q.blocks + k], pb);
-        float past[kTok];
-#pragma unroll
-        for (int j = 0; j < kTok; ++j) {
-            past[j] = h;
-            h = __builtin_fmaf(a[j], h, b[j]);
-        }
-        // the walk back: the last lane comes first
-        A = 1.f;
-        B = 0.f;
-#pragma unroll
-        for (int j = kTok - 1; j >= 0; --j) {
-            B = a[j] * (d[j] + B);
-            A *= a[j];
-        }
-        A = __shfl(A, 63 - lane);
-        B = __shfl(B, 63 - lane);
-        scan_wave(A, B);
-        const float total = __builtin_fmaf(__shfl(A, 63), end, __shfl(B, 63));
-        pa = __shfl_up(A, 1);
-        pb = __shfl_up(B, 1);
-        if (lane == 0) {
-            pa = 1.f;
-            pb = 0.f;
-        }
-        pa = __shfl(pa, 63 - lane);
-        pb = __shfl(pb, 63 - lane);
-        float E = __builtin_fmaf(pa, end, pb);
-        float part = 0.f;
-#pragma unroll
-        for (int j = kTok - 1; j >= 0; --j) {
-            const int64_t v = v0 + j, at = REV ? q.len - 1 - v : v;
-            const float D = d[j] + E;
-            E = a[j] * D;
-            const float u = si[j] * xv[j];
-            const float K = D * (la[j] * a[j] * past[j] - u * (a[j] * a[j]) * (la[j] * inv[j]));
-            const float gx = D * (p[j] * inv[j]) * si[j];
-            const bool live = on >> j & 1u;
-            part += live ? K : 0.f;
-            if (v < q.len) {
-                Elt<T>::st(dr + at, live ? K * rr[j] : 0.f);
-                Elt<T>::st(di + at, live ? gx * xv[j] * ri[j] : 0.f);
-                Elt<T>::st(dx + at, live ? gx : 0.f);
-            }
-        }
-        sum += (double)part;
-        end = total;
+        cur = nxt;
+        past0 = past1;
     }
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) sums[wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int j = 1; j < waves; ++j) sum += sums[j];
+        q.part[(int64_t)ch * (q.rows / q.c) * q.segs + vol * q.segs + seg] = (float)sum;
+        if (q.h_last && seg == q.segs - 1) q.h_last[row] = state;
+    }
+}
+
+// The gradient's walk through each segment: decays, and what reaches its end from dy.
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_join_k(RecArgs q) {
+    constexpr int TOK = tok<T>(), BLOCK = block<T>();
+    __shared__ float2 tot[2][kWaves];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int waves = blockDim.x >> 6;
+    const int64_t row = blockIdx.x / q.segs;
+    const int seg = blockIdx.x - (int)(row * q.segs);
+    const int64_t vol = row / q.c;
+    const int ch = (int)(row - vol * q.c);
+    const float w = q.rate * softplusf(q.lam[ch]);
+    const T* const in[2] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
+    const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
+    const Segment sg(q, seg);
+    float state = 0.f, prod = 1.f;
+    int par = 0;
+    for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
+        const int k = k0 + wave;
+        float A = 1.f, B = 0.f;
+        if (k < sg.count) {
+            const int at = DOWN ? q.blocks - 1 - (sg.first + k) : sg.first + k;
+            Raw<T, 2> d;
+            read<T, 2, false>(d, in, mask, (int64_t)at * BLOCK + lane * TOK, q.len);
+#pragma unroll
+            for (int e = 0; e < TOK; ++e) {
+                const int j = DOWN ? TOK - 1 - e : e;
+                const float a = __builtin_amdgcn_exp2f(-w * Sig(d.t[0][j]).s * 1.44269504f);
+                const bool is = d.at.live >> j & 1u;
+                B = is ? a * (d.t[1][j] + B) : B;
+                A = is ? A * a : A;
+            }
+        }
+        const WaveWalk<DOWN> walk(A, B);
+        if (lane == 0) tot[par][wave] = walk.all();
+        __syncthreads();
+        for (int j = 0; j < waves; ++j) {
+            const float2 o = tot[par][j];
+            state = __builtin_fmaf(o.x, state, o.y);
+            prod *= o.x;
+        }
+    }
+    if (threadIdx.x == 0) {
+        ((float2*)q.joined)[row * q.segs + seg] = make_float2(prod, state);
+        if (seg == 0) q.joined[2 * q.rows * q.segs + row] = q.h0 ? q.h0[row] : 0.f;
+    }
+}
+
+// Rows of up to 16 lanes: several a wave, each on `lanes` (a power of two) of them.
+template <typename T, int N>
+__device__ __forceinline__ void read_short(Raw<T, N>& d, const T* const (&row)[N],
+                                           const uint8_t* mask, int64_t v, int64_t len) {
+    constexpr int TOK = tok<T>();
+    if (len >= TOK) {
+        read<T, N, false>(d, row, mask, v, len);
+        return;
+    }
+    // by elements, those behind the end as the last one
+    d.at.template find<false>(v, len);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        T e[TOK];
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) e[j] = row[i][j < len ? j : len - 1];
+#pragma unroll
+        for (int j = 0; j < TOK; ++j) {
+            if constexpr (sizeof(T) == 4) d.t[i].u.w[j] = __float_as_uint(e[j]);
+            else if (j & 1) d.t[i].u.w[j / 2] |= (uint32_t)e[j] << 16;
+            else d.t[i].u.w[j / 2] = e[j];
+        }
+    }
+    if (mask)
+#pragma unroll
+        for (int j = 0; j < TOK; ++j)
+            if (!mask[j < len ? j : len - 1]) d.at.live &= ~(1u << j);
+}
+
+// Joins the lanes of each row up (or DOWN) and returns what the lane begins with if its
+// row begins with s; s becomes what the row ends with.
+template <bool DOWN> __device__ __forceinline__ float short_walk(float a, float b, int lanes, float& s) {
+    const int lane = threadIdx.x & (lanes - 1), k = DOWN ? lanes - 1 - lane : lane;
+    for (int m = 1; m < lanes; m <<= 1) {
+        const float pa = DOWN ? __shfl_down(a, m) : __shfl_up(a, m);
+        const float pb = DOWN ? __shfl_down(b, m) : __shfl_up(b, m);
+        if (k >= m) {
+            b = __builtin_fmaf(a, pb, b);
+            a *= pa;
+        }
+    }
+    const float end = __builtin_fmaf(a, s, b);
+    const float before = DOWN ? __shfl_down(end, 1) : __shfl_up(end, 1);
+    const float begin = k == 0 ? s : before;
+    s = __shfl(end, (threadIdx.x & 63) - lane + (DOWN ? 0 : lanes - 1));
+    return begin;
+}
+
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(256) void recurrence_short_fwd_k(RecArgs q) {
+    constexpr int TOK = tok<T>();
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r_ = id / q.lanes, row = r_ < q.rows ? r_ : q.rows - 1;
+    const int lane = (int)(id & (q.lanes - 1));
+    const int64_t vol = row / q.c;
+    const int ch = (int)(row - vol * q.c);
+    const T* const in[3] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len};
+    Raw<T, 3> d;
+    read_short<T, 3>(d, in, q.mask ? q.mask + vol * q.len : nullptr, lane * TOK, q.len);
+    float state = q.h0 ? q.h0[row] : 0.f;
+    const float first = state;
+    Steps<T> s;
+    s.template form<false>(d, q.rate * softplusf(q.lam[ch]));
+    const float2 mine = s.template all<DOWN>();
+    float o[TOK];
+    s.template states<DOWN>(short_walk<DOWN>(mine.x, mine.y, q.lanes, state), o);
+    d.at.clear(o);
+    if (r_ >= q.rows) return;
+    put_tokens<T, TOK, false>((T*)q.y + vol * q.sy + (int64_t)ch * q.len + d.at.at, 0,
+                              TOK - d.at.over, o, false);
     if (lane == 0) {
-        q.part[(int64_t)ch * (gridDim.x / q.c) + vol] = (float)sum;
-        if (q.dh0) q.dh0[row] = end;
+        if (q.carry) q.carry[row] = first;
+        if (q.h_last) q.h_last[row] = state;
+    }
+}
+
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(256) void recurrence_short_bwd_k(RecArgs q) {
+    constexpr int TOK = tok<T>();
+    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t r_ = id / q.lanes, row = r_ < q.rows ? r_ : q.rows - 1;
+    const int lane = (int)(id & (q.lanes - 1));
+    const int64_t vol = row / q.c;
+    const int ch = (int)(row - vol * q.c);
+    const T* const in[4] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len,
+                            (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
+    Raw<T, 4> d;
+    read_short<T, 4>(d, in, q.mask ? q.mask + vol * q.len : nullptr, lane * TOK, q.len);
+    GradSteps<T, DOWN> s;
+    s.template form<false>(d, q.rate * softplusf(q.lam[ch]));
+    float A, B, F;
+    s.all(A, B, F);
+    float state = q.h0 ? q.h0[row] : 0.f, fwd = q.carry[row];
+    const float E = short_walk<DOWN>(A, B, q.lanes, state);
+    const float h = short_walk<!DOWN>(A, F, q.lanes, fwd);
+    float o[3][TOK];
+    float part = s.grads(E, h, o[0], o[1], o[2]);
+    for (auto& v : o) d.at.clear(v);
+    for (int m = q.lanes / 2; m >= 1; m >>= 1) part += __shfl_xor(part, m);
+    if (r_ >= q.rows) return;
+    const int64_t at = (int64_t)ch * q.len + d.at.at;
+    const int left = TOK - d.at.over;
+    put_tokens<T, TOK, false>((T*)q.dr + vol * q.sr + at, 0, left, o[0], false);
+    put_tokens<T, TOK, false>((T*)q.di + vol * q.si + at, 0, left, o[1], false);
+    put_tokens<T, TOK, false>((T*)q.dx + vol * q.sx + at, 0, left, o[2], false);
+    if (lane == 0) {
+        q.part[(int64_t)ch * (q.rows / q.c) + vol] = part;
+        if (q.h_last) q.h_last[row] = state;
     }
 }
 
@@ -250,24 +645,50 @@ __global__ __launch_bounds__(256) void recurrence_lambda_k(const float* __restri
 }
 
 // ------------------------------------------------------------------ host
-static void rec_plan(const rat3d_recurrence_desc& d, RecArgs* q) {
+static void rec_plan(const rat3d_recurrence_desc& d, RecArgs* q, int* waves) {
     const int64_t packed = (int64_t)d.c * d.len;
+    const int tok = d.dtype == RAT3D_BF16 ? 8 : 4;
     q->sr = d.r_stride ? d.r_stride : packed;
     q->si = d.i_stride ? d.i_stride : packed;
     q->sx = d.x_stride ? d.x_stride : packed;
     q->sy = d.y_stride ? d.y_stride : packed;
     q->len = d.len;
     q->c = d.c;
-    q->blocks = (int)ceil_div(d.len, kBlock);
+    q->rows = (int64_t)d.n * d.c;
     q->rate = d.rate;
+    q->blocks = (int)ceil_div(d.len, 64 * tok);
+    q->segs = 1;
+    q->lanes = 0;
+    q->stream = (double)packed * d.n * 16 / tok > 256e6;
+    if (d.len <= 16 * tok) {
+        q->lanes = 1;
+        while (q->lanes * tok < d.len) q->lanes *= 2;
+        return;
+    }
+    *waves = q->blocks < 8 ? q->blocks : 8;
+    // two workgroups a CU
+    const int64_t want = ceil_div(2 * (int64_t)device_cus(), q->rows);
+    const int64_t most = ceil_div(q->blocks, *waves);
+    const int64_t segs = want < most ? want : most;
+    q->segs = (int)(segs < kSegs ? segs : kSegs);
 }
 
 size_t recurrence_carry_bytes(const rat3d_recurrence_desc& d) {
-    return (size_t)d.n * d.c * ceil_div(d.len, kBlock) * sizeof(float);
+    RecArgs q = {};
+    int waves;
+    rec_plan(d, &q, &waves);
+    return (size_t)q.rows * q.blocks * sizeof(float);
 }
 
+// The joined segments and first states, then the parts of dlambda.
+static size_t rec_joined(const RecArgs& q) {
+    return q.segs > 1 ? (size_t)q.rows * (2 * q.segs + 1) : 0;
+}
 size_t recurrence_ws_bytes(const rat3d_recurrence_desc& d, int pass) {
-    return pass ? (size_t)d.n * d.c * sizeof(float) : 0;
+    RecArgs q = {};
+    int waves;
+    rec_plan(d, &q, &waves);
+    return (rec_joined(q) + (pass ? (size_t)q.rows * q.segs : 0)) * sizeof(float);
 }
 
 static double rec_bytes(const rat3d_recurrence_desc& d, int tensors) {
@@ -278,7 +699,8 @@ rat3d_status recurrence_fwd(const rat3d_recurrence_desc& d, const void* r, const
                             const void* x, const float* lam, const uint8_t* mask, const float* h0,
                             void* y, float* h_last, float* carry, void* ws, hipStream_t st) {
     RecArgs q = {};
-    rec_plan(d, &q);
+    int waves = 0;
+    rec_plan(d, &q, &waves);
     q.r = r;
     q.i = i;
     q.x = x;
@@ -288,16 +710,41 @@ rat3d_status recurrence_fwd(const rat3d_recurrence_desc& d, const void* r, const
     q.y = y;
     q.h_last = h_last;
     q.carry = carry;
-    const unsigned grid = (unsigned)(d.n * d.c);
-    ProfScope ps("recurrence_fwd", st, 0.0, rec_bytes(d, 4));
-    if (d.dtype == RAT3D_BF16) {
-        if (d.reverse) recurrence_fwd_k<bf16, true><<<grid, 64, 0, st>>>(q);
-        else recurrence_fwd_k<bf16, false><<<grid, 64, 0, st>>>(q);
-    } else {
-        if (d.reverse) recurrence_fwd_k<float, true><<<grid, 64, 0, st>>>(q);
-        else recurrence_fwd_k<float, false><<<grid, 64, 0, st>>>(q);
+    q.joined = (float*)ws;
+    if (q.lanes) {
+        const unsigned grid = (unsigned)ceil_div(q.rows * q.lanes, 256);
+        ProfScope ps("recurrence_short_fwd", st, 0.0, rec_bytes(d, 4));
+#define RAT3D_REC(T, DOWN) recurrence_short_fwd_k<T, DOWN><<<grid, 256, 0, st>>>(q)
+        if (d.dtype == RAT3D_BF16) {
+            if (d.reverse) RAT3D_REC(bf16, true);
+            else RAT3D_REC(bf16, false);
+        } else {
+            if (d.reverse) RAT3D_REC(float, true);
+            else RAT3D_REC(float, false);
+        }
+#undef RAT3D_REC
+        RAT3D_LAUNCH_CHECK();
+        return RAT3D_OK;
     }
-    RAT3D_LAUNCH_CHECK();
+    const unsigned grid = (unsigned)(q.rows * q.segs), threads = 64 * waves;
+#define RAT3D_REC(JOIN)                                                                       \
+    do {                                                                                      \
+        if (d.dtype == RAT3D_BF16) {                                                          \
+            if (d.reverse) recurrence_fwd_k<bf16, true, JOIN><<<grid, threads, 0, st>>>(q);   \
+            else recurrence_fwd_k<bf16, false, JOIN><<<grid, threads, 0, st>>>(q);            \
+        } else {                                                                              \
+            if (d.reverse) recurrence_fwd_k<float, true, JOIN><<<grid, threads, 0, st>>>(q);  \
+            else recurrence_fwd_k<float, false, JOIN><<<grid, threads, 0, st>>>(q);           \
+        }                                                                                     \
+        RAT3D_LAUNCH_CHECK();                                                                 \
+    } while (0)
+    if (q.segs > 1) {
+        ProfScope ps("recurrence_fwd_join", st, 0.0, rec_bytes(d, 3));
+        RAT3D_REC(true);
+    }
+    ProfScope ps(q.segs > 1 ? "recurrence_fwd_cut" : "recurrence_fwd", st, 0.0, rec_bytes(d, 4));
+    RAT3D_REC(false);
+#undef RAT3D_REC
     return RAT3D_OK;
 }
 
@@ -306,9 +753,10 @@ rat3d_status recurrence_bwd(const rat3d_recurrence_desc& d, const void* dy, cons
                             const uint8_t* mask, const float* carry, void* dr, void* di, void* dx,
                             float* dlam, float* dh0, int accumulate, void* ws, hipStream_t st) {
     RecArgs q = {};
-    rec_plan(d, &q);
+    int waves = 0;
+    rec_plan(d, &q, &waves);
     q.dy = dy;
-    q.dh = dh_last;
+    q.h0 = dh_last;
     q.r = r;
     q.i = i;
     q.x = x;
@@ -318,22 +766,38 @@ rat3d_status recurrence_bwd(const rat3d_recurrence_desc& d, const void* dy, cons
     q.dr = dr;
     q.di = di;
     q.dx = dx;
-    q.dh0 = dh0;
-    q.part = (float*)ws;
-    const unsigned grid = (unsigned)(d.n * d.c);
-    {
-        ProfScope ps("recurrence_bwd", st, 0.0, rec_bytes(d, 7));
-        if (d.dtype == RAT3D_BF16) {
-            if (d.reverse) recurrence_bwd_k<bf16, true><<<grid, 64, 0, st>>>(q);
-            else recurrence_bwd_k<bf16, false><<<grid, 64, 0, st>>>(q);
-        } else {
-            if (d.reverse) recurrence_bwd_k<float, true><<<grid, 64, 0, st>>>(q);
-            else recurrence_bwd_k<float, false><<<grid, 64, 0, st>>>(q);
+    q.h_last = dh0;
+    q.joined = (float*)ws;
+    q.part = (float*)ws + rec_joined(q);
+    // the gradient walks against the forward
+#define RAT3D_REC(KERNEL, GRID, THREADS)                                           \
+    do {                                                                           \
+        if (d.dtype == RAT3D_BF16) {                                               \
+            if (d.reverse) KERNEL<bf16, false><<<GRID, THREADS, 0, st>>>(q);       \
+            else KERNEL<bf16, true><<<GRID, THREADS, 0, st>>>(q);                  \
+        } else {                                                                   \
+            if (d.reverse) KERNEL<float, false><<<GRID, THREADS, 0, st>>>(q);      \
+            else KERNEL<float, true><<<GRID, THREADS, 0, st>>>(q);                 \
+        }                                                                          \
+        RAT3D_LAUNCH_CHECK();                                                      \
+    } while (0)
+    if (q.lanes) {
+        const unsigned grid = (unsigned)ceil_div(q.rows * q.lanes, 256);
+        ProfScope ps("recurrence_short_bwd", st, 0.0, rec_bytes(d, 7));
+        RAT3D_REC(recurrence_short_bwd_k, grid, 256);
+    } else {
+        const unsigned grid = (unsigned)(q.rows * q.segs), threads = 64 * waves;
+        if (q.segs > 1) {
+            ProfScope ps("recurrence_bwd_join", st, 0.0, rec_bytes(d, 2));
+            RAT3D_REC(recurrence_bwd_join_k, grid, threads);
         }
-        RAT3D_LAUNCH_CHECK();
+        ProfScope ps(q.segs > 1 ? "recurrence_bwd_cut" : "recurrence_bwd", st, 0.0, rec_bytes(d, 7));
+        RAT3D_REC(recurrence_bwd_k, grid, threads);
     }
-    ProfScope ps("recurrence_lambda", st, 0.0, 4.0 * d.n * d.c);
-    recurrence_lambda_k<<<d.c, 256, 0, st>>>(q.part, d.n, lam, dlam, accumulate);
+#undef RAT3D_REC
+    const int parts = d.n * q.segs;
+    ProfScope ps("recurrence_lambda", st, 0.0, 4.0 * parts * d.c);
+    recurrence_lambda_k<<<d.c, 256, 0, st>>>(q.part, parts, lam, dlam, accumulate);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }

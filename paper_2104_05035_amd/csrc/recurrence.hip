@@ -30,7 +30,7 @@ namespace rat3d {
 
 template <typename T> constexpr int tok() { return 16 / (int)sizeof(T); }  // voxels a lane
 template <typename T> constexpr int block() { return 64 * tok<T>(); }      // voxels a wave
-constexpr int kWaves = 8;   // of a workgroup, at most
+constexpr int kWaves = 16;  // of a workgroup, at most
 constexpr int kSegs = 64;   // segments of a row, at most
 
 struct RecArgs {
@@ -67,6 +67,7 @@ struct Step {
         s = __builtin_fmaf(t, s, 1.f / 6.f);
         s = __builtin_fmaf(t, s, -0.5f);
         s = t * __builtin_fmaf(t, s, 1.f);
+        asm volatile("" : "+v"(s));  // formed in every lane: a branch would keep voxels apart
         p = t < 0.125f ? s : __builtin_fmaf(-a, a, 1.f);
     }
 };
@@ -276,13 +277,16 @@ template <typename T, bool DOWN> struct GradSteps {
     }
 };
 
-// The walk's state at the beginning of a segment: the segments before it joined.
+// The walk's state at the beginning of a segment: the segments before it joined, one a
+// lane, so that their loads are under way together.
 __device__ __forceinline__ float segment_begin(const RecArgs& q, int64_t row, int seg) {
+    static_assert(kSegs <= 64, "a segment a lane");
     if (q.segs == 1) return q.h0 ? q.h0[row] : 0.f;
-    const float2* join = (const float2*)q.joined + row * q.segs;
-    float s = q.joined[2 * q.rows * q.segs + row];
-    for (int k = 0; k < seg; ++k) s = __builtin_fmaf(join[k].x, s, join[k].y);
-    return s;
+    const int lane = threadIdx.x & 63;
+    const float2 o = ((const float2*)q.joined)[row * q.segs + (lane < seg ? lane : 0)];
+    const float s = q.joined[2 * q.rows * q.segs + row];
+    const float2 all = WaveWalk<false>(lane < seg ? o.x : 1.f, lane < seg ? o.y : 0.f).all();
+    return __builtin_fmaf(all.x, s, all.y);
 }
 
 // The blocks of a segment, first to last in the order of the walk.
@@ -298,24 +302,21 @@ struct Segment {
 
 // Rows beyond 16 lanes: a workgroup a segment of a row.  JOIN: only the segments' steps.
 template <typename T, bool DOWN, bool JOIN>
-__global__ __launch_bounds__(64 * kWaves) void recurrence_fwd_k(RecArgs q) {
+__global__ __launch_bounds__(64 * kWaves, 8) void recurrence_fwd_k(RecArgs q) {
     constexpr int TOK = tok<T>(), BLOCK = block<T>();
     __shared__ float2 tot[2][kWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    const int64_t row = blockIdx.x / q.segs;
-    const int seg = blockIdx.x - (int)(row * q.segs);
-    const int64_t vol = row / q.c;
-    const int ch = (int)(row - vol * q.c);
-    const float w = q.rate * softplusf(q.lam[ch]);
+    const uint32_t row_ = blockIdx.x / (uint32_t)q.segs, vol_ = row_ / (uint32_t)q.c;
+    const int seg = (int)(blockIdx.x - row_ * q.segs), ch = (int)(row_ - vol_ * q.c);
+    const int64_t row = row_, vol = vol_;
+    const float lam = q.lam[ch];
     const T* const in[3] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
                             (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
                             (const T*)q.x + vol * q.sx + (int64_t)ch * q.len};
     T* y = (T*)q.y + vol * q.sy + (int64_t)ch * q.len;
     const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
     const Segment sg(q, seg);
-    float state = JOIN ? 0.f : segment_begin(q, row, seg), prod = 1.f;
-
     auto place = [&](int k) {  // the block in memory of the walk's k-th
         return DOWN ? q.blocks - 1 - (sg.first + k) : sg.first + k;
     };
@@ -327,7 +328,9 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_fwd_k(RecArgs q) {
         if (whole(k)) read<T, 3, true>(d, in, mask, v, q.len);
         else read<T, 3, false>(d, in, mask, v, q.len);
     };
-    fetch(cur, wave);
+    fetch(cur, wave);  // under way while the walk's beginning is found
+    const float w = q.rate * softplusf(lam);
+    float state = JOIN ? 0.f : segment_begin(q, row, seg), prod = 1.f;
     int par = 0;
     for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
         const int k = k0 + wave;
@@ -374,17 +377,16 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_fwd_k(RecArgs q) {
 
 // DOWN: the way of the gradient's walk, against that of the forward.
 template <typename T, bool DOWN>
-__global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_k(RecArgs q) {
+__global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_k(RecArgs q) {
     constexpr int TOK = tok<T>(), BLOCK = block<T>();
     __shared__ float2 tot[2][kWaves];
     __shared__ double sums[kWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    const int64_t row = blockIdx.x / q.segs;
-    const int seg = blockIdx.x - (int)(row * q.segs);
-    const int64_t vol = row / q.c;
-    const int ch = (int)(row - vol * q.c);
-    const float w = q.rate * softplusf(q.lam[ch]);
+    const uint32_t row_ = blockIdx.x / (uint32_t)q.segs, vol_ = row_ / (uint32_t)q.c;
+    const int seg = (int)(blockIdx.x - row_ * q.segs), ch = (int)(row_ - vol_ * q.c);
+    const int64_t row = row_, vol = vol_;
+    const float lam = q.lam[ch];
     const T* const in[4] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
                             (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
                             (const T*)q.x + vol * q.sx + (int64_t)ch * q.len,
@@ -394,9 +396,6 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_k(RecArgs q) {
     T* dx = (T*)q.dx + vol * q.sx + (int64_t)ch * q.len;
     const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
     const Segment sg(q, seg);
-    float state = segment_begin(q, row, seg);  // E
-    double sum = 0.0;
-
     auto place = [&](int k) { return DOWN ? q.blocks - 1 - (sg.first + k) : sg.first + k; };
     auto whole = [&](int k) { return !mask && (int64_t)(place(k) + 1) * BLOCK <= q.len; };
     Raw<T, 4> cur, nxt;
@@ -409,6 +408,9 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_k(RecArgs q) {
         else read<T, 4, false>(d, in, mask, v, q.len);
     };
     fetch(cur, past0, wave);
+    const float w = q.rate * softplusf(lam);
+    float state = segment_begin(q, row, seg);  // E
+    double sum = 0.0;
     int par = 0;
     for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
         const int k = k0 + wave;
@@ -466,15 +468,15 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_join_k(RecArgs q) 
     __shared__ float2 tot[2][kWaves];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int waves = blockDim.x >> 6;
-    const int64_t row = blockIdx.x / q.segs;
-    const int seg = blockIdx.x - (int)(row * q.segs);
-    const int64_t vol = row / q.c;
-    const int ch = (int)(row - vol * q.c);
-    const float w = q.rate * softplusf(q.lam[ch]);
+    const uint32_t row_ = blockIdx.x / (uint32_t)q.segs, vol_ = row_ / (uint32_t)q.c;
+    const int seg = (int)(blockIdx.x - row_ * q.segs), ch = (int)(row_ - vol_ * q.c);
+    const int64_t row = row_, vol = vol_;
+    const float lam = q.lam[ch];
     const T* const in[2] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
                             (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
     const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
     const Segment sg(q, seg);
+    const float w = q.rate * softplusf(lam);
     float state = 0.f, prod = 1.f;
     int par = 0;
     for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
@@ -559,11 +561,12 @@ template <bool DOWN> __device__ __forceinline__ float short_walk(float a, float 
 template <typename T, bool DOWN>
 __global__ __launch_bounds__(256) void recurrence_short_fwd_k(RecArgs q) {
     constexpr int TOK = tok<T>();
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r_ = id / q.lanes, row = r_ < q.rows ? r_ : q.rows - 1;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x;
+    const int64_t r_ = id >> (31 - __builtin_clz(q.lanes)), row = r_ < q.rows ? r_ : q.rows - 1;
     const int lane = (int)(id & (q.lanes - 1));
-    const int64_t vol = row / q.c;
+    const int64_t vol = (uint32_t)row / (uint32_t)q.c;
     const int ch = (int)(row - vol * q.c);
+    const float lam = q.lam[ch];
     const T* const in[3] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
                             (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
                             (const T*)q.x + vol * q.sx + (int64_t)ch * q.len};
@@ -572,7 +575,7 @@ __global__ __launch_bounds__(256) void recurrence_short_fwd_k(RecArgs q) {
     float state = q.h0 ? q.h0[row] : 0.f;
     const float first = state;
     Steps<T> s;
-    s.template form<false>(d, q.rate * softplusf(q.lam[ch]));
+    s.template form<false>(d, q.rate * softplusf(lam));
     const float2 mine = s.template all<DOWN>();
     float o[TOK];
     s.template states<DOWN>(short_walk<DOWN>(mine.x, mine.y, q.lanes, state), o);
@@ -589,11 +592,12 @@ __global__ __launch_bounds__(256) void recurrence_short_fwd_k(RecArgs q) {
 template <typename T, bool DOWN>
 __global__ __launch_bounds__(256) void recurrence_short_bwd_k(RecArgs q) {
     constexpr int TOK = tok<T>();
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int64_t r_ = id / q.lanes, row = r_ < q.rows ? r_ : q.rows - 1;
+    const uint32_t id = blockIdx.x * 256 + threadIdx.x;
+    const int64_t r_ = id >> (31 - __builtin_clz(q.lanes)), row = r_ < q.rows ? r_ : q.rows - 1;
     const int lane = (int)(id & (q.lanes - 1));
-    const int64_t vol = row / q.c;
+    const int64_t vol = (uint32_t)row / (uint32_t)q.c;
     const int ch = (int)(row - vol * q.c);
+    const float lam = q.lam[ch];
     const T* const in[4] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
                             (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
                             (const T*)q.x + vol * q.sx + (int64_t)ch * q.len,
@@ -601,7 +605,7 @@ __global__ __launch_bounds__(256) void recurrence_short_bwd_k(RecArgs q) {
     Raw<T, 4> d;
     read_short<T, 4>(d, in, q.mask ? q.mask + vol * q.len : nullptr, lane * TOK, q.len);
     GradSteps<T, DOWN> s;
-    s.template form<false>(d, q.rate * softplusf(q.lam[ch]));
+    s.template form<false>(d, q.rate * softplusf(lam));
     float A, B, F;
     s.all(A, B, F);
     float state = q.h0 ? q.h0[row] : 0.f, fwd = q.carry[row];
@@ -665,12 +669,20 @@ static void rec_plan(const rat3d_recurrence_desc& d, RecArgs* q, int* waves) {
         while (q->lanes * tok < d.len) q->lanes *= 2;
         return;
     }
-    *waves = q->blocks < 8 ? q->blocks : 8;
-    // two workgroups a CU
-    const int64_t want = ceil_div(2 * (int64_t)device_cus(), q->rows);
-    const int64_t most = ceil_div(q->blocks, *waves);
-    const int64_t segs = want < most ? want : most;
-    q->segs = (int)(segs < kSegs ? segs : kSegs);
+    // Eight waves a row (four take the same time from 1024 rows on), sixteen where a CU has
+    // one row or little more, and fewer rows cut until there are two workgroups a CU: a
+    // forward over 256 rows of 129024 voxels in bfloat16 takes 65 us with sixteen waves, 77
+    // with eight, 108 cut; over 128 rows 70 with eight waves, 59 cut.
+    const int64_t cus = device_cus();
+    int most = 8;
+    if (q->rows >= cus) {
+        if (2 * q->rows < 3 * cus && q->blocks >= 64) most = 16;
+    } else {
+        const int64_t want = ceil_div(2 * cus, q->rows), turns = ceil_div(q->blocks, most);
+        const int64_t segs = want < turns ? want : turns;
+        q->segs = (int)(segs < kSegs ? segs : kSegs);
+    }
+    *waves = q->blocks < most ? q->blocks : most;
 }
 
 size_t recurrence_carry_bytes(const rat3d_recurrence_desc& d) {

@@ -499,10 +499,14 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 
 // ------------------------------------------------------------------ host
 // Tokens and channels a thread, and groups of threads along the channels (whole waves).
-// Beyond 128 channels of bfloat16 the backward keeps half as many tokens of twice the
-// channels, so that a workgroup has 512 threads and their registers: 4 x 256 channels over
-// 64512 voxels 546 -> 280 us behind a block, 146 -> 136 before one; the forward does not
-// gain (145 and 153 us).
+// In bfloat16 half as many tokens,
+//   where there are fewer than two tiles a CU, so that one loads while another sums or
+//   stores: 16 x 128 channels of 12x14x12 voxels 15.3 -> 12.5 us behind a block, its
+//   gradient 34.9 -> 31.1, before a block 7.5 -> 6.5 and 16.4 -> 13.7 (at 8 x 64 of
+//   24x28x24, four tiles a CU, 18.4 -> 19.5 and 35.5 -> 36.9);
+//   in the backward of more than 128 channels, of twice the channels, so that a workgroup
+//   has 512 threads and their registers: 4 x 256 channels over 64512 voxels 546 -> 280 us
+//   behind a block, 146 -> 136 before one (the forward does not gain: 145 and 153 us).
 struct NormShape {
     int tok, pc, groups;
 };
@@ -511,9 +515,10 @@ static NormShape norm_shape(const rat3d_norm_desc& d, bool bwd) {
     // a group's rows are reached with 32 bits: at least 4 of them up to 2^28 tokens
     const int64_t most = ((int64_t)1 << 32) / (d.v * es);
     if (d.c <= 256) {
-        const bool half = bwd && tok == 8 && d.c > 128;
-        const int pc = half ? 8 : 4, groups = (int)ceil_div(d.c, 4 * pc) * 4;
-        if (groups <= most) return {half ? 4 : tok, pc, groups};
+        const bool wide = bwd && tok == 8 && d.c > 128;
+        const bool few = tok == 8 && ceil_div(d.v, kLanes * tok) * d.n < 2 * device_cus();
+        const int pc = wide ? 8 : 4, groups = (int)ceil_div(d.c, 4 * pc) * 4;
+        if (groups <= most) return {wide || few ? 4 : tok, pc, groups};
     }
     int groups = 16;
     while (groups > most) groups /= 2;
@@ -586,18 +591,23 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream
         if (all) RAT3D_NORM1(TOK, PC, true, THREADS); \
         else RAT3D_NORM1(TOK, PC, false, THREADS);    \
     } while (0)
+    // a workgroup has at most as many threads as its kernel is built for
     if (shape.tok == 1) {
         if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
         else RAT3D_NORM1(1, 0, false, 256);
     } else if (shape.pc == 0) {
         RAT3D_NORM(TOK, 0, 256);
-    } else if constexpr (!kBwd) {
-        RAT3D_NORM(TOK, 4, 1024);  // 128 registers are enough
-    } else {
-        if (threads <= 256 && shape.pc == 4) RAT3D_NORM(TOK, 4, 256);
-        else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(TOK, 4, 512);
-        else if constexpr (sizeof(T) == 2) RAT3D_NORM(4, 8, 512);
+    } else if constexpr (!kBwd) {  // 128 registers are enough
+        if (shape.tok == 4) RAT3D_NORM(4, 4, 1024);
+        else if constexpr (TOK == 8) RAT3D_NORM(8, 4, 1024);
+    } else if (shape.tok == 4) {
+        if (shape.pc == 4 && threads <= 256) RAT3D_NORM(4, 4, 256);
+        else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(4, 4, 512);
+        else if constexpr (TOK == 8) RAT3D_NORM(4, 8, 512);
         else RAT3D_NORM(4, 4, 1024);
+    } else if constexpr (TOK == 8) {
+        if (threads <= 256) RAT3D_NORM(8, 4, 256);
+        else RAT3D_NORM(8, 4, 512);
     }
 #undef RAT3D_NORM
 #undef RAT3D_NORM1
@@ -609,6 +619,16 @@ static void norm_launch(const rat3d_norm_desc& d, NormArgs& a, hipStream_t st) {
     if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, a, st);
     else norm_launch_t<float, MODE, GATED, NEXT>(d, a, st);
 }
+
+// Names of the measurement: channels held in registers (of 16 or 8 bytes of tokens), read
+// again for every sum, or single tokens.
+static const char* norm_tag(const rat3d_norm_desc& d, bool bwd, const char* const (&names)[4]) {
+    const NormShape s = norm_shape(d, bwd);
+    const int full = d.dtype == RAT3D_BF16 ? 8 : 4;
+    return names[s.tok == 1 ? 3 : s.pc == 0 ? 2 : s.tok < full ? 1 : 0];
+}
+#define RAT3D_NORM_TAG(name, bwd) \
+    norm_tag(d, bwd, {name, name "_half", name "_any", name "_one"})
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
     return (double)d.n * d.c * d.v * tensors * (d.dtype == RAT3D_BF16 ? 2 : 4);
@@ -622,7 +642,7 @@ rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* 
     a.gamma = gamma;
     a.mask = mask;
     a.ou = u;
-    ProfScope ps("pre_norm_fwd", st, 0.0, norm_bytes(d, 2));
+    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", false), st, 0.0, norm_bytes(d, 2));
     norm_launch<PRE_FWD, false, false>(d, a, st);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
@@ -642,7 +662,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.mask = mask;
     a.oy = y;
     a.ou = u;
-    ProfScope ps("post_norm_fwd", st, 0.0, norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
+    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", false), st, 0.0, norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
     if (d.gate && next) norm_launch<POST_FWD, true, true>(d, a, st);
     else if (d.gate) norm_launch<POST_FWD, true, false>(d, a, st);
     else if (next) norm_launch<POST_FWD, false, true>(d, a, st);
@@ -675,7 +695,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.dx = dx;
     a.part = (float*)ws;
     {
-        ProfScope ps("pre_norm_bwd", st, 0.0, norm_bytes(d, 3 + (dres != nullptr)));
+        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", true), st, 0.0, norm_bytes(d, 3 + (dres != nullptr)));
         norm_launch<PRE_BWD, false, true>(d, a, st);
         RAT3D_LAUNCH_CHECK();
     }
@@ -703,7 +723,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dg = dg;
     a.part = (float*)ws;
     {
-        ProfScope ps("post_norm_bwd", st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", true), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
         if (d.gate && next) norm_launch<POST_BWD, true, true>(d, a, st);
         else if (d.gate) norm_launch<POST_BWD, true, false>(d, a, st);

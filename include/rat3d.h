@@ -441,7 +441,8 @@ typedef struct {
 } rat3d_recurrence_desc;
 
 /* Bytes of the states that the forward saves for the backward, and of workspace (pass 0
- * = fwd, 1 = bwd); (size_t)-1 if the descriptor is invalid. */
+ * = fwd, 1 = bwd); (size_t)-1 if the descriptor is invalid.  Calls that may run at the
+ * same time (streams, graphs) need a workspace each. */
 size_t rat3d_recurrence_carry_size(const rat3d_recurrence_desc* desc);
 size_t rat3d_recurrence_workspace_size(const rat3d_recurrence_desc* desc, int pass);
 

@@ -16,9 +16,15 @@
 // read from single lanes, the waves of a workgroup through LDS: a workgroup takes as many
 // blocks at once as it has waves, one barrier a turn, the next turn's loads in flight.
 // h_{t-1} is formed again in the backward from the states that the forward left before
-// every block, in float32.  Rows of up to 16 lanes share a wave.  Few rows are cut into
-// segments: a first launch joins each segment's steps, the second begins each segment
-// with the joined steps before it.
+// every block, in float32.  Rows of up to 16 lanes share a wave.
+// Few rows are cut into segments of one turn: a workgroup leaves its segment's joined
+// steps in the workspace, takes those of the segments before it, and goes on with the
+// voxels that it holds in registers, so every tensor passes once.  A workgroup waits only
+// for ones that drew their segment before it from a counter, so each of them is running
+// or done, and none of them waits before it has left its own: every wait ends.  What is
+// joined is the same in any order of arrival.  Beyond kSegs segments a launch of its own
+// joins each segment's steps first (a workgroup reads all segments before its own, so the
+// reads would grow with their square).
 //
 // beta: 1 - a^2 is -expm1(-2 w sigmoid(r)), by its series where the argument is small.
 // Bound: HBM.
@@ -31,7 +37,10 @@ namespace rat3d {
 template <typename T> constexpr int tok() { return 16 / (int)sizeof(T); }  // voxels a lane
 template <typename T> constexpr int block() { return 64 * tok<T>(); }      // voxels a wave
 constexpr int kWaves = 16;  // of a workgroup, at most
-constexpr int kSegs = 64;   // segments of a row, at most
+constexpr int kCuts = 64;    // segments of a row that a launch of their own joins, at most
+constexpr int kSegs = 2048;  // segments of a row that find one another, at most
+constexpr int kPolls = 1 << 22;
+constexpr int kLine = 32;    // words of a cache line
 
 struct RecArgs {
     const void *r, *i, *x, *dy;
@@ -41,10 +50,13 @@ struct RecArgs {
     void *y, *dr, *di, *dx;
     float *h_last;     // what it ends with
     float *carry, *part;
-    float* joined;     // [row][segment] (a, b) of each segment, then [row] the walk's first state
+    // segments: (a, b) of each, [row][segment], and the walk's first state, [row]
+    float2* joined;
+    float* first;
+    uint32_t* drawn;   // segments of each row that workgroups have taken on, a line each
     int64_t sr, si, sx, sy, len;
     int64_t rows;
-    int c, blocks, segs, lanes, stream;  // of a row; lanes: of a short row
+    int c, blocks, segs, one, lanes, stream;  // of a row; lanes: of a short row
     float rate;
 };
 
@@ -280,11 +292,11 @@ template <typename T, bool DOWN> struct GradSteps {
 // The walk's state at the beginning of a segment: the segments before it joined, one a
 // lane, so that their loads are under way together.
 __device__ __forceinline__ float segment_begin(const RecArgs& q, int64_t row, int seg) {
-    static_assert(kSegs <= 64, "a segment a lane");
+    static_assert(kCuts <= 64, "a segment a lane");
     if (q.segs == 1) return q.h0 ? q.h0[row] : 0.f;
     const int lane = threadIdx.x & 63;
-    const float2 o = ((const float2*)q.joined)[row * q.segs + (lane < seg ? lane : 0)];
-    const float s = q.joined[2 * q.rows * q.segs + row];
+    const float2 o = q.joined[row * q.segs + (lane < seg ? lane : 0)];
+    const float s = q.first[row];
     const float2 all = WaveWalk<false>(lane < seg ? o.x : 1.f, lane < seg ? o.y : 0.f).all();
     return __builtin_fmaf(all.x, s, all.y);
 }
@@ -366,9 +378,9 @@ __global__ __launch_bounds__(64 * kWaves, 8) void recurrence_fwd_k(RecArgs q) {
     }
     if (threadIdx.x == 0) {
         if (JOIN) {
-            ((float2*)q.joined)[row * q.segs + seg] = make_float2(prod, state);
+            q.joined[row * q.segs + seg] = make_float2(prod, state);
             // kept, for the walk's last state may take the first one's place
-            if (seg == 0) q.joined[2 * q.rows * q.segs + row] = q.h0 ? q.h0[row] : 0.f;
+            if (seg == 0) q.first[row] = q.h0 ? q.h0[row] : 0.f;
         } else if (q.h_last && seg == q.segs - 1) {
             q.h_last[row] = state;
         }
@@ -505,8 +517,198 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_join_k(RecArgs q) 
         }
     }
     if (threadIdx.x == 0) {
-        ((float2*)q.joined)[row * q.segs + seg] = make_float2(prod, state);
-        if (seg == 0) q.joined[2 * q.rows * q.segs + row] = q.h0 ? q.h0[row] : 0.f;
+        q.joined[row * q.segs + seg] = make_float2(prod, state);
+        if (seg == 0) q.first[row] = q.h0 ? q.h0[row] : 0.f;
+    }
+}
+
+// Before the segments that find one another: nothing drawn, nothing joined, and the walks'
+// first states, for their last ones may take their place.
+__global__ __launch_bounds__(256) void recurrence_begin_k(RecArgs q) {
+    const int64_t k = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    if (k < q.rows * q.segs) q.joined[k] = make_float2(0.f, 0.f);
+    if (k < q.rows) {
+        q.drawn[k * kLine] = 0;
+        q.first[k] = q.h0 ? q.h0[k] : 0.f;
+    }
+}
+
+// A workgroup's segment of one turn.  (a, b) lie in one word of 64 bits, so that they
+// arrive together; a is never negative, and its sign bit says that they are there.
+struct OneTurn {
+    int64_t row;
+    int seg, wave, waves;
+    float pa, pb;  // the waves before this one, joined
+
+    __device__ __forceinline__ OneTurn(const RecArgs& q, int* draw)
+        : wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), waves(blockDim.x >> 6) {
+        // a counter a row: one for all took 15 us for 1000 workgroups
+        row = blockIdx.x % (uint32_t)q.rows;
+        if (threadIdx.x == 0)
+            *draw = (int)__hip_atomic_fetch_add(q.drawn + row * kLine, 1u, __ATOMIC_RELAXED,
+                                                __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        seg = __builtin_amdgcn_readfirstlane(*draw);
+    }
+    // the block in the walk's order
+    __device__ __forceinline__ int block() const { return seg * waves + wave; }
+    // Joins the waves' steps, leaves the segment's, and returns what the wave begins with;
+    // `end` becomes what the segment ends with.
+    __device__ __forceinline__ float begin(const RecArgs& q, float2 mine, float2* tot,
+                                           float* from, float& end) {
+        const int lane = threadIdx.x & 63;
+        if (lane == 0) tot[wave] = mine;
+        __syncthreads();
+        float A = 1.f, B = 0.f;
+        for (int j = 0; j < waves; ++j) {
+            if (j == wave) {
+                pa = A;
+                pb = B;
+            }
+            const float2 o = tot[j];
+            B = __builtin_fmaf(o.x, B, o.y);
+            A *= o.x;
+        }
+        if (wave == 0) {
+            uint64_t* to = (uint64_t*)q.joined + row * q.segs;
+            const uint64_t there = (uint64_t)1 << 63;
+            if (lane == 0)
+                __hip_atomic_store(to + seg,
+                                   there | (uint64_t)__float_as_uint(A) << 32 | __float_as_uint(B),
+                                   __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            float s = q.first[row];
+            for (int k0 = 0; k0 < seg; k0 += 64) {  // the segments before, one a lane
+                uint64_t v = (uint64_t)0x3f800000u << 32;
+                if (k0 + lane < seg) {
+                    for (int i = 0; i < kPolls; ++i) {
+                        v = __hip_atomic_load(to + k0 + lane, __ATOMIC_RELAXED,
+                                              __HIP_MEMORY_SCOPE_AGENT);
+                        if (v & there) break;
+                        __builtin_amdgcn_s_sleep(1);
+                    }
+                    if (!(v & there)) v = (uint64_t)0x7fc00000u << 32;  // NaN: no wait is endless
+                }
+                const WaveWalk<false> all(__uint_as_float((uint32_t)(v >> 32) & 0x7fffffffu),
+                                          __uint_as_float((uint32_t)v));
+                const float2 o = all.all();
+                s = __builtin_fmaf(o.x, s, o.y);
+            }
+            if (lane == 0) *from = s;
+        }
+        __syncthreads();
+        const float s = *from;
+        end = __builtin_fmaf(A, s, B);
+        return __builtin_fmaf(pa, s, pb);
+    }
+};
+
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(64 * kWaves, 8) void recurrence_fwd_one_k(RecArgs q) {
+    constexpr int TOK = tok<T>(), BLOCK = block<T>();
+    __shared__ float2 tot[kWaves];
+    __shared__ float from;
+    __shared__ int draw;
+    OneTurn turn(q, &draw);
+    const int lane = threadIdx.x & 63;
+    const int64_t row = turn.row, vol = (uint32_t)row / (uint32_t)q.c;
+    const int ch = (int)(row - vol * q.c);
+    const float lam = q.lam[ch];
+    const T* const in[3] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len};
+    const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
+    const int k = turn.block(), at = DOWN ? q.blocks - 1 - k : k;
+    const bool there = k < q.blocks, all = there && !mask && (int64_t)(at + 1) * BLOCK <= q.len;
+    Raw<T, 3> d;
+    d.at.live = 0;
+    const int64_t v = (int64_t)at * BLOCK + lane * TOK;
+    if (all) read<T, 3, true>(d, in, mask, v, q.len);
+    else if (there) read<T, 3, false>(d, in, mask, v, q.len);
+    const float w = q.rate * softplusf(lam);
+    Steps<T> s;
+    if (all) s.template form<true>(d, w);
+    else s.template form<false>(d, w);
+    const float2 mine = s.template all<DOWN>();
+    const WaveWalk<DOWN> walk(mine.x, mine.y);
+    float end;
+    const float begin = turn.begin(q, walk.all(), tot, &from, end);
+    if (there) {
+        if (q.carry && lane == 0) q.carry[row * q.blocks + at] = begin;
+        T* y = (T*)q.y + vol * q.sy + (int64_t)ch * q.len;
+        float o[TOK];
+        s.template states<DOWN>(walk.begin(begin), o);
+        if (all) {
+            put_tokens<T, TOK, true>(y + d.at.at, 0, TOK, o, q.stream);
+        } else {
+            d.at.clear(o);
+            put_tokens<T, TOK, false>(y + d.at.at, 0, TOK - d.at.over, o, q.stream);
+        }
+    }
+    if (q.h_last && turn.seg == q.segs - 1 && threadIdx.x == 0) q.h_last[row] = end;
+}
+
+template <typename T, bool DOWN>
+__global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_one_k(RecArgs q) {
+    constexpr int TOK = tok<T>(), BLOCK = block<T>();
+    __shared__ float2 tot[kWaves];
+    __shared__ double sums[kWaves];
+    __shared__ float from;
+    __shared__ int draw;
+    OneTurn turn(q, &draw);
+    const int lane = threadIdx.x & 63;
+    const int64_t row = turn.row, vol = (uint32_t)row / (uint32_t)q.c;
+    const int ch = (int)(row - vol * q.c);
+    const float lam = q.lam[ch];
+    const T* const in[4] = {(const T*)q.r + vol * q.sr + (int64_t)ch * q.len,
+                            (const T*)q.i + vol * q.si + (int64_t)ch * q.len,
+                            (const T*)q.x + vol * q.sx + (int64_t)ch * q.len,
+                            (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
+    const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
+    const int k = turn.block(), at = DOWN ? q.blocks - 1 - k : k;
+    const bool there = k < q.blocks, all = there && !mask && (int64_t)(at + 1) * BLOCK <= q.len;
+    Raw<T, 4> d;
+    d.at.live = 0;
+    float past = 0.f;
+    if (there) past = q.carry[row * q.blocks + at];
+    const int64_t v = (int64_t)at * BLOCK + lane * TOK;
+    if (all) read<T, 4, true>(d, in, mask, v, q.len);
+    else if (there) read<T, 4, false>(d, in, mask, v, q.len);
+    const float w = q.rate * softplusf(lam);
+    GradSteps<T, DOWN> s;
+    if (all) s.template form<true>(d, w);
+    else s.template form<false>(d, w);
+    float A, B, F, end;
+    s.all(A, B, F);
+    const WaveWalk<DOWN> walk(A, B);
+    const float h = WaveWalk<!DOWN>(A, F).begin(past);
+    const float begin = turn.begin(q, walk.all(), tot, &from, end);
+    double sum = 0.0;
+    if (there) {
+        float o[3][TOK];
+        sum = (double)s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+        T* const out[3] = {(T*)q.dr + vol * q.sr + (int64_t)ch * q.len,
+                           (T*)q.di + vol * q.si + (int64_t)ch * q.len,
+                           (T*)q.dx + vol * q.sx + (int64_t)ch * q.len};
+        if (all) {
+#pragma unroll
+            for (int i = 0; i < 3; ++i)
+                put_tokens<T, TOK, true>(out[i] + d.at.at, 0, TOK, o[i], q.stream);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 3; ++i) {
+                d.at.clear(o[i]);
+                put_tokens<T, TOK, false>(out[i] + d.at.at, 0, TOK - d.at.over, o[i], q.stream);
+            }
+        }
+    }
+#pragma unroll
+    for (int m = 32; m >= 1; m >>= 1) sum += __shfl_xor(sum, m);
+    if (lane == 0) sums[turn.wave] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int j = 1; j < turn.waves; ++j) sum += sums[j];
+        q.part[((int64_t)ch * (q.rows / q.c) + vol) * q.segs + turn.seg] = (float)sum;
+        if (q.h_last && turn.seg == q.segs - 1) q.h_last[row] = end;
     }
 }
 
@@ -670,17 +872,17 @@ static void rec_plan(const rat3d_recurrence_desc& d, RecArgs* q, int* waves) {
         return;
     }
     // Eight waves a row (four take the same time from 1024 rows on), sixteen where a CU has
-    // one row or little more, and fewer rows cut until there are two workgroups a CU: a
-    // forward over 256 rows of 129024 voxels in bfloat16 takes 65 us with sixteen waves, 77
-    // with eight, 108 cut; over 128 rows 70 with eight waves, 59 cut.
+    // one row or little more; fewer rows are cut.
     const int64_t cus = device_cus();
     int most = 8;
     if (q->rows >= cus) {
         if (2 * q->rows < 3 * cus && q->blocks >= 64) most = 16;
     } else {
-        const int64_t want = ceil_div(2 * cus, q->rows), turns = ceil_div(q->blocks, most);
-        const int64_t segs = want < turns ? want : turns;
-        q->segs = (int)(segs < kSegs ? segs : kSegs);
+        const int64_t turns = ceil_div(q->blocks, most);
+        q->one = turns > 1 && turns <= kSegs;
+        const int64_t want = ceil_div(2 * cus, q->rows);
+        const int64_t segs = q->one || turns < want ? turns : want;
+        q->segs = (int)(q->one || segs < kCuts ? segs : kCuts);
     }
     *waves = q->blocks < most ? q->blocks : most;
 }
@@ -692,15 +894,32 @@ size_t recurrence_carry_bytes(const rat3d_recurrence_desc& d) {
     return (size_t)q.rows * q.blocks * sizeof(float);
 }
 
-// The joined segments and first states, then the parts of dlambda.
-static size_t rec_joined(const RecArgs& q) {
-    return q.segs > 1 ? (size_t)q.rows * (2 * q.segs + 1) : 0;
+// Workspace: the rows' counters, the joined segments, the first states, and for the backward
+// the parts of dlambda.
+static size_t rec_workspace(RecArgs* q, void* ws, int pass) {
+    const size_t pairs = q->segs > 1 ? (size_t)q->rows * q->segs : 0;
+    const size_t at = q->one ? 4 * kLine * (size_t)q->rows : 0, first = at + 8 * pairs;
+    const size_t part = first + (q->segs > 1 ? 4 * (size_t)q->rows : 0);
+    if (ws) {
+        q->drawn = (uint32_t*)ws;
+        q->joined = (float2*)((char*)ws + at);
+        q->first = (float*)((char*)ws + first);
+        q->part = (float*)((char*)ws + part);
+    }
+    return part + (pass ? 4 * (size_t)q->rows * q->segs : 0);
 }
 size_t recurrence_ws_bytes(const rat3d_recurrence_desc& d, int pass) {
     RecArgs q = {};
     int waves;
     rec_plan(d, &q, &waves);
-    return (rec_joined(q) + (pass ? (size_t)q.rows * q.segs : 0)) * sizeof(float);
+    return rec_workspace(&q, nullptr, pass);
+}
+
+static rat3d_status rec_begin(const RecArgs& q, hipStream_t st) {
+    ProfScope ps("recurrence_begin", st, 0.0, 8.0 * q.rows * q.segs);
+    recurrence_begin_k<<<(unsigned)ceil_div(q.rows * q.segs, 256), 256, 0, st>>>(q);
+    RAT3D_LAUNCH_CHECK();
+    return RAT3D_OK;
 }
 
 static double rec_bytes(const rat3d_recurrence_desc& d, int tensors) {
@@ -722,7 +941,7 @@ rat3d_status recurrence_fwd(const rat3d_recurrence_desc& d, const void* r, const
     q.y = y;
     q.h_last = h_last;
     q.carry = carry;
-    q.joined = (float*)ws;
+    rec_workspace(&q, ws, 0);
     if (q.lanes) {
         const unsigned grid = (unsigned)ceil_div(q.rows * q.lanes, 256);
         ProfScope ps("recurrence_short_fwd", st, 0.0, rec_bytes(d, 4));
@@ -739,23 +958,32 @@ rat3d_status recurrence_fwd(const rat3d_recurrence_desc& d, const void* r, const
         return RAT3D_OK;
     }
     const unsigned grid = (unsigned)(q.rows * q.segs), threads = 64 * waves;
-#define RAT3D_REC(JOIN)                                                                       \
-    do {                                                                                      \
-        if (d.dtype == RAT3D_BF16) {                                                          \
-            if (d.reverse) recurrence_fwd_k<bf16, true, JOIN><<<grid, threads, 0, st>>>(q);   \
-            else recurrence_fwd_k<bf16, false, JOIN><<<grid, threads, 0, st>>>(q);            \
-        } else {                                                                              \
-            if (d.reverse) recurrence_fwd_k<float, true, JOIN><<<grid, threads, 0, st>>>(q);  \
-            else recurrence_fwd_k<float, false, JOIN><<<grid, threads, 0, st>>>(q);           \
-        }                                                                                     \
-        RAT3D_LAUNCH_CHECK();                                                                 \
+#define RAT3D_REC(KERNEL, ...)                                                           \
+    do {                                                                                 \
+        if (d.dtype == RAT3D_BF16) {                                                     \
+            if (d.reverse) KERNEL<bf16, true __VA_ARGS__><<<grid, threads, 0, st>>>(q);  \
+            else KERNEL<bf16, false __VA_ARGS__><<<grid, threads, 0, st>>>(q);           \
+        } else {                                                                         \
+            if (d.reverse) KERNEL<float, true __VA_ARGS__><<<grid, threads, 0, st>>>(q); \
+            else KERNEL<float, false __VA_ARGS__><<<grid, threads, 0, st>>>(q);          \
+        }                                                                                \
+        RAT3D_LAUNCH_CHECK();                                                            \
     } while (0)
+#define RAT3D_COMMA ,
+    if (q.one) {
+        const rat3d_status s = rec_begin(q, st);
+        if (s != RAT3D_OK) return s;
+        ProfScope ps("recurrence_fwd_one", st, 0.0, rec_bytes(d, 4));
+        RAT3D_REC(recurrence_fwd_one_k);
+        return RAT3D_OK;
+    }
     if (q.segs > 1) {
         ProfScope ps("recurrence_fwd_join", st, 0.0, rec_bytes(d, 3));
-        RAT3D_REC(true);
+        RAT3D_REC(recurrence_fwd_k, RAT3D_COMMA true);
     }
     ProfScope ps(q.segs > 1 ? "recurrence_fwd_cut" : "recurrence_fwd", st, 0.0, rec_bytes(d, 4));
-    RAT3D_REC(false);
+    RAT3D_REC(recurrence_fwd_k, RAT3D_COMMA false);
+#undef RAT3D_COMMA
 #undef RAT3D_REC
     return RAT3D_OK;
 }
@@ -779,8 +1007,7 @@ rat3d_status recurrence_bwd(const rat3d_recurrence_desc& d, const void* dy, cons
     q.di = di;
     q.dx = dx;
     q.h_last = dh0;
-    q.joined = (float*)ws;
-    q.part = (float*)ws + rec_joined(q);
+    rec_workspace(&q, ws, 1);
     // the gradient walks against the forward
 #define RAT3D_REC(KERNEL, GRID, THREADS)                                           \
     do {                                                                           \
@@ -799,12 +1026,20 @@ rat3d_status recurrence_bwd(const rat3d_recurrence_desc& d, const void* dy, cons
         RAT3D_REC(recurrence_short_bwd_k, grid, 256);
     } else {
         const unsigned grid = (unsigned)(q.rows * q.segs), threads = 64 * waves;
-        if (q.segs > 1) {
-            ProfScope ps("recurrence_bwd_join", st, 0.0, rec_bytes(d, 2));
-            RAT3D_REC(recurrence_bwd_join_k, grid, threads);
+        if (q.one) {
+            const rat3d_status s = rec_begin(q, st);
+            if (s != RAT3D_OK) return s;
+            ProfScope ps("recurrence_bwd_one", st, 0.0, rec_bytes(d, 7));
+            RAT3D_REC(recurrence_bwd_one_k, grid, threads);
+        } else {
+            if (q.segs > 1) {
+                ProfScope ps("recurrence_bwd_join", st, 0.0, rec_bytes(d, 2));
+                RAT3D_REC(recurrence_bwd_join_k, grid, threads);
+            }
+            ProfScope ps(q.segs > 1 ? "recurrence_bwd_cut" : "recurrence_bwd", st, 0.0,
+                         rec_bytes(d, 7));
+            RAT3D_REC(recurrence_bwd_k, grid, threads);
         }
-        ProfScope ps(q.segs > 1 ? "recurrence_bwd_cut" : "recurrence_bwd", st, 0.0, rec_bytes(d, 7));
-        RAT3D_REC(recurrence_bwd_k, grid, threads);
     }
 #undef RAT3D_REC
     const int parts = d.n * q.segs;

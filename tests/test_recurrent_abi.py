@@ -164,6 +164,12 @@ def test_recurrence_pointers():
         _refused(R.EALIGN, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[i] + 1), 0, ws, need[1])
     _refused(R.EWORKSPACE, R.rat3d_recurrence_bwd, d, *bwd, 0, ws, need[1] - 1)
     _refused(R.EALIGN, R.rat3d_recurrence_bwd, d, *bwd, 0, ws + 4, need[1])
+    # few long rows are cut, and the pieces joined through the workspace
+    d = _rec(n=1, c=2, length=1 << 20)
+    need = [R.rat3d_recurrence_workspace_size(d, i) for i in (0, 1)]
+    assert 0 < need[0] < need[1] < BAD
+    _refused(R.EWORKSPACE, R.rat3d_recurrence_fwd, d, *fwd, ws, need[0] - 1)
+    _refused(R.EALIGN, R.rat3d_recurrence_fwd, d, *fwd, ws + 8, need[0])
 
 
 def test_recurrence_overlaps():

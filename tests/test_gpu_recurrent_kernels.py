@@ -129,7 +129,7 @@ def test_norm_rows_of_2_28_voxels():
 # ------------------------------------------------------------------ recurrence
 # rows (0: more than a CU each), tokens of bfloat16, the name's end
 WALKS = [(3, 100, "recurrence_short_"), (5, 128, "recurrence_short_"), (5, 129, "recurrence_"),
-         (3, 4096, "recurrence_"), (3, 4097, "recurrence_one"), (2, 41000, "recurrence_one"),
+         (3, 4097, "recurrence_"), (3, 8192, "recurrence_"), (3, 8193, "recurrence_one"), (2, 41000, "recurrence_one"),
          (0, 9001, "recurrence_")]
 
 

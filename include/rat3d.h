@@ -387,7 +387,7 @@ typedef struct {
     rat3d_dtype dtype;
 } rat3d_norm_desc;
 
-/* gamma float32 [c]; gate, z_stride, g_stride and y_stride are ignored. */
+/* gamma float32 [c]; gate, z_stride, g_stride and y_stride have no part in it. */
 rat3d_status rat3d_pre_norm_fwd(const rat3d_norm_desc* desc, const void* x, const float* gamma,
                                 const uint8_t* mask, void* u, void* stream);
 

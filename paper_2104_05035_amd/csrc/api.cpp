@@ -105,6 +105,70 @@ static rat3d_status check_ws(void* ws, size_t ws_bytes, size_t need) {
 
 using namespace rat3d;
 
+// What a call reads or writes: n parts of `held` bytes, `stride` bytes apart.  A result
+// must lie nowhere in another of the call's tensors, unless it is an input of the same
+// `kind` (above 0), part for part.
+struct Span {
+    const void* p;
+    int64_t n, stride, held;
+    int kind;
+    const char* name;
+};
+enum { SPAN_VECTOR = 0, SPAN_MAP = 1, SPAN_STATE = 2 };
+
+static bool spans_meet(const Span& a, const Span& b) {
+    const int64_t pa = (int64_t)(uintptr_t)a.p, pb = (int64_t)(uintptr_t)b.p;
+    if (pa + (a.n - 1) * a.stride + a.held <= pb || pb + (b.n - 1) * b.stride + b.held <= pa)
+        return false;
+    if (a.n == b.n && a.stride == b.stride) {  // one distance for all parts, up to whole strides
+        const int64_t m = (pb - pa) / a.stride;
+        for (int64_t k = m - 1; k <= m + 1; ++k) {
+            const int64_t off = pb - pa - k * a.stride;
+            if (k > -a.n && k < a.n && off < a.held && -off < b.held) return true;
+        }
+        return false;
+    }
+    // (beyond 2^16 parts of different strides only the first are looked at)
+    const int64_t most = a.n < 1 << 16 ? a.n : 1 << 16;
+    for (int64_t k = 0; k < most; ++k) {
+        const int64_t lo = pa + k * a.stride, d = lo - b.held - pb;
+        const int64_t j = d < 0 ? 0 : d / b.stride + 1;  // b's first part that ends behind lo
+        if (j < b.n && pb + j * b.stride < lo + a.held) return true;
+    }
+    return false;
+}
+
+template <int OUTS, int INS>
+static rat3d_status check_spans(const Span (&outs)[OUTS], const Span (&ins)[INS]) {
+    for (int o = 0; o < OUTS; ++o) {
+        const Span& a = outs[o];
+        if (!a.p) continue;
+        for (int k = o + 1; k < OUTS; ++k)
+            RAT3D_REQUIRE(!outs[k].p || !spans_meet(a, outs[k]), RAT3D_EINVAL,
+                          "%s and %s must not overlap", a.name, outs[k].name);
+        for (const Span& b : ins) {
+            const bool same = a.kind && a.kind == b.kind && a.p == b.p &&
+                              (a.n == 1 || a.stride == b.stride);
+            RAT3D_REQUIRE(!b.p || same || !spans_meet(a, b), RAT3D_EINVAL,
+                          "%s must not overlap %s", a.name, b.name);
+        }
+    }
+    return RAT3D_OK;
+}
+
+// A tensor of the map's shape, float32 numbers of each channel, and bytes (a mask, a
+// workspace).
+static Span map_span(const void* p, int64_t n, int64_t stride, int64_t packed, size_t es,
+                     const char* name) {
+    return {p, n, (int64_t)es * (stride ? stride : packed), (int64_t)es * packed, SPAN_MAP, name};
+}
+static Span vec_span(const void* p, int64_t count, const char* name, int kind = SPAN_VECTOR) {
+    return {p, 1, 4 * count, 4 * count, kind, name};
+}
+static Span raw_span(const void* p, int64_t bytes, const char* name) {
+    return {bytes ? p : nullptr, 1, bytes, bytes, SPAN_VECTOR, name};
+}
+
 extern "C" {
 
 const char* rat3d_last_error(void) { return g_last_error.c_str(); }
@@ -576,52 +640,6 @@ rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
                    accumulate ? dx : nullptr, dx, (hipStream_t)stream);
 }
 
-// Tensors of n parts of `held` bytes, `stride` bytes apart: what a call writes must not
-// lie over another of its tensors, unless the two are one.
-struct Span {
-    const void* p;
-    int64_t stride, held;
-    const char* name;
-};
-
-static bool spans_meet(const Span& a, const Span& b, int64_t n) {
-    const int64_t pa = (int64_t)(uintptr_t)a.p, pb = (int64_t)(uintptr_t)b.p;
-    if (pa + (n - 1) * a.stride + a.held <= pb || pb + (n - 1) * b.stride + b.held <= pa)
-        return false;
-    if (a.stride == b.stride) {  // one distance for all parts, up to whole strides
-        const int64_t m = (pb - pa) / a.stride;
-        for (int64_t k = m - 1; k <= m + 1; ++k) {
-            const int64_t off = pb - pa - k * a.stride;
-            if (k > -n && k < n && off < a.held && -off < b.held) return true;
-        }
-        return false;
-    }
-    for (int64_t k = 0; k < n; ++k) {
-        const int64_t lo = pa + k * a.stride, d = lo - b.held - pb;
-        const int64_t j = d < 0 ? 0 : d / b.stride + 1;  // b's first part that ends behind lo
-        if (j < n && pb + j * b.stride < lo + a.held) return true;
-    }
-    return false;
-}
-
-// outs must not meet one another, nor an input, unless it is that input.
-static rat3d_status check_spans(const Span* outs, int n_outs, const Span* ins, int n_ins, int64_t n,
-                                bool in_place) {
-    for (int o = 0; o < n_outs; ++o) {
-        if (!outs[o].p) continue;
-        for (int k = o + 1; k < n_outs; ++k)
-            RAT3D_REQUIRE(!outs[k].p || !spans_meet(outs[o], outs[k], n), RAT3D_EINVAL,
-                          "%s and %s must not overlap", outs[o].name, outs[k].name);
-        for (int k = 0; k < n_ins; ++k) {
-            const bool same = in_place && outs[o].p == ins[k].p &&
-                              (n == 1 || outs[o].stride == ins[k].stride);
-            RAT3D_REQUIRE(!ins[k].p || same || !spans_meet(outs[o], ins[k], n), RAT3D_EINVAL,
-                          "%s must not overlap %s", outs[o].name, ins[k].name);
-        }
-    }
-    return RAT3D_OK;
-}
-
 static rat3d_status check_norm(const rat3d_norm_desc* d) {
     RAT3D_REQUIRE(d != nullptr, RAT3D_EINVAL, "norm descriptor is NULL");
     RAT3D_REQUIRE(d->n >= 1 && d->c >= 1 && d->v >= 1, RAT3D_EINVAL, "norm sizes must be >= 1");
@@ -635,7 +653,7 @@ static rat3d_status check_norm(const rat3d_norm_desc* d) {
                   (int)d->dtype);
     RAT3D_REQUIRE(d->c <= 1 << 20, RAT3D_EUNSUPPORTED, "more than 2^20 channels");
     RAT3D_REQUIRE(d->v <= (int64_t)1 << 28 && ((double)d->v / 16 + 1) * d->n < 2.0e9,
-                  RAT3D_EUNSUPPORTED, "map too large for one launch");
+                  RAT3D_EUNSUPPORTED, "map too large");
     const double held = (double)d->c * d->v;
     RAT3D_STRIDE(d->x_stride, held);
     RAT3D_STRIDE(d->z_stride, held);
@@ -643,14 +661,6 @@ static rat3d_status check_norm(const rat3d_norm_desc* d) {
     RAT3D_STRIDE(d->y_stride, held);
     RAT3D_STRIDE(d->u_stride, held);
     return RAT3D_OK;
-}
-
-// A tensor of the map's shape, and a float32 vector of its channels.
-static Span map_span(const void* p, int64_t stride, int64_t packed, size_t es, const char* name) {
-    return {p, (int64_t)es * (stride ? stride : packed), (int64_t)es * packed, name};
-}
-static Span vec_span(const void* p, int64_t count, const char* name) {
-    return {p, 4 * count, 4 * count, name};
 }
 
 size_t rat3d_norm_workspace_size(const rat3d_norm_desc* desc) {
@@ -667,9 +677,10 @@ rat3d_status rat3d_pre_norm_fwd(const rat3d_norm_desc* desc, const void* x, cons
     RAT3D_ELT(gamma, sizeof(float), "gamma");
     RAT3D_ELT(u, es, "u");
     const int64_t packed = desc->c * desc->v;
-    const Span outs[] = {map_span(u, desc->u_stride, packed, es, "u")};
-    const Span ins[] = {map_span(x, desc->x_stride, packed, es, "x")};
-    s = check_spans(outs, 1, ins, 1, desc->n, true);
+    const Span outs[] = {map_span(u, desc->n, desc->u_stride, packed, es, "u")};
+    const Span ins[] = {map_span(x, desc->n, desc->x_stride, packed, es, "x"),
+                        vec_span(gamma, desc->c, "gamma"), raw_span(mask, desc->n * desc->v, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return pre_norm_fwd(*desc, x, gamma, mask, u, (hipStream_t)stream);
 }
@@ -690,14 +701,15 @@ rat3d_status rat3d_pre_norm_bwd(const rat3d_norm_desc* desc, const void* du, con
     s = check_ws(ws, ws_bytes, norm_ws_bytes(*desc));
     if (s != RAT3D_OK) return s;
     const int64_t packed = desc->c * desc->v;
-    const Span outs[] = {map_span(dx, desc->x_stride, packed, es, "dx")};
-    const Span ins[] = {map_span(du, desc->u_stride, packed, es, "du"),
-                        map_span(x, desc->x_stride, packed, es, "x"),
-                        map_span(dres, desc->x_stride, packed, es, "dres")};
-    s = check_spans(outs, 1, ins, 3, desc->n, true);
-    if (s != RAT3D_OK) return s;
-    const Span vec[] = {vec_span(dgamma, desc->c, "dgamma"), vec_span(gamma, desc->c, "gamma")};
-    s = check_spans(vec, 1, vec + 1, 1, 1, false);
+    const int64_t n = desc->n;
+    const Span outs[] = {map_span(dx, n, desc->x_stride, packed, es, "dx"),
+                         vec_span(dgamma, desc->c, "dgamma"),
+                         raw_span(ws, (int64_t)norm_ws_bytes(*desc), "the workspace")};
+    const Span ins[] = {map_span(du, n, desc->u_stride, packed, es, "du"),
+                        map_span(x, n, desc->x_stride, packed, es, "x"),
+                        map_span(dres, n, desc->x_stride, packed, es, "dres"),
+                        vec_span(gamma, desc->c, "gamma"), raw_span(mask, n * desc->v, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return pre_norm_bwd(*desc, du, x, gamma, mask, dres, dx, dgamma, accumulate ? 1 : 0, ws,
                         (hipStream_t)stream);
@@ -721,12 +733,15 @@ rat3d_status rat3d_post_norm_fwd(const rat3d_norm_desc* desc, const void* x, con
         RAT3D_ELT(u, es, "u");
     }
     const int64_t packed = desc->c * desc->v;
-    const Span outs[] = {map_span(y, desc->y_stride, packed, es, "y"),
-                         map_span(gamma_next ? u : nullptr, desc->u_stride, packed, es, "u")};
-    const Span ins[] = {map_span(x, desc->x_stride, packed, es, "x"),
-                        map_span(z, desc->z_stride, packed, es, "z"),
-                        map_span(desc->gate ? g : nullptr, desc->g_stride, packed, es, "g")};
-    s = check_spans(outs, 2, ins, 3, desc->n, true);
+    const int64_t n = desc->n, c = desc->c;
+    const Span outs[] = {map_span(y, n, desc->y_stride, packed, es, "y"),
+                         map_span(gamma_next ? u : nullptr, n, desc->u_stride, packed, es, "u")};
+    const Span ins[] = {map_span(x, n, desc->x_stride, packed, es, "x"),
+                        map_span(z, n, desc->z_stride, packed, es, "z"),
+                        map_span(desc->gate ? g : nullptr, n, desc->g_stride, packed, es, "g"),
+                        vec_span(gamma, c, "gamma"), vec_span(scale, c, "scale"),
+                        vec_span(gamma_next, c, "gamma_next"), raw_span(mask, n * desc->v, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return post_norm_fwd(*desc, x, z, g, gamma, scale, gamma_next, mask, y, u,
                          (hipStream_t)stream);
@@ -765,21 +780,21 @@ rat3d_status rat3d_post_norm_bwd(const rat3d_norm_desc* desc, const void* dy, co
     if (s != RAT3D_OK) return s;
     const bool gated = desc->gate != RAT3D_GATE_NONE;
     const int64_t packed = desc->c * desc->v, c = desc->c;
-    const Span outs[] = {map_span(dx, desc->x_stride, packed, es, "dx"),
-                         map_span(dz, desc->z_stride, packed, es, "dz"),
-                         map_span(gated ? dg : nullptr, desc->g_stride, packed, es, "dg")};
-    const Span ins[] = {map_span(dy, desc->y_stride, packed, es, "dy"),
-                        map_span(gamma_next ? du : nullptr, desc->u_stride, packed, es, "du"),
-                        map_span(gamma_next ? y : nullptr, desc->y_stride, packed, es, "y"),
-                        map_span(z, desc->z_stride, packed, es, "z"),
-                        map_span(gated ? g : nullptr, desc->g_stride, packed, es, "g")};
-    s = check_spans(outs, 3, ins, 5, desc->n, true);
-    if (s != RAT3D_OK) return s;
-    const Span vec[] = {vec_span(dgamma, c, "dgamma"), vec_span(dscale, c, "dscale"),
-                        vec_span(gamma_next ? dgamma_next : nullptr, c, "dgamma_next"),
+    const int64_t n = desc->n;
+    const Span outs[] = {map_span(dx, n, desc->x_stride, packed, es, "dx"),
+                         map_span(dz, n, desc->z_stride, packed, es, "dz"),
+                         map_span(gated ? dg : nullptr, n, desc->g_stride, packed, es, "dg"),
+                         vec_span(dgamma, c, "dgamma"), vec_span(dscale, c, "dscale"),
+                         vec_span(gamma_next ? dgamma_next : nullptr, c, "dgamma_next"),
+                         raw_span(ws, (int64_t)norm_ws_bytes(*desc), "the workspace")};
+    const Span ins[] = {map_span(dy, n, desc->y_stride, packed, es, "dy"),
+                        map_span(gamma_next ? du : nullptr, n, desc->u_stride, packed, es, "du"),
+                        map_span(gamma_next ? y : nullptr, n, desc->y_stride, packed, es, "y"),
+                        map_span(z, n, desc->z_stride, packed, es, "z"),
+                        map_span(gated ? g : nullptr, n, desc->g_stride, packed, es, "g"),
                         vec_span(gamma, c, "gamma"), vec_span(scale, c, "scale"),
-                        vec_span(gamma_next, c, "gamma_next")};
-    s = check_spans(vec, 3, vec + 3, 3, 1, false);
+                        vec_span(gamma_next, c, "gamma_next"), raw_span(mask, n * desc->v, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return post_norm_bwd(*desc, dy, du, y, z, g, gamma, scale, gamma_next, mask, dx, dz, dg, dgamma,
                          dscale, gamma_next ? dgamma_next : nullptr, accumulate ? 1 : 0, ws,
@@ -833,20 +848,17 @@ rat3d_status rat3d_recurrence_fwd(const rat3d_recurrence_desc* desc, const void*
     if (carry) RAT3D_ELT(carry, sizeof(float), "carry");
     s = check_ws(ws, ws_bytes, recurrence_ws_bytes(*desc, 0));
     if (s != RAT3D_OK) return s;
-    const int64_t packed = desc->c * desc->len, rows = (int64_t)desc->n * desc->c;
-    const Span outs[] = {map_span(y, desc->y_stride, packed, es, "y")};
-    const Span ins[] = {map_span(r, desc->r_stride, packed, es, "r"),
-                        map_span(i, desc->i_stride, packed, es, "i"),
-                        map_span(x, desc->x_stride, packed, es, "x")};
-    s = check_spans(outs, 1, ins, 3, desc->n, true);
-    if (s != RAT3D_OK) return s;
-    const Span vec[] = {vec_span(h_last, rows, "h_last"),
-                        vec_span(carry, (int64_t)recurrence_carry_bytes(*desc) / 4, "carry"),
-                        vec_span(lambda, desc->c, "lambda"),
-                        vec_span(h_last == h0 ? nullptr : h0, rows, "h0"),
-                        vec_span(h0, rows, "h0")};
-    s = check_spans(vec, 2, vec + 2, 2, 1, false);
-    if (s == RAT3D_OK) s = check_spans(vec + 1, 1, vec + 4, 1, 1, false);
+    const int64_t packed = desc->c * desc->len, n = desc->n, rows = n * desc->c;
+    const Span outs[] = {map_span(y, n, desc->y_stride, packed, es, "y"),
+                         vec_span(h_last, rows, "h_last", SPAN_STATE),
+                         raw_span(carry, (int64_t)recurrence_carry_bytes(*desc), "carry"),
+                         raw_span(ws, (int64_t)recurrence_ws_bytes(*desc, 0), "the workspace")};
+    const Span ins[] = {map_span(r, n, desc->r_stride, packed, es, "r"),
+                        map_span(i, n, desc->i_stride, packed, es, "i"),
+                        map_span(x, n, desc->x_stride, packed, es, "x"),
+                        vec_span(lambda, desc->c, "lambda"), vec_span(h0, rows, "h0", SPAN_STATE),
+                        raw_span(mask, n * desc->len, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return recurrence_fwd(*desc, r, i, x, lambda, mask, h0, y, h_last, carry, ws,
                           (hipStream_t)stream);
@@ -875,23 +887,22 @@ rat3d_status rat3d_recurrence_bwd(const rat3d_recurrence_desc* desc, const void*
     if (dh0) RAT3D_ELT(dh0, sizeof(float), "dh0");
     s = check_ws(ws, ws_bytes, recurrence_ws_bytes(*desc, 1));
     if (s != RAT3D_OK) return s;
-    const int64_t packed = desc->c * desc->len, rows = (int64_t)desc->n * desc->c;
-    const Span outs[] = {map_span(dr, desc->r_stride, packed, es, "dr"),
-                         map_span(di, desc->i_stride, packed, es, "di"),
-                         map_span(dx, desc->x_stride, packed, es, "dx")};
-    const Span ins[] = {map_span(dy, desc->y_stride, packed, es, "dy"),
-                        map_span(r, desc->r_stride, packed, es, "r"),
-                        map_span(i, desc->i_stride, packed, es, "i"),
-                        map_span(x, desc->x_stride, packed, es, "x")};
-    s = check_spans(outs, 3, ins, 4, desc->n, true);
-    if (s != RAT3D_OK) return s;
-    const Span vec[] = {vec_span(dlambda, desc->c, "dlambda"), vec_span(dh0, rows, "dh0"),
+    const int64_t packed = desc->c * desc->len, n = desc->n, rows = n * desc->c;
+    const Span outs[] = {map_span(dr, n, desc->r_stride, packed, es, "dr"),
+                         map_span(di, n, desc->i_stride, packed, es, "di"),
+                         map_span(dx, n, desc->x_stride, packed, es, "dx"),
+                         vec_span(dlambda, desc->c, "dlambda"),
+                         vec_span(dh0, rows, "dh0", SPAN_STATE),
+                         raw_span(ws, (int64_t)recurrence_ws_bytes(*desc, 1), "the workspace")};
+    const Span ins[] = {map_span(dy, n, desc->y_stride, packed, es, "dy"),
+                        map_span(r, n, desc->r_stride, packed, es, "r"),
+                        map_span(i, n, desc->i_stride, packed, es, "i"),
+                        map_span(x, n, desc->x_stride, packed, es, "x"),
+                        vec_span(dh_last, rows, "dh_last", SPAN_STATE),
                         vec_span(lambda, desc->c, "lambda"),
-                        vec_span(carry, (int64_t)recurrence_carry_bytes(*desc) / 4, "carry"),
-                        vec_span(dh_last == dh0 ? nullptr : dh_last, rows, "dh_last"),
-                        vec_span(dh_last, rows, "dh_last")};
-    s = check_spans(vec, 2, vec + 2, 3, 1, false);
-    if (s == RAT3D_OK) s = check_spans(vec, 1, vec + 5, 1, 1, false);
+                        raw_span(carry, (int64_t)recurrence_carry_bytes(*desc), "carry"),
+                        raw_span(mask, n * desc->len, "mask")};
+    s = check_spans(outs, ins);
     if (s != RAT3D_OK) return s;
     return recurrence_bwd(*desc, dy, dh_last, r, i, x, lambda, mask, carry, dr, di, dx, dlambda,
                           dh0, accumulate ? 1 : 0, ws, (hipStream_t)stream);

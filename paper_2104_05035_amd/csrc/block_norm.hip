@@ -41,6 +41,7 @@ struct NormArgs {
     int c, groups, gate;
     int stream, near;  // stores past the cache; neighbouring tiles on one XCD
     uint32_t tiles, all;  // of one volume, of all (below 2^31)
+    uint32_t base;        // this launch's first tile
     float eps;
 };
 
@@ -453,7 +454,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     };
 
     // backward: several tiles a workgroup, so that the gains' parts stay few
-    const uint32_t t0 = a.near ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x;
+    const uint32_t t0 = a.base + (a.near ? xcd_remap(blockIdx.x, gridDim.x) : blockIdx.x);
     uint32_t t = t0;
     do {
         const uint32_t vol = t / a.tiles;
@@ -576,11 +577,10 @@ static void norm_lines(const rat3d_norm_desc& d, NormArgs* a) {
 }
 
 template <typename T, NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream_t st) {
+static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr int TOK = 16 / (int)sizeof(T);
     const NormShape shape = norm_shape(d, kBwd);
-    const unsigned grid = norm_grid(a, kBwd);
     const int threads = a.groups * kLanes;
     const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
                      d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
@@ -591,23 +591,29 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormArgs& a, hipStream
         if (all) RAT3D_NORM1(TOK, PC, true, THREADS); \
         else RAT3D_NORM1(TOK, PC, false, THREADS);    \
     } while (0)
-    // a workgroup has at most as many threads as its kernel is built for
-    if (shape.tok == 1) {
-        if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
-        else RAT3D_NORM1(1, 0, false, 256);
-    } else if (shape.pc == 0) {
-        RAT3D_NORM(TOK, 0, 256);
-    } else if constexpr (!kBwd) {  // 128 registers are enough
-        if (shape.tok == 4) RAT3D_NORM(4, 4, 1024);
-        else if constexpr (TOK == 8) RAT3D_NORM(8, 4, 1024);
-    } else if (shape.tok == 4) {
-        if (shape.pc == 4 && threads <= 256) RAT3D_NORM(4, 4, 256);
-        else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(4, 4, 512);
-        else if constexpr (TOK == 8) RAT3D_NORM(4, 8, 512);
-        else RAT3D_NORM(4, 4, 1024);
-    } else if constexpr (TOK == 8) {
-        if (threads <= 256) RAT3D_NORM(8, 4, 256);
-        else RAT3D_NORM(8, 4, 512);
+    // a launch holds fewer than 2^32 threads; a workgroup at most as many as its kernel is
+    // built for
+    const uint32_t most = ((uint32_t)1 << 31) / (uint32_t)threads;
+    for (uint32_t left = norm_grid(a, kBwd); left; left -= left < most ? left : most) {
+        const unsigned grid = left < most ? left : most;
+        if (shape.tok == 1) {
+            if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
+            else RAT3D_NORM1(1, 0, false, 256);
+        } else if (shape.pc == 0) {
+            RAT3D_NORM(TOK, 0, 256);
+        } else if constexpr (!kBwd) {  // 128 registers are enough
+            if (shape.tok == 4) RAT3D_NORM(4, 4, 1024);
+            else if constexpr (TOK == 8) RAT3D_NORM(8, 4, 1024);
+        } else if (shape.tok == 4) {
+            if (shape.pc == 4 && threads <= 256) RAT3D_NORM(4, 4, 256);
+            else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(4, 4, 512);
+            else if constexpr (TOK == 8) RAT3D_NORM(4, 8, 512);
+            else RAT3D_NORM(4, 4, 1024);
+        } else if constexpr (TOK == 8) {
+            if (threads <= 256) RAT3D_NORM(8, 4, 256);
+            else RAT3D_NORM(8, 4, 512);
+        }
+        a.base += grid;
     }
 #undef RAT3D_NORM
 #undef RAT3D_NORM1

@@ -60,8 +60,10 @@ struct RecArgs {
     float rate;
 };
 
-__device__ __forceinline__ float softplusf(float v) {
-    return v > 0.f ? v + log1pf(expf(-v)) : log1pf(expf(v));
+// rate softplus(lambda), finite: with an infinite one a shut gate would give 0 times it.
+__device__ __forceinline__ float decay_of(float rate, float lam) {
+    const float w = rate * (lam > 0.f ? lam + log1pf(expf(-lam)) : log1pf(expf(lam)));
+    return w > 1e30f ? 1e30f : w;
 }
 
 // One voxel's step.
@@ -341,7 +343,7 @@ __global__ __launch_bounds__(64 * kWaves, 8) void recurrence_fwd_k(RecArgs q) {
         else read<T, 3, false>(d, in, mask, v, q.len);
     };
     fetch(cur, wave);  // under way while the walk's beginning is found
-    const float w = q.rate * softplusf(lam);
+    const float w = decay_of(q.rate, lam);
     float state = JOIN ? 0.f : segment_begin(q, row, seg), prod = 1.f;
     int par = 0;
     for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
@@ -420,7 +422,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_k(RecArgs q) {
         else read<T, 4, false>(d, in, mask, v, q.len);
     };
     fetch(cur, past0, wave);
-    const float w = q.rate * softplusf(lam);
+    const float w = decay_of(q.rate, lam);
     float state = segment_begin(q, row, seg);  // E
     double sum = 0.0;
     int par = 0;
@@ -488,7 +490,7 @@ __global__ __launch_bounds__(64 * kWaves) void recurrence_bwd_join_k(RecArgs q) 
                             (const T*)q.dy + vol * q.sy + (int64_t)ch * q.len};
     const uint8_t* mask = q.mask ? q.mask + vol * q.len : nullptr;
     const Segment sg(q, seg);
-    const float w = q.rate * softplusf(lam);
+    const float w = decay_of(q.rate, lam);
     float state = 0.f, prod = 1.f;
     int par = 0;
     for (int k0 = 0; k0 < sg.count; k0 += waves, par ^= 1) {
@@ -624,7 +626,7 @@ __global__ __launch_bounds__(64 * kWaves, 8) void recurrence_fwd_one_k(RecArgs q
     const int64_t v = (int64_t)at * BLOCK + lane * TOK;
     if (all) read<T, 3, true>(d, in, mask, v, q.len);
     else if (there) read<T, 3, false>(d, in, mask, v, q.len);
-    const float w = q.rate * softplusf(lam);
+    const float w = decay_of(q.rate, lam);
     Steps<T> s;
     if (all) s.template form<true>(d, w);
     else s.template form<false>(d, w);
@@ -673,7 +675,7 @@ __global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_one_k(RecArgs q
     const int64_t v = (int64_t)at * BLOCK + lane * TOK;
     if (all) read<T, 4, true>(d, in, mask, v, q.len);
     else if (there) read<T, 4, false>(d, in, mask, v, q.len);
-    const float w = q.rate * softplusf(lam);
+    const float w = decay_of(q.rate, lam);
     GradSteps<T, DOWN> s;
     if (all) s.template form<true>(d, w);
     else s.template form<false>(d, w);
@@ -777,7 +779,7 @@ __global__ __launch_bounds__(256) void recurrence_short_fwd_k(RecArgs q) {
     float state = q.h0 ? q.h0[row] : 0.f;
     const float first = state;
     Steps<T> s;
-    s.template form<false>(d, q.rate * softplusf(lam));
+    s.template form<false>(d, decay_of(q.rate, lam));
     const float2 mine = s.template all<DOWN>();
     float o[TOK];
     s.template states<DOWN>(short_walk<DOWN>(mine.x, mine.y, q.lanes, state), o);
@@ -807,7 +809,7 @@ __global__ __launch_bounds__(256) void recurrence_short_bwd_k(RecArgs q) {
     Raw<T, 4> d;
     read_short<T, 4>(d, in, q.mask ? q.mask + vol * q.len : nullptr, lane * TOK, q.len);
     GradSteps<T, DOWN> s;
-    s.template form<false>(d, q.rate * softplusf(lam));
+    s.template form<false>(d, decay_of(q.rate, lam));
     float A, B, F;
     s.all(A, B, F);
     float state = q.h0 ? q.h0[row] : 0.f, fwd = q.carry[row];

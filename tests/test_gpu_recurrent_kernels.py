@@ -126,6 +126,20 @@ def test_norm_rows_of_2_28_voxels():
                     2.0 ** -7 * want.float().abs().max())
 
 
+def test_norm_of_more_workgroups_than_a_launch_holds():
+    """2^26 volumes of one voxel: more than 2^32 threads, so more than one launch."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    n = (1 << 26) + 77
+    x = torch.arange(n, device="cuda:0").remainder_(5).sub_(2).float().view(n, 1, 1)
+    u = torch.full_like(x, 9.0)
+    R.rat3d_pre_norm_fwd(R.norm_desc(n, 1, 1, R.F32, eps=2.0 ** -100), x, torch.ones(1, device="cuda:0"),
+                         None, u)
+    U.sync()
+    # x / |x|: the root of a square is exact to a unit
+    assert bool(((u - x.sign()).abs() <= 4 * 2.0 ** -24).all())
+
+
 # ------------------------------------------------------------------ recurrence
 # rows (0: more than a CU each), tokens of bfloat16, the name's end
 WALKS = [(3, 100, "recurrence_short_"), (5, 128, "recurrence_short_"), (5, 129, "recurrence_"),

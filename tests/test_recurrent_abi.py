@@ -117,6 +117,13 @@ def test_norm_overlaps():
     _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, 6, p[2] + 4), 0, ws, need)
     for k in (0, 1, 4):
         _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, 5, bwd[k] + 2), 0, ws, need)
+    # results of one kind in tensors of another
+    for i, at in ((6, p[4]), (6, p[0] + 8), (5, ws), (6, ws), (5, p[2])):
+        _refused(R.EINVAL, R.rat3d_pre_norm_bwd, d, *_with(bwd, i, at), 0, ws, need)
+    _refused(R.EINVAL, R.rat3d_pre_norm_fwd, d, p[0], p[1], p[3], p[3])  # u over the mask
+    _refused(R.EINVAL, R.rat3d_pre_norm_fwd, d, p[0], p[1], None, p[1])  # u over gamma
+    _refused(R.EINVAL, R.rat3d_post_norm_fwd, d, *_with(post, 7, p[4]))
+    _refused(R.EINVAL, R.rat3d_post_norm_bwd, d, *_with(back, 13, back[9]), 0, ws, need)
 
 
 def _rec(**kw):
@@ -188,6 +195,13 @@ def test_recurrence_overlaps():
                       (10, 3, held), (8, 4, -2), (11, 5, 0), (11, 12, 0), (11, 7, 0), (12, 7, 0),
                       (12, 1, 4), (11, 1, 0), (12, 5, 4)):
         _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(bwd, i, bwd[k] + off), 0, ws, BIG)
+    # results of one kind in tensors of another: states and saved states, masks, workspaces
+    m = p[12]
+    for i, at in ((7, fwd[6]), (7, fwd[0] + 4), (8, fwd[2]), (8, fwd[6] + 8), (8, m), (6, m)):
+        _refused(R.EINVAL, R.rat3d_recurrence_fwd, d, *_with(_with(fwd, 4, m), i, at), ws, BIG)
+    need = R.rat3d_recurrence_workspace_size(d, 1)
+    for i, at in ((12, bwd[0]), (11, bwd[8]), (12, bwd[10] + 4), (10, m), (8, ws)):
+        _refused(R.EINVAL, R.rat3d_recurrence_bwd, d, *_with(_with(bwd, 6, m), i, at), 0, ws, need)
     # the gates and values side by side in one tensor: ranges between one another's volumes
     w = 3 * 24 * 60
     d = _rec(r_stride=w, i_stride=w, x_stride=w)

@@ -508,15 +508,20 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 //   in the backward of more than 128 channels, of twice the channels, so that a workgroup
 //   has 512 threads and their registers: 4 x 256 channels over 64512 voxels 546 -> 280 us
 //   behind a block, 146 -> 136 before one (the forward does not gain: 145 and 153 us).
+// and in the forward of 257 to 512 channels the same with 1024 threads: 2 x 512 channels
+// over 64512 voxels 215 -> 160 us behind a block, before one 56 -> 52.  (The gradients
+// spill: behind a block 586 us against 435 read again, before one with a mask 246 against
+// 200.)
 struct NormShape {
     int tok, pc, groups;
 };
-static NormShape norm_shape(const rat3d_norm_desc& d, bool bwd) {
+static NormShape norm_shape(const rat3d_norm_desc& d, NormMode mode) {
     const int es = d.dtype == RAT3D_BF16 ? 2 : 4, tok = d.v < 16 / es ? 1 : 16 / es;
+    const bool bwd = mode == PRE_BWD || mode == POST_BWD;
     // a group's rows are reached with 32 bits: at least 4 of them up to 2^28 tokens
     const int64_t most = ((int64_t)1 << 32) / (d.v * es);
-    if (d.c <= 256) {
-        const bool wide = bwd && tok == 8 && d.c > 128;
+    const bool wide = tok == 8 && d.c > (bwd ? 128 : 256);
+    if (d.c <= (wide && !bwd ? 512 : 256)) {
         const bool few = tok == 8 && ceil_div(d.v, kLanes * tok) * d.n < 2 * device_cus();
         const int pc = wide ? 8 : 4, groups = (int)ceil_div(d.c, 4 * pc) * 4;
         if (groups <= most) return {wide || few ? 4 : tok, pc, groups};
@@ -526,9 +531,9 @@ static NormShape norm_shape(const rat3d_norm_desc& d, bool bwd) {
     return {tok, 0, groups};
 }
 
-static void norm_plan(const rat3d_norm_desc& d, bool bwd, NormArgs* a) {
+static void norm_plan(const rat3d_norm_desc& d, NormMode mode, NormArgs* a) {
     const int64_t packed = (int64_t)d.c * d.v;
-    const NormShape shape = norm_shape(d, bwd);
+    const NormShape shape = norm_shape(d, mode);
     a->sx = d.x_stride ? d.x_stride : packed;
     a->sz = d.z_stride ? d.z_stride : packed;
     a->sg = d.g_stride ? d.g_stride : packed;
@@ -549,15 +554,20 @@ static void norm_plan(const rat3d_norm_desc& d, bool bwd, NormArgs* a) {
 
 // Backward: a few tiles a workgroup, so that the gains' parts stay few (2 to 32 workgroups
 // a CU take the same time within 3 % at 64 channels, 239 to 265 us at 128).
-static uint32_t norm_grid(const NormArgs& a, bool bwd) {
+static uint32_t norm_grid(const NormArgs& a, NormMode mode) {
     const uint32_t most = 4 * device_cus();
-    return bwd && a.all > most ? most : a.all;
+    return (mode == PRE_BWD || mode == POST_BWD) && a.all > most ? most : a.all;
 }
 
 size_t norm_ws_bytes(const rat3d_norm_desc& d) {
-    NormArgs a = {};
-    norm_plan(d, true, &a);
-    return (size_t)norm_grid(a, true) * 2 * d.c * sizeof(float);
+    uint32_t parts = 0;
+    for (NormMode mode : {PRE_BWD, POST_BWD}) {
+        NormArgs a = {};
+        norm_plan(d, mode, &a);
+        const uint32_t n = norm_grid(a, mode);
+        parts = n > parts ? n : parts;
+    }
+    return (size_t)parts * 2 * d.c * sizeof(float);
 }
 
 // Rows that begin inside a cache line: neighbouring tiles share lines, and one XCD's
@@ -580,7 +590,7 @@ template <typename T, NormMode MODE, bool GATED, bool NEXT>
 static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr int TOK = 16 / (int)sizeof(T);
-    const NormShape shape = norm_shape(d, kBwd);
+    const NormShape shape = norm_shape(d, MODE);
     const int threads = a.groups * kLanes;
     const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
                      d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
@@ -594,7 +604,7 @@ static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) 
     // a launch holds fewer than 2^32 threads; a workgroup at most as many as its kernel is
     // built for
     const uint32_t most = ((uint32_t)1 << 31) / (uint32_t)threads;
-    for (uint32_t left = norm_grid(a, kBwd); left; left -= left < most ? left : most) {
+    for (uint32_t left = norm_grid(a, MODE); left; left -= left < most ? left : most) {
         const unsigned grid = left < most ? left : most;
         if (shape.tok == 1) {
             if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
@@ -602,13 +612,16 @@ static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) 
         } else if (shape.pc == 0) {
             RAT3D_NORM(TOK, 0, 256);
         } else if constexpr (!kBwd) {  // 128 registers are enough
-            if (shape.tok == 4) RAT3D_NORM(4, 4, 1024);
-            else if constexpr (TOK == 8) RAT3D_NORM(8, 4, 1024);
+            if (shape.tok == 4 && shape.pc == 4) RAT3D_NORM(4, 4, 1024);
+            else if constexpr (TOK == 8) {
+                if (shape.pc == 8) RAT3D_NORM(4, 8, 1024);
+                else RAT3D_NORM(8, 4, 1024);
+            }
         } else if (shape.tok == 4) {
             if (shape.pc == 4 && threads <= 256) RAT3D_NORM(4, 4, 256);
             else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(4, 4, 512);
-            else if constexpr (TOK == 8) RAT3D_NORM(4, 8, 512);
-            else RAT3D_NORM(4, 4, 1024);
+            else if constexpr (TOK == 4) RAT3D_NORM(4, 4, 1024);
+            else RAT3D_NORM(4, 8, 512);
         } else if constexpr (TOK == 8) {
             if (threads <= 256) RAT3D_NORM(8, 4, 256);
             else RAT3D_NORM(8, 4, 512);
@@ -628,13 +641,14 @@ static void norm_launch(const rat3d_norm_desc& d, NormArgs& a, hipStream_t st) {
 
 // Names of the measurement: channels held in registers (of 16 or 8 bytes of tokens), read
 // again for every sum, or single tokens.
-static const char* norm_tag(const rat3d_norm_desc& d, bool bwd, const char* const (&names)[4]) {
-    const NormShape s = norm_shape(d, bwd);
+static const char* norm_tag(const rat3d_norm_desc& d, NormMode mode,
+                            const char* const (&names)[4]) {
+    const NormShape s = norm_shape(d, mode);
     const int full = d.dtype == RAT3D_BF16 ? 8 : 4;
     return names[s.tok == 1 ? 3 : s.pc == 0 ? 2 : s.tok < full ? 1 : 0];
 }
-#define RAT3D_NORM_TAG(name, bwd) \
-    norm_tag(d, bwd, {name, name "_half", name "_any", name "_one"})
+#define RAT3D_NORM_TAG(name, mode) \
+    norm_tag(d, mode, {name, name "_half", name "_any", name "_one"})
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
     return (double)d.n * d.c * d.v * tensors * (d.dtype == RAT3D_BF16 ? 2 : 4);
@@ -643,12 +657,12 @@ static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
 rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* gamma,
                           const uint8_t* mask, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, false, &a);
+    norm_plan(d, PRE_FWD, &a);
     a.x = x;
     a.gamma = gamma;
     a.mask = mask;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", false), st, 0.0, norm_bytes(d, 2));
+    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", PRE_FWD), st, 0.0, norm_bytes(d, 2));
     norm_launch<PRE_FWD, false, false>(d, a, st);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
@@ -658,7 +672,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
                            const float* gamma, const float* scale, const float* next,
                            const uint8_t* mask, void* y, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, false, &a);
+    norm_plan(d, POST_FWD, &a);
     a.x = x;
     a.z = z;
     a.g = g;
@@ -668,7 +682,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.mask = mask;
     a.oy = y;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", false), st, 0.0, norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
+    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD), st, 0.0, norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
     if (d.gate && next) norm_launch<POST_FWD, true, true>(d, a, st);
     else if (d.gate) norm_launch<POST_FWD, true, false>(d, a, st);
     else if (next) norm_launch<POST_FWD, false, true>(d, a, st);
@@ -677,9 +691,9 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     return RAT3D_OK;
 }
 
-static rat3d_status norm_gains(const NormArgs& a, float* dnext, float* dgamma, float* dscale,
+static rat3d_status norm_gains(const NormArgs& a, NormMode mode, float* dnext, float* dgamma, float* dscale,
                                int accumulate, hipStream_t st) {
-    const int parts = (int)norm_grid(a, true);
+    const int parts = (int)norm_grid(a, mode);
     ProfScope ps("norm_gain", st, 0.0, 8.0 * a.c * parts);
     norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
                                               dscale, accumulate);
@@ -691,7 +705,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
                           const float* gamma, const uint8_t* mask, const void* dres, void* dx,
                           float* dgamma, int accumulate, void* ws, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, true, &a);
+    norm_plan(d, PRE_BWD, &a);
     a.du = du;
     a.y = x;
     a.sy = a.sx;
@@ -701,11 +715,11 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.dx = dx;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", true), st, 0.0, norm_bytes(d, 3 + (dres != nullptr)));
+        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD), st, 0.0, norm_bytes(d, 3 + (dres != nullptr)));
         norm_launch<PRE_BWD, false, true>(d, a, st);
         RAT3D_LAUNCH_CHECK();
     }
-    return norm_gains(a, dgamma, nullptr, nullptr, accumulate, st);
+    return norm_gains(a, PRE_BWD, dgamma, nullptr, nullptr, accumulate, st);
 }
 
 rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void* du, const void* y,
@@ -714,7 +728,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
                            float* dgamma, float* dscale, float* dnext, int accumulate, void* ws,
                            hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, true, &a);
+    norm_plan(d, POST_BWD, &a);
     a.dy = dy;
     a.du = du;
     a.y = y;
@@ -729,7 +743,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dg = dg;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", true), st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", POST_BWD), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
         if (d.gate && next) norm_launch<POST_BWD, true, true>(d, a, st);
         else if (d.gate) norm_launch<POST_BWD, true, false>(d, a, st);
@@ -737,7 +751,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
         else norm_launch<POST_BWD, false, false>(d, a, st);
         RAT3D_LAUNCH_CHECK();
     }
-    return norm_gains(a, dnext, dgamma, dscale, accumulate, st);
+    return norm_gains(a, POST_BWD, dnext, dgamma, dscale, accumulate, st);
 }
 
 }  // namespace rat3d

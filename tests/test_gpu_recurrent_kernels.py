@@ -20,30 +20,32 @@ def _cus():
 
 # ------------------------------------------------------------------ norms
 # tokens, channels, whether there are tiles enough for eight tokens of bfloat16 a thread,
-# the name's end forward and backward in bfloat16, and in float32
-NORMS = [(7, 40, False, "_one", "_one", None), (3, 300, False, "_one", "_one", "_one"),
-         (130, 24, False, "_half", "_half", ""), (90, 128, True, "", "", ""),
-         (33, 100, True, "", "", ""), (256, 64, False, "_half", "_half", ""),
-         (40, 160, True, "", "_half", ""), (70, 256, False, "_half", "_half", ""),
-         (50, 257, False, "_any", "_any", "_any"), (129, 513, False, "_any", "_any", "_any")]
+# the name's end in bfloat16 (forward; gradient before and behind a block), and in float32
+NORMS = [(7, 40, False, "_one", "_one", "_one", None), (3, 300, False, "_one", "_one", "_one", "_one"),
+         (130, 24, False, "_half", "_half", "_half", ""), (90, 128, True, "", "", "", ""),
+         (33, 100, True, "", "", "", ""), (256, 64, False, "_half", "_half", "_half", ""),
+         (40, 160, True, "", "_half", "_half", ""), (70, 256, False, "_half", "_half", "_half", ""),
+         (50, 257, False, "_half", "_any", "_any", "_any"),
+         (128, 512, False, "_half", "_any", "_any", "_any"),
+         (129, 513, False, "_any", "_any", "_any", "_any")]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("case", NORMS, ids=lambda c: "v%d_c%d_%s" % (
     c[0], c[1], "many" if c[2] else "few"))
 def test_norm_kernels(case, dt):
-    v, c, many, fwd, bwd, f32 = case
+    v, c, many, fwd, pre, post, f32 = case
     if dt == "f32":
         if f32 is None:
             return
-        fwd = bwd = f32
+        fwd = pre = post = f32
     n = -(-int(2.1 * _cus()) // -(-v // 128)) if many else 2
     for mask in (None, "holes"):
         for kind, nxt in (("silu", True), (None, False)):
             tags = _tags(lambda: TN.test_post_norm((n, c, v, kind, nxt, mask), dt))
-            assert set(tags) == {"post_norm_fwd" + fwd, "post_norm_bwd" + bwd, "norm_gain"}
+            assert set(tags) == {"post_norm_fwd" + fwd, "post_norm_bwd" + post, "norm_gain"}
         tags = _tags(lambda: TN.test_pre_norm((n, c, v, None, False, mask), dt))
-        assert set(tags) == {"pre_norm_fwd" + fwd, "pre_norm_bwd" + bwd, "norm_gain"}
+        assert set(tags) == {"pre_norm_fwd" + fwd, "pre_norm_bwd" + pre, "norm_gain"}
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])

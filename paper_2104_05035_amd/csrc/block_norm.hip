@@ -18,7 +18,9 @@
 // once; beyond, each sum reads its tensors again.  Sums over a voxel's channels are
 // joined by lane swaps that leave each of a wave's four groups a quarter of the voxels,
 // and through LDS.  Rows need no alignment.
-// Bound: HBM.
+// Bound: HBM.  Bfloat16, 16 x 64 channels of 48x56x48 voxels: before a block 76 us (its
+// input partly in the memory-side cache), its gradient 201 us (5.3 TB/s); behind one with
+// gate and next norm 254 us (5.2), its gradient with all eight tensors 438 us (4.8).
 #include "kernels.hpp"
 #include "prof.hpp"
 #include "tokens.hpp"
@@ -510,8 +512,7 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 //   behind a block, 146 -> 136 before one (the forward does not gain: 145 and 153 us).
 // and in the forward of 257 to 512 channels the same with 1024 threads: 2 x 512 channels
 // over 64512 voxels 215 -> 160 us behind a block, before one 56 -> 52.  (The gradients
-// spill: behind a block 586 us against 435 read again, before one with a mask 246 against
-// 200.)
+// spill: behind a block 586 us against 428 read again.)
 struct NormShape {
     int tok, pc, groups;
 };
@@ -552,10 +553,12 @@ static void norm_plan(const rat3d_norm_desc& d, NormMode mode, NormArgs* a) {
     a->all = a->tiles * d.n;
 }
 
-// Backward: a few tiles a workgroup, so that the gains' parts stay few (2 to 32 workgroups
-// a CU take the same time within 3 % at 64 channels, 239 to 265 us at 128).
+// Backward: a few tiles a workgroup, so that the gains' parts stay few: two workgroups a CU,
+// more of fewer than 256 threads (gradient before a block over 16 x 64 channels of
+// 48x56x48 203 us with two, 217 with four; behind one over 16 x 32 251 and 225).
 static uint32_t norm_grid(const NormArgs& a, NormMode mode) {
-    const uint32_t most = 4 * device_cus();
+    const int threads = a.groups * kLanes;
+    const uint32_t most = (threads < 256 ? 512 / threads : 2) * device_cus();
     return (mode == PRE_BWD || mode == POST_BWD) && a.all > most ? most : a.all;
 }
 

@@ -27,7 +27,8 @@
 // reads would grow with their square).
 //
 // beta: 1 - a^2 is -expm1(-2 w sigmoid(r)), by its series where the argument is small.
-// Bound: HBM.
+// Bound: HBM.  Bfloat16, 16 x 64 rows of 48x56x48 voxels: forward 219 us (4.8 TB/s),
+// gradient 375 us (4.9); 32 such rows, cut, 15 and 28 us.
 #include "kernels.hpp"
 #include "prof.hpp"
 #include "tokens.hpp"

@@ -242,8 +242,9 @@ template <typename T, bool DOWN> struct GradSteps {
         for (int j = 0; j < TOK; ++j) {
             const Step s(q.t[0][j], w);
             const Sig gi(q.t[1][j]);
-            // at p = 0 (a shut gate) la inv and p inv come out as 0, their limits
-            const float inv = __builtin_amdgcn_rsqf(s.p < 0x1p-100f ? 0x1p-100f : s.p);
+            // at p = 0 (a shut gate) la inv and p inv come out as 0, their limits; a root
+            // of less than the smallest normal number would be infinite
+            const float inv = __builtin_amdgcn_rsqf(s.p < 0x1p-126f ? 0x1p-126f : s.p);
             const bool is = ALL || q.at.live >> j & 1u;
             a[j] = is ? s.a : 1.f;
             la[j] = is ? s.la * s.a : 0.f;                        // by the past state

@@ -25,8 +25,9 @@ from oracle import recurrent as Q
 from tests import attn_util as AU
 
 F, U, TINY = AU.F, AU.U, AU.TINY
-# beta below 2^-50 may come out as p 2^50 (p = beta^2), and 1/beta is at most 2^50
-SHUT = 2.0 ** -49
+# beta below 2^-63 may come out as p 2^63 (p = beta^2), and 1/beta is at most 2^63; a
+# sigmoid below 2^-126 may come out as 0, and beta^2 is at most 2^10 times that
+SHUT = 2.0 ** -58
 within = AU.within
 
 

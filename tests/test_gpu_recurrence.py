@@ -346,6 +346,42 @@ def test_shut_and_open_gates(dt):
             assert bool((dh0 == 0).all()) and bool((dr == 0).all())
 
 
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("v", [1, 40, 1300, 9000])
+def test_nearly_shut_gates(v, dt):
+    """Gates of -85 to -60, whose results are tiny and hold their digits all the same.  By
+    magnitudes, for nothing cancels: sigmoid(r) is off by e = (2 |r| + 10) f, the decay's
+    logarithm by e + 18 f, beta and 1/beta by half of it + 4 f and one rounding each, D and
+    the states by 64 f for the walk; products of up to six factors round six times."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    rng = _rng((v, dt))
+    ref, dev = {}, {}
+    for k, a in (("r", rng.uniform(-85, -60, (1, 3, v))), ("i", rng.standard_normal((1, 3, v))),
+                 ("x", rng.uniform(0.5, 2, (1, 3, v))), ("dy", rng.uniform(0.5, 2, (1, 3, v)))):
+        dev[k], ref[k] = U.dev_input(a, dt)
+    dev["lam"], ref["lam"] = U.dev_input(np.array([-3.0, 0.0, 2.0]), "f32")
+    d = R.recurrence_desc(1, 3, v, U.code(dt))
+    need = [R.rat3d_recurrence_workspace_size(d, p) for p in (0, 1)]
+    carry = _ws(R.rat3d_recurrence_carry_size(d))
+    y, dr, di, dx = (torch.empty_like(dev["x"]) for _ in range(4))
+    last, dlam = torch.empty((1, 3), device="cuda:0"), torch.empty(3, device="cuda:0")
+    R.rat3d_recurrence_fwd(d, dev["r"], dev["i"], dev["x"], dev["lam"], None, None, y, last, carry,
+                           _ws(need[0]), need[0])
+    R.rat3d_recurrence_bwd(d, dev["dy"], None, dev["r"], dev["i"], dev["x"], dev["lam"], None,
+                           carry, dr, di, dx, dlam, None, 0, _ws(need[1]), need[1])
+    U.sync()
+    ye, le, past = Q.recurrence(ref["r"], ref["i"], ref["x"], ref["lam"], None, None, 8.0, False)
+    want = Q.recurrence_bwd(ref["dy"], None, ref["r"], ref["i"], ref["x"], ref["lam"], None, past,
+                            8.0, False)
+    e = 1.5 * (2 * 85 + 10 + 18) * RU.F + (2 * 6 + 10) * RU.F + 128 * RU.F
+    for k, got, exact in (("y", y, ye), ("h_last", last, le), ("dx", dx, want["dx"]),
+                          ("di", di, want["di"]), ("dr", dr, want["dr"]),
+                          ("dlam", dlam, want["dlam"])):
+        rel = np.abs(U.f64(got) / exact - 1.0)
+        assert rel.max() <= e + RU.U["f32" if k in ("h_last", "dlam") else dt], (k, rel.max())
+
+
 @pytest.mark.parametrize("v", [3, 40, 1300, 20000])
 @pytest.mark.parametrize("name", ["r", "i", "x"])
 def test_nan_stays_in_its_row(v, name):

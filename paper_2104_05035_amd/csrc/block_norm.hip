@@ -32,7 +32,8 @@ constexpr int kLanes = 16;  // along the voxels
 enum NormMode { PRE_FWD, PRE_BWD, POST_FWD, POST_BWD };
 
 struct NormArgs {
-    // forward: x, z, g -> y, u.  Backward: dy, du, y (before: x, dres for y, dy), z, g -> dx, dz, dg
+    // forward: x, z, g -> y, u.  Backward: dy, du, y (before a block dres, du, x), z, g ->
+    // dx, dz, dg
     const void *x, *z, *g, *y, *dy, *du;
     void *oy, *ou, *dx, *dz, *dg;
     const float *gamma, *scale, *next;
@@ -685,7 +686,8 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.mask = mask;
     a.oy = y;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD), st, 0.0, norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
+    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD), st, 0.0,
+                 norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
     if (d.gate && next) norm_launch<POST_FWD, true, true>(d, a, st);
     else if (d.gate) norm_launch<POST_FWD, true, false>(d, a, st);
     else if (next) norm_launch<POST_FWD, false, true>(d, a, st);
@@ -694,8 +696,8 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     return RAT3D_OK;
 }
 
-static rat3d_status norm_gains(const NormArgs& a, NormMode mode, float* dnext, float* dgamma, float* dscale,
-                               int accumulate, hipStream_t st) {
+static rat3d_status norm_gains(const NormArgs& a, NormMode mode, float* dnext, float* dgamma,
+                               float* dscale, int accumulate, hipStream_t st) {
     const int parts = (int)norm_grid(a, mode);
     ProfScope ps("norm_gain", st, 0.0, 8.0 * a.c * parts);
     norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
@@ -718,7 +720,8 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.dx = dx;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD), st, 0.0, norm_bytes(d, 3 + (dres != nullptr)));
+        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD), st, 0.0,
+                     norm_bytes(d, 3 + (dres != nullptr)));
         norm_launch<PRE_BWD, false, true>(d, a, st);
         RAT3D_LAUNCH_CHECK();
     }

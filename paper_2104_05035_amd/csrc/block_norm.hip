@@ -14,8 +14,9 @@
 // Layout: 16 lanes along the voxels, 16 bytes each, by groups of threads along the
 // channels, so a channel's row is read in pieces of 256 bytes; a group takes the
 // channels grp, grp + groups, ... Up to 512 channels a thread keeps what it has read of
-// its channels (4, or 8 of half as many voxels) in registers, so every tensor passes
-// once; beyond, each sum reads its tensors again.  Sums over a voxel's channels are
+// its 4 or 8 channels in registers (of half or a quarter as many voxels where they would
+// not fit), so every tensor passes once; beyond, and in the backward of large maps beyond
+// 256, each sum reads its tensors again.  Sums over a voxel's channels are
 // joined by lane swaps that leave each of a wave's four groups a quarter of the voxels,
 // and through LDS.  Rows need no alignment.
 // Bound: HBM.  Bfloat16, 16 x 64 channels of 48x56x48 voxels: before a block 76 us (its
@@ -73,6 +74,10 @@ __device__ __forceinline__ void channel_sums(float (&s)[K][TOK], float* lds, int
             const float h = join32(s[k][0], s[k][0]);
             const float v = join16(h, h);
             if (row == 0) *to = v;
+        } else if constexpr (TOK == 2) {
+            const float h = join32(s[k][0], s[k][1]);
+            const float v = join16(h, h);
+            if (!(row & 1)) to[row >> 1] = v;
         } else {
             constexpr int PART = TOK / 4;  // tokens that one group of a wave sums up
             float h[TOK / 2];
@@ -503,39 +508,68 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
 
 // ------------------------------------------------------------------ host
 // Tokens and channels a thread, and groups of threads along the channels (whole waves).
-// In bfloat16 half as many tokens,
-//   where there are fewer than two tiles a CU, so that one loads while another sums or
-//   stores: 16 x 128 channels of 12x14x12 voxels 15.3 -> 12.5 us behind a block, its
-//   gradient 34.9 -> 31.1, before a block 7.5 -> 6.5 and 16.4 -> 13.7 (at 8 x 64 of
-//   24x28x24, four tiles a CU, 18.4 -> 19.5 and 35.5 -> 36.9);
-//   in the backward of more than 128 channels, of twice the channels, so that a workgroup
-//   has 512 threads and their registers: 4 x 256 channels over 64512 voxels 546 -> 280 us
-//   behind a block, 146 -> 136 before one (the forward does not gain: 145 and 153 us).
-// and in the forward of 257 to 512 channels the same with 1024 threads: 2 x 512 channels
-// over 64512 voxels 215 -> 160 us behind a block, before one 56 -> 52.  (The gradients
-// spill: behind a block 586 us against 428 read again.)
+// Fewer tokens than 16 bytes hold,
+//   half, where there are few tiles, so that one loads while another sums or stores: in
+//   bfloat16 below two a CU (16 x 128 channels of 12x14x12 voxels 15.3 -> 12.5 us behind a
+//   block, its gradient 34.9 -> 31.1, before a block 7.5 -> 6.5 and 16.4 -> 13.7; at 8 x 64
+//   of 24x28x24, four tiles a CU, 18.4 -> 19.5 and 35.5 -> 36.9), in float32 up to one for
+//   two CUs (16 x 256 channels of 252 voxels 13.1 -> 9.0 and 35.5 -> 19.0, before a block
+//   15.5 -> 12.1; at 2 x 256 of 16128, two tiles a CU, 36.7 -> 39.8 behind a block);
+//   half, with twice the channels, in the forward of more than 256 channels: 4 x 512
+//   channels over 16128 voxels in float32 215 -> 150 us behind a block, 55 -> 41 before one
+//   (bfloat16, also of up to 512 channels 215 -> 160 and 56 -> 52 over 2 x 64512 voxels);
+//   half in the backward of more than 128 channels, where the registers of the full number
+//   spill: in bfloat16 with twice the channels (4 x 256 channels over 64512 voxels 546 ->
+//   280 us behind a block, 146 -> 136 before one), in float32 for the gradient behind a
+//   block with a next norm and a mask, unwhole tiles or channels (4 x 256 channels over
+//   16127 voxels 193 -> 154 us; over 16128 without a mask it does not gain, and neither do
+//   the other gradients: 76 -> 85 without a next norm);
+//   a quarter in the backward of 257 to 512 channels, where rows are no whole tiles (4 x 512
+//   channels over 16127 voxels in float32 567 -> 399 us behind a block, 253 -> 149 before
+//   one) or tiles are few (one of 400 channels and 27 voxels 92 -> 20 us), and in bfloat16
+//   of 129 to 256 channels where tiles are few (one of 256 channels 24 -> 16 us).  Large
+//   maps of whole tiles are read again instead: 4 x 512 over 16128 in float32 349 us
+//   against 362, bfloat16 183 against 193, before a block 151 against 184 and 85 against 97.
+// Channels that are read again have 64 groups, few rounds: 4 x 600 channels over 16128
+// voxels in bfloat16 244 -> 233 us, before a block 135 -> 102, behind one 162 -> 115,
+// against 16 groups.
 struct NormShape {
     int tok, pc, groups;
 };
-static NormShape norm_shape(const rat3d_norm_desc& d, NormMode mode) {
+static NormShape norm_shape(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next) {
     const int es = d.dtype == RAT3D_BF16 ? 2 : 4, tok = d.v < 16 / es ? 1 : 16 / es;
     const bool bwd = mode == PRE_BWD || mode == POST_BWD;
+    const int64_t tiles = ceil_div(d.v, kLanes * tok) * d.n;
+    const bool few = tok == 8 ? tiles < 2 * device_cus() : 2 * tiles <= device_cus();
+    const bool least = 4 * tiles < device_cus();
     // a group's rows are reached with 32 bits: at least 4 of them up to 2^28 tokens
     const int64_t most = ((int64_t)1 << 32) / (d.v * es);
-    const bool wide = tok == 8 && d.c > (bwd ? 128 : 256);
-    if (d.c <= (wide && !bwd ? 512 : 256)) {
-        const bool few = tok == 8 && ceil_div(d.v, kLanes * tok) * d.n < 2 * device_cus();
-        const int pc = wide ? 8 : 4, groups = (int)ceil_div(d.c, 4 * pc) * 4;
-        if (groups <= most) return {wide || few ? 4 : tok, pc, groups};
+    NormShape s = {tok, 4, 0};
+    if (tok == 1) {
+        if (d.c > 256) s.pc = 0;
+    } else if (d.c > 512) {
+        s.pc = 0;
+    } else if (d.c > 256) {
+        if (!bwd) s = {tok / 2, 8, 0};
+        else if (least || d.v % 64) s = {tok / 4, 8, 0};
+        else s.pc = 0;
+    } else if (d.c <= 128 || !bwd) {
+        if (few) s.tok = tok / 2;
+    } else if (tok == 8) {
+        s = least ? NormShape{2, 4, 0} : NormShape{4, 8, 0};
+    } else if (few || (mode == POST_BWD && next && (masked || d.v % 64 || d.c % 16))) {
+        s.tok = 2;
     }
-    int groups = 16;
-    while (groups > most) groups /= 2;
-    return {tok, 0, groups};
+    if (s.pc) s.groups = (int)ceil_div(d.c, 4 * s.pc) * 4;
+    if (!s.pc || s.groups > most) s = {tok, 0, 64};
+    while (s.groups > most) s.groups /= 2;
+    return s;
 }
 
-static void norm_plan(const rat3d_norm_desc& d, NormMode mode, NormArgs* a) {
+static void norm_plan(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next,
+                      NormArgs* a) {
     const int64_t packed = (int64_t)d.c * d.v;
-    const NormShape shape = norm_shape(d, mode);
+    const NormShape shape = norm_shape(d, mode, masked, next);
     a->sx = d.x_stride ? d.x_stride : packed;
     a->sz = d.z_stride ? d.z_stride : packed;
     a->sg = d.g_stride ? d.g_stride : packed;
@@ -563,15 +597,13 @@ static uint32_t norm_grid(const NormArgs& a, NormMode mode) {
     return (mode == PRE_BWD || mode == POST_BWD) && a.all > most ? most : a.all;
 }
 
+// The parts of the shape with the shortest tiles, and the most workgroups: of 64 channels
+// on, and where 32 bits reach 16 groups, they have 256 threads or more.
 size_t norm_ws_bytes(const rat3d_norm_desc& d) {
-    uint32_t parts = 0;
-    for (NormMode mode : {PRE_BWD, POST_BWD}) {
-        NormArgs a = {};
-        norm_plan(d, mode, &a);
-        const uint32_t n = norm_grid(a, mode);
-        parts = n > parts ? n : parts;
-    }
-    return (size_t)parts * 2 * d.c * sizeof(float);
+    const int full = d.dtype == RAT3D_BF16 ? 8 : 4, tok = d.v < full ? 1 : full / 4;
+    const int64_t tiles = ceil_div(d.v, kLanes * tok) * d.n;
+    const int64_t most = (d.c < 64 || d.v > 1 << 24 ? 8 : 2) * (int64_t)device_cus();
+    return (size_t)(tiles < most ? tiles : most) * 2 * d.c * sizeof(float);
 }
 
 // Rows that begin inside a cache line: neighbouring tiles share lines, and one XCD's
@@ -594,7 +626,7 @@ template <typename T, NormMode MODE, bool GATED, bool NEXT>
 static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr int TOK = 16 / (int)sizeof(T);
-    const NormShape shape = norm_shape(d, MODE);
+    const NormShape shape = norm_shape(d, MODE, a.mask != nullptr, NEXT);
     const int threads = a.groups * kLanes;
     const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
                      d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
@@ -610,25 +642,29 @@ static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) 
     const uint32_t most = ((uint32_t)1 << 31) / (uint32_t)threads;
     for (uint32_t left = norm_grid(a, MODE); left; left -= left < most ? left : most) {
         const unsigned grid = left < most ? left : most;
-        if (shape.tok == 1) {
+        if (d.v < TOK) {
             if (shape.pc) RAT3D_NORM1(1, 4, false, 1024);
-            else RAT3D_NORM1(1, 0, false, 256);
+            else RAT3D_NORM1(1, 0, false, 1024);
         } else if (shape.pc == 0) {
-            RAT3D_NORM(TOK, 0, 256);
+            RAT3D_NORM(TOK, 0, 1024);
         } else if constexpr (!kBwd) {  // 128 registers are enough
-            if (shape.tok == 4 && shape.pc == 4) RAT3D_NORM(4, 4, 1024);
-            else if constexpr (TOK == 8) {
-                if (shape.pc == 8) RAT3D_NORM(4, 8, 1024);
-                else RAT3D_NORM(8, 4, 1024);
-            }
-        } else if (shape.tok == 4) {
-            if (shape.pc == 4 && threads <= 256) RAT3D_NORM(4, 4, 256);
-            else if (shape.pc == 4 && threads <= 512) RAT3D_NORM(4, 4, 512);
-            else if constexpr (TOK == 4) RAT3D_NORM(4, 4, 1024);
-            else RAT3D_NORM(4, 8, 512);
+            if (shape.tok == TOK) RAT3D_NORM(TOK, 4, 1024);
+            else if (shape.pc == 4) RAT3D_NORM(TOK / 2, 4, 1024);
+            else RAT3D_NORM(TOK / 2, 8, 1024);
+        } else if (shape.tok == TOK) {
+            if (threads <= 256) RAT3D_NORM(TOK, 4, 256);
+            else if (TOK == 8 || threads <= 512) RAT3D_NORM(TOK, 4, 512);
+            else if constexpr (TOK == 4 && MODE == POST_BWD && NEXT) RAT3D_NORM1(TOK, 4, true, 1024);
+            else if constexpr (TOK == 4) RAT3D_NORM(TOK, 4, 1024);
+        } else if (shape.tok == TOK / 2 && shape.pc == 4) {
+            if (threads <= 256) RAT3D_NORM(TOK / 2, 4, 256);
+            else if (TOK == 8 || threads <= 512) RAT3D_NORM(TOK / 2, 4, 512);
+            else if constexpr (TOK == 4) RAT3D_NORM(TOK / 2, 4, 1024);
+        } else if (shape.pc == 8) {
+            if (shape.tok == TOK / 4) RAT3D_NORM(TOK / 4, 8, 1024);
+            else if constexpr (TOK == 8) RAT3D_NORM(TOK / 2, 8, 512);
         } else if constexpr (TOK == 8) {
-            if (threads <= 256) RAT3D_NORM(8, 4, 256);
-            else RAT3D_NORM(8, 4, 512);
+            RAT3D_NORM(TOK / 4, 4, 1024);
         }
         a.base += grid;
     }
@@ -643,16 +679,16 @@ static void norm_launch(const rat3d_norm_desc& d, NormArgs& a, hipStream_t st) {
     else norm_launch_t<float, MODE, GATED, NEXT>(d, a, st);
 }
 
-// Names of the measurement: channels held in registers (of 16 or 8 bytes of tokens), read
-// again for every sum, or single tokens.
-static const char* norm_tag(const rat3d_norm_desc& d, NormMode mode,
-                            const char* const (&names)[4]) {
-    const NormShape s = norm_shape(d, mode);
+// Names of the measurement: channels held in registers (of 16, 8 or 4 bytes of tokens),
+// read again for every sum, or single tokens.
+static const char* norm_tag(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next,
+                            const char* const (&names)[5]) {
+    const NormShape s = norm_shape(d, mode, masked, next);
     const int full = d.dtype == RAT3D_BF16 ? 8 : 4;
-    return names[s.tok == 1 ? 3 : s.pc == 0 ? 2 : s.tok < full ? 1 : 0];
+    return names[d.v < full ? 4 : s.pc == 0 ? 3 : s.tok == full ? 0 : 2 * s.tok == full ? 1 : 2];
 }
-#define RAT3D_NORM_TAG(name, mode) \
-    norm_tag(d, mode, {name, name "_half", name "_any", name "_one"})
+#define RAT3D_NORM_TAG(name, mode, next) \
+    norm_tag(d, mode, mask != nullptr, next, {name, name "_half", name "_quarter", name "_any", name "_one"})
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
     return (double)d.n * d.c * d.v * tensors * (d.dtype == RAT3D_BF16 ? 2 : 4);
@@ -661,12 +697,12 @@ static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
 rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* gamma,
                           const uint8_t* mask, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, PRE_FWD, &a);
+    norm_plan(d, PRE_FWD, mask != nullptr, false, &a);
     a.x = x;
     a.gamma = gamma;
     a.mask = mask;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", PRE_FWD), st, 0.0, norm_bytes(d, 2));
+    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", PRE_FWD, false), st, 0.0, norm_bytes(d, 2));
     norm_launch<PRE_FWD, false, false>(d, a, st);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
@@ -676,7 +712,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
                            const float* gamma, const float* scale, const float* next,
                            const uint8_t* mask, void* y, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, POST_FWD, &a);
+    norm_plan(d, POST_FWD, mask != nullptr, next != nullptr, &a);
     a.x = x;
     a.z = z;
     a.g = g;
@@ -686,7 +722,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.mask = mask;
     a.oy = y;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD), st, 0.0,
+    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD, next != nullptr), st, 0.0,
                  norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
     if (d.gate && next) norm_launch<POST_FWD, true, true>(d, a, st);
     else if (d.gate) norm_launch<POST_FWD, true, false>(d, a, st);
@@ -710,7 +746,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
                           const float* gamma, const uint8_t* mask, const void* dres, void* dx,
                           float* dgamma, int accumulate, void* ws, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, PRE_BWD, &a);
+    norm_plan(d, PRE_BWD, mask != nullptr, true, &a);
     a.du = du;
     a.y = x;
     a.sy = a.sx;
@@ -720,7 +756,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.dx = dx;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD), st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD, true), st, 0.0,
                      norm_bytes(d, 3 + (dres != nullptr)));
         norm_launch<PRE_BWD, false, true>(d, a, st);
         RAT3D_LAUNCH_CHECK();
@@ -734,7 +770,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
                            float* dgamma, float* dscale, float* dnext, int accumulate, void* ws,
                            hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, POST_BWD, &a);
+    norm_plan(d, POST_BWD, mask != nullptr, next != nullptr, &a);
     a.dy = dy;
     a.du = du;
     a.y = y;
@@ -749,7 +785,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dg = dg;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", POST_BWD), st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", POST_BWD, next != nullptr), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
         if (d.gate && next) norm_launch<POST_BWD, true, true>(d, a, st);
         else if (d.gate) norm_launch<POST_BWD, true, false>(d, a, st);

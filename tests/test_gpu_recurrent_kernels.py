@@ -19,30 +19,34 @@ def _cus():
 
 
 # ------------------------------------------------------------------ norms
-# tokens, channels, whether there are tiles enough for eight tokens of bfloat16 a thread,
-# the name's end in bfloat16 (forward; gradient before and behind a block), and in float32
-NORMS = [(7, 40, False, "_one", "_one", "_one", None), (3, 300, False, "_one", "_one", "_one", "_one"),
-         (130, 24, False, "_half", "_half", "_half", ""), (90, 128, True, "", "", "", ""),
-         (33, 100, True, "", "", "", ""), (256, 64, False, "_half", "_half", "_half", ""),
-         (40, 160, True, "", "_half", "_half", ""), (70, 256, False, "_half", "_half", "_half", ""),
-         (50, 257, False, "_half", "_any", "_any", "_any"),
-         (128, 512, False, "_half", "_any", "_any", "_any"),
-         (129, 513, False, "_any", "_any", "_any", "_any")]
+# tokens, channels, volumes, and the names' ends in bfloat16 and float32: forward, gradient
+# before a block, behind one with and without a next norm (a pair: without and with a mask)
+ONE, HALF, QUARTER, ANY, FULL = (("_one",) * 4, ("_half",) * 4, ("_half",) + ("_quarter",) * 3,
+                                 ("_any",) * 4, ("",) * 4)
+REST = ("_half",) + ("_any",) * 3
+NORMS = [
+    (7, 40, "few", ONE, HALF), (3, 300, "few", ONE, ONE), (130, 24, "few", HALF, HALF),
+    (90, 128, "many", FULL, FULL), (33, 100, "many", FULL, FULL), (33, 100, "few", HALF, HALF),
+    (256, 64, "few", HALF, HALF), (128, 128, "few", HALF, HALF), (70, 256, "few", QUARTER, HALF),
+    (64, 256, "few", QUARTER, HALF), (40, 160, "many", ("",) + ("_half",) * 3, ("", "", "_half", "")),
+    (64, 256, "some", HALF, ("", "", ("", "_half"), "")),
+    (64, 200, "some", HALF, ("", "", "_half", "")), (50, 257, "few", QUARTER, QUARTER),
+    (128, 512, "few", QUARTER, QUARTER), (128, 384, "some", REST, REST),
+    (64, 270, "some", REST, REST), (129, 300, "some", QUARTER, QUARTER),
+    (129, 513, "few", ANY, ANY), (128, 640, "few", ANY, ANY)]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
-@pytest.mark.parametrize("case", NORMS, ids=lambda c: "v%d_c%d_%s" % (
-    c[0], c[1], "many" if c[2] else "few"))
+@pytest.mark.parametrize("case", NORMS, ids=lambda c: "v%d_c%d_%s" % c[:3])
 def test_norm_kernels(case, dt):
-    v, c, many, fwd, pre, post, f32 = case
-    if dt == "f32":
-        if f32 is None:
-            return
-        fwd = pre = post = f32
-    n = -(-int(2.1 * _cus()) // -(-v // 128)) if many else 2
-    for mask in (None, "holes"):
-        for kind, nxt in (("silu", True), (None, False)):
-            tags = _tags(lambda: TN.test_post_norm((n, c, v, kind, nxt, mask), dt))
+    v, c, volumes, *ends = case
+    # of 16 bytes of tokens a thread: tiles more than two a CU, or one for two CUs
+    n = dict(few=2, some=_cus() // 2 + 12, many=-(-int(2.1 * _cus()) // -(-v // 128)))[volumes]
+    ends = [e if isinstance(e, tuple) else (e, e) for e in ends[dt == "f32"]]
+    for k, mask in enumerate((None, "holes")):
+        fwd, pre, nxt, last = (e[k] for e in ends)
+        for kind, is_next, post in (("silu", True, nxt), (None, False, last)):
+            tags = _tags(lambda: TN.test_post_norm((n, c, v, kind, is_next, mask), dt))
             assert set(tags) == {"post_norm_fwd" + fwd, "post_norm_bwd" + post, "norm_gain"}
         tags = _tags(lambda: TN.test_pre_norm((n, c, v, None, False, mask), dt))
         assert set(tags) == {"pre_norm_fwd" + fwd, "pre_norm_bwd" + pre, "norm_gain"}

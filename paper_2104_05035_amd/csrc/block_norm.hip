@@ -540,8 +540,8 @@ static NormShape norm_shape(const rat3d_norm_desc& d, NormMode mode, bool masked
     const int es = d.dtype == RAT3D_BF16 ? 2 : 4, tok = d.v < 16 / es ? 1 : 16 / es;
     const bool bwd = mode == PRE_BWD || mode == POST_BWD;
     const int64_t tiles = ceil_div(d.v, kLanes * tok) * d.n;
-    const bool few = tok == 8 ? tiles < 2 * device_cus() : 2 * tiles <= device_cus();
-    const bool least = 4 * tiles < device_cus();
+    const int64_t cus = device_cus();
+    const bool few = tok == 8 ? tiles < 2 * cus : 2 * tiles <= cus, least = 4 * tiles < cus;
     // a group's rows are reached with 32 bits: at least 4 of them up to 2^28 tokens
     const int64_t most = ((int64_t)1 << 32) / (d.v * es);
     NormShape s = {tok, 4, 0};
@@ -566,8 +566,8 @@ static NormShape norm_shape(const rat3d_norm_desc& d, NormMode mode, bool masked
     return s;
 }
 
-static void norm_plan(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next,
-                      NormArgs* a) {
+static NormShape norm_plan(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next,
+                           NormArgs* a) {
     const int64_t packed = (int64_t)d.c * d.v;
     const NormShape shape = norm_shape(d, mode, masked, next);
     a->sx = d.x_stride ? d.x_stride : packed;
@@ -586,15 +586,17 @@ static void norm_plan(const rat3d_norm_desc& d, NormMode mode, bool masked, bool
     a->groups = shape.groups;
     a->tiles = (uint32_t)ceil_div(d.v, kLanes * shape.tok);
     a->all = a->tiles * d.n;
+    return shape;
 }
 
 // Backward: a few tiles a workgroup, so that the gains' parts stay few: two workgroups a CU,
 // more of fewer than 256 threads (gradient before a block over 16 x 64 channels of
 // 48x56x48 203 us with two, 217 with four; behind one over 16 x 32 251 and 225).
 static uint32_t norm_grid(const NormArgs& a, NormMode mode) {
+    if (mode == PRE_FWD || mode == POST_FWD) return a.all;
     const int threads = a.groups * kLanes;
     const uint32_t most = (threads < 256 ? 512 / threads : 2) * device_cus();
-    return (mode == PRE_BWD || mode == POST_BWD) && a.all > most ? most : a.all;
+    return a.all > most ? most : a.all;
 }
 
 // The parts of the shape with the shortest tiles, and the most workgroups: of 64 channels
@@ -623,10 +625,10 @@ static void norm_lines(const rat3d_norm_desc& d, NormArgs* a) {
 }
 
 template <typename T, NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) {
+static void norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, NormArgs a,
+                          hipStream_t st) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr int TOK = 16 / (int)sizeof(T);
-    const NormShape shape = norm_shape(d, MODE, a.mask != nullptr, NEXT);
     const int threads = a.groups * kLanes;
     const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
                      d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
@@ -673,22 +675,22 @@ static void norm_launch_t(const rat3d_norm_desc& d, NormArgs a, hipStream_t st) 
 }
 
 template <NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch(const rat3d_norm_desc& d, NormArgs& a, hipStream_t st) {
+static void norm_launch(const rat3d_norm_desc& d, const NormShape& shape, NormArgs& a,
+                        hipStream_t st) {
     norm_lines(d, &a);
-    if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, a, st);
-    else norm_launch_t<float, MODE, GATED, NEXT>(d, a, st);
+    if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, shape, a, st);
+    else norm_launch_t<float, MODE, GATED, NEXT>(d, shape, a, st);
 }
 
 // Names of the measurement: channels held in registers (of 16, 8 or 4 bytes of tokens),
 // read again for every sum, or single tokens.
-static const char* norm_tag(const rat3d_norm_desc& d, NormMode mode, bool masked, bool next,
+static const char* norm_tag(const rat3d_norm_desc& d, const NormShape& s,
                             const char* const (&names)[5]) {
-    const NormShape s = norm_shape(d, mode, masked, next);
     const int full = d.dtype == RAT3D_BF16 ? 8 : 4;
     return names[d.v < full ? 4 : s.pc == 0 ? 3 : s.tok == full ? 0 : 2 * s.tok == full ? 1 : 2];
 }
-#define RAT3D_NORM_TAG(name, mode, next) \
-    norm_tag(d, mode, mask != nullptr, next, {name, name "_half", name "_quarter", name "_any", name "_one"})
+#define RAT3D_NORM_TAG(name) \
+    norm_tag(d, shape, {name, name "_half", name "_quarter", name "_any", name "_one"})
 
 static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
     return (double)d.n * d.c * d.v * tensors * (d.dtype == RAT3D_BF16 ? 2 : 4);
@@ -697,13 +699,13 @@ static double norm_bytes(const rat3d_norm_desc& d, int tensors) {
 rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* gamma,
                           const uint8_t* mask, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, PRE_FWD, mask != nullptr, false, &a);
+    const NormShape shape = norm_plan(d, PRE_FWD, mask != nullptr, false, &a);
     a.x = x;
     a.gamma = gamma;
     a.mask = mask;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd", PRE_FWD, false), st, 0.0, norm_bytes(d, 2));
-    norm_launch<PRE_FWD, false, false>(d, a, st);
+    ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd"), st, 0.0, norm_bytes(d, 2));
+    norm_launch<PRE_FWD, false, false>(d, shape, a, st);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }
@@ -712,7 +714,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
                            const float* gamma, const float* scale, const float* next,
                            const uint8_t* mask, void* y, void* u, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, POST_FWD, mask != nullptr, next != nullptr, &a);
+    const NormShape shape = norm_plan(d, POST_FWD, mask != nullptr, next != nullptr, &a);
     a.x = x;
     a.z = z;
     a.g = g;
@@ -722,12 +724,12 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.mask = mask;
     a.oy = y;
     a.ou = u;
-    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd", POST_FWD, next != nullptr), st, 0.0,
+    ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd"), st, 0.0,
                  norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
-    if (d.gate && next) norm_launch<POST_FWD, true, true>(d, a, st);
-    else if (d.gate) norm_launch<POST_FWD, true, false>(d, a, st);
-    else if (next) norm_launch<POST_FWD, false, true>(d, a, st);
-    else norm_launch<POST_FWD, false, false>(d, a, st);
+    if (d.gate && next) norm_launch<POST_FWD, true, true>(d, shape, a, st);
+    else if (d.gate) norm_launch<POST_FWD, true, false>(d, shape, a, st);
+    else if (next) norm_launch<POST_FWD, false, true>(d, shape, a, st);
+    else norm_launch<POST_FWD, false, false>(d, shape, a, st);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }
@@ -746,7 +748,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
                           const float* gamma, const uint8_t* mask, const void* dres, void* dx,
                           float* dgamma, int accumulate, void* ws, hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, PRE_BWD, mask != nullptr, true, &a);
+    const NormShape shape = norm_plan(d, PRE_BWD, mask != nullptr, true, &a);
     a.du = du;
     a.y = x;
     a.sy = a.sx;
@@ -756,9 +758,9 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.dx = dx;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd", PRE_BWD, true), st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + (dres != nullptr)));
-        norm_launch<PRE_BWD, false, true>(d, a, st);
+        norm_launch<PRE_BWD, false, true>(d, shape, a, st);
         RAT3D_LAUNCH_CHECK();
     }
     return norm_gains(a, PRE_BWD, dgamma, nullptr, nullptr, accumulate, st);
@@ -770,7 +772,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
                            float* dgamma, float* dscale, float* dnext, int accumulate, void* ws,
                            hipStream_t st) {
     NormArgs a = {};
-    norm_plan(d, POST_BWD, mask != nullptr, next != nullptr, &a);
+    const NormShape shape = norm_plan(d, POST_BWD, mask != nullptr, next != nullptr, &a);
     a.dy = dy;
     a.du = du;
     a.y = y;
@@ -785,12 +787,12 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dg = dg;
     a.part = (float*)ws;
     {
-        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd", POST_BWD, next != nullptr), st, 0.0,
+        ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
-        if (d.gate && next) norm_launch<POST_BWD, true, true>(d, a, st);
-        else if (d.gate) norm_launch<POST_BWD, true, false>(d, a, st);
-        else if (next) norm_launch<POST_BWD, false, true>(d, a, st);
-        else norm_launch<POST_BWD, false, false>(d, a, st);
+        if (d.gate && next) norm_launch<POST_BWD, true, true>(d, shape, a, st);
+        else if (d.gate) norm_launch<POST_BWD, true, false>(d, shape, a, st);
+        else if (next) norm_launch<POST_BWD, false, true>(d, shape, a, st);
+        else norm_launch<POST_BWD, false, false>(d, shape, a, st);
         RAT3D_LAUNCH_CHECK();
     }
     return norm_gains(a, POST_BWD, dnext, dgamma, dscale, accumulate, st);

@@ -656,7 +656,8 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, Norm
         } else if (shape.tok == TOK) {
             if (threads <= 256) RAT3D_NORM(TOK, 4, 256);
             else if (TOK == 8 || threads <= 512) RAT3D_NORM(TOK, 4, 512);
-            else if constexpr (TOK == 4 && MODE == POST_BWD && NEXT) RAT3D_NORM1(TOK, 4, true, 1024);
+            else if constexpr (TOK == 4 && MODE == POST_BWD && NEXT)
+                RAT3D_NORM1(TOK, 4, true, 1024);  // the others have half the tokens
             else if constexpr (TOK == 4) RAT3D_NORM(TOK, 4, 1024);
         } else if (shape.tok == TOK / 2 && shape.pc == 4) {
             if (threads <= 256) RAT3D_NORM(TOK / 2, 4, 256);

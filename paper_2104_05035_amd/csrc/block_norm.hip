@@ -39,7 +39,7 @@ struct NormArgs {
     void *oy, *ou, *dx, *dz, *dg;
     const float *gamma, *scale, *next;
     const uint8_t* mask;
-    float* part;  // [gain][channel][workgroup]
+    double* part;  // [gain][channel][workgroup]
     int64_t sx, sz, sg, sy, su;  // from one volume to the next
     int64_t V;
     int c, groups, gate;
@@ -127,8 +127,8 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
 #pragma unroll
         for (int m = 8; m >= 1; m >>= 1) v += __shfl_xor(v, m);
         if (at == 0 && ch < a.c) {
-            float* to = a.part + ((int64_t)which * a.c + ch) * gridDim.x + blockIdx.x;
-            *to = more ? *to + (float)v : (float)v;
+            double* to = a.part + ((int64_t)which * a.c + ch) * gridDim.x + blockIdx.x;
+            *to = more ? *to + v : v;
         }
     };
 
@@ -478,8 +478,10 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     }
 }
 
-// The gains' gradients: the parts of the workgroups added in float64, in a fixed order.
-__global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ part, int parts, int c,
+// The gains' gradients: the parts of the workgroups added in float64, in a fixed order.  The
+// parts are float64 too: where channels are read again a workgroup adds every tile's to its
+// part, and a float32 one drifts by 190 units of 2^-24 over 862 equal tiles.
+__global__ __launch_bounds__(256) void norm_gain_k(const double* __restrict__ part, int parts, int c,
                                                    const float* gamma, const float* scale,
                                                    float* dnext, float* dgamma, float* dscale,
                                                    int accumulate) {
@@ -487,7 +489,7 @@ __global__ __launch_bounds__(256) void norm_gain_k(const float* __restrict__ par
     const int ch = blockIdx.x, which = blockIdx.y;  // 0: the norm read by du, 1: the branch's
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256)
-        s += (double)part[((int64_t)which * c + ch) * parts + i];
+        s += part[((int64_t)which * c + ch) * parts + i];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -605,7 +607,7 @@ size_t norm_ws_bytes(const rat3d_norm_desc& d) {
     const int full = d.dtype == RAT3D_BF16 ? 8 : 4, tok = d.v < full ? 1 : full / 4;
     const int64_t tiles = ceil_div(d.v, kLanes * tok) * d.n;
     const int64_t most = (d.c < 64 || d.v > 1 << 24 ? 8 : 2) * (int64_t)device_cus();
-    return (size_t)(tiles < most ? tiles : most) * 2 * d.c * sizeof(float);
+    return (size_t)(tiles < most ? tiles : most) * 2 * d.c * sizeof(double);
 }
 
 // Rows that begin inside a cache line: neighbouring tiles share lines, and one XCD's
@@ -738,7 +740,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
 static rat3d_status norm_gains(const NormArgs& a, NormMode mode, float* dnext, float* dgamma,
                                float* dscale, int accumulate, hipStream_t st) {
     const int parts = (int)norm_grid(a, mode);
-    ProfScope ps("norm_gain", st, 0.0, 8.0 * a.c * parts);
+    ProfScope ps("norm_gain", st, 0.0, 16.0 * a.c * parts);
     norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
                                               dscale, accumulate);
     RAT3D_LAUNCH_CHECK();
@@ -757,7 +759,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.gamma = gamma;
     a.mask = mask;
     a.dx = dx;
-    a.part = (float*)ws;
+    a.part = (double*)ws;
     {
         ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + (dres != nullptr)));
@@ -786,7 +788,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dx = dx;
     a.dz = dz;
     a.dg = dg;
-    a.part = (float*)ws;
+    a.part = (double*)ws;
     {
         ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));

@@ -372,7 +372,8 @@ typedef enum {
 } rat3d_gate;
 
 /* Norms over a voxel's channels, N(x) = x / sqrt(mean_c x^2 + eps), x^2 summed in
- * float32 (beyond |x| of about 10^18 the sum is infinite and N(x) is 0):
+ * float32 (beyond |x| of about 10^18 the sum is infinite and N(x) is 0, NaN where x itself
+ * is infinite; scale phi(g) gamma is to stay below 10^19):
  *   before a block   u = gamma N(x)
  *   behind a block   y = x + scale phi(g) gamma N(z)        one rounding, and
  *                    u = gamma_next N(y), y before its rounding (gamma_next != NULL)

@@ -264,6 +264,8 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
             for (int j = 0; j < TOK; ++j)
                 r[j] = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[j], inv_c, a.eps));
         };
+        // mean(e x) r^2 of the sum e x; at a root of 0 the sum may be no number any more
+        auto mean = [&](float sum, float r) { return r == 0.f ? 0.f : sum * inv_c * (r * r); };
         auto clear = [&](auto& v) {
             for (auto& row : v)
                 for (float& x : row) x = 0.f;
@@ -290,7 +292,9 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
             });
         }
         if constexpr (MODE == POST_FWD) {
-            // held in the place of z and g: the branch without its root, then y
+            // held in the place of z and g: the branch without its root, then y.  A z whose
+            // square is infinite has a root of 0, and its product with gains and gate may be
+            // infinite: it counts as 0 (an infinite z as NaN).
             float b[NP][TOK], r[TOK];
             auto branch = [&](int p) {
                 const float k = wgt[p];
@@ -298,7 +302,8 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 for (int j = 0; j < TOK; ++j) {
                     float phi, slope;
                     gate(p, j, phi, slope);
-                    b[p][j] = k * phi * Z[p][j];
+                    const float z = Z[p][j];
+                    b[p][j] = z * z < __builtin_inff() ? k * phi * z : 0.f * z;
                 }
             };
             auto sum = [&](int p) {
@@ -377,7 +382,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
             if constexpr (kNext) {
                 root(ry, s[K - 2]);
 #pragma unroll
-                for (int j = 0; j < TOK; ++j) my[j] = s[K - 1][j] * inv_c * (ry[j] * ry[j]);
+                for (int j = 0; j < TOK; ++j) my[j] = mean(s[K - 1][j], ry[j]);
             }
             if constexpr (kPost) root(rz, s[0]);
             // dY, and its part in the next norm's gain
@@ -447,7 +452,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 channel_sums(e, lds[1], waves);
                 forget(Z);
 #pragma unroll
-                for (int j = 0; j < TOK; ++j) mz[j] = e[0][j] * inv_c * (rz[j] * rz[j]);
+                for (int j = 0; j < TOK; ++j) mz[j] = mean(e[0][j], rz[j]);
                 each([&](int p) {
                     if (!PC) middle(p, true);
 #pragma unroll

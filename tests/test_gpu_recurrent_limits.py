@@ -69,3 +69,82 @@ def test_gains_of_rows_beyond_2_27_voxels():
     assert {"pre_norm_bwd_any", "post_norm_bwd_any"} <= set(tags)
     for g in got:
         np.testing.assert_allclose(g, v * 0.5 ** 0.5, rtol=EQUAL)
+
+
+# ------------------------------------------------------------------ values far out
+# channels and voxels of kernels that hold whole and other tiles, and that read again
+SHAPES = [(16, 3), (24, 37), (64, 128), (200, 65), (300, 65), (384, 64), (600, 33), (640, 64)]
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", SHAPES)
+@pytest.mark.parametrize("kind,nxt", [("silu", True), (None, True), ("sigmoid", False)])
+def test_squares_beyond_the_largest_float(c, v, dt, kind, nxt):
+    """Voxels whose sum of squares is infinite have N = 0, though their values times gains and
+    gate are no float any more: as masked ones they change nothing but themselves."""
+    s = TN.Norms((2, c, v, kind, nxt, None), dt)
+    R, r, torch = s.R, s.ref, U.torch_mod()
+    rng = np.random.default_rng(c + v)
+    big = rng.random((2, v)) < 0.4
+    big[0, 0] = True
+    for name in ("x", "z"):  # in every channel, or in one of them
+        some = rng.random((2, c, v)) < 0.5
+        some[:, rng.integers(c)] = True
+        far = rng.choice([-3e38, 3e38, 2.5e38], (2, c, v)) * (some | (rng.random((2, 1, v)) < 0.5))
+        t, f = U.dev_input(np.where(big[:, None, :], far, r[name]), dt)
+        setattr(s, name, t)
+        r[name] = f
+    s.g[torch.from_numpy(big).to("cuda:0")[:, None, :].expand(s.g.shape)] = 4.0
+    s.gamma *= 3
+    r["gamma"] = U.f64(s.gamma)
+    live = (~big).astype(np.uint8)
+    g, gn = s.g if kind else None, s.gnext if nxt else None
+    y, u, dx, dz, dg, pre, pdx = (s.out() for _ in range(7))
+    v0, v1, v2, v3 = (s.out((c,), "f32") for _ in range(4))
+    R.rat3d_post_norm_fwd(s.desc, s.x, s.z, g, s.gamma, s.scale, gn, None, y, u if nxt else None)
+    R.rat3d_post_norm_bwd(s.desc, s.dy, s.du if nxt else None, s.x if nxt else None, s.z, g, s.gamma,
+                          s.scale, gn, None, dx if nxt else None, dz, dg if kind else None, v0, v1,
+                          v2 if nxt else None, 0, _ws(s.need), s.need)
+    R.rat3d_pre_norm_fwd(s.desc, s.x, s.gamma, None, pre)
+    R.rat3d_pre_norm_bwd(s.desc, s.du, s.x, s.gamma, None, s.dres, pdx, v3, 0, _ws(s.need), s.need)
+    U.sync()
+    gnr = r["gnext"] if nxt else None
+    want = RU.post_norm_refs(r["x"], r["z"], r["g"], kind, r["gamma"], r["scale"], gnr, live, TN.EPS,
+                             dt)
+    want.update(RU.post_norm_bwd_refs(r["dy"], r["du"], r["x"], r["z"], r["g"], kind, r["gamma"],
+                                      r["scale"], gnr, live, TN.EPS, dt))
+    if not nxt:
+        del want["dx"]
+    p = RU.pre_norm_refs(r["x"], r["gamma"], live, TN.EPS, dt, r["du"], r["dres"])
+    want.update(pre=p["u"], pdx=p["dx"], v3=p["dgamma"])
+    got = dict(y=y, u=u, dx=dx, dz=dz, dg=dg, dgamma=v0, dscale=v1, dgamma_next=v2, pre=pre, pdx=pdx,
+               v3=v3)
+    for k in want:
+        RU.within(U.f64(got[k]), want[k], k)
+    s.intact()
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", SHAPES)
+def test_infinite_values_are_not_hidden(c, v, dt):
+    """An infinity is NaN in its own channel; the voxel's other channels have N = 0."""
+    s = TN.Norms((1, c, v, "silu", True, None), dt)
+    R, torch = s.R, U.torch_mod()
+    ch, at = c // 2, v // 2
+    s.z[0, ch, at] = INF
+    s.g[0, ch, at] = 1.0
+    y, u, dz, dx, dg, pre = (s.out() for _ in range(6))
+    vec = [s.out((c,), "f32") for _ in range(3)]
+    R.rat3d_pre_norm_fwd(s.desc, s.z, s.gamma, None, pre)
+    R.rat3d_post_norm_fwd(s.desc, s.x, s.z, s.g, s.gamma, s.scale, None, None, y, None)
+    R.rat3d_post_norm_bwd(s.desc, s.dy, s.du, s.x, s.z, s.g, s.gamma, s.scale, s.gnext, None, dx, dz,
+                          dg, *vec, 0, _ws(s.need), s.need)
+    U.sync()
+    rest = torch.arange(c, device="cuda:0") != ch
+    for t in (y, dz, pre):
+        assert bool(torch.isnan(t[0, ch, at]))
+        assert int(torch.isnan(t).sum()) == 1
+    assert torch.equal(y[0, rest, at], s.x[0, rest, at])
+    assert bool((dz[0, rest, at] == 0).all()) and bool((pre[0, rest, at] == 0).all())
+    assert bool(torch.isfinite(dx).all())
+    s.intact()

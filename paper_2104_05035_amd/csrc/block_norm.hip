@@ -39,7 +39,7 @@ struct NormArgs {
     void *oy, *ou, *dx, *dz, *dg;
     const float *gamma, *scale, *next;
     const uint8_t* mask;
-    double* part;  // [gain][channel][workgroup]
+    void* part;  // [gain][channel][workgroup], NormPart
     int64_t sx, sz, sg, sy, su;  // from one volume to the next
     int64_t V;
     int c, groups, gate;
@@ -102,6 +102,10 @@ __device__ __forceinline__ void channel_sums(float (&s)[K][TOK], float* lds, int
     }
 }
 
+// Parts of the gains' gradients.  Where channels are read again (PC = 0) a workgroup adds
+// every tile's to its part: a float32 one drifts by 190 units of 2^-24 over 862 equal tiles.
+template <int PC> using NormPart = typename std::conditional<PC == 0, double, float>::type;
+
 // PC: channels a thread, held in registers, c <= PC * groups; 0: any number, read again
 // for every sum.  ALL: no mask, whole tiles, c = PC * groups (in kernels of their own, for
 // what the other case needs is formed before the loop and takes registers).
@@ -127,8 +131,9 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
 #pragma unroll
         for (int m = 8; m >= 1; m >>= 1) v += __shfl_xor(v, m);
         if (at == 0 && ch < a.c) {
-            double* to = a.part + ((int64_t)which * a.c + ch) * gridDim.x + blockIdx.x;
-            *to = more ? *to + v : v;
+            typedef NormPart<PC> Part;
+            Part* to = (Part*)a.part + ((int64_t)which * a.c + ch) * gridDim.x + blockIdx.x;
+            *to = (Part)(more ? *to + v : v);
         }
     };
 
@@ -483,10 +488,9 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     }
 }
 
-// The gains' gradients: the parts of the workgroups added in float64, in a fixed order.  The
-// parts are float64 too: where channels are read again a workgroup adds every tile's to its
-// part, and a float32 one drifts by 190 units of 2^-24 over 862 equal tiles.
-__global__ __launch_bounds__(256) void norm_gain_k(const double* __restrict__ part, int parts, int c,
+// The gains' gradients: the parts of the workgroups added in float64, in a fixed order.
+template <typename Part>
+__global__ __launch_bounds__(256) void norm_gain_k(const Part* __restrict__ part, int parts, int c,
                                                    const float* gamma, const float* scale,
                                                    float* dnext, float* dgamma, float* dscale,
                                                    int accumulate) {
@@ -494,7 +498,7 @@ __global__ __launch_bounds__(256) void norm_gain_k(const double* __restrict__ pa
     const int ch = blockIdx.x, which = blockIdx.y;  // 0: the norm read by du, 1: the branch's
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256)
-        s += part[((int64_t)which * c + ch) * parts + i];
+        s += (double)part[((int64_t)which * c + ch) * parts + i];
 #pragma unroll
     for (int m = 32; m >= 1; m >>= 1) s += __shfl_xor(s, m);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = s;
@@ -742,12 +746,17 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     return RAT3D_OK;
 }
 
-static rat3d_status norm_gains(const NormArgs& a, NormMode mode, float* dnext, float* dgamma,
-                               float* dscale, int accumulate, hipStream_t st) {
+static rat3d_status norm_gains(const NormArgs& a, const NormShape& shape, NormMode mode,
+                               float* dnext, float* dgamma, float* dscale, int accumulate,
+                               hipStream_t st) {
     const int parts = (int)norm_grid(a, mode);
-    ProfScope ps("norm_gain", st, 0.0, 16.0 * a.c * parts);
-    norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(a.part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
-                                              dscale, accumulate);
+    ProfScope ps("norm_gain", st, 0.0, (shape.pc ? 8.0 : 16.0) * a.c * parts);
+    auto sum = [&](auto* part) {
+        norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
+                                                  dscale, accumulate);
+    };
+    if (shape.pc) sum((const NormPart<1>*)a.part);
+    else sum((const NormPart<0>*)a.part);
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }
@@ -764,14 +773,14 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     a.gamma = gamma;
     a.mask = mask;
     a.dx = dx;
-    a.part = (double*)ws;
+    a.part = ws;
     {
         ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + (dres != nullptr)));
         norm_launch<PRE_BWD, false, true>(d, shape, a, st);
         RAT3D_LAUNCH_CHECK();
     }
-    return norm_gains(a, PRE_BWD, dgamma, nullptr, nullptr, accumulate, st);
+    return norm_gains(a, shape, PRE_BWD, dgamma, nullptr, nullptr, accumulate, st);
 }
 
 rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void* du, const void* y,
@@ -793,7 +802,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     a.dx = dx;
     a.dz = dz;
     a.dg = dg;
-    a.part = (double*)ws;
+    a.part = ws;
     {
         ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
@@ -803,7 +812,7 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
         else norm_launch<POST_BWD, false, false>(d, shape, a, st);
         RAT3D_LAUNCH_CHECK();
     }
-    return norm_gains(a, POST_BWD, dnext, dgamma, dscale, accumulate, st);
+    return norm_gains(a, shape, POST_BWD, dnext, dgamma, dscale, accumulate, st);
 }
 
 }  // namespace rat3d

@@ -488,14 +488,15 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
     }
 }
 
-// The gains' gradients: the parts of the workgroups added in float64, in a fixed order.
+// The gains' gradients: the parts of the workgroups added in float64, in a fixed order, of
+// the gains from `gain` on that the call has written.
 template <typename Part>
 __global__ __launch_bounds__(256) void norm_gain_k(const Part* __restrict__ part, int parts, int c,
                                                    const float* gamma, const float* scale,
                                                    float* dnext, float* dgamma, float* dscale,
-                                                   int accumulate) {
+                                                   int gain, int accumulate) {
     __shared__ double red[4];
-    const int ch = blockIdx.x, which = blockIdx.y;  // 0: the norm read by du, 1: the branch's
+    const int ch = blockIdx.x, which = gain + blockIdx.y;  // 0: the norm du reads, 1: the branch's
     double s = 0.0;
     for (int i = threadIdx.x; i < parts; i += 256)
         s += (double)part[((int64_t)which * c + ch) * parts + i];
@@ -750,10 +751,11 @@ static rat3d_status norm_gains(const NormArgs& a, const NormShape& shape, NormMo
                                float* dnext, float* dgamma, float* dscale, int accumulate,
                                hipStream_t st) {
     const int parts = (int)norm_grid(a, mode);
-    ProfScope ps("norm_gain", st, 0.0, (shape.pc ? 8.0 : 16.0) * a.c * parts);
+    const int gain = dnext ? 0 : 1, gains = (dgamma ? 2 : 1) - gain;
+    ProfScope ps("norm_gain", st, 0.0, (shape.pc ? 4.0 : 8.0) * a.c * parts * gains);
     auto sum = [&](auto* part) {
-        norm_gain_k<<<dim3(a.c, 2), 256, 0, st>>>(part, parts, a.c, a.gamma, a.scale, dnext, dgamma,
-                                                  dscale, accumulate);
+        norm_gain_k<<<dim3(a.c, gains), 256, 0, st>>>(part, parts, a.c, a.gamma, a.scale, dnext,
+                                                      dgamma, dscale, gain, accumulate);
     };
     if (shape.pc) sum((const NormPart<1>*)a.part);
     else sum((const NormPart<0>*)a.part);

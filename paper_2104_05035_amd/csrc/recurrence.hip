@@ -268,7 +268,9 @@ template <typename T, bool DOWN> struct GradSteps {
             F = __builtin_fmaf(a[i], F, g[i] * x[i]);
         }
     }
-    // dr, di, dx from E behind the lane's voxels and h before them; returns the sum of K
+    // dr, di, dx from E behind the lane's voxels and h before them; returns the sum of K.
+    // Where no voxel is live the caller drops it: the factors are 0, but a state or gradient
+    // that is handed on need not be finite.
     __device__ __forceinline__ float grads(float E, float h, float (&dr)[TOK], float (&di)[TOK],
                                            float (&dx)[TOK]) const {
 #pragma unroll
@@ -450,7 +452,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_k(RecArgs q) {
         }
         if (k < sg.count) {
             float o[3][TOK];
-            sum += (double)s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+            const float K = s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+            sum += (double)(all || cur.at.live ? K : 0.f);
             auto put = [&](auto all) {
                 constexpr bool ALL = decltype(all)::value;
                 const int left = TOK - cur.at.over;
@@ -689,7 +692,8 @@ __global__ __launch_bounds__(64 * kWaves, 4) void recurrence_bwd_one_k(RecArgs q
     double sum = 0.0;
     if (there) {
         float o[3][TOK];
-        sum = (double)s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+        const float K = s.grads(walk.begin(begin), h, o[0], o[1], o[2]);
+        sum = (double)(all || d.at.live ? K : 0.f);
         T* const out[3] = {(T*)q.dr + vol * q.sr + (int64_t)ch * q.len,
                            (T*)q.di + vol * q.si + (int64_t)ch * q.len,
                            (T*)q.dx + vol * q.sx + (int64_t)ch * q.len};
@@ -819,6 +823,7 @@ __global__ __launch_bounds__(256) void recurrence_short_bwd_k(RecArgs q) {
     const float h = short_walk<!DOWN>(A, F, q.lanes, fwd);
     float o[3][TOK];
     float part = s.grads(E, h, o[0], o[1], o[2]);
+    if (!d.at.live) part = 0.f;
     for (auto& v : o) d.at.clear(v);
     for (int m = q.lanes / 2; m >= 1; m >>= 1) part += __shfl_xor(part, m);
     if (r_ >= q.rows) return;

@@ -1,5 +1,5 @@
 """What the recurrent block's calls promise at their limits: long sums of gains, values near
-the largest float, gains, states and gradients that are not finite beside masked voxels, the
+the largest float, states and gradients that are not finite beside masked voxels, the
 longest rows."""
 import numpy as np
 import pytest
@@ -148,3 +148,28 @@ def test_infinite_values_are_not_hidden(c, v, dt):
     assert bool((dz[0, rest, at] == 0).all()) and bool((pre[0, rest, at] == 0).all())
     assert bool(torch.isfinite(dx).all())
     s.intact()
+
+
+# ------------------------------------------------------------------ beside masked voxels
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", [(3, 5), (6, 37), (4, 700), (300, 1100), (2, 9003), (1, 70000)])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_masked_rows_give_lambda_nothing(c, v, reverse, dt):
+    """A volume that is masked as a whole hands its states on whatever they are, and has no
+    part in lambda's gradient."""
+    torch = U.torch_mod()
+    s = TR.Walk((3, c, v, reverse, "holes", 1.0, 8.0), dt)
+    assert not s.mask[1].any()
+    want, got = s.results(), s.results()
+    s.fwd(want)
+    s.bwd(want)
+    s.h0[1], s.dh[1] = INF, NAN
+    s.fwd(got)
+    s.bwd(got)
+    U.sync()
+    assert bool((got["h_last"][1] == INF).all()) and bool(torch.isnan(got["dh0"][1]).all())
+    got["h_last"][1], got["dh0"][1] = want["h_last"][1], want["dh0"][1]
+    for k in want:
+        assert torch.equal(got[k], want[k]), k
+    for b in s.guards:
+        U.guard_intact(b)

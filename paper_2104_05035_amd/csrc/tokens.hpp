@@ -8,8 +8,10 @@
 
 namespace rat3d {
 
-// A thread's tokens of one channel, as they lie.
-template <typename T, int TOK> struct __attribute__((packed, aligned(sizeof(T)))) Words {
+// A thread's tokens of one channel, as they lie.  A result may lie over an input that is
+// read as other words or as elements: the compiler takes no two accesses for apart.
+template <typename T, int TOK>
+struct __attribute__((packed, aligned(sizeof(T)), may_alias)) Words {
     typename std::conditional<TOK * sizeof(T) < 4, uint16_t, uint32_t>::type
         w[TOK * sizeof(T) < 4 ? 1 : TOK * sizeof(T) / 4];
 };
@@ -70,7 +72,7 @@ __device__ __forceinline__ void put_tokens(T* base, uint32_t off, int left,
         if constexpr (TOK * sizeof(T) == 16) {
             if (stream) {
                 typedef uint32_t __attribute__((ext_vector_type(4))) u4;
-                typedef u4 __attribute__((aligned(2))) u4_any;
+                typedef u4 __attribute__((aligned(2), may_alias)) u4_any;
                 __builtin_nontemporal_store(u4{u.w[0], u.w[1], u.w[2], u.w[3]}, (u4_any*)p);
                 return;
             }

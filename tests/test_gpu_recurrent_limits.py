@@ -1,6 +1,8 @@
 """What the recurrent block's calls promise at their limits: long sums of gains, values near
 the largest float, states and gradients that are not finite beside masked voxels, the
 longest rows."""
+import itertools
+
 import numpy as np
 import pytest
 
@@ -173,3 +175,40 @@ def test_masked_rows_give_lambda_nothing(c, v, reverse, dt):
         assert torch.equal(got[k], want[k]), k
     for b in s.guards:
         U.guard_intact(b)
+
+
+# ------------------------------------------------------------------ results over inputs
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v,mask", [(40, 203, "holes"), (64, 128, None), (300, 67, None),
+                                      (600, 203, "holes"), (640, 64, None), (270, 3, "holes")])
+def test_every_result_over_every_input(c, v, mask, dt):
+    """Each choice of inputs that results may lie over: the bits of tensors of their own."""
+    s = TN.Norms((2, c, v, "silu", True, mask), dt)
+    R, torch = s.R, U.torch_mod()
+    same = lambda a, b: torch.equal(torch.nan_to_num(a.float()), torch.nan_to_num(b.float()))  # noqa: E731
+    vec = [torch.empty(c, device="cuda:0") for _ in range(4)]
+    ws = _ws(s.need)
+
+    def forward(t, y, u):
+        R.rat3d_post_norm_fwd(s.desc, t["x"], t["z"], t["g"], s.gamma, s.scale, s.gnext, s.dmask, y, u)
+        return y, u
+
+    def behind(t, dx, dz, dg):
+        R.rat3d_post_norm_bwd(s.desc, t["dy"], t["du"], t["x"], t["z"], t["g"], s.gamma, s.scale,
+                              s.gnext, s.dmask, dx, dz, dg, *vec[:3], 0, ws, s.need)
+        return dx, dz, dg
+
+    def before(t, dx):
+        R.rat3d_pre_norm_bwd(s.desc, t["du"], t["x"], s.gamma, s.dmask, t["dres"], dx, vec[3], 0, ws,
+                             s.need)
+        return (dx,)
+
+    for call, names, results in ((forward, ("x", "z", "g"), 2),
+                                 (behind, ("dy", "du", "x", "z", "g"), 3),
+                                 (before, ("du", "x", "dres"), 1)):
+        src = {k: getattr(s, k) for k in names}
+        own = call(src, *(torch.empty_like(s.x) for _ in range(results)))
+        for over in itertools.permutations(names, results):
+            t = {k: a.clone() for k, a in src.items()}
+            for a, b in zip(own, call(t, *(t[k] for k in over))):
+                assert same(a, b), (call.__name__, over)

@@ -23,7 +23,7 @@ template <typename T, int TOK> struct Toks {
         Words<T, TOK> m;
         if constexpr (sizeof(T) == 4 || TOK == 1) {
 #pragma unroll
-            for (int j = 0; j < TOK; ++j) m.w[j] = on >> j & 1u ? ~0u : 0u;
+            for (int j = 0; j < TOK; ++j) m.w[j] = 0u - (on >> j & 1u);
         } else {
 #pragma unroll
             for (int j = 0; j < TOK; j += 2)

@@ -213,13 +213,43 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
             if (!kBwd) get(X, a.x, a.sx, !kPost);
             else if (MODE == POST_BWD) get(X, a.dy, a.sy, false);
             else if (a.dy) get(X, a.dy, a.sx, false);
+            else
+#pragma unroll
+                for (int p = 0; p < NP; ++p) X[p].u = {};
         };
         int round = 0;
-        auto put = [&](void* q, int64_t stride, int p, const float (&o)[TOK]) {
+        // Results, at masked voxels 0 or (put_past) X as it lies: chosen by bits, for a gain
+        // that is not finite leaves no 0 of what is formed there.
+        auto put_bits = [&](void* q, int64_t stride, int p, const float (&o)[TOK], auto edit) {
             if (kAll || ch[p] < a.c)
-                put_tokens<T, TOK, kAll>(
+                put_edited<T, TOK, kAll>(
                     (T*)q + vol * stride + (int64_t)(round + p) * a.groups * a.V, off, left, o,
-                    a.stream);
+                    a.stream, edit);
+        };
+        // keep, in kernels without a gate formed again: two registers more are one workgroup a
+        // CU fewer for some of them (16 x 128 channels of 2016 voxels 22.1 -> 25.4 us)
+        auto stay = [&] {
+            constexpr bool AGAIN = PC && TOK > 1 && !GATED;
+            uint32_t on = live;
+            if (AGAIN) asm volatile("" : "+v"(on));
+            return AGAIN ? V::bits(on) : keep;
+        };
+        auto put = [&](void* q, int64_t stride, int p, const float (&o)[TOK]) {
+            put_bits(q, stride, p, o, [&](Words<T, TOK>& u) {
+                if (kAll) return;
+                const Words<T, TOK> m = stay();
+#pragma unroll
+                for (int i = 0; i < V::N; ++i) u.w[i] &= m.w[i];
+            });
+        };
+        auto put_past = [&](void* q, int64_t stride, int p, const float (&o)[TOK]) {
+            put_bits(q, stride, p, o, [&](Words<T, TOK>& u) {
+                if (kAll) return;
+                const Words<T, TOK> m = stay();
+#pragma unroll
+                for (int i = 0; i < V::N; ++i)
+                    u.w[i] = (u.w[i] & m.w[i]) | (X[p].u.w[i] & ~m.w[i]);
+            });
         };
         // What is formed from a held value is formed again behind a barrier, not held too.
         auto forget = [&](V(&v)[NP]) {
@@ -270,7 +300,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 r[j] = __builtin_amdgcn_rsqf(__builtin_fmaf(sum[j], inv_c, a.eps));
         };
         // mean(e x) r^2 of the sum e x; at a root of 0 the sum may be no number any more
-        auto mean = [&](float sum, float r) { return r == 0.f ? 0.f : sum * inv_c * (r * r); };
+        auto mean = [&](float sum, float r) { return (r == 0.f ? 0.f : sum) * inv_c * (r * r); };
         auto clear = [&](auto& v) {
             for (auto& row : v)
                 for (float& x : row) x = 0.f;
@@ -333,7 +363,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 each([&](int p) {
                     if (!PC) branch(p);
                     sum(p);
-                    if (PC) put(a.oy, a.sy, p, b[p]);
+                    if (PC) put_past(a.oy, a.sy, p, b[p]);
                     const bool is = kAll || ch[p] < a.c;
 #pragma unroll
                     for (int j = 0; j < TOK; ++j) e[0][j] += is ? b[p][j] * b[p][j] : 0.f;
@@ -347,13 +377,12 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 if (!PC) branch(p);
                 if (!PC || !NEXT) {
                     sum(p);
-                    put(a.oy, a.sy, p, b[p]);
+                    put_past(a.oy, a.sy, p, b[p]);
                 }
                 if constexpr (NEXT) {
                     const float k = nxt[p];
 #pragma unroll
-                    for (int j = 0; j < TOK; ++j)
-                        b[p][j] = is_live(p, j) ? k * (b[p][j] * ry[j]) : 0.f;
+                    for (int j = 0; j < TOK; ++j) b[p][j] = k * (b[p][j] * ry[j]);
                     put(a.ou, a.su, p, b[p]);
                 }
             });
@@ -396,7 +425,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 float n = 0.f;
 #pragma unroll
                 for (int j = 0; j < TOK; ++j) {
-                    d[j] = MODE == POST_BWD || a.dy ? X[p][j] : 0.f;
+                    d[j] = X[p][j];
                     if constexpr (kNext) {
                         const float y = Y[p][j], du = DU[p][j];
                         d[j] += ry[j] * (k * du - y * my[j]);
@@ -419,18 +448,19 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                 each([&](int p) {
                     float d[TOK];
                     add_n(p, residual(p, d));
-                    put(a.dx, a.sx, p, d);
+                    put_past(a.dx, a.sx, p, d);
                 });
             } else {
                 // e = dY s gamma phi, held in the place of what it is formed from; where
                 // nothing is held, results wait for the last pass, which reads all again
                 float E[NP][TOK], mz[TOK];
+                constexpr bool kMaskDz = GATED || NEXT;  // or e is 0 at masked voxels
                 auto middle = [&](int p, bool out) {
                     const float w = wgt[p];
                     const float n = residual(p, E[p]);
                     if (out) {
                         add_n(p, n);
-                        if (kNext) put(a.dx, a.sx, p, E[p]);
+                        if (kNext) put_past(a.dx, a.sx, p, E[p]);
                     }
                     float dg[TOK], q = 0.f;
 #pragma unroll
@@ -440,7 +470,7 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                         const float d = is_live(p, j) ? E[p][j] : 0.f, zr = Z[p][j] * rz[j];
                         q += d * phi * zr;
                         dg[j] = d * w * zr * slope;
-                        E[p][j] = d * w * phi;
+                        E[p][j] = kMaskDz || is_live(p, j) ? d * w * phi : 0.f;
                     }
                     if (out) {
                         add_t(p, q);
@@ -462,7 +492,8 @@ __global__ __launch_bounds__(THREADS) void block_norm_k(NormArgs a) {
                     if (!PC) middle(p, true);
 #pragma unroll
                     for (int j = 0; j < TOK; ++j) E[p][j] = rz[j] * (E[p][j] - Z[p][j] * mz[j]);
-                    put(a.dz, a.sz, p, E[p]);
+                    if (kMaskDz) put(a.dz, a.sz, p, E[p]);
+                    else put_bits(a.dz, a.sz, p, E[p], [](Words<T, TOK>&) {});
                 });
             }
         }

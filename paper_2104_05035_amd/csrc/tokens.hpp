@@ -57,18 +57,23 @@ template <typename T, int TOK> struct Toks {
         }
     }
 };
+template <typename T, int TOK>
+__device__ __forceinline__ void pack_tokens(Words<T, TOK>& u, const float (&o)[TOK]) {
+#pragma unroll
+    for (int j = 0; j < TOK; j += 4 / (int)sizeof(T)) {
+        if constexpr (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
+        else if constexpr (TOK == 1) u.w[0] = Elt<T>::to_bits(o[0]);
+        else u.w[j / 2] = pack_bf16x2(o[j], o[j + 1]);
+    }
+}
+// The first `left` tokens (ALL: each); `stream`: past the memory-side cache.
 template <typename T, int TOK, bool ALL>
 __device__ __forceinline__ void put_tokens(T* base, uint32_t off, int left,
                                            const float (&o)[TOK], bool stream) {
     T* p = (T*)((char*)base + off);
     if (ALL || left == TOK) {
         Words<T, TOK> u;
-#pragma unroll
-        for (int j = 0; j < TOK; j += 4 / (int)sizeof(T)) {
-            if constexpr (sizeof(T) == 4) u.w[j] = __float_as_uint(o[j]);
-            else if constexpr (TOK == 1) u.w[0] = Elt<T>::to_bits(o[0]);
-            else u.w[j / 2] = pack_bf16x2(o[j], o[j + 1]);
-        }
+        pack_tokens<T, TOK>(u, o);
         if constexpr (TOK * sizeof(T) == 16) {
             if (stream) {
                 typedef uint32_t __attribute__((ext_vector_type(4))) u4;
@@ -82,6 +87,34 @@ __device__ __forceinline__ void put_tokens(T* base, uint32_t off, int left,
 #pragma unroll
         for (int j = 0; j < TOK; ++j)
             if (j < left) Elt<T>::st(p + j, o[j]);
+    }
+}
+// The same, the tokens changed by `edit` as words.
+template <typename T, int TOK, bool ALL, typename F>
+__device__ __forceinline__ void put_edited(T* base, uint32_t off, int left,
+                                           const float (&o)[TOK], bool stream, F edit) {
+    T* p = (T*)((char*)base + off);
+    Words<T, TOK> u;
+    pack_tokens<T, TOK>(u, o);
+    edit(u);
+    if (ALL || left == TOK) {
+        if constexpr (TOK * sizeof(T) == 16) {
+            if (stream) {
+                typedef uint32_t __attribute__((ext_vector_type(4))) u4;
+                typedef u4 __attribute__((aligned(2), may_alias)) u4_any;
+                __builtin_nontemporal_store(u4{u.w[0], u.w[1], u.w[2], u.w[3]}, (u4_any*)p);
+                return;
+            }
+        }
+        *reinterpret_cast<Words<T, TOK>*>(p) = u;
+    } else if constexpr (TOK > 1) {
+#pragma unroll
+        for (int j = 0; j < TOK; ++j)
+            if (j < left) {
+                Words<T, 1> e;
+                e.w[0] = sizeof(T) == 4 ? u.w[j] : u.w[j / 2] >> (j & 1 ? 16 : 0);
+                *reinterpret_cast<Words<T, 1>*>(p + j) = e;
+            }
     }
 }
 

@@ -1,5 +1,5 @@
 """What the recurrent block's calls promise at their limits: long sums of gains, values near
-the largest float, states and gradients that are not finite beside masked voxels, the
+the largest float, gains, states and gradients that are not finite beside masked voxels, the
 longest rows."""
 import itertools
 
@@ -153,6 +153,47 @@ def test_infinite_values_are_not_hidden(c, v, dt):
 
 
 # ------------------------------------------------------------------ beside masked voxels
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("c,v", SHAPES)
+@pytest.mark.parametrize("kind,nxt", [("silu", True), (None, True), ("sigmoid", False)])
+def test_masked_voxels_whatever_the_gains(c, v, dt, kind, nxt):
+    """u = 0, y = x, dx = dres or dy, dz = dg = 0 at masked voxels, also where a gain is
+    infinite or no number."""
+    s = TN.Norms((3, c, v, kind, nxt, "holes"), dt)
+    R, torch = s.R, U.torch_mod()
+    off = torch.from_numpy(s.mask == 0).to("cuda:0")[:, None, :].expand(s.x.shape)
+    g = s.g if kind else None
+    for bad in (INF, NAN):
+        for name in ("gamma", "scale", "gnext"):
+            kept = getattr(s, name).clone()
+            getattr(s, name)[:: max(1, c // 3)] = bad
+            gn = s.gnext if nxt else None
+            y, u, dx, dz, dg, pre, pdx, pdx0 = (s.out() for _ in range(8))
+            vec = [s.out((c,), "f32") for _ in range(4)]
+            R.rat3d_post_norm_fwd(s.desc, s.x, s.z, g, s.gamma, s.scale, gn, s.dmask, y,
+                                  u if nxt else None)
+            R.rat3d_post_norm_bwd(s.desc, s.dy, s.du if nxt else None, s.x if nxt else None, s.z, g,
+                                  s.gamma, s.scale, gn, s.dmask, dx if nxt else None, dz,
+                                  dg if kind else None, vec[0], vec[1], vec[2] if nxt else None, 0,
+                                  _ws(s.need), s.need)
+            R.rat3d_pre_norm_fwd(s.desc, s.x, s.gamma, s.dmask, pre)
+            for res, to in ((s.dres, pdx), (None, pdx0)):
+                R.rat3d_pre_norm_bwd(s.desc, s.du, s.x, s.gamma, s.dmask, res, to, vec[3], 0,
+                                     _ws(s.need), s.need)
+            U.sync()
+            zero = torch.zeros_like(s.x)
+            want = dict(y=(y, s.x), dz=(dz, zero), pre=(pre, zero), pdx=(pdx, s.dres),
+                        pdx0=(pdx0, zero))
+            if nxt:
+                want.update(u=(u, zero), dx=(dx, s.dy))
+            if kind:
+                want["dg"] = (dg, zero)
+            for k, (got, w) in want.items():
+                assert bool((got[off] == w[off]).all()), (name, bad, k)
+            getattr(s, name).copy_(kept)
+    s.intact()
+
+
 @pytest.mark.parametrize("dt", ["bf16", "f32"])
 @pytest.mark.parametrize("c,v", [(3, 5), (6, 37), (4, 700), (300, 1100), (2, 9003), (1, 70000)])
 @pytest.mark.parametrize("reverse", [False, True])

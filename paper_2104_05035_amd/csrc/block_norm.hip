@@ -667,16 +667,25 @@ static void norm_lines(const rat3d_norm_desc& d, NormArgs* a) {
     if (a->near) a->stream = 0;
 }
 
+// False where no kernel is built for the shape: each is launched only where what it assumes
+// holds.  dry: nothing is launched.
 template <typename T, NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, NormArgs a,
-                          hipStream_t st) {
+static bool norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, NormArgs a,
+                          hipStream_t st, bool dry) {
     constexpr bool kBwd = MODE == PRE_BWD || MODE == POST_BWD;
     constexpr int TOK = 16 / (int)sizeof(T);
     const int threads = a.groups * kLanes;
     const bool all = !a.mask && d.v % (kLanes * shape.tok) == 0 &&
                      d.c % (a.groups * (shape.pc ? shape.pc : 1)) == 0;
-#define RAT3D_NORM1(TOK, PC, ALL, THREADS) \
-    block_norm_k<T, TOK, PC, MODE, GATED, NEXT, ALL, THREADS><<<grid, threads, 0, st>>>(a)
+#define RAT3D_NORM1(TOK, PC, ALL, THREADS)                                                     \
+    do {                                                                                       \
+        if ((ALL && !all) || threads > THREADS || (TOK) != shape.tok || (PC) != shape.pc ||    \
+            ((PC) && (PC) * a.groups < d.c))                                                   \
+            return false;                                                                      \
+        if (!dry)                                                                              \
+            block_norm_k<T, TOK, PC, MODE, GATED, NEXT, ALL, THREADS>                          \
+                <<<grid, threads, 0, st>>>(a);                                                 \
+    } while (0)
 #define RAT3D_NORM(TOK, PC, THREADS)                  \
     do {                                              \
         if (all) RAT3D_NORM1(TOK, PC, true, THREADS); \
@@ -700,7 +709,7 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, Norm
             if (threads <= 256) RAT3D_NORM(TOK, 4, 256);
             else if (TOK == 8 || threads <= 512) RAT3D_NORM(TOK, 4, 512);
             else if constexpr (TOK == 4 && MODE == POST_BWD && NEXT)
-                RAT3D_NORM1(TOK, 4, true, 1024);  // the others have half the tokens
+                RAT3D_NORM1(TOK, 4, true, 1024);  // norm_shape gives the others half the tokens
             else if constexpr (TOK == 4) RAT3D_NORM(TOK, 4, 1024);
         } else if (shape.tok == TOK / 2 && shape.pc == 4) {
             if (threads <= 256) RAT3D_NORM(TOK / 2, 4, 256);
@@ -711,19 +720,38 @@ static void norm_launch_t(const rat3d_norm_desc& d, const NormShape& shape, Norm
             else if constexpr (TOK == 8) RAT3D_NORM(TOK / 2, 8, 512);
         } else if constexpr (TOK == 8) {
             RAT3D_NORM(TOK / 4, 4, 1024);
+        } else {
+            return false;
         }
         a.base += grid;
     }
+    return true;
 #undef RAT3D_NORM
 #undef RAT3D_NORM1
 }
 
 template <NormMode MODE, bool GATED, bool NEXT>
-static void norm_launch(const rat3d_norm_desc& d, const NormShape& shape, NormArgs& a,
-                        hipStream_t st) {
+static bool norm_launch_g(const rat3d_norm_desc& d, const NormShape& shape, const NormArgs& a,
+                          hipStream_t st, bool dry) {
+    return d.dtype == RAT3D_BF16 ? norm_launch_t<bf16, MODE, GATED, NEXT>(d, shape, a, st, dry)
+                                 : norm_launch_t<float, MODE, GATED, NEXT>(d, shape, a, st, dry);
+}
+template <NormMode MODE>
+static bool norm_launch(const rat3d_norm_desc& d, const NormShape& shape, NormArgs& a,
+                        hipStream_t st, bool dry = false) {
     norm_lines(d, &a);
-    if (d.dtype == RAT3D_BF16) norm_launch_t<bf16, MODE, GATED, NEXT>(d, shape, a, st);
-    else norm_launch_t<float, MODE, GATED, NEXT>(d, shape, a, st);
+    if constexpr (MODE == PRE_FWD || MODE == PRE_BWD) {
+        return norm_launch_g<MODE, false, MODE == PRE_BWD>(d, shape, a, st, dry);
+    } else {
+        if (d.gate && a.next) return norm_launch_g<MODE, true, true>(d, shape, a, st, dry);
+        if (d.gate) return norm_launch_g<MODE, true, false>(d, shape, a, st, dry);
+        if (a.next) return norm_launch_g<MODE, false, true>(d, shape, a, st, dry);
+        return norm_launch_g<MODE, false, false>(d, shape, a, st, dry);
+    }
+}
+static rat3d_status norm_none() {
+    set_error("no kernel is built for this norm");
+    return RAT3D_EUNSUPPORTED;
 }
 
 // Names of the measurement: channels held in registers (of 16, 8 or 4 bytes of tokens),
@@ -749,7 +777,7 @@ rat3d_status pre_norm_fwd(const rat3d_norm_desc& d, const void* x, const float* 
     a.mask = mask;
     a.ou = u;
     ProfScope ps(RAT3D_NORM_TAG("pre_norm_fwd"), st, 0.0, norm_bytes(d, 2));
-    norm_launch<PRE_FWD, false, false>(d, shape, a, st);
+    if (!norm_launch<PRE_FWD>(d, shape, a, st)) return norm_none();
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }
@@ -770,10 +798,7 @@ rat3d_status post_norm_fwd(const rat3d_norm_desc& d, const void* x, const void* 
     a.ou = u;
     ProfScope ps(RAT3D_NORM_TAG("post_norm_fwd"), st, 0.0,
                  norm_bytes(d, 3 + (d.gate != 0) + (next != nullptr)));
-    if (d.gate && next) norm_launch<POST_FWD, true, true>(d, shape, a, st);
-    else if (d.gate) norm_launch<POST_FWD, true, false>(d, shape, a, st);
-    else if (next) norm_launch<POST_FWD, false, true>(d, shape, a, st);
-    else norm_launch<POST_FWD, false, false>(d, shape, a, st);
+    if (!norm_launch<POST_FWD>(d, shape, a, st)) return norm_none();
     RAT3D_LAUNCH_CHECK();
     return RAT3D_OK;
 }
@@ -810,7 +835,7 @@ rat3d_status pre_norm_bwd(const rat3d_norm_desc& d, const void* du, const void* 
     {
         ProfScope ps(RAT3D_NORM_TAG("pre_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + (dres != nullptr)));
-        norm_launch<PRE_BWD, false, true>(d, shape, a, st);
+        if (!norm_launch<PRE_BWD>(d, shape, a, st)) return norm_none();
         RAT3D_LAUNCH_CHECK();
     }
     return norm_gains(a, shape, PRE_BWD, dgamma, nullptr, nullptr, accumulate, st);
@@ -839,13 +864,36 @@ rat3d_status post_norm_bwd(const rat3d_norm_desc& d, const void* dy, const void*
     {
         ProfScope ps(RAT3D_NORM_TAG("post_norm_bwd"), st, 0.0,
                      norm_bytes(d, 3 + 2 * (d.gate != 0) + (next ? 3 : 0)));
-        if (d.gate && next) norm_launch<POST_BWD, true, true>(d, shape, a, st);
-        else if (d.gate) norm_launch<POST_BWD, true, false>(d, shape, a, st);
-        else if (next) norm_launch<POST_BWD, false, true>(d, shape, a, st);
-        else norm_launch<POST_BWD, false, false>(d, shape, a, st);
+        if (!norm_launch<POST_BWD>(d, shape, a, st)) return norm_none();
         RAT3D_LAUNCH_CHECK();
     }
     return norm_gains(a, shape, POST_BWD, dnext, dgamma, dscale, accumulate, st);
 }
 
 }  // namespace rat3d
+
+// What a call is planned as, for the tests that keep every size on a kernel that is built for
+// it.  pass: 0 and 1 forward and gradient before a block, 2 and 3 behind one.  Returns 0 where
+// no kernel takes it, else 1 and out = {tokens a thread, channels a thread or 0, groups, tiles,
+// workgroups}.
+extern "C" int rat3d_norm_plan(const rat3d_norm_desc* desc, int pass, int masked, int next,
+                               int64_t out[5]) {
+    using namespace rat3d;
+    if (!out || pass < 0 || pass > 3 || rat3d_norm_workspace_size(desc) == (size_t)-1) return 0;
+    const NormMode modes[4] = {PRE_FWD, PRE_BWD, POST_FWD, POST_BWD};
+    const NormMode mode = modes[pass];
+    static const uint8_t mask = 1;
+    static const float gain = 1.f;
+    NormArgs a = {};
+    const NormShape shape = norm_plan(*desc, mode, masked != 0, pass == 1 || next, &a);
+    a.mask = masked ? &mask : nullptr;
+    a.next = next ? &gain : nullptr;
+    const bool built = mode == PRE_FWD   ? norm_launch<PRE_FWD>(*desc, shape, a, nullptr, true)
+                       : mode == PRE_BWD ? norm_launch<PRE_BWD>(*desc, shape, a, nullptr, true)
+                       : mode == POST_FWD
+                           ? norm_launch<POST_FWD>(*desc, shape, a, nullptr, true)
+                           : norm_launch<POST_BWD>(*desc, shape, a, nullptr, true);
+    const int64_t o[5] = {shape.tok, shape.pc, shape.groups, a.all, norm_grid(a, mode)};
+    for (int i = 0; i < 5; ++i) out[i] = o[i];
+    return built;
+}

@@ -360,9 +360,9 @@ rat3d_status rat3d_dropout_bwd(const rat3d_dropout_desc* desc, uint64_t step,
  * and the next (0: packed, c * v); a gradient lies as the tensor it belongs to.
  * mask is uint8 [n][v], or NULL: all voxels.  What a masked voxel's inputs hold is not
  * read into a result, but for the residual's.
- * A result may be one of the call's inputs of the same shape (the same pointer and, for
- * n > 1, the same stride); any other overlap of a result with an input or another
- * result is RAT3D_EINVAL.
+ * A result that is a map may be one of the call's input maps (the same pointer and, for
+ * n > 1, the same stride), h_last may be h0 and dh0 dh_last; any other overlap of a result
+ * with an input or another result is RAT3D_EINVAL, also of gains and of masks.
  * ------------------------------------------------------------------------ */
 
 typedef enum {

@@ -3,6 +3,7 @@
 #include <cstdarg>
 #include <cstdio>
 #include <string>
+#include <utility>
 
 #include "kernels.hpp"
 
@@ -116,9 +117,36 @@ struct Span {
 };
 enum { SPAN_VECTOR = 0, SPAN_MAP = 1, SPAN_STATE = 2 };
 
+// The sum of floor((x + i step) / m) over i below n, by Euclid's algorithm.
+typedef __int128 wide;
+static wide floor_sum(wide n, wide m, wide step, wide x) {
+    wide sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (step / m) + n * (x / m);
+        step %= m;
+        x %= m;
+        const wide top = step * n + x;
+        n = top / m;
+        x = top % m;
+        std::swap(m, step);
+    }
+    return sum;
+}
+// Over all parts i of a: how many parts j of b have j b.stride - i a.stride <= most.
+static wide parts_within(const Span& a, const Span& b, wide most) {
+    const auto first = [&](wide at) {  // the first i with most + i a.stride >= at
+        const wide i = at <= most ? 0 : (at - most + a.stride - 1) / a.stride;
+        return i < a.n ? i : (wide)a.n;
+    };
+    const wide some = first(0), all = first((wide)(b.n - 1) * b.stride), n = all - some;
+    return n + floor_sum(n, b.stride, a.stride, n > 0 ? most + some * a.stride : 0) +
+           (a.n - all) * b.n;
+}
+
 static bool spans_meet(const Span& a, const Span& b) {
     const int64_t pa = (int64_t)(uintptr_t)a.p, pb = (int64_t)(uintptr_t)b.p;
-    if (pa + (a.n - 1) * a.stride + a.held <= pb || pb + (b.n - 1) * b.stride + b.held <= pa)
+    if (pa + (wide)(a.n - 1) * a.stride + a.held <= pb ||
+        pb + (wide)(b.n - 1) * b.stride + b.held <= pa)
         return false;
     if (a.n == b.n && a.stride == b.stride) {  // one distance for all parts, up to whole strides
         const int64_t m = (pb - pa) / a.stride;
@@ -128,14 +156,9 @@ static bool spans_meet(const Span& a, const Span& b) {
         }
         return false;
     }
-    // (beyond 2^16 parts of different strides only the first are looked at)
-    const int64_t most = a.n < 1 << 16 ? a.n : 1 << 16;
-    for (int64_t k = 0; k < most; ++k) {
-        const int64_t lo = pa + k * a.stride, d = lo - b.held - pb;
-        const int64_t j = d < 0 ? 0 : d / b.stride + 1;  // b's first part that ends behind lo
-        if (j < b.n && pb + j * b.stride < lo + a.held) return true;
-    }
-    return false;
+    // parts meet where j b.stride - i a.stride is between -b.held and a.held around pa - pb
+    const wide off = (wide)pa - pb;
+    return parts_within(a, b, off + a.held - 1) > parts_within(a, b, off - b.held);
 }
 
 template <int OUTS, int INS>
@@ -906,6 +929,15 @@ rat3d_status rat3d_recurrence_bwd(const rat3d_recurrence_desc* desc, const void*
     if (s != RAT3D_OK) return s;
     return recurrence_bwd(*desc, dy, dh_last, r, i, x, lambda, mask, carry, dr, di, dx, dlambda,
                           dh0, accumulate ? 1 : 0, ws, (hipStream_t)stream);
+}
+
+// Whether n parts of `held` bytes, `stride` bytes apart from address p on, meet those of
+// another tensor: what refuses results over other tensors, for the tests.
+int rat3d_spans_meet(const int64_t a[4], const int64_t b[4]) {
+    auto span = [](const int64_t* t) {
+        return Span{(const void*)(uintptr_t)t[0], t[1], t[2], t[3], SPAN_MAP, ""};
+    };
+    return spans_meet(span(a), span(b));
 }
 
 size_t rat3d_head_workspace_size(int n, int c, int classes) {

@@ -253,3 +253,118 @@ def test_every_result_over_every_input(c, v, mask, dt):
             t = {k: a.clone() for k, a in src.items()}
             for a, b in zip(own, call(t, *(t[k] for k in over))):
                 assert same(a, b), (call.__name__, over)
+
+
+# ------------------------------------------------------------------ the longest rows
+@pytest.mark.parametrize("c,tag", [(6, ""), (17, "_any")])
+def test_float32_rows_of_2_28_voxels(c, tag):
+    """Rows of which 32 bits reach four: every piece of 4096 voxels has the bits of the first,
+    and these are right."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    v = 1 << 28
+    g = torch.Generator(device="cuda:0").manual_seed(4)
+    small = torch.randn((c, 4096), generator=g, device="cuda:0")
+    x = torch.empty((c, v), device="cuda:0")
+    x.view(c, -1, 4096).copy_(small[:, None, :])
+    gamma = 1 + 0.1 * torch.arange(c, device="cuda:0", dtype=torch.float32)
+    d = R.norm_desc(1, c, v, R.F32, eps=1e-5)
+    tags = _tags(lambda: R.rat3d_pre_norm_fwd(d, x, gamma, None, x))
+    assert tags == ["pre_norm_fwd" + tag]
+    want = RU.pre_norm_refs(U.f64(small)[None], U.f64(gamma), None, 1e-5, "f32")["u"]
+    RU.within(U.f64(x[:, :4096])[None], want, "u")
+    for k in range(c):
+        row = x[k].view(-1, 4096)
+        assert bool((row == row[:1]).all()), k
+
+
+@pytest.mark.parametrize("dt", ["bf16", "f32"])
+@pytest.mark.parametrize("reverse", [False, True])
+def test_joined_segments_of_several_masked_rows(reverse, dt):
+    """Rows of more segments than find one another, with masks, states and results in place:
+    the bits of each row alone, and a row's values in pieces."""
+    from paper_2104_05035_amd import rat3d as R
+    torch = U.torch_mod()
+    block = 8 * (512 if dt == "bf16" else 256)
+    n, c, v = 2, 2, 2048 * block + 5
+    g = torch.Generator(device="cuda:0").manual_seed(19)
+    ins = [torch.randn((n, c, v), generator=g, device="cuda:0").to(U.tdtype(dt)) for _ in range(4)]
+    mask = (torch.rand((n, v), generator=g, device="cuda:0") < 0.6).to(torch.uint8)
+    mask[1, v // 3:v // 2] = 0  # whole segments
+    lam = torch.tensor([-9.0, -3.0], device="cuda:0")
+    h0 = torch.randn((n, c), generator=g, device="cuda:0")
+    dh = torch.randn((n, c), generator=g, device="cuda:0")
+
+    def run(r, i, x, dy, mask, lam, h0, dh):
+        m, k, t = r.shape
+        d = R.recurrence_desc(m, k, t, U.code(dt), reverse=reverse)
+        need = [R.rat3d_recurrence_workspace_size(d, p) for p in (0, 1)]
+        carry = _ws(R.rat3d_recurrence_carry_size(d))
+        y, dlam = torch.empty_like(r), torch.empty_like(lam)
+        r, i, x, last, first = r.clone(), i.clone(), x.clone(), h0.clone(), dh.clone()
+        R.rat3d_recurrence_fwd(d, r, i, x, lam, mask, last, y, last, carry, _ws(need[0]), need[0])
+        R.rat3d_recurrence_bwd(d, dy, first, r, i, x, lam, mask, carry, r, i, x, dlam, first, 0,
+                               _ws(need[1]), need[1])
+        U.sync()
+        return dict(y=y, h_last=last, dr=r, di=i, dx=x, dh0=first, dlam=dlam)
+
+    tags = []
+    tags.append(_tags(lambda: tags.append(run(*ins, mask, lam, h0, dh))))
+    whole, tags = tags
+    assert {"recurrence_fwd_join", "recurrence_bwd_join"} <= set(tags)
+    total, size = torch.zeros((2, c), dtype=torch.float64, device="cuda:0")
+    for j in range(n):
+        for k in range(c):
+            o = run(*(t[j:j + 1, k:k + 1].contiguous() for t in ins), mask[j:j + 1], lam[k:k + 1],
+                    h0[j:j + 1, k:k + 1].contiguous(), dh[j:j + 1, k:k + 1].contiguous())
+            total[k] += o["dlam"][0].double()
+            size[k] += o["dlam"][0].double().abs()
+            for name in o:
+                if name != "dlam":
+                    assert torch.equal(o[name][0, 0], whole[name][j, k]), (name, j, k)
+    # each row's sum is rounded once, and that of both
+    assert bool(((whole["dlam"].double() - total).abs() <= 2 * RU.F * size).all())
+    # the second volume with the short memory in pieces: a segment's edges lie inside them
+    r, i, x, dy = (t[1:, 1:] for t in ins)
+    size = -(-v // 7)
+    cuts = [(a, min(a + size, v)) for a in range(0, v, size)][::-1 if reverse else 1]
+    state = h0[1:, 1:].contiguous()
+    for a, b in cuts:
+        o = run(*(t[..., a:b].contiguous() for t in (r, i, x, dy)), mask[1:, a:b].contiguous(), lam[1:],
+                state, torch.zeros_like(state))
+        state = o["h_last"]
+        got, want = whole["y"][1:, 1:, a:b].float(), o["y"].float()
+        # decays of 0.68 at the mean: a state's error is that of some hundred steps, 64 f each,
+        # of values up to 8, and both are rounded
+        assert bool(((got - want).abs() <= 2 * RU.U[dt] * want.abs() + 8 * 64 * 100 * RU.F).all())
+
+
+# ------------------------------------------------------------------ streams
+def test_walks_on_two_streams():
+    """Forward and backward on two streams at once, everything allocated and filled before: the
+    bits of one after another, and nothing beside the results."""
+    torch = U.torch_mod()
+    s = [TR.Walk((1, 4, 50000, False, None, 1.0, 8.0), "bf16"),
+         TR.Walk((2, 3, 60001, True, "holes", 1.0, 8.0), "bf16")]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+
+    def run(walks):
+        out = [(t, t.results(), [_ws(b) for b in t.need], st) for t, st in walks]
+        U.sync()  # the fills are on the current stream
+        for t, o, ws, st in out:
+            p = st.cuda_stream
+            t.R.rat3d_recurrence_fwd(t.desc, t.r, t.i, t.x, t.lam, t.dmask, t.h0, o["y"], o["h_last"],
+                                     t.carry, ws[0], t.need[0], stream=p)
+            t.R.rat3d_recurrence_bwd(t.desc, t.dy, t.dh, t.r, t.i, t.x, t.lam, t.dmask, t.carry,
+                                     o["dr"], o["di"], o["dx"], o["dlam"], o["dh0"], 0, ws[1],
+                                     t.need[1], stream=p)
+        U.sync()
+        return [o for _, o, _, _ in out]
+
+    alone = [run([w])[0] for w in zip(s, streams)]
+    for _ in range(3):
+        for o, a in zip(run(list(zip(s, streams))), alone):
+            assert all(torch.equal(o[k], a[k]) for k in a)
+    for t in s:
+        for b in t.guards:
+            U.guard_intact(b)

@@ -428,6 +428,7 @@ rat3d_status rat3d_post_norm_bwd(const rat3d_norm_desc* desc, const void* dy, co
  * (De et al. 2024, arXiv 2402.19427, equations 1 to 4):
  *   a_t = exp(-rate softplus(lambda_c) sigmoid(r_t))
  *   h_t = a_t h_{t-1} + sqrt(1 - a_t^2) sigmoid(i_t) x_t,   y = h
+ * (a decay stored as a = sigmoid(L), so that log a = -softplus(-L), has lambda = -L),
  * from the first token to the last, or from the last to the first if reverse; h before
  * the walk is h0 (nullable: 0).  A masked token hands the state on unchanged and has
  * y = 0.  States, decays and sums are float32.  One token from a kept state is a call
@@ -457,7 +458,8 @@ rat3d_status rat3d_recurrence_fwd(const rat3d_recurrence_desc* desc, const void*
 
 /* Gradients from dy and dh_last (nullable: 0), the forward's inputs and its carry: dr,
  * di, dx (0 at masked tokens), dlambda float32 [c] (written, or added to when accumulate
- * != 0) and dh0 float32 [n][c] (nullable, written). */
+ * != 0) and dh0 float32 [n][c] (nullable, written).  dr, di and dx are written, never added
+ * to: where two walks, there and back, share their gates and values, the caller adds them. */
 rat3d_status rat3d_recurrence_bwd(const rat3d_recurrence_desc* desc, const void* dy,
                                   const float* dh_last, const void* r, const void* i,
                                   const void* x, const float* lambda, const uint8_t* mask,

@@ -20,8 +20,9 @@
 // joined by lane swaps that leave each of a wave's four groups a quarter of the voxels,
 // and through LDS.  Rows need no alignment.
 // Bound: HBM.  Bfloat16, 16 x 64 channels of 48x56x48 voxels: before a block 76 us (its
-// input partly in the memory-side cache), its gradient 201 us (5.3 TB/s); behind one with
-// gate and next norm 254 us (5.2), its gradient with all eight tensors 438 us (4.8).
+// input partly in the memory-side cache), its gradient 200 us (5.3 TB/s); behind one with
+// gate and next norm 252 us (5.2), its gradient with all eight tensors 437 us (4.8); with a
+// mask 93, 209, 254 and 445; float32, 8 x 64 channels: 77, 207, 261 and 430.
 #include "kernels.hpp"
 #include "prof.hpp"
 #include "tokens.hpp"
@@ -574,8 +575,12 @@ __global__ __launch_bounds__(256) void norm_gain_k(const Part* __restrict__ part
 //   maps of whole tiles are read again instead: 4 x 512 over 16128 in float32 349 us
 //   against 362, bfloat16 183 against 193, before a block 151 against 184 and 85 against 97.
 // Channels that are read again have 64 groups, few rounds: 4 x 600 channels over 16128
-// voxels in bfloat16 244 -> 233 us, before a block 135 -> 102, behind one 162 -> 115,
+// voxels in bfloat16 244 -> 235 us, before a block 135 -> 96, behind one 162 -> 116,
 // against 16 groups.
+// Kernels of 1024 threads have 128 registers, and some gradients behind a block with a next
+// norm spill over them: two voxels of eight channels in bfloat16 65 registers where tiles are
+// masked or unwhole (53 without a gate), 11 (9) on whole ones, four of four in float32 on
+// whole tiles 18 (2), one of eight in float32 11, read again in bfloat16 13.
 struct NormShape {
     int tok, pc, groups;
 };
@@ -652,8 +657,8 @@ size_t norm_ws_bytes(const rat3d_norm_desc& d) {
 }
 
 // Rows that begin inside a cache line: neighbouring tiles share lines, and one XCD's
-// L2 should see both (16 x 64 channels of 129023 voxels: 407 -> 348 us behind a block,
-// its gradient 692 -> 544; whole lines are 2 to 4 % faster dealt out).  Streaming stores
+// L2 should see both (16 x 64 channels of 129023 voxels: 407 -> 341 us behind a block,
+// its gradient 692 -> 509; whole lines are 2 to 4 % faster dealt out).  Streaming stores
 // would write the shared lines twice.
 static void norm_lines(const rat3d_norm_desc& d, NormArgs* a) {
     const int64_t es = d.dtype == RAT3D_BF16 ? 2 : 4;

@@ -27,8 +27,9 @@
 // reads would grow with their square).
 //
 // beta: 1 - a^2 is -expm1(-2 w sigmoid(r)), by its series where the argument is small.
-// Bound: HBM.  Bfloat16, 16 x 64 rows of 48x56x48 voxels: forward 219 us (4.8 TB/s),
-// gradient 375 us (4.9); 32 such rows, cut, 15 and 28 us.
+// Bound: HBM.  Bfloat16, 16 x 64 rows of 48x56x48 voxels: forward 222 us (4.8 TB/s),
+// gradient 374 us (4.9), with a mask 242 and 413; 32 such rows, cut, 14 and 27 us.  (Calls
+// among others; single kernels under a profiler take 230 and 405.)
 #include "kernels.hpp"
 #include "prof.hpp"
 #include "tokens.hpp"
@@ -874,17 +875,26 @@ static void rec_plan(const rat3d_recurrence_desc& d, RecArgs* q, int* waves) {
     q->blocks = (int)ceil_div(d.len, 64 * tok);
     q->segs = 1;
     q->lanes = 0;
+    // Past the memory-side cache, whether rows begin on cache lines or not: 16 x 64 rows of
+    // 129024 voxels 224 -> 218 us, gradient 385 -> 373; of 129023 254 -> 250 and 444 -> 442,
+    // 8 x 64 in float32 212 -> 210 and 385 -> 388.
     q->stream = (double)packed * d.n * 16 / tok > 256e6;
     if (d.len <= 16 * tok) {
         q->lanes = 1;
         while (q->lanes * tok < d.len) q->lanes *= 2;
         return;
     }
-    // Eight waves a row (four take the same time from 1024 rows on), sixteen where a CU has
-    // one row or little more and where that is the whole row.  Fewer rows are cut: a forward
-    // over 128 rows of 129024 voxels in bfloat16 takes 70 us uncut, 59 with a launch that
-    // joins segments, 39 as segments that find one another, over 256 rows 64 uncut (sixteen
-    // waves; 77 with eight) and 108 cut with joins.
+    // Eight waves a row (four take the same time from 1024 rows on), sixteen where that is
+    // the whole row, and where a CU has one row or little more of 64 blocks or more: of 64 to
+    // 252 blocks, in bfloat16, 256 rows take 12 to 17 % less time than with eight, their
+    // gradient 6 to 9 %; 320 and 383 rows 1 to 7 % less, their gradient 5 to 8 % more.  Of 17
+    // to 63 blocks sixteen waves are slower from 320 rows on (by up to 21 %; 256 rows of 32 to
+    // 63 blocks would be 3 to 9 % faster).
+    // Rows of less than one a CU are cut: a forward over 128 rows of 129024 voxels takes 70 us
+    // uncut, 59 with a launch that joins segments, 39 as segments that find one another.  From
+    // a row a CU on cutting loses: 256 such rows take 63 us uncut, 69 as segments that find one
+    // another (gradient 108 and 132) and 108 with joins; 512 of 16128 voxels 20 and 25 (36
+    // and 44).
     const int64_t cus = device_cus();
     int most = 8;
     if (q->rows >= cus ? 2 * q->rows < 3 * cus && q->blocks >= 64 : q->blocks <= kWaves) {
